@@ -39,6 +39,8 @@
  *   inv entry outside [-1, n_rows), a coordinate outside [0, B) x [0, V)) are
  *   treated as absent rows, never dereferenced.
  * - Inputs and outputs of one call must not overlap.
+ * - The row operators (embedding rows, layer norm, distillation) take rows of
+ *   any width at any stride: their comment block states their own rules.
  * - Return value: SHC_OK (0) or a negative SHC_ERR_* code.  Nothing is
  *   launched when validation fails.  SHC_ERR_HIP reports a HIP runtime or
  *   launch failure; shc_last_error() then holds the message (thread-local).
@@ -724,6 +726,147 @@ int shc_sparse_neighbor_conv_backward(const void* S, const int32_t* table, const
                                       int64_t n_rows, int32_t K, int32_t Cin, int32_t Cout,
                                       int32_t dtype, int32_t act, void* dS, float* dW, float* db,
                                       void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Row operators of a training step: embedding rows, layer norm, distillation */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * What a network on active rows needs to be trained, beside its layers: rows
+ * learned per vertex (or per token of any id space), a norm with weight and
+ * bias, and a loss against a teacher.  Their rules, where they differ from the
+ * conventions above:
+ * - Rows have any width: C in [1, 65536] (embedding rows), [1, 16384] (layer
+ *   norm), V in [1, 2^24] (logits).
+ * - A row tensor comes with its row stride in elements, at least its width: a
+ *   slice of wider rows is an operand like any other.  n_rows * stride must
+ *   stay below 2^40 elements.
+ * - Pointers need the alignment of their elements only (SHC_ERR_MISALIGNED);
+ *   16-byte aligned rows are the fastest.
+ * - Per-channel parameters, statistics, losses and gradients of parameters are
+ *   fp32, contiguous.  Sums and statistics are held in fp32; every output is
+ *   rounded once.
+ * - With `accumulate` 1 a parameter's gradient is added to what the output
+ *   holds, else it is written.
+ * - Workspaces are device memory of at least the size that the matching
+ *   _workspace call returns (for n_rows, or any larger count), their contents on
+ *   entry do not matter.
+ * - Results repeat bit for bit.  n_rows = 0 writes no row; gradients of
+ *   parameters are then zero (left alone with `accumulate`).
+ */
+#define SHC_IDS_I32 0
+#define SHC_IDS_I64 1
+
+/*
+ * Embedding rows with scaling:
+ *
+ *   out[i] = scale * E[id_i] (+ add[i]),
+ *
+ * an id outside [0, n_entries) having no row: out[i] = add[i], or zeros.
+ *   E    [n_entries] rows of C, E_stride apart.  n_entries in [1, 2^22].
+ *   ids  [n_rows] int32 or int64 (id_type), id_stride elements apart (>= 0):
+ *        the vertex of every active row is coords + 1 with stride 2.
+ *   add  [n_rows] rows of C, or NULL.   scale finite.
+ * The product and sum are one fp32 operation, rounded once.
+ */
+int shc_embed_rows(const void* E, int64_t E_stride, int64_t n_entries, const void* ids,
+                   int32_t id_type, int64_t id_stride, int64_t n_rows, int32_t C, float scale,
+                   const void* add, int64_t add_stride, int32_t dtype, void* out,
+                   int64_t out_stride, hipStream_t stream);
+
+/*
+ * Gradient of the embedding rows by sorted ids:
+ *
+ *   dE[r] = scale * sum over i with id_i = r of dY[i]     for every r < n_entries
+ *
+ * (rows without an id are zero, or left alone with `accumulate`); ids outside
+ * [0, n_entries) and ids equal to pad_id (-1: none) give nothing.
+ *   dY [n_rows] rows of C of `dtype`; dE [n_entries] rows of C, fp32.
+ * The positions are ordered by id, and each id's rows are added in ascending
+ * order in fp32, in chunks whose sums are added in order.
+ */
+size_t shc_embed_rows_backward_workspace(int64_t n_rows, int64_t n_entries, int32_t C);
+int shc_embed_rows_backward(const void* dY, int64_t dY_stride, const void* ids, int32_t id_type,
+                            int64_t id_stride, int64_t n_rows, int64_t n_entries, int32_t C,
+                            float scale, int64_t pad_id, int32_t dtype, int32_t accumulate,
+                            float* dE, int64_t dE_stride, void* ws, size_t ws_bytes,
+                            hipStream_t stream);
+
+/*
+ * Layer norm of every row over its C channels:
+ *
+ *   mu = mean of x,  rs = 1 / sqrt(mean of (x - mu)^2 + eps)
+ *   y  = (x - mu) rs gamma + beta
+ *
+ *   x, y [n_rows] rows of C; gamma, beta [C] fp32, each may be NULL (1, 0);
+ *   mean, rstd [n_rows] fp32 out (mu and rs, for the backward), each may be
+ *   NULL.  eps positive and finite.
+ */
+int shc_layer_norm(const void* x, int64_t x_stride, int64_t n_rows, int32_t C,
+                   const float* gamma, const float* beta, float eps, int32_t dtype, void* y,
+                   int64_t y_stride, float* mean, float* rstd, hipStream_t stream);
+
+/*
+ * Gradients of the layer norm, with h = (x - mean) rstd and g = dy gamma:
+ *
+ *   dx     = rstd (g - mean of g - h * mean of g h)
+ *   dgamma = sum over rows of dy h,   dbeta = sum over rows of dy
+ *
+ *   dy, x, dx [n_rows] rows of C; gamma [C] or NULL (1); mean, rstd [n_rows]
+ *   as shc_layer_norm wrote them; dgamma, dbeta [C] fp32 out.  dx, dgamma and
+ *   dbeta may each be NULL (not computed); ws may be NULL without dgamma and
+ *   dbeta.
+ * The column sums have a fixed order that follows n_rows, C and dtype.
+ */
+size_t shc_layer_norm_backward_workspace(int64_t n_rows, int32_t C);
+int shc_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
+                            int64_t n_rows, int32_t C, const float* gamma, const float* mean,
+                            const float* rstd, int32_t dtype, int32_t accumulate, void* dx,
+                            int64_t dx_stride, float* dgamma, float* dbeta, void* ws,
+                            size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Distillation from a teacher's top logits.  For every row of V logits z and
+ * its k teacher entries (id_j, t_j), at temperature T:
+ *
+ *   p = softmax over the entries of t / T,   q = softmax over V of z / T
+ *   loss = T^2 * sum_j p_j (log p_j - log q_{id_j})
+ *   dz_v = w T (q_v - sum of p_j with id_j = v)
+ *
+ * An entry whose id is outside [0, V), or whose t is -inf, is absent; ids may
+ * repeat.  A row without entries (padding) has loss 0, lse 0 and gradient 0,
+ * and its logits are not read.  A logit of -inf has q = 0 (an entry with p > 0
+ * there makes the loss +inf; the gradient stays finite), in a row of nothing
+ * but -inf every q is 0.  NaN and +inf make the row's own results NaN.  With
+ * T < 1 the logits' maximum over T must be within fp32.
+ *   logits, dlogits [n_rows] rows of V of `dtype`; top_ids [n_rows][k] int32,
+ *   top_logits [n_rows][k] fp32; k in [1, 256]; temperature positive, finite.
+ *   loss [n_rows] fp32 out; row_weight [n_rows] fp32 = w, the upstream gradient
+ *   of every row's loss, or NULL (1).
+ *
+ * shc_distill_top          -- loss, and lse = log of sum exp(z / T) [n_rows]
+ *                             fp32 (may be NULL), for evaluation or a backward
+ *                             whose w is not known yet.
+ * shc_distill_top_backward -- dlogits from lse as shc_distill_top wrote it.
+ * shc_distill_top_step     -- loss and dlogits in one pass over the logits.
+ * shc_distill_top and _step take a workspace of shc_distill_top_workspace
+ * bytes (which may be 0; ws may then be NULL).
+ */
+size_t shc_distill_top_workspace(int64_t n_rows, int32_t V);
+int shc_distill_top(const void* logits, int64_t logits_stride, int64_t n_rows, int32_t V,
+                    const int32_t* top_ids, const float* top_logits, int32_t k,
+                    float temperature, int32_t dtype, float* loss, float* lse, void* ws,
+                    size_t ws_bytes, hipStream_t stream);
+int shc_distill_top_backward(const void* logits, int64_t logits_stride, int64_t n_rows, int32_t V,
+                             const int32_t* top_ids, const float* top_logits, int32_t k,
+                             float temperature, const float* lse, const float* row_weight,
+                             int32_t dtype, void* dlogits, int64_t dlogits_stride,
+                             hipStream_t stream);
+int shc_distill_top_step(const void* logits, int64_t logits_stride, int64_t n_rows, int32_t V,
+                         const int32_t* top_ids, const float* top_logits, int32_t k,
+                         float temperature, const float* row_weight, int32_t dtype, float* loss,
+                         void* dlogits, int64_t dlogits_stride, void* ws, size_t ws_bytes,
+                         hipStream_t stream);
 
 /*
  * Stream-ordering events -- a runtime helper, not an operator of the paper.

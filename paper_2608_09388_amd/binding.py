@@ -166,6 +166,28 @@ _SIGS = {
                                                          _c_ptr, _c_i64, _c_i32, _c_i32, _c_i32,
                                                          _c_i32, _c_i32, _c_ptr, _c_ptr, _c_ptr,
                                                          _c_ptr, _c_sz, _c_ptr]),
+    "shc_embed_rows": (ctypes.c_int, [_c_ptr, _c_i64, _c_i64, _c_ptr, _c_i32, _c_i64, _c_i64,
+                                      _c_i32, _c_f, _c_ptr, _c_i64, _c_i32, _c_ptr, _c_i64,
+                                      _c_ptr]),
+    "shc_embed_rows_backward_workspace": (_c_sz, [_c_i64, _c_i64, _c_i32]),
+    "shc_embed_rows_backward": (ctypes.c_int, [_c_ptr, _c_i64, _c_ptr, _c_i32, _c_i64, _c_i64,
+                                               _c_i64, _c_i32, _c_f, _c_i64, _c_i32, _c_i32,
+                                               _c_ptr, _c_i64, _c_ptr, _c_sz, _c_ptr]),
+    "shc_layer_norm": (ctypes.c_int, [_c_ptr, _c_i64, _c_i64, _c_i32, _c_ptr, _c_ptr, _c_f,
+                                      _c_i32, _c_ptr, _c_i64, _c_ptr, _c_ptr, _c_ptr]),
+    "shc_layer_norm_backward_workspace": (_c_sz, [_c_i64, _c_i32]),
+    "shc_layer_norm_backward": (ctypes.c_int, [_c_ptr, _c_i64, _c_ptr, _c_i64, _c_i64, _c_i32,
+                                               _c_ptr, _c_ptr, _c_ptr, _c_i32, _c_i32, _c_ptr,
+                                               _c_i64, _c_ptr, _c_ptr, _c_ptr, _c_sz, _c_ptr]),
+    "shc_distill_top_workspace": (_c_sz, [_c_i64, _c_i32]),
+    "shc_distill_top": (ctypes.c_int, [_c_ptr, _c_i64, _c_i64, _c_i32, _c_ptr, _c_ptr, _c_i32,
+                                       _c_f, _c_i32, _c_ptr, _c_ptr, _c_ptr, _c_sz, _c_ptr]),
+    "shc_distill_top_backward": (ctypes.c_int, [_c_ptr, _c_i64, _c_i64, _c_i32, _c_ptr, _c_ptr,
+                                                _c_i32, _c_f, _c_ptr, _c_ptr, _c_i32, _c_ptr,
+                                                _c_i64, _c_ptr]),
+    "shc_distill_top_step": (ctypes.c_int, [_c_ptr, _c_i64, _c_i64, _c_i32, _c_ptr, _c_ptr,
+                                            _c_i32, _c_f, _c_ptr, _c_i32, _c_ptr, _c_ptr, _c_i64,
+                                            _c_ptr, _c_sz, _c_ptr]),
     "shc_event_create": (ctypes.c_int, [ctypes.POINTER(_c_ptr)]),
     "shc_event_record": (ctypes.c_int, [_c_ptr, _c_ptr]),
     "shc_stream_wait_event": (ctypes.c_int, [_c_ptr, _c_ptr]),
@@ -1144,3 +1166,317 @@ def prepare_segment_maxpool(S, row_ptr, B, P, empty_value=0.0, stream=None) -> P
     args = [_dev(S, "S", P.dtype), _dev(row_ptr, "row_ptr", torch.int32, B + 1), 0, B, C,
             _dtype_code(P), float(empty_value), _dev(P, "P", P.dtype, B * C), _stream(stream)]
     return Prepared("shc_segment_maxpool", args, 2, S.numel() // C, (S, row_ptr, P))
+
+
+# ----------------------------------------------------------------------------
+# row operators of a training step: embedding rows, layer norm, distillation.
+# Row tensors are [n][C] with any row stride (a slice of wider rows will do);
+# ids are int32 or int64 with any stride (coords[:, 1] is the list of the active
+# rows' vertices).  Each operator as a prepared call, for any row count up to
+# its tensors', and as a plain one over the tensors' rows.
+# ----------------------------------------------------------------------------
+
+SHC_IDS_I32, SHC_IDS_I64 = 0, 1
+LAYER_NORM_MAX_C = 16384
+DISTILL_MAX_TOP = 256
+
+
+def _new(shape, dtype, device, stream):
+    """A tensor for work on `stream`, from that stream's memory: the allocator
+    hands out memory that work on the allocating stream may still use."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class _Operands:
+    """Checks the tensors of one call: all on one device, the current one."""
+
+    def __init__(self):
+        self.device = None
+
+    def _place(self, t, name):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be on the GPU")
+        if self.device is None:
+            self.device = t.device
+            if t.device.index != torch.cuda.current_device():
+                raise ValueError(f"{name} is on {t.device}, the current device is "
+                                 f"cuda:{torch.cuda.current_device()}")
+        elif t.device != self.device:
+            raise ValueError(f"{name} is on {t.device}, not on {self.device}")
+
+    def rows(self, t, name, dtype=None, width=None):
+        """(pointer, row stride, rows, width) of a row tensor."""
+        self._place(t, name)
+        if dtype is not None and t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.dim() != 2:
+            raise ValueError(f"{name} must be two-dimensional, got {tuple(t.shape)}")
+        n, C = t.shape
+        if width is not None and C != width:
+            raise ValueError(f"{name} has rows of {C}, not of {width}")
+        if C > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name}: the elements of a row must be adjacent")
+        # one row, or none, has no stride to speak of
+        stride = t.stride(0) if n > 1 else max(C, 1)
+        if stride < C:
+            raise ValueError(f"{name}: rows overlap (stride {stride}, width {C})")
+        return t.data_ptr(), stride, n, C
+
+    def array(self, t, name, dtype, numel, optional=False):
+        """Pointer of a contiguous array of at least `numel` elements."""
+        if t is None:
+            if optional:
+                return None
+            raise TypeError(f"{name} must be a torch.Tensor")
+        self._place(t, name)
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        if t.numel() < numel:
+            raise ValueError(f"{name} holds {t.numel()} elements, needs {numel}")
+        return t.data_ptr()
+
+    def ids(self, t):
+        """(pointer, type code, stride, count) of a list of ids."""
+        self._place(t, "ids")
+        if t.dtype not in (torch.int32, torch.int64):
+            raise TypeError(f"ids must be int32 or int64, got {t.dtype}")
+        if t.dim() != 1:
+            raise ValueError(f"ids must be one-dimensional, got {tuple(t.shape)}")
+        code = SHC_IDS_I64 if t.dtype == torch.int64 else SHC_IDS_I32
+        return t.data_ptr(), code, t.stride(0) if t.numel() > 1 else 1, t.numel()
+
+    def workspace(self, ws, need, stream):
+        """(tensor, pointer, bytes): the given workspace, or a new one of `need` bytes."""
+        if ws is None:
+            if need == 0:
+                return None, None, 0
+            ws = _new(need, torch.uint8, self.device, stream)
+        else:
+            self._place(ws, "ws")
+            if not ws.is_contiguous():
+                raise ValueError("ws must be contiguous")
+            if ws.numel() * ws.element_size() < need:
+                raise ValueError(f"ws holds {ws.numel() * ws.element_size()} bytes, "
+                                 f"needs {need}")
+        return ws, ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def embed_rows_backward_workspace(n_rows: int, n_entries: int, C: int) -> int:
+    """shc_embed_rows_backward_workspace."""
+    return int(load().shc_embed_rows_backward_workspace(n_rows, n_entries, C))
+
+
+def layer_norm_backward_workspace(n_rows: int, C: int) -> int:
+    """shc_layer_norm_backward_workspace."""
+    return int(load().shc_layer_norm_backward_workspace(n_rows, C))
+
+
+def distill_top_workspace(n_rows: int, V: int) -> int:
+    """shc_distill_top_workspace."""
+    return int(load().shc_distill_top_workspace(n_rows, V))
+
+
+def prepare_embed_rows(E, ids, out, scale: float = 1.0, add=None, stream=None) -> Prepared:
+    """shc_embed_rows: out[i] = scale * E[ids[i]] (+ add[i])."""
+    o = _Operands()
+    e_ptr, e_ld, R, C = o.rows(E, "E")
+    dt = _dtype_code(E)
+    i_ptr, code, i_ld, n = o.ids(ids)
+    o_ptr, o_ld, n_out, _ = o.rows(out, "out", E.dtype, C)
+    a_ptr, a_ld, n_add = None, C, n
+    if add is not None:
+        a_ptr, a_ld, n_add, _ = o.rows(add, "add", E.dtype, C)
+    args = [e_ptr, e_ld, R, i_ptr, code, i_ld, 0, C, float(scale), a_ptr, a_ld, dt, o_ptr, o_ld,
+            _stream(stream)]
+    return Prepared("shc_embed_rows", args, 6, min(n, n_out, n_add), (E, ids, out, add))
+
+
+def embed_rows(E, ids, out=None, scale: float = 1.0, add=None, stream=None):
+    """shc_embed_rows over all of ids; returns out ([n][C], made here when None)."""
+    if out is None:
+        out = _new((ids.numel(), E.shape[-1]), E.dtype, E.device, stream)
+    call = prepare_embed_rows(E, ids, out, scale, add, stream)
+    call(ids.numel())
+    return out
+
+
+def prepare_embed_rows_backward(dY, ids, dE, scale: float = 1.0, pad_id: int = -1,
+                                accumulate: bool = False, ws=None, stream=None) -> Prepared:
+    """shc_embed_rows_backward: dE[r] (+)= scale * sum of dY[i] with ids[i] = r."""
+    o = _Operands()
+    y_ptr, y_ld, n_y, C = o.rows(dY, "dY")
+    dt = _dtype_code(dY)
+    i_ptr, code, i_ld, n = o.ids(ids)
+    e_ptr, e_ld, R, _ = o.rows(dE, "dE", torch.float32, C)
+    n_max = min(n, n_y)
+    ws, w_ptr, w_bytes = o.workspace(ws, embed_rows_backward_workspace(n_max, R, C), stream)
+    args = [y_ptr, y_ld, i_ptr, code, i_ld, 0, R, C, float(scale), int(pad_id), dt,
+            int(bool(accumulate)), e_ptr, e_ld, w_ptr, w_bytes, _stream(stream)]
+    return Prepared("shc_embed_rows_backward", args, 5, n_max, (dY, ids, dE, ws))
+
+
+def embed_rows_backward(dY, ids, dE, scale: float = 1.0, pad_id: int = -1,
+                        accumulate: bool = False, ws=None, stream=None):
+    """shc_embed_rows_backward over all of ids; returns dE."""
+    prepare_embed_rows_backward(dY, ids, dE, scale, pad_id, accumulate, ws, stream)(ids.numel())
+    return dE
+
+
+def prepare_layer_norm(x, gamma, beta, y, mean=None, rstd=None, eps: float = 1e-5,
+                       stream=None) -> Prepared:
+    """shc_layer_norm; gamma, beta [C] fp32 or None; mean, rstd [n] fp32 or None."""
+    o = _Operands()
+    x_ptr, x_ld, n, C = o.rows(x, "x")
+    dt = _dtype_code(x)
+    y_ptr, y_ld, n_y, _ = o.rows(y, "y", x.dtype, C)
+    f32 = torch.float32
+    n_max = min(n, n_y)
+    args = [x_ptr, x_ld, 0, C, o.array(gamma, "gamma", f32, C, True),
+            o.array(beta, "beta", f32, C, True), float(eps), dt, y_ptr, y_ld,
+            o.array(mean, "mean", f32, n_max, True), o.array(rstd, "rstd", f32, n_max, True),
+            _stream(stream)]
+    return Prepared("shc_layer_norm", args, 2, n_max, (x, gamma, beta, y, mean, rstd))
+
+
+def layer_norm(x, gamma=None, beta=None, y=None, mean=None, rstd=None, eps: float = 1e-5,
+               stream=None):
+    """shc_layer_norm over all rows of x; returns y (made here when None)."""
+    if y is None:
+        y = _new(x.shape, x.dtype, x.device, stream)
+    call = prepare_layer_norm(x, gamma, beta, y, mean, rstd, eps, stream)
+    call(x.shape[0])
+    return y
+
+
+def prepare_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None,
+                                accumulate: bool = False, ws=None, stream=None) -> Prepared:
+    """shc_layer_norm_backward; dx [n][C], dgamma, dbeta [C] fp32, each or None."""
+    o = _Operands()
+    y_ptr, y_ld, n_y, C = o.rows(dy, "dy")
+    dt = _dtype_code(dy)
+    x_ptr, x_ld, n, _ = o.rows(x, "x", dy.dtype, C)
+    n_max = min(n, n_y)
+    d_ptr, d_ld = None, C
+    if dx is not None:
+        d_ptr, d_ld, n_d, _ = o.rows(dx, "dx", dy.dtype, C)
+        n_max = min(n_max, n_d)
+    f32 = torch.float32
+    need = 0
+    if dgamma is not None or dbeta is not None:
+        need = layer_norm_backward_workspace(n_max, C)
+    ws, w_ptr, w_bytes = o.workspace(ws, need, stream)
+    args = [y_ptr, y_ld, x_ptr, x_ld, 0, C, o.array(gamma, "gamma", f32, C, True),
+            o.array(mean, "mean", f32, n_max), o.array(rstd, "rstd", f32, n_max), dt,
+            int(bool(accumulate)), d_ptr, d_ld, o.array(dgamma, "dgamma", f32, C, True),
+            o.array(dbeta, "dbeta", f32, C, True), w_ptr, w_bytes, _stream(stream)]
+    return Prepared("shc_layer_norm_backward", args, 4, n_max,
+                    (dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws))
+
+
+def layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None,
+                        accumulate: bool = False, ws=None, stream=None):
+    """shc_layer_norm_backward over all rows of dy; writes those of dx, dgamma
+    and dbeta that are given."""
+    prepare_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, accumulate, ws,
+                                stream)(dy.shape[0])
+
+
+def _distill(o, logits, top_ids, top_logits):
+    z_ptr, z_ld, n, V = o.rows(logits, "logits")
+    dt = _dtype_code(logits)
+    if top_ids.dim() != 2 or tuple(top_logits.shape) != tuple(top_ids.shape):
+        raise ValueError(f"top_ids {tuple(top_ids.shape)} and top_logits "
+                         f"{tuple(top_logits.shape)} must be [n][k] alike")
+    k = top_ids.shape[1]
+    n_max = min(n, top_ids.shape[0])
+    args = [z_ptr, z_ld, 0, V, o.array(top_ids, "top_ids", torch.int32, n_max * k),
+            o.array(top_logits, "top_logits", torch.float32, n_max * k), k]
+    return args, dt, n_max, V
+
+
+def prepare_distill_top(logits, top_ids, top_logits, loss, lse=None, temperature: float = 1.0,
+                        ws=None, stream=None) -> Prepared:
+    """shc_distill_top: loss [n] (and lse [n]) fp32 of logits [n][V] against the
+    teacher's top_ids [n][k] int32, top_logits [n][k] fp32."""
+    o = _Operands()
+    args, dt, n_max, V = _distill(o, logits, top_ids, top_logits)
+    f32 = torch.float32
+    args += [float(temperature), dt, o.array(loss, "loss", f32, n_max),
+             o.array(lse, "lse", f32, n_max, True)]
+    ws, w_ptr, w_bytes = o.workspace(ws, distill_top_workspace(n_max, V), stream)
+    args += [w_ptr, w_bytes, _stream(stream)]
+    return Prepared("shc_distill_top", args, 2, n_max, (logits, top_ids, top_logits, loss, lse, ws))
+
+
+def distill_top(logits, top_ids, top_logits, loss=None, lse=None, temperature: float = 1.0,
+                ws=None, stream=None):
+    """shc_distill_top over all rows; returns loss (made here when None)."""
+    if loss is None:
+        loss = _new(logits.shape[0], torch.float32, logits.device, stream)
+    call = prepare_distill_top(logits, top_ids, top_logits, loss, lse, temperature, ws, stream)
+    call(logits.shape[0])
+    return loss
+
+
+def prepare_distill_top_backward(logits, top_ids, top_logits, lse, row_weight, dlogits,
+                                 temperature: float = 1.0, stream=None) -> Prepared:
+    """shc_distill_top_backward: dlogits [n][V] from lse; row_weight [n] fp32 or None."""
+    o = _Operands()
+    args, dt, n_max, V = _distill(o, logits, top_ids, top_logits)
+    d_ptr, d_ld, n_d, _ = o.rows(dlogits, "dlogits", logits.dtype, V)
+    n_max = min(n_max, n_d)
+    f32 = torch.float32
+    args += [float(temperature), o.array(lse, "lse", f32, n_max),
+             o.array(row_weight, "row_weight", f32, n_max, True), dt, d_ptr, d_ld,
+             _stream(stream)]
+    return Prepared("shc_distill_top_backward", args, 2, n_max,
+                    (logits, top_ids, top_logits, lse, row_weight, dlogits))
+
+
+def distill_top_backward(logits, top_ids, top_logits, lse, row_weight=None, dlogits=None,
+                         temperature: float = 1.0, stream=None):
+    """shc_distill_top_backward over all rows; returns dlogits (made here when None)."""
+    if dlogits is None:
+        dlogits = _new(logits.shape, logits.dtype, logits.device, stream)
+    call = prepare_distill_top_backward(logits, top_ids, top_logits, lse, row_weight, dlogits,
+                                        temperature, stream)
+    call(logits.shape[0])
+    return dlogits
+
+
+def prepare_distill_top_step(logits, top_ids, top_logits, row_weight, loss, dlogits,
+                             temperature: float = 1.0, ws=None, stream=None) -> Prepared:
+    """shc_distill_top_step: loss [n] fp32 and dlogits [n][V] in one pass."""
+    o = _Operands()
+    args, dt, n_max, V = _distill(o, logits, top_ids, top_logits)
+    d_ptr, d_ld, n_d, _ = o.rows(dlogits, "dlogits", logits.dtype, V)
+    n_max = min(n_max, n_d)
+    f32 = torch.float32
+    args += [float(temperature), o.array(row_weight, "row_weight", f32, n_max, True), dt,
+             o.array(loss, "loss", f32, n_max), d_ptr, d_ld]
+    ws, w_ptr, w_bytes = o.workspace(ws, distill_top_workspace(n_max, V), stream)
+    args += [w_ptr, w_bytes, _stream(stream)]
+    return Prepared("shc_distill_top_step", args, 2, n_max,
+                    (logits, top_ids, top_logits, row_weight, loss, dlogits, ws))
+
+
+def distill_top_step(logits, top_ids, top_logits, row_weight=None, loss=None, dlogits=None,
+                     temperature: float = 1.0, ws=None, stream=None):
+    """shc_distill_top_step over all rows; returns (loss, dlogits)."""
+    if loss is None:
+        loss = _new(logits.shape[0], torch.float32, logits.device, stream)
+    if dlogits is None:
+        dlogits = _new(logits.shape, logits.dtype, logits.device, stream)
+    call = prepare_distill_top_step(logits, top_ids, top_logits, row_weight, loss, dlogits,
+                                    temperature, ws, stream)
+    call(logits.shape[0])
+    return loss, dlogits

@@ -1187,6 +1187,275 @@ int shc_segment_maxpool(const void* S, const int32_t* row_ptr, int64_t n_rows, i
                     "segment_maxpool launch");
 }
 
+// -- row operators -------------------------------------------------------------
+
+namespace {
+
+constexpr int32_t kMaxEmbedChannels = 65536;
+constexpr int32_t kMaxNormChannels = 16384;
+constexpr int32_t kMaxLogits = 1 << 24;
+constexpr int32_t kMaxTop = 256;
+constexpr int64_t kMaxElements = (int64_t)1 << 40;
+constexpr int64_t kMaxSortedRows = (int64_t)1 << 28;
+
+size_t elem_size(int32_t dtype) { return dtype == SHC_BF16 ? 2 : 4; }
+
+int check_width(const char* name, int32_t C, int32_t most) {
+  if (C <= 0) return fail(SHC_ERR_INVALID_ARG, "%s = %d must be positive", name, C);
+  if (C > most) return fail(SHC_ERR_UNSUPPORTED, "%s = %d exceeds %d", name, C, most);
+  return SHC_OK;
+}
+
+// A row tensor of n rows of C elements, `stride` apart; p may be NULL where
+// `optional` or where there is no row.
+int check_row_tensor(const char* name, const void* p, int64_t n, int32_t C, int64_t stride,
+                     size_t elem, bool optional) {
+  if (p == nullptr) {
+    if (optional || n == 0) return SHC_OK;
+    return fail(SHC_ERR_INVALID_ARG, "%s is NULL", name);
+  }
+  if (reinterpret_cast<uintptr_t>(p) % elem != 0)
+    return fail(SHC_ERR_MISALIGNED, "%s is not aligned to its elements of %zu bytes", name, elem);
+  if (stride < C)
+    return fail(SHC_ERR_INVALID_ARG, "%s: row stride %lld is below the width %d", name,
+                (long long)stride, C);
+  if (stride > kMaxElements || (n > 0 && stride > kMaxElements / n))
+    return fail(SHC_ERR_UNSUPPORTED, "%s: %lld rows of stride %lld reach 2^40 elements", name,
+                (long long)n, (long long)stride);
+  return SHC_OK;
+}
+
+// A contiguous fp32 or int32 array.
+int check_array(const char* name, const void* p, bool optional) {
+  if (p == nullptr)
+    return optional ? SHC_OK : fail(SHC_ERR_INVALID_ARG, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(p) % 4 != 0)
+    return fail(SHC_ERR_MISALIGNED, "%s is not aligned to its elements of 4 bytes", name);
+  return SHC_OK;
+}
+
+int check_ids(const void* ids, int32_t id_type, int64_t id_stride, int64_t n) {
+  if (id_type != SHC_IDS_I32 && id_type != SHC_IDS_I64)
+    return fail(SHC_ERR_UNSUPPORTED, "unknown id type code %d", id_type);
+  if (id_stride < 0 || id_stride > kMaxElements || (n > 0 && id_stride > kMaxElements / n))
+    return fail(SHC_ERR_INVALID_ARG, "id_stride = %lld outside [0, 2^40 / n_rows]",
+                (long long)id_stride);
+  if (n == 0) return SHC_OK;
+  if (ids == nullptr) return fail(SHC_ERR_INVALID_ARG, "ids is NULL");
+  const size_t elem = id_type == SHC_IDS_I64 ? 8 : 4;
+  if (reinterpret_cast<uintptr_t>(ids) % elem != 0)
+    return fail(SHC_ERR_MISALIGNED, "ids is not aligned to its elements of %zu bytes", elem);
+  return SHC_OK;
+}
+
+int check_entries(int64_t R) {
+  if (R <= 0) return fail(SHC_ERR_INVALID_ARG, "n_entries = %lld must be positive", (long long)R);
+  if (R > shc::kMaxEmbedRows)
+    return fail(SHC_ERR_UNSUPPORTED, "n_entries = %lld exceeds 2^22", (long long)R);
+  return SHC_OK;
+}
+
+int check_ws(const void* ws, size_t ws_bytes, size_t need) {
+  if (need == 0) return SHC_OK;
+  if (ws == nullptr) return fail(SHC_ERR_INVALID_ARG, "ws is NULL");
+  if (!aligned16(ws)) return fail(SHC_ERR_MISALIGNED, "ws is not 16-byte aligned");
+  if (ws_bytes < need)
+    return fail(SHC_ERR_CAPACITY, "workspace of %zu bytes is below the %zu needed", ws_bytes, need);
+  return SHC_OK;
+}
+
+int check_flag(const char* name, int32_t flag) {
+  if (flag != 0 && flag != 1)
+    return fail(SHC_ERR_INVALID_ARG, "%s = %d must be 0 or 1", name, flag);
+  return SHC_OK;
+}
+
+int check_distill(const void* logits, int64_t stride, int64_t n, int32_t V, const int32_t* ids,
+                  const float* top, int32_t k, float temperature, int32_t dtype) {
+  SHC_TRY(check_rows(n));
+  SHC_TRY(check_dtype(dtype));
+  SHC_TRY(check_width("V", V, kMaxLogits));
+  SHC_TRY(check_width("k", k, kMaxTop));
+  if (!(temperature > 0.0f) || !std::isfinite(temperature))
+    return fail(SHC_ERR_INVALID_ARG, "temperature = %g must be positive and finite",
+                (double)temperature);
+  SHC_TRY(check_row_tensor("logits", logits, n, V, stride, elem_size(dtype), false));
+  SHC_TRY(check_array("top_ids", ids, n == 0));
+  return check_array("top_logits", top, n == 0);
+}
+
+}  // namespace
+
+int shc_embed_rows(const void* E, int64_t E_stride, int64_t n_entries, const void* ids,
+                   int32_t id_type, int64_t id_stride, int64_t n_rows, int32_t C, float scale,
+                   const void* add, int64_t add_stride, int32_t dtype, void* out,
+                   int64_t out_stride, hipStream_t stream) {
+  g_last_error[0] = 0;
+  SHC_TRY(check_rows(n_rows));
+  SHC_TRY(check_dtype(dtype));
+  SHC_TRY(check_width("C", C, kMaxEmbedChannels));
+  SHC_TRY(check_entries(n_entries));
+  if (!std::isfinite(scale)) return fail(SHC_ERR_INVALID_ARG, "scale must be finite");
+  SHC_TRY(check_ids(ids, id_type, id_stride, n_rows));
+  const size_t e = elem_size(dtype);
+  SHC_TRY(check_row_tensor("E", E, n_rows > 0 ? n_entries : 0, C, E_stride, e, false));
+  SHC_TRY(check_row_tensor("add", add, n_rows, C, add_stride, e, true));
+  SHC_TRY(check_row_tensor("out", out, n_rows, C, out_stride, e, false));
+  if (n_rows == 0) return SHC_OK;
+  return hip_status(shc::launch_embed_rows(E, n_entries, E_stride, ids, id_type == SHC_IDS_I64,
+                                           id_stride, n_rows, C, scale, add, add_stride,
+                                           dtype == SHC_BF16, out, out_stride, stream),
+                    "embed_rows launch");
+}
+
+size_t shc_embed_rows_backward_workspace(int64_t n_rows, int64_t n_entries, int32_t C) {
+  if (n_rows < 0 || n_rows > kMaxSortedRows || n_entries <= 0 || n_entries > shc::kMaxEmbedRows ||
+      C <= 0 || C > kMaxEmbedChannels)
+    return 0;
+  return shc::embed_rows_backward_workspace_bytes(n_rows, n_entries, C);
+}
+
+int shc_embed_rows_backward(const void* dY, int64_t dY_stride, const void* ids, int32_t id_type,
+                            int64_t id_stride, int64_t n_rows, int64_t n_entries, int32_t C,
+                            float scale, int64_t pad_id, int32_t dtype, int32_t accumulate,
+                            float* dE, int64_t dE_stride, void* ws, size_t ws_bytes,
+                            hipStream_t stream) {
+  g_last_error[0] = 0;
+  SHC_TRY(check_rows(n_rows));
+  SHC_TRY(check_dtype(dtype));
+  SHC_TRY(check_width("C", C, kMaxEmbedChannels));
+  SHC_TRY(check_entries(n_entries));
+  if (n_rows > kMaxSortedRows)
+    return fail(SHC_ERR_UNSUPPORTED, "n_rows = %lld exceeds 2^28", (long long)n_rows);
+  if (!std::isfinite(scale)) return fail(SHC_ERR_INVALID_ARG, "scale must be finite");
+  SHC_TRY(check_flag("accumulate", accumulate));
+  SHC_TRY(check_ids(ids, id_type, id_stride, n_rows));
+  SHC_TRY(check_row_tensor("dY", dY, n_rows, C, dY_stride, elem_size(dtype), false));
+  SHC_TRY(check_row_tensor("dE", dE, n_entries, C, dE_stride, 4, false));
+  SHC_TRY(check_ws(ws, ws_bytes, shc_embed_rows_backward_workspace(n_rows, n_entries, C)));
+  return hip_status(shc::launch_embed_rows_backward(dY, dY_stride, ids, id_type == SHC_IDS_I64,
+                                                    id_stride, n_rows, n_entries, C, scale, pad_id,
+                                                    dtype == SHC_BF16, accumulate, dE, dE_stride,
+                                                    ws, stream),
+                    "embed_rows_backward launch");
+}
+
+int shc_layer_norm(const void* x, int64_t x_stride, int64_t n_rows, int32_t C, const float* gamma,
+                   const float* beta, float eps, int32_t dtype, void* y, int64_t y_stride,
+                   float* mean, float* rstd, hipStream_t stream) {
+  g_last_error[0] = 0;
+  SHC_TRY(check_rows(n_rows));
+  SHC_TRY(check_dtype(dtype));
+  SHC_TRY(check_width("C", C, kMaxNormChannels));
+  if (!(eps > 0.0f) || !std::isfinite(eps))
+    return fail(SHC_ERR_INVALID_ARG, "eps = %g must be positive and finite", (double)eps);
+  const size_t e = elem_size(dtype);
+  SHC_TRY(check_row_tensor("x", x, n_rows, C, x_stride, e, false));
+  SHC_TRY(check_row_tensor("y", y, n_rows, C, y_stride, e, false));
+  SHC_TRY(check_array("gamma", gamma, true));
+  SHC_TRY(check_array("beta", beta, true));
+  SHC_TRY(check_array("mean", mean, true));
+  SHC_TRY(check_array("rstd", rstd, true));
+  if (n_rows == 0) return SHC_OK;
+  return hip_status(shc::launch_layer_norm(x, x_stride, n_rows, C, gamma, beta, eps,
+                                           dtype == SHC_BF16, y, y_stride, mean, rstd, stream),
+                    "layer_norm launch");
+}
+
+size_t shc_layer_norm_backward_workspace(int64_t n_rows, int32_t C) {
+  if (n_rows < 0 || n_rows > INT32_MAX || C <= 0 || C > kMaxNormChannels) return 0;
+  return shc::layer_norm_backward_workspace_bytes(n_rows, C);
+}
+
+int shc_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
+                            int64_t n_rows, int32_t C, const float* gamma, const float* mean,
+                            const float* rstd, int32_t dtype, int32_t accumulate, void* dx,
+                            int64_t dx_stride, float* dgamma, float* dbeta, void* ws,
+                            size_t ws_bytes, hipStream_t stream) {
+  g_last_error[0] = 0;
+  SHC_TRY(check_rows(n_rows));
+  SHC_TRY(check_dtype(dtype));
+  SHC_TRY(check_width("C", C, kMaxNormChannels));
+  SHC_TRY(check_flag("accumulate", accumulate));
+  const size_t e = elem_size(dtype);
+  SHC_TRY(check_row_tensor("dy", dy, n_rows, C, dy_stride, e, false));
+  SHC_TRY(check_row_tensor("x", x, n_rows, C, x_stride, e, false));
+  SHC_TRY(check_row_tensor("dx", dx, n_rows, C, dx_stride, e, true));
+  SHC_TRY(check_array("gamma", gamma, true));
+  SHC_TRY(check_array("mean", mean, n_rows == 0));
+  SHC_TRY(check_array("rstd", rstd, n_rows == 0));
+  SHC_TRY(check_array("dgamma", dgamma, true));
+  SHC_TRY(check_array("dbeta", dbeta, true));
+  if (dgamma != nullptr || dbeta != nullptr)
+    SHC_TRY(check_ws(ws, ws_bytes, shc_layer_norm_backward_workspace(n_rows, C)));
+  return hip_status(shc::launch_layer_norm_backward(dy, dy_stride, x, x_stride, n_rows, C, gamma,
+                                                    mean, rstd, dtype == SHC_BF16, accumulate, dx,
+                                                    dx_stride, dgamma, dbeta, ws, stream),
+                    "layer_norm_backward launch");
+}
+
+size_t shc_distill_top_workspace(int64_t n_rows, int32_t V) {
+  if (n_rows <= 0 || n_rows > INT32_MAX || V <= 0 || V > kMaxLogits) return 0;
+  return shc::distill_workspace_bytes(n_rows, V);
+}
+
+int shc_distill_top(const void* logits, int64_t logits_stride, int64_t n_rows, int32_t V,
+                    const int32_t* top_ids, const float* top_logits, int32_t k,
+                    float temperature, int32_t dtype, float* loss, float* lse, void* ws,
+                    size_t ws_bytes, hipStream_t stream) {
+  g_last_error[0] = 0;
+  SHC_TRY(check_distill(logits, logits_stride, n_rows, V, top_ids, top_logits, k, temperature,
+                        dtype));
+  SHC_TRY(check_array("loss", loss, n_rows == 0));
+  SHC_TRY(check_array("lse", lse, true));
+  if (n_rows == 0) return SHC_OK;
+  SHC_TRY(check_ws(ws, ws_bytes, shc_distill_top_workspace(n_rows, V)));
+  const shc::DistillArgs a{logits, logits_stride, n_rows, V,   top_ids, top_logits, k,
+                           temperature, nullptr, loss, lse, nullptr, 0, ws};
+  return hip_status(shc::launch_distill(a, shc::DistillPass::kForward, dtype == SHC_BF16, stream),
+                    "distill_top launch");
+}
+
+int shc_distill_top_backward(const void* logits, int64_t logits_stride, int64_t n_rows, int32_t V,
+                             const int32_t* top_ids, const float* top_logits, int32_t k,
+                             float temperature, const float* lse, const float* row_weight,
+                             int32_t dtype, void* dlogits, int64_t dlogits_stride,
+                             hipStream_t stream) {
+  g_last_error[0] = 0;
+  SHC_TRY(check_distill(logits, logits_stride, n_rows, V, top_ids, top_logits, k, temperature,
+                        dtype));
+  SHC_TRY(check_array("lse", lse, n_rows == 0));
+  SHC_TRY(check_array("row_weight", row_weight, true));
+  SHC_TRY(check_row_tensor("dlogits", dlogits, n_rows, V, dlogits_stride, elem_size(dtype),
+                           false));
+  if (n_rows == 0) return SHC_OK;
+  const shc::DistillArgs a{logits, logits_stride, n_rows, V, top_ids, top_logits, k, temperature,
+                           row_weight, nullptr, const_cast<float*>(lse), dlogits, dlogits_stride,
+                           nullptr};
+  return hip_status(shc::launch_distill(a, shc::DistillPass::kBackward, dtype == SHC_BF16, stream),
+                    "distill_top_backward launch");
+}
+
+int shc_distill_top_step(const void* logits, int64_t logits_stride, int64_t n_rows, int32_t V,
+                         const int32_t* top_ids, const float* top_logits, int32_t k,
+                         float temperature, const float* row_weight, int32_t dtype, float* loss,
+                         void* dlogits, int64_t dlogits_stride, void* ws, size_t ws_bytes,
+                         hipStream_t stream) {
+  g_last_error[0] = 0;
+  SHC_TRY(check_distill(logits, logits_stride, n_rows, V, top_ids, top_logits, k, temperature,
+                        dtype));
+  SHC_TRY(check_array("row_weight", row_weight, true));
+  SHC_TRY(check_array("loss", loss, n_rows == 0));
+  SHC_TRY(check_row_tensor("dlogits", dlogits, n_rows, V, dlogits_stride, elem_size(dtype),
+                           false));
+  if (n_rows == 0) return SHC_OK;
+  SHC_TRY(check_ws(ws, ws_bytes, shc_distill_top_workspace(n_rows, V)));
+  const shc::DistillArgs a{logits, logits_stride, n_rows, V, top_ids, top_logits, k, temperature,
+                           row_weight, loss, nullptr, dlogits, dlogits_stride, ws};
+  return hip_status(shc::launch_distill(a, shc::DistillPass::kStep, dtype == SHC_BF16, stream),
+                    "distill_top_step launch");
+}
+
 // -- stream-ordering events ---------------------------------------------------
 
 int shc_event_create(void** event) {

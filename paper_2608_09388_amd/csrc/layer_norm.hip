@@ -1,0 +1,361 @@
+// Layer norm over the channels of a row, with weight and bias, and its
+// gradient:
+//
+//   mu = sum(x) / C,  var = sum((x - mu)^2) / C,  rs = 1 / sqrt(var + eps)
+//   y  = (x - mu) rs gamma + beta
+//
+//   h = (x - mu) rs,  g = dy gamma,
+//   dx = rs (g - sum(g) / C - h sum(g h) / C)
+//   dgamma = sum over rows of dy h,  dbeta = sum over rows of dy
+//
+// Both are bound by HBM: a row is read once into registers (G lanes hold NV
+// 16-byte vectors each), reduced there, and written.  The variance is taken
+// from the deviations of the values in registers, so a large mean costs no
+// digits.  A group of lanes walks rows a grid apart with gamma (and beta, or
+// the two column sums) in registers and the next row's vectors in flight.
+//
+// The column sums dgamma and dbeta: every thread sums its columns over its
+// rows, the groups of a workgroup are added in LDS in order, every workgroup
+// writes one partial row to the workspace, and a second launch adds the
+// partial rows in a fixed order.  The number of workgroups follows the sizes
+// alone, so results repeat bit for bit.
+#include <algorithm>
+
+#include "row_ops.h"
+
+namespace shc {
+namespace {
+
+using namespace rowops;
+
+template <typename T, int G, int NV>
+__global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_kernel(
+    const T* __restrict__ x, int64_t ldx, int64_t n, int C, const float* __restrict__ gamma,
+    const float* __restrict__ beta, float eps, T* __restrict__ y, int64_t ldy,
+    float* __restrict__ mean, float* __restrict__ rstd) {
+  constexpr int N = Row<T>::N, BLOCK = G > 256 ? G : 256, R = BLOCK / G;
+  __shared__ float part[G > 64 ? BLOCK / 64 : 1];
+  const int lane = threadIdx.x % G;
+  const int nvec = (C + N - 1) / N;
+  const float inv_c = 1.0f / (float)C;
+  // a group of more than a wavefront has LDS partials of its own
+  float* my_part = G > 64 ? part + (threadIdx.x / G) * (G / 64) : part;
+
+  float ga[NV][N], be[NV][N];
+#pragma unroll
+  for (int q = 0; q < NV; ++q) {
+    const int v = q * G + lane;
+#pragma unroll
+    for (int e = 0; e < N; ++e) ga[q][e] = 1.f, be[q][e] = 0.f;
+    if (v < nvec) {
+      if (gamma != nullptr) load_channels<N>(gamma, v, C, ga[q]);
+      if (beta != nullptr) load_channels<N>(beta, v, C, be[q]);
+    }
+  }
+  const int64_t step = (int64_t)gridDim.x * R;
+  int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / G;
+  i32x4 cur[NV];
+  auto fetch = [&](int64_t r, i32x4* to) {
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      const int v = q * G + lane;
+      to[q] = v < nvec ? load_vec(x + r * ldx, v, C) : i32x4{};
+    }
+  };
+  if (row < n) fetch(row, cur);
+  // with a barrier in the reduction (R == 1) every thread of the workgroup has
+  // the same row, so the loop's length is uniform
+  for (; row < n; row += step) {
+    i32x4 next[NV];
+    if (row + step < n) fetch(row + step, next);
+    float sum = 0.f;
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      float f[N];
+      Row<T>::widen(cur[q], f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum += f[e];  // past the row's end: zeros
+    }
+    const float mu = group_reduce<G>(sum, AddOp{}, my_part) * inv_c;
+    float sq = 0.f;
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      const int left = C - (q * G + lane) * N;
+      float f[N];
+      Row<T>::widen(cur[q], f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float d = f[e] - mu;
+        if (e < left) sq = fmaf(d, d, sq);
+      }
+    }
+    const float var = group_reduce<G>(sq, AddOp{}, my_part) * inv_c;
+    const float rs = 1.0f / sqrtf(var + eps);
+    if (lane == 0) {
+      if (mean != nullptr) mean[row] = mu;
+      if (rstd != nullptr) rstd[row] = rs;
+    }
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      const int v = q * G + lane;
+      if (v < nvec) {
+        float f[N];
+        Row<T>::widen(cur[q], f);
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = fmaf((f[e] - mu) * rs, ga[q][e], be[q][e]);
+        store_vec(y + row * ldy, v, C, Row<T>::narrow(f));
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < NV; ++q) cur[q] = next[q];
+  }
+}
+
+template <typename T, int G, int NV>
+__global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_backward_kernel(
+    const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx, int64_t n,
+    int C, const float* __restrict__ gamma, const float* __restrict__ mean,
+    const float* __restrict__ rstd, T* __restrict__ dx, int64_t lddx, float* __restrict__ col) {
+  constexpr int N = Row<T>::N, BLOCK = G > 256 ? G : 256, R = BLOCK / G;
+  __shared__ float part[G > 64 ? BLOCK / 64 : 1];
+  // column sums of the workgroup's groups (R > 1), one group's at a time
+  __shared__ float cols[R > 1 ? 2 * G * NV * N : 1];
+  const int lane = threadIdx.x % G;
+  const int nvec = (C + N - 1) / N;
+  const float inv_c = 1.0f / (float)C;
+  float* my_part = G > 64 ? part + (threadIdx.x / G) * (G / 64) : part;
+
+  float ga[NV][N], dg[NV][N], db[NV][N];
+#pragma unroll
+  for (int q = 0; q < NV; ++q) {
+    const int v = q * G + lane;
+#pragma unroll
+    for (int e = 0; e < N; ++e) ga[q][e] = 1.f, dg[q][e] = 0.f, db[q][e] = 0.f;
+    if (v < nvec && gamma != nullptr) load_channels<N>(gamma, v, C, ga[q]);
+  }
+  const int64_t step = (int64_t)gridDim.x * R;
+  int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / G;
+  i32x4 cx[NV], cy[NV];
+  float cmu = 0.f, crs = 0.f;
+  auto fetch = [&](int64_t r, i32x4* tx, i32x4* ty, float* mu, float* rs) {
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      const int v = q * G + lane;
+      tx[q] = v < nvec ? load_vec(x + r * ldx, v, C) : i32x4{};
+      ty[q] = v < nvec ? load_vec(dy + r * lddy, v, C) : i32x4{};
+    }
+    *mu = mean[r];
+    *rs = rstd[r];
+  };
+  if (row < n) fetch(row, cx, cy, &cmu, &crs);
+  for (; row < n; row += step) {
+    i32x4 nx[NV], ny[NV];
+    float nmu = 0.f, nrs = 0.f;
+    if (row + step < n) fetch(row + step, nx, ny, &nmu, &nrs);
+    float sg = 0.f, sgh = 0.f;  // past the row's end dy = 0: nothing is added
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      float fx[N], fy[N];
+      Row<T>::widen(cx[q], fx);
+      Row<T>::widen(cy[q], fy);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float h = (fx[e] - cmu) * crs, g = fy[e] * ga[q][e];
+        sg += g;
+        sgh = fmaf(g, h, sgh);
+        dg[q][e] = fmaf(fy[e], h, dg[q][e]);
+        db[q][e] += fy[e];
+      }
+    }
+    if (dx != nullptr) {
+      const float mg = group_reduce<G>(sg, AddOp{}, my_part) * inv_c;
+      const float mgh = group_reduce<G>(sgh, AddOp{}, my_part) * inv_c;
+#pragma unroll
+      for (int q = 0; q < NV; ++q) {
+        const int v = q * G + lane;
+        if (v < nvec) {
+          float fx[N], fy[N];
+          Row<T>::widen(cx[q], fx);
+          Row<T>::widen(cy[q], fy);
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const float h = (fx[e] - cmu) * crs;
+            fx[e] = crs * (fmaf(fy[e], ga[q][e], -mg) - h * mgh);
+          }
+          store_vec(dx + row * lddx, v, C, Row<T>::narrow(fx));
+        }
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < NV; ++q) cx[q] = nx[q], cy[q] = ny[q];
+    cmu = nmu;
+    crs = nrs;
+  }
+  if (col == nullptr) return;
+  // the groups' sums, added one group after the other
+  if constexpr (R > 1) {
+    for (int r = 1; r < R; ++r) {
+      __syncthreads();
+      if (threadIdx.x / G == r) {
+#pragma unroll
+        for (int q = 0; q < NV; ++q)
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            cols[((q * N + e) * 2) * G + lane] = dg[q][e];
+            cols[((q * N + e) * 2 + 1) * G + lane] = db[q][e];
+          }
+      }
+      __syncthreads();
+      if (threadIdx.x < G) {
+#pragma unroll
+        for (int q = 0; q < NV; ++q)
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            dg[q][e] += cols[((q * N + e) * 2) * G + lane];
+            db[q][e] += cols[((q * N + e) * 2 + 1) * G + lane];
+          }
+      }
+    }
+  }
+  if (threadIdx.x < G) {
+    float* out = col + (int64_t)blockIdx.x * 2 * C;
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      const int v = q * G + lane;
+      if (v < nvec) {
+        store_channels<N>(out, v, C, dg[q]);
+        store_channels<N>(out + C, v, C, db[q]);
+      }
+    }
+  }
+}
+
+// Adds `parts` partial rows of 2 C columns (dgamma, then dbeta): 32 columns a
+// workgroup, the rows in 32 interleaved shares added in order through LDS.
+__global__ __launch_bounds__(1024) void column_sum_kernel(const float* __restrict__ col, int parts,
+                                                          int C, int accumulate,
+                                                          float* __restrict__ dgamma,
+                                                          float* __restrict__ dbeta) {
+  __shared__ float s[32][33];
+  const int c = threadIdx.x & 31, share = threadIdx.x >> 5;
+  const int at = blockIdx.x * 32 + c;
+  float a = 0.f;
+  if (at < 2 * C)
+    for (int p = share; p < parts; p += 32) a += col[(int64_t)p * 2 * C + at];
+  s[share][c] = a;
+  __syncthreads();
+  if (share != 0 || at >= 2 * C) return;
+  float* out = at < C ? dgamma : dbeta;
+  if (out == nullptr) return;
+  out += at < C ? at : at - C;
+  for (int q = 1; q < 32; ++q) a += s[q][c];
+  *out = accumulate ? *out + a : a;
+}
+
+// Calls f with the lanes of a row and the vectors a lane, as types, for rows of
+// nvec vectors (up to 16,384 channels).
+template <typename T, typename F>
+auto with_shape(int nvec, F&& f) {
+  using std::integral_constant;
+#define SHC_SHAPE(limit, g, v) \
+  if (nvec <= limit) return f(integral_constant<int, g>{}, integral_constant<int, v>{})
+  SHC_SHAPE(16, 16, 1);
+  SHC_SHAPE(32, 32, 1);
+  SHC_SHAPE(64, 64, 1);
+  SHC_SHAPE(128, 64, 2);
+  SHC_SHAPE(256, 256, 1);
+  SHC_SHAPE(512, 256, 2);
+  SHC_SHAPE(1024, 512, 2);
+  if constexpr (sizeof(T) == 4) {
+    SHC_SHAPE(2048, 1024, 2);
+    return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+  } else {
+    return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  }
+#undef SHC_SHAPE
+}
+
+template <typename T>
+int vectors_of(int32_t C) {
+  return (C + Row<T>::N - 1) / Row<T>::N;
+}
+
+// Workgroups of the row kernels: enough to fill the CUs several times over,
+// few enough that gamma is read (and a partial row of column sums written) once
+// per many rows.
+int norm_blocks(int64_t n, int G, int per_cu) {
+  const int rows = G > 256 ? 1 : 256 / G;
+  const int64_t need = (n + rows - 1) / rows;
+  return (int)std::min<int64_t>(need, 256 * per_cu);
+}
+
+template <typename T>
+int backward_blocks(int64_t n, int32_t C) {
+  return with_shape<T>(vectors_of<T>(C), [&](auto g, auto) {
+    return norm_blocks(n, decltype(g)::value, 2);
+  });
+}
+
+template <typename T>
+hipError_t norm(const void* x, int64_t ldx, int64_t n, int32_t C, const float* gamma,
+                const float* beta, float eps, void* y, int64_t ldy, float* mean, float* rstd,
+                hipStream_t stream) {
+  return with_shape<T>(vectors_of<T>(C), [&](auto g, auto v) {
+    constexpr int G = decltype(g)::value, NV = decltype(v)::value;
+    layer_norm_kernel<T, G, NV><<<norm_blocks(n, G, 4), G > 256 ? G : 256, 0, stream>>>(
+        static_cast<const T*>(x), ldx, n, C, gamma, beta, eps, static_cast<T*>(y), ldy, mean,
+        rstd);
+    return hipGetLastError();
+  });
+}
+
+template <typename T>
+hipError_t norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t n,
+                         int32_t C, const float* gamma, const float* mean, const float* rstd,
+                         void* dx, int64_t lddx, float* col, hipStream_t stream) {
+  return with_shape<T>(vectors_of<T>(C), [&](auto g, auto v) {
+    constexpr int G = decltype(g)::value, NV = decltype(v)::value;
+    layer_norm_backward_kernel<T, G, NV>
+        <<<norm_blocks(n, G, 2), G > 256 ? G : 256, 0, stream>>>(
+            static_cast<const T*>(dy), lddy, static_cast<const T*>(x), ldx, n, C, gamma, mean,
+            rstd, static_cast<T*>(dx), lddx, col);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace
+
+size_t layer_norm_backward_workspace_bytes(int64_t n, int32_t C) {
+  // the larger of the two dtypes' partial rows: the caller's dtype need not be known
+  const int b = std::max(backward_blocks<float>(n, C), backward_blocks<uint16_t>(n, C));
+  return (size_t)b * 2 * (size_t)C * sizeof(float);
+}
+
+hipError_t launch_layer_norm(const void* x, int64_t ldx, int64_t n, int32_t C, const float* gamma,
+                             const float* beta, float eps, int is_bf16, void* y, int64_t ldy,
+                             float* mean, float* rstd, hipStream_t stream) {
+  return (is_bf16 ? norm<uint16_t> : norm<float>)(x, ldx, n, C, gamma, beta, eps, y, ldy, mean,
+                                                  rstd, stream);
+}
+
+hipError_t launch_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                                      int64_t n, int32_t C, const float* gamma, const float* mean,
+                                      const float* rstd, int is_bf16, int accumulate, void* dx,
+                                      int64_t lddx, float* dgamma, float* dbeta, void* ws,
+                                      hipStream_t stream) {
+  const bool want_cols = dgamma != nullptr || dbeta != nullptr;
+  float* col = want_cols ? static_cast<float*>(ws) : nullptr;
+  int blocks = 0;
+  if (n > 0 && (want_cols || dx != nullptr)) {
+    blocks = is_bf16 ? backward_blocks<uint16_t>(n, C) : backward_blocks<float>(n, C);
+    const hipError_t e = (is_bf16 ? norm_backward<uint16_t> : norm_backward<float>)(
+        dy, lddy, x, ldx, n, C, gamma, mean, rstd, dx, lddx, col, stream);
+    if (e != hipSuccess) return e;
+  }
+  if (!want_cols || (n == 0 && accumulate)) return hipSuccess;
+  column_sum_kernel<<<(2 * C + 31) / 32, 1024, 0, stream>>>(col, blocks, C, accumulate, dgamma,
+                                                           dbeta);
+  return hipGetLastError();
+}
+
+}  // namespace shc

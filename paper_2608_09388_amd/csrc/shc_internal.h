@@ -295,4 +295,49 @@ hipError_t launch_conv_packed_planned(const void* S, const void* plan, int64_t n
                                       int32_t Cout, int32_t relu, void* out, int num_cus,
                                       hipStream_t stream);
 
+// embedding rows and their gradient by sorted ids (embed.hip); strides in
+// elements, ids int64 where id64, int32 otherwise
+constexpr int64_t kMaxEmbedRows = 1 << 22;
+hipError_t launch_embed_rows(const void* E, int64_t R, int64_t ldE, const void* ids, int id64,
+                             int64_t id_stride, int64_t n, int32_t C, float scale, const void* add,
+                             int64_t ldadd, int is_bf16, void* out, int64_t ldout,
+                             hipStream_t stream);
+size_t embed_rows_backward_workspace_bytes(int64_t n, int64_t R, int32_t C);
+hipError_t launch_embed_rows_backward(const void* dY, int64_t lddy, const void* ids, int id64,
+                                      int64_t id_stride, int64_t n, int64_t R, int32_t C,
+                                      float scale, int64_t pad, int is_bf16, int accumulate,
+                                      float* dE, int64_t ldE, void* ws, hipStream_t stream);
+
+// layer norm of rows and its gradient (layer_norm.hip)
+hipError_t launch_layer_norm(const void* x, int64_t ldx, int64_t n, int32_t C, const float* gamma,
+                             const float* beta, float eps, int is_bf16, void* y, int64_t ldy,
+                             float* mean, float* rstd, hipStream_t stream);
+size_t layer_norm_backward_workspace_bytes(int64_t n, int32_t C);
+hipError_t launch_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                                      int64_t n, int32_t C, const float* gamma, const float* mean,
+                                      const float* rstd, int is_bf16, int accumulate, void* dx,
+                                      int64_t lddx, float* dgamma, float* dbeta, void* ws,
+                                      hipStream_t stream);
+
+// distillation from a teacher's top logits (distill.hip)
+struct DistillArgs {
+  const void* z;  // [n] rows of V logits, ldz apart
+  int64_t ldz, n;
+  int32_t V;
+  const int32_t* ids;  // [n][k]
+  const float* top;    // [n][k]
+  int32_t k;
+  float temp;
+  const float* weight;  // [n] or null: the rows' upstream gradient
+  float* loss;          // [n] (forward, step)
+  float* lse;           // [n] (forward: out or null; backward: in; step: null)
+  void* dz;             // [n] rows, lddz apart (backward, step)
+  int64_t lddz;
+  void* parts;  // workspace
+};
+enum class DistillPass { kForward, kBackward, kStep };
+size_t distill_workspace_bytes(int64_t n, int32_t V);
+hipError_t launch_distill(const DistillArgs& a, DistillPass pass, int is_bf16,
+                          hipStream_t stream);
+
 }  // namespace shc
