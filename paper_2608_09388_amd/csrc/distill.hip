@@ -12,16 +12,15 @@
 // entries has loss 0 and gradient 0 and its logits are not read.
 //
 // Bound by HBM: V elements read, and V written by the gradient.
-// - Rows that fit a workgroup's registers (up to 16 vectors a thread) are read
-//   once, by G lanes: maximum, sum, loss and, in the step, the gradient from the
-//   registers.
-// - Longer rows, and long rows of which there are few, are cut into parts: a
-//   first launch leaves every part's maximum and sum in the workspace, the
-//   second joins them in order and computes the loss or its part of the
-//   gradient.
-// The gradient writes w T q first; the k entries are corrected behind a fence
-// by the lanes that share the row, entries of the same id all with the id's
-// whole p, added in their order.
+// - Rows of up to 4096 vectors are read once, into the registers of the G threads
+//   that share them: maximum, sum, loss and gradient from there.
+// - A workgroup of 1024 threads reads a longer row twice, the second time from
+//   the caches (256 rows in flight fit the Infinity Cache).
+// - Long rows of which there are few are cut into parts: a first launch leaves
+//   every part's maximum and sum in the workspace, the second joins them in order
+//   and computes the loss or its part of the gradient.
+// The gradient writes w T q first; the k entries are corrected behind a fence,
+// entries of the same id all with the id's whole p, added in their order.
 #include <algorithm>
 
 #include "row_ops.h"
@@ -54,158 +53,356 @@ struct RowSoftmax {
   float m, l;
 };
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
-// What a sum over a maximum m becomes over `base` >= m; 0 where there was no
-// logit yet (m = -inf: the sum is 0, and base may be far below 0).
-__device__ __forceinline__ float rescale(float m, float base, float c) {
-  return m == -INFINITY ? 0.f : exp2_hw((m - base) * c);
-}
 __device__ __forceinline__ float prob(float z, const RowSoftmax& r, float c) {
   return z == -INFINITY ? 0.f : exp2_hw((z - r.m) * c - r.l);
 }
 
-// The teacher's entries of a row, by the G lanes that share it: ids (-1 where
-// there is none) and p to LDS.  Returns whether the row has any.
-struct Teacher {
-  float tm, l;  // log2 p_j = (t_j - tm) c - l
-  bool live;
+// The teacher's entries of a row, in LDS: id (-1 where there is none), its own p,
+// the p of all the row's entries with that id, and the logit there.
+__host__ __device__ constexpr int entry_slots(int k) { return (k + 3) & ~3; }
+__host__ __device__ constexpr int entry_words(int k) { return 4 * entry_slots(k); }
+struct Entries {
+  int* id;
+  float *p, *all, *z;
+  __device__ __forceinline__ Entries(int* lds, int k)
+      : id(lds), p(reinterpret_cast<float*>(lds) + entry_slots(k)), all(p + entry_slots(k)),
+        z(all + entry_slots(k)) {}
 };
-template <int G>
-__device__ __forceinline__ Teacher teach(const int32_t* __restrict__ ids,
-                                         const float* __restrict__ top, int k, int V, float c,
-                                         int lane, float* red, int* sid, float* sp) {
+
+// Fills them, by L lanes of one wavefront; whether the row has any.  All of it,
+// the logits' gather and the comparison of the ids too, is done before the
+// row's maximum is needed, beside the loads of the row.
+template <typename T, int L, bool GRAD>
+__device__ __forceinline__ bool teach(const T* __restrict__ z, const int32_t* __restrict__ ids,
+                                      const float* __restrict__ top, int k, int V, float c,
+                                      int lane, const Entries& en) {
   float tm = -INFINITY, any = 0.f;
-  for (int e = lane; e < k; e += G) {
+  for (int e = lane; e < k; e += L) {
     const int id = ids[e];
     const float t = top[e];
     const bool ok = id >= 0 && id < V && t != -INFINITY;
-    sid[e] = ok ? id : -1;
-    sp[e] = t;
+    en.id[e] = ok ? id : -1;
+    en.p[e] = t;
     if (ok) {
+      en.z[e] = Row<T>::get(z + id);
       tm = fmaxf(tm, t);
       any = 1.f;
     }
   }
-  Teacher out;
-  out.tm = finite_max(group_reduce<G>(tm, MaxOp{}, red));
-  out.live = group_reduce<G>(any, MaxOp{}, red) != 0.f;
+  tm = finite_max(lanes_reduce<L>(tm, MaxOp{}));
+  if (lanes_reduce<L>(any, MaxOp{}) == 0.f) return false;
   float s = 0.f;
-  for (int e = lane; e < k; e += G)
-    if (sid[e] >= 0) s += exp2_hw((sp[e] - out.tm) * c);
-  s = group_reduce<G>(s, AddOp{}, red);
-  out.l = log2_hw(s);
-  for (int e = lane; e < k; e += G)
-    sp[e] = sid[e] >= 0 ? exp2_hw((sp[e] - out.tm) * c) / s : 0.f;
-  group_fence<G>();
-  return out;
+  for (int e = lane; e < k; e += L)
+    if (en.id[e] >= 0) s += exp2_hw((en.p[e] - tm) * c);
+  s = lanes_reduce<L>(s, AddOp{});
+  for (int e = lane; e < k; e += L)
+    en.p[e] = en.id[e] >= 0 ? exp2_hw((en.p[e] - tm) * c) / s : 0.f;
+  if constexpr (GRAD) {
+    const int slots = entry_slots(k);
+    if (lane < slots - k) {  // the last four are whole: no id of the row's
+      en.id[k + lane] = -2;
+      en.p[k + lane] = 0.f;
+    }
+    group_fence<64>();
+    for (int e = lane; e < k; e += L) {
+      const int id = en.id[e];
+      float p = 0.f;
+#pragma unroll 4
+      for (int o = 0; o < slots; o += 4) {
+        const i32x4 ids4 = *reinterpret_cast<const i32x4*>(en.id + o);
+        const f32x4 p4 = *reinterpret_cast<const f32x4*>(en.p + o);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) p += ids4[q] == id ? p4[q] : 0.f;
+      }
+      en.all[e] = p;
+    }
+  }
+  return true;
 }
 
-// sum_j p_j (log p_j - log q_j) over the row's entries (z, top: the row's), in
-// natural units: an entry on a logit of the type's lowest value stays finite.
-template <typename T, int G>
-__device__ __forceinline__ float loss_terms(const T* __restrict__ z,
-                                            const float* __restrict__ top, int k, float temp,
-                                            const Teacher& t, const RowSoftmax& r, int lane,
-                                            float* red, const int* sid, const float* sp) {
+// sum_j p_j (log p_j - log q_j) over the row's entries, in natural units: an
+// entry on a logit of the type's lowest value stays finite.  By the lanes that
+// filled them.
+template <int L>
+__device__ __forceinline__ float loss_terms(int k, float temp, const RowSoftmax& r, int lane,
+                                            const Entries& en) {
   float a = 0.f;
-  for (int e = lane; e < k; e += G) {
-    if (sid[e] < 0) continue;
-    const float zi = Row<T>::get(z + sid[e]), p = sp[e];
+  for (int e = lane; e < k; e += L) {
+    const float p = en.p[e];
+    if (en.id[e] < 0 || p == 0.f) continue;
+    const float zi = en.z[e];
     const float lq = zi == -INFINITY ? -INFINITY : (zi - r.m) / temp - kLn2 * r.l;
-    const float lp = (top[e] - t.tm) / temp - kLn2 * t.l;
-    if (!(p == 0.f)) a += p * (lp - lq);
+    a += p * (kLn2 * log2_hw(p) - lq);
   }
-  return group_reduce<G>(a, AddOp{}, red);
+  return lanes_reduce<L>(a, AddOp{});
 }
 
-// The entries with ids in [lo, hi) of the gradient, behind the row's q.
-template <typename T, int G>
-__device__ __forceinline__ void fix_entries(const T* __restrict__ z, T* dz, int k, float c,
-                                            float wt, const RowSoftmax& r, int lane, int lo,
-                                            int hi, const int* sid, const float* sp) {
-  for (int e = lane; e < k; e += G) {
-    const int id = sid[e];
-    if (id < lo || id >= hi) continue;
-    float p = 0.f;
-    for (int o = 0; o < k; ++o) p += sid[o] == id ? sp[o] : 0.f;
-    Row<T>::put(dz + id, wt * (prob(Row<T>::get(z + id), r, c) - p));
+// The entries with ids in [lo, hi) of the gradient, behind the row's q, by the
+// lanes that filled them.
+template <typename T, int L>
+__device__ __forceinline__ void fix_entries(T* dz, int k, float c, float wt, const RowSoftmax& r,
+                                            int lane, int lo, int hi, const Entries& en) {
+  for (int e = lane; e < k; e += L) {
+    const int id = en.id[e];
+    if (id >= lo && id < hi) Row<T>::put(dz + id, wt * (prob(en.z[e], r, c) - en.all[e]));
   }
 }
 
-// Rows in registers: G lanes hold NV vectors each.
-template <typename T, int G, int NV, bool STEP>
+// Largest logit among vectors of a row.  bf16 pairs are compared as 16-bit
+// integers, two to an instruction and without widening: among patterns with a
+// positive one the signed maximum is the largest value, among negative ones the
+// unsigned minimum is.
+template <typename T>
+struct VecMax;
+template <>
+struct VecMax<float> {
+  float m = -INFINITY;
+  __device__ __forceinline__ void take(const i32x4& v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m = fmaxf(m, __int_as_float(v[e]));
+  }
+  __device__ __forceinline__ float value() const { return m; }
+};
+template <>
+struct VecMax<uint16_t> {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  s16x2 hi = {(short)0xFF80, (short)0xFF80};                    // -inf
+  u16x2 lo = {(unsigned short)0xFF80, (unsigned short)0xFF80};  // -inf
+  __device__ __forceinline__ void take(const i32x4& v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int pair = v[e];  // a bit cast of the element itself reads element 0
+      hi = __builtin_elementwise_max(hi, __builtin_bit_cast(s16x2, pair));
+      lo = __builtin_elementwise_min(lo, __builtin_bit_cast(u16x2, pair));
+    }
+  }
+  __device__ __forceinline__ float value() const {
+    const short h = hi[0] > hi[1] ? hi[0] : hi[1];
+    const unsigned short l = lo[0] < lo[1] ? lo[0] : lo[1];
+    return bf16_bits_to_f32(h >= 0 ? (uint16_t)h : l);
+  }
+};
+
+// A row's exponents as one operation: x = z c - mc, mc = m c rounded.  Any
+// constant in its place gives the same q, so its rounding costs nothing as long
+// as 2^x stays in range: the rounding of mc below 2^20 moves x by less than 1/8.
+// Larger ones (logits of 10^5 and more) take (z - m) c.
+constexpr float kFar = 1048576.f;
+struct Exponent {
+  float c, mc, m;
+  bool near;
+  __device__ __forceinline__ Exponent(float m_, float c_) : c(c_), mc(m_ * c_), m(m_) {
+    near = fabsf(mc) < kFar;
+  }
+  // log2 of sum 2^((z - m) c) from the sum of 2^x
+  __device__ __forceinline__ float log_sum(float s) const {
+    return near ? log2_hw(s) - fmaf(m, c, -mc) : log2_hw(s);
+  }
+};
+template <typename T, bool NEAR>
+__device__ __forceinline__ float exp_sum(const i32x4& v, const Exponent& x, float s) {
+  constexpr int N = Row<T>::N;
+  float f[N];
+  Row<T>::widen(v, f);
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    s += exp2_hw(NEAR ? fmaf(f[e], x.c, -x.mc) : (f[e] - x.m) * x.c);
+  return s;
+}
+template <typename T, bool NEAR>
+__device__ __forceinline__ i32x4 exp_scaled(const i32x4& v, const Exponent& x, float by) {
+  constexpr int N = Row<T>::N;
+  float f[N];
+  Row<T>::widen(v, f);
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    f[e] = by * exp2_hw(NEAR ? fmaf(f[e], x.c, -x.mc) : (f[e] - x.m) * x.c);
+  return Row<T>::narrow(f);
+}
+
+// A thread's running maximum and sum over vectors that it does not keep: the sum
+// is of 2^(z c - mc) with mc the maximum's z c, or -kFar where that is lower (no
+// logit yet, or masks of the lowest value: next to a row's maximum above it they
+// add nothing, and a row whose maximum is that far from 0 is summed again).
+template <typename T>
+struct RunningSum {
+  float m = -INFINITY, mc = -kFar, s = 0.f;
+  template <int U>
+  __device__ __forceinline__ void take(const i32x4 (&v)[U], float c) {
+    VecMax<T> vm;
+#pragma unroll
+    for (int u = 0; u < U; ++u) vm.take(v[u]);
+    m = fmaxf(m, vm.value());
+    over(fmaxf(m * c, mc));
+    Exponent x(0.f, c);
+    x.mc = mc;
+#pragma unroll
+    for (int u = 0; u < U; ++u) s = exp_sum<T, true>(v[u], x, s);
+  }
+  __device__ __forceinline__ void over(float to) {  // mc = to >= mc
+    s *= exp2_hw(mc - to);
+    mc = to;
+  }
+};
+
+// What the threads that share a row tell each other; one barrier a value.
+template <int G>
+struct GroupShare {
+  float m[G / 64], s[G / 64];
+  int live;
+};
+template <>
+struct GroupShare<8> {};
+template <>
+struct GroupShare<16> {};
+template <>
+struct GroupShare<32> {};
+template <>
+struct GroupShare<64> {};
+
+enum class Pass { kForward, kBackward, kStep };
+
+// A row of logits by the G threads of a wavefront's part, a wavefront or the
+// workgroup.  NV > 0: the row is held in registers, NV vectors a thread, and read
+// once.  NV = 0: it is read twice, the second time from the caches, where the
+// stores of the gradient pass by them (non-temporal).
+template <typename T, int G, int NV, Pass PASS>
 __global__ __launch_bounds__(G > 256 ? G : 256) void distill_row_kernel(
     const T* __restrict__ z, int64_t ldz, int64_t n, int V, const int32_t* __restrict__ ids,
     const float* __restrict__ top, int k, float temp, const float* __restrict__ weight,
     float* __restrict__ loss, float* __restrict__ lse, T* __restrict__ dz, int64_t lddz) {
   constexpr int N = Row<T>::N, BLOCK = G > 256 ? G : 256, R = BLOCK / G;
-  extern __shared__ int smem[];  // per group: k ids, k probabilities
-  __shared__ float part[G > 64 ? BLOCK / 64 : 1];
+  constexpr int L = G < 64 ? G : 64;  // the lanes that take the teacher's entries
+  constexpr int U = 4;                // vectors in flight of a row read twice
+  extern __shared__ __align__(16) int smem[];       // the groups' entries
+  __shared__ GroupShare<G> sh;
   const int lane = threadIdx.x % G, group = threadIdx.x / G;
-  int* sid = smem + (int64_t)group * 2 * k;
-  float* sp = reinterpret_cast<float*>(sid + k);
+  const Entries en(smem + group * entry_words(k), k);
   const int64_t row = (int64_t)blockIdx.x * R + group;
   if (row >= n) return;  // whole groups
   const float c = kLog2E / temp;
   const T* zr = z + row * ldz;
+  T* dr = PASS == Pass::kForward ? nullptr : dz + row * lddz;
   const int nvec = (V + N - 1) / N;
 
-  i32x4 raw[NV];
+  i32x4 raw[NV > 0 ? NV : 1];
 #pragma unroll
   for (int q = 0; q < NV; ++q) raw[q] = load_logits(zr, q * G + lane, V);
-  const Teacher t = teach<G>(ids + row * k, top + row * k, k, V, c, lane, part, sid, sp);
-  if (!t.live) {
-    if (lane == 0) {
-      loss[row] = 0.f;
-      if (!STEP && lse != nullptr) lse[row] = 0.f;
-    }
-    if constexpr (STEP) {
+  const float w = PASS != Pass::kForward && weight != nullptr ? weight[row] : 1.f;
+  float saved = PASS == Pass::kBackward ? lse[row] : 0.f;
+  bool live = false;
+  if (lane < L)
+    live = teach<T, L, PASS != Pass::kForward>(zr, ids + row * k, top + row * k, k, V, c, lane,
+                                               en);
+
+  // maximum; a row read twice has its sum over the running maximum too
+  float m = -INFINITY, s = 0.f;
+  RunningSum<T> run;
+  if constexpr (PASS != Pass::kBackward) {
+    if constexpr (NV > 0) {
+      VecMax<T> vm;
 #pragma unroll
-      for (int q = 0; q < NV; ++q)
-        if (q * G + lane < nvec) store_vec(dz + row * lddz, q * G + lane, V, i32x4{});
+      for (int q = 0; q < NV; ++q) vm.take(raw[q]);
+      m = vm.value();
+    } else {
+      for (int v = lane; v < nvec; v += G * U) {
+        i32x4 in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) in[u] = load_logits(zr, v + G * u, V);
+        run.take(in, c);
+      }
+      m = run.m;
     }
+  }
+  float all = lanes_reduce<L>(m, MaxOp{});
+  if constexpr (G > 64) {
+    if ((threadIdx.x & 63) == 0) sh.m[threadIdx.x >> 6] = all;
+    if (threadIdx.x == 0) sh.live = live;
+    __syncthreads();
+    live = sh.live;
+    all = sh.m[0];
+#pragma unroll
+    for (int i = 1; i < G / 64; ++i) all = fmaxf(all, sh.m[i]);
+  }
+  if (!live) {
+    if (lane == 0) {
+      if (PASS != Pass::kBackward) loss[row] = 0.f;
+      if (PASS == Pass::kForward && lse != nullptr) lse[row] = 0.f;
+    }
+    if constexpr (PASS != Pass::kForward)
+      for (int v = lane; v < nvec; v += G) store_vec(dr, v, V, i32x4{});
     return;  // the whole group
   }
-  float m = -INFINITY;
-#pragma unroll
-  for (int q = 0; q < NV; ++q) {
-    float f[N];
-    Row<T>::widen(raw[q], f);
-#pragma unroll
-    for (int e = 0; e < N; ++e) m = fmaxf(m, f[e]);
-  }
+
+  // sum
   RowSoftmax r;
-  r.m = finite_max(group_reduce<G>(m, MaxOp{}, part));
-  float s = 0.f;
-#pragma unroll
-  for (int q = 0; q < NV; ++q) {
-    float f[N];
-    Row<T>::widen(raw[q], f);
-#pragma unroll
-    for (int e = 0; e < N; ++e) s += exp2_hw((f[e] - r.m) * c);
+  if constexpr (PASS == Pass::kBackward) {
+    // z/T - lse: the saved lse takes the place of the maximum
+    saved *= temp;
+    r.m = finite_max(saved);
+    r.l = 0.f;
+    s = 1.f;
+  } else {
+    r.m = finite_max(all);
   }
-  s = group_reduce<G>(s, AddOp{}, part);
-  r.l = log2_hw(s);
-  const float a = loss_terms<T, G>(zr, top + row * k, k, temp, t, r, lane, part, sid, sp);
-  if (lane == 0) {
-    loss[row] = temp * temp * a;
-    if (!STEP && lse != nullptr) lse[row] = r.m / temp + kLn2 * r.l;
+  const Exponent x(r.m, c);
+  if constexpr (PASS != Pass::kBackward) {
+    if (!x.near) {
+      for (int v = lane; v < nvec; v += G) s = exp_sum<T, false>(load_logits(zr, v, V), x, s);
+    } else if constexpr (NV > 0) {
+#pragma unroll
+      for (int q = 0; q < NV; ++q) s = exp_sum<T, true>(raw[q], x, s);
+    } else {
+      run.over(x.mc);
+      s = run.s;
+    }
+    s = lanes_reduce<L>(s, AddOp{});
+    if constexpr (G > 64) {
+      if ((threadIdx.x & 63) == 0) sh.s[threadIdx.x >> 6] = s;
+      __syncthreads();
+      s = sh.s[0];
+#pragma unroll
+      for (int i = 1; i < G / 64; ++i) s += sh.s[i];
+    }
+    r.l = x.log_sum(s);
+    if (lane < L) {
+      const float a = loss_terms<L>(k, temp, r, lane, en);
+      if (lane == 0) {
+        loss[row] = temp * temp * a;
+        if (PASS == Pass::kForward && lse != nullptr) lse[row] = r.m / temp + kLn2 * r.l;
+      }
+    }
+  } else if (x.near) {
+    s = exp2_hw(fmaf(r.m, c, -x.mc));
   }
-  if constexpr (STEP) {
-    const float wt = (weight != nullptr ? weight[row] : 1.f) * temp;
-    if (r.l == -INFINITY) r.l = 0.f;  // no logit but -inf: every q is 0
+
+  if constexpr (PASS != Pass::kForward) {
+    const float wt = w * temp;
+    if (s == 0.f) r.l = 0.f;  // no logit but -inf: every q is 0
+    const float by = s == 0.f ? 0.f : wt / s;
+    if (!x.near) {
+      for (int v = lane; v < nvec; v += G)
+        store_vec(dr, v, V, exp_scaled<T, false>(load_logits(zr, v, V), x, by));
+    } else if constexpr (NV > 0) {
 #pragma unroll
-    for (int q = 0; q < NV; ++q) {
-      const int v = q * G + lane;
-      if (v < nvec) {
-        float f[N];
-        Row<T>::widen(raw[q], f);
+      for (int q = 0; q < NV; ++q) {
+        const int v = q * G + lane;
+        if (v < nvec) store_vec(dr, v, V, exp_scaled<T, true>(raw[q], x, by));
+      }
+    } else {
+      for (int v = lane; v < nvec; v += G * U) {
+        i32x4 in[U];
 #pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = wt * exp2_hw((f[e] - r.m) * c - r.l);
-        store_vec(dz + row * lddz, v, V, Row<T>::narrow(f));
+        for (int u = 0; u < U; ++u) in[u] = load_logits(zr, v + G * u, V);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (v + G * u < nvec)
+            store_vec<T, true>(dr, v + G * u, V, exp_scaled<T, true>(in[u], x, by));
       }
     }
     group_fence<G>();
-    fix_entries<T, G>(zr, dz + row * lddz, k, c, wt, r, lane, 0, V, sid, sp);
+    if (lane < L) fix_entries<T, L>(dr, k, c, wt, r, lane, 0, V, en);
   }
 }
 
@@ -220,49 +417,47 @@ __global__ __launch_bounds__(256) void distill_part_kernel(const T* __restrict__
   const float c = kLog2E / temp;
   const int nvec = (V + N - 1) / N;
   const int v0 = blockIdx.y * per, v1 = min(v0 + per, nvec);
-  float m = -INFINITY, s = 0.f;
+  RunningSum<T> run;
   for (int v = v0 + threadIdx.x; v < v1; v += 256 * U) {
-    i32x4 raw[U];
+    i32x4 in[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = load_logits(zr, v + 256 * u < v1 ? v + 256 * u : nvec, V);
-    float top = m;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float f[N];
-      Row<T>::widen(raw[u], f);
-#pragma unroll
-      for (int e = 0; e < N; ++e) top = fmaxf(top, f[e]);
-    }
-    const float base = finite_max(top);
-    s *= rescale(m, base, c);
-    m = top;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float f[N];
-      Row<T>::widen(raw[u], f);
-#pragma unroll
-      for (int e = 0; e < N; ++e) s += exp2_hw((f[e] - base) * c);
-    }
+    for (int u = 0; u < U; ++u) in[u] = load_logits(zr, v + 256 * u < v1 ? v + 256 * u : nvec, V);
+    run.take(in, c);
   }
-  const float all = group_reduce<256>(m, MaxOp{}, part);
-  s *= rescale(m, all, c);
+  const float m = group_reduce<256>(run.m, MaxOp{}, part);
+  const Exponent x(finite_max(m), c);
+  float s = 0.f;
+  if (x.near) {
+    run.over(x.mc);
+    s = run.s;
+  } else {
+    for (int v = v0 + threadIdx.x; v < v1; v += 256)
+      s = exp_sum<T, false>(load_logits(zr, v, V), x, s);
+  }
   s = group_reduce<256>(s, AddOp{}, part);
-  if (threadIdx.x == 0) parts[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = f32x2{all, s};
+  // the sum of 2^((z - m) c)
+  if (x.near) s *= exp2_hw(-fmaf(x.m, c, -x.mc));
+  if (threadIdx.x == 0) parts[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = f32x2{m, s};
 }
 
 // A row's parts joined, by the lanes of a wavefront (every wavefront of the
-// workgroup alike).
+// workgroup alike); *sum = sum 2^((z - m) c).
 __device__ __forceinline__ RowSoftmax join_parts(const f32x2* __restrict__ parts, int count,
-                                                 float c) {
+                                                 float c, float* sum) {
   const int lane = threadIdx.x & 63;
-  float m = -INFINITY;
-  for (int i = lane; i < count; i += 64) m = fmaxf(m, parts[i][0]);
+  const f32x2 first = lane < count ? parts[lane] : f32x2{-INFINITY, 0.f};
+  float m = first[0];
+  for (int i = lane + 64; i < count; i += 64) m = fmaxf(m, parts[i][0]);
   RowSoftmax r;
   r.m = finite_max(lanes_reduce<64>(m, MaxOp{}));
-  float s = 0.f;
-  for (int i = lane; i < count; i += 64)
-    s += parts[i][1] * rescale(parts[i][0], r.m, c);
-  r.l = log2_hw(lanes_reduce<64>(s, AddOp{}));
+  // a part without a logit but -inf has no sum; r.m may be far below its 0
+  auto part = [&](const f32x2& p) {
+    return p[0] == -INFINITY ? 0.f : p[1] * exp2_hw((p[0] - r.m) * c);
+  };
+  float s = part(first);
+  for (int i = lane + 64; i < count; i += 64) s += part(parts[i]);
+  *sum = lanes_reduce<64>(s, AddOp{});
+  r.l = log2_hw(*sum);
   return r;
 }
 
@@ -272,142 +467,150 @@ __global__ __launch_bounds__(64) void distill_join_kernel(
     const T* __restrict__ z, int64_t ldz, int V, const f32x2* __restrict__ parts, int count,
     const int32_t* __restrict__ ids, const float* __restrict__ top, int k, float temp,
     float* __restrict__ loss, float* __restrict__ lse) {
-  extern __shared__ int smem[];
-  int* sid = smem;
-  float* sp = reinterpret_cast<float*>(sid + k);
+  extern __shared__ __align__(16) int smem[];
+  const Entries en(smem, k);
   const int64_t row = blockIdx.x;
   const int lane = threadIdx.x;
   const float c = kLog2E / temp;
-  const Teacher t = teach<64>(ids + row * k, top + row * k, k, V, c, lane, nullptr, sid, sp);
-  if (!t.live) {
+  const bool live =
+      teach<T, 64, false>(z + row * ldz, ids + row * k, top + row * k, k, V, c, lane, en);
+  if (!live) {
     if (lane == 0) {
       loss[row] = 0.f;
       if (lse != nullptr) lse[row] = 0.f;
     }
     return;
   }
-  const RowSoftmax r = join_parts(parts + row * count, count, c);
-  const float a = loss_terms<T, 64>(z + row * ldz, top + row * k, k, temp, t, r, lane, nullptr, sid,
-                                    sp);
+  float s;
+  const RowSoftmax r = join_parts(parts + row * count, count, c, &s);
+  const float a = loss_terms<64>(k, temp, r, lane, en);
   if (lane == 0) {
     loss[row] = temp * temp * a;
     if (lse != nullptr) lse[row] = r.m / temp + kLn2 * r.l;
   }
 }
 
-// Gradient of part blockIdx.y (per vectors) of the rows, G lanes a row, from
-// lse (backward) or from the row's parts (step: the first part also writes the
-// loss).
-template <typename T, int G>
+// Gradient of part blockIdx.y (per vectors) of row blockIdx.x, from lse (backward)
+// or from the row's parts (step: the first part also writes the loss).
+template <typename T>
 __global__ __launch_bounds__(256) void distill_grad_kernel(
-    const T* __restrict__ z, int64_t ldz, int64_t n, int V, int per,
-    const f32x2* __restrict__ parts, int count, const float* __restrict__ lse,
-    const int32_t* __restrict__ ids, const float* __restrict__ top, int k, float temp,
-    const float* __restrict__ weight, float* __restrict__ loss, T* __restrict__ dz,
-    int64_t lddz) {
-  constexpr int N = Row<T>::N, R = 256 / G;
-  extern __shared__ int smem[];
-  __shared__ float part[4];
-  const int lane = threadIdx.x % G, group = threadIdx.x / G;
-  int* sid = smem + (int64_t)group * 2 * k;
-  float* sp = reinterpret_cast<float*>(sid + k);
-  const int64_t row = (int64_t)blockIdx.x * R + group;
-  if (row >= n) return;  // whole groups
+    const T* __restrict__ z, int64_t ldz, int V, int per, const f32x2* __restrict__ parts,
+    int count, const float* __restrict__ lse, const int32_t* __restrict__ ids,
+    const float* __restrict__ top, int k, float temp, const float* __restrict__ weight,
+    float* __restrict__ loss, T* __restrict__ dz, int64_t lddz) {
+  constexpr int N = Row<T>::N, U = 4;
+  extern __shared__ __align__(16) int smem[];
+  __shared__ int live_sh;
+  const int lane = threadIdx.x;
+  const Entries en(smem, k);
+  const int64_t row = blockIdx.x;
   const float c = kLog2E / temp;
   const T* zr = z + row * ldz;
   T* dr = dz + row * lddz;
   const int nvec = (V + N - 1) / N;
   const int v0 = blockIdx.y * per, v1 = min(v0 + per, nvec);
-  const Teacher t = teach<G>(ids + row * k, top + row * k, k, V, c, lane, part, sid, sp);
-  if (!t.live) {
-    if (loss != nullptr && lane == 0 && blockIdx.y == 0) loss[row] = 0.f;
-    for (int v = v0 + lane; v < v1; v += G) store_vec(dr, v, V, i32x4{});
-    return;
-  }
   RowSoftmax r;
+  float s = 1.f;
   if (lse != nullptr) {
-    // z/T - lse: the saved lse takes the place of the maximum
-    r.m = lse[row] * temp;
+    r.m = finite_max(lse[row] * temp);  // z/T - lse: in the place of the maximum
     r.l = 0.f;
-    if (r.m == -INFINITY) r.m = 0.f;
   } else {
-    r = join_parts(parts + row * count, count, c);
+    r = join_parts(parts + row * count, count, c, &s);
+  }
+  if (lane < 64) {
+    const bool live = teach<T, 64, true>(zr, ids + row * k, top + row * k, k, V, c, lane, en);
     if (loss != nullptr && blockIdx.y == 0) {
-      const float a = loss_terms<T, G>(zr, top + row * k, k, temp, t, r, lane, part, sid, sp);
+      const float a = live ? loss_terms<64>(k, temp, r, lane, en) : 0.f;
       if (lane == 0) loss[row] = temp * temp * a;
     }
-    if (r.l == -INFINITY) r.l = 0.f;
+    if (lane == 0) live_sh = live;
+  }
+  __syncthreads();
+  if (!live_sh) {
+    for (int v = v0 + lane; v < v1; v += 256) store_vec(dr, v, V, i32x4{});
+    return;
   }
   const float wt = (weight != nullptr ? weight[row] : 1.f) * temp;
-  for (int v = v0 + lane; v < v1; v += G) {
-    float f[N];
-    Row<T>::widen(load_logits(zr, v, V), f);
+  if (s == 0.f) r.l = 0.f;  // no logit but -inf: every q is 0
+  const Exponent x(r.m, c);
+  if (x.near) s *= exp2_hw(fmaf(r.m, c, -x.mc));
+  const float by = s == 0.f ? 0.f : wt / s;
+  if (x.near) {
+    for (int v = v0 + lane; v < v1; v += 256 * U) {
+      i32x4 in[U];
 #pragma unroll
-    for (int e = 0; e < N; ++e) f[e] = wt * exp2_hw((f[e] - r.m) * c - r.l);
-    store_vec(dr, v, V, Row<T>::narrow(f));
+      for (int u = 0; u < U; ++u)
+        in[u] = load_logits(zr, v + 256 * u < v1 ? v + 256 * u : nvec, V);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (v + 256 * u < v1)
+          store_vec(dr, v + 256 * u, V, exp_scaled<T, true>(in[u], x, by));
+    }
+  } else {
+    for (int v = v0 + lane; v < v1; v += 256)
+      store_vec(dr, v, V, exp_scaled<T, false>(load_logits(zr, v, V), x, by));
   }
-  group_fence<G>();
-  fix_entries<T, G>(zr, dr, k, c, wt, r, lane, v0 * N, min(v1 * N, V), sid, sp);
+  __syncthreads();
+  if (lane < 64) fix_entries<T, 64>(dr, k, c, wt, r, lane, v0 * N, min(v1 * N, V), en);
 }
 
 int vectors_of(int32_t V, int is_bf16) { return is_bf16 ? (V + 7) / 8 : (V + 3) / 4; }
 
-constexpr int kRowVectors = 1024 * 16;  // vectors of the longest row held in registers
+// Entries a row up to which 32 (16) rows share a workgroup: theirs fill half of
+// the 64 KB of LDS that a launch has without asking.
+constexpr int kTop32 = 64, kTop16 = 128;
 
-// Parts of a row: 1 where rows are held in registers.
+constexpr int kRowVectors = 4096;  // the longest row held in registers
+
+// Parts of a row: 1 where a workgroup has a row to itself.  Rows in registers
+// always do: one launch, where two wait for the host (16 rows of 16,384 bf16,
+// loss: 4.7 us, in parts 6.5).  Longer rows are cut up where they are few: 64
+// rows of 131,072 bf16, step: 16.2 us in parts, 19.4 whole; 100 rows: 20.8, 19.8.
 int row_parts(int64_t n, int nvec) {
-  if (nvec <= kRowVectors && (n >= 256 || nvec <= 1024)) return 1;
-  const int64_t want = std::max<int64_t>(1, (1024 + n - 1) / n);
+  if (nvec <= kRowVectors || n * 192 >= nvec) return 1;
+  const int64_t want = (1024 + n - 1) / n;
   const int64_t most = (nvec + 511) / 512;
-  return (int)std::max<int64_t>(2, std::min<int64_t>(want, most));
+  return (int)std::min<int64_t>(want, most);
 }
 
-template <typename T, bool STEP>
+template <typename T, Pass PASS>
 hipError_t run_rows(const DistillArgs& a, hipStream_t stream) {
   const int nvec = vectors_of(a.V, sizeof(T) == 2);
   auto go = [&](auto g, auto v) {
     constexpr int G = decltype(g)::value, NV = decltype(v)::value;
     constexpr int BLOCK = G > 256 ? G : 256, R = BLOCK / G;
-    distill_row_kernel<T, G, NV, STEP>
-        <<<(unsigned)((a.n + R - 1) / R), BLOCK, (size_t)R * 2 * a.k * 4, stream>>>(
+    distill_row_kernel<T, G, NV, PASS>
+        <<<(unsigned)((a.n + R - 1) / R), BLOCK, (size_t)R * entry_words(a.k) * 4, stream>>>(
             static_cast<const T*>(a.z), a.ldz, a.n, a.V, a.ids, a.top, a.k, a.temp, a.weight,
             a.loss, a.lse, static_cast<T*>(a.dz), a.lddz);
     return hipGetLastError();
   };
 #define SHC_ROW(limit, g, v) \
   if (nvec <= limit) return go(std::integral_constant<int, g>{}, std::integral_constant<int, v>{})
-  SHC_ROW(16, 16, 1);
-  SHC_ROW(32, 32, 1);
-  SHC_ROW(64, 64, 1);
-  SHC_ROW(128, 64, 2);
+  // few lanes a row, so that the entries' share of the lanes and the row's steps
+  // are spread over more rows: 524,288 rows of 128 bf16, 8 entries, step: 71 us
+  // with 8 lanes a row, 94 with 16; of 512 (134,217 rows): 74 with 16, 108 with 64
+  if (a.k <= kTop32) SHC_ROW(16, 8, 2);
+  if (a.k <= kTop16) SHC_ROW(32, 16, 2);
+  if (a.k <= kTop16) SHC_ROW(64, 16, 4);
+  SHC_ROW(128, 32, 4);
   SHC_ROW(256, 64, 4);
-  SHC_ROW(512, 256, 2);
+  SHC_ROW(512, 64, 8);
   SHC_ROW(1024, 256, 4);
   SHC_ROW(2048, 256, 8);
-  SHC_ROW(4096, 512, 8);
-  SHC_ROW(8192, 1024, 8);
-  SHC_ROW(kRowVectors, 1024, 16);
+  SHC_ROW(kRowVectors, 512, 8);
 #undef SHC_ROW
-  return hipErrorInvalidValue;
+  return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
 }
 
 template <typename T>
 hipError_t run_grad(const DistillArgs& a, int count, int per, hipStream_t stream) {
   const int nvec = vectors_of(a.V, sizeof(T) == 2);
-  const int nparts = (nvec + per - 1) / per;
-  auto go = [&](auto g) {
-    constexpr int G = decltype(g)::value;
-    constexpr int R = 256 / G;
-    const dim3 grid((unsigned)((a.n + R - 1) / R), nparts);
-    distill_grad_kernel<T, G><<<grid, 256, (size_t)R * 2 * a.k * 4, stream>>>(
-        static_cast<const T*>(a.z), a.ldz, a.n, a.V, per,
-        static_cast<const f32x2*>(a.parts), count, a.lse, a.ids, a.top, a.k, a.temp, a.weight,
-        a.loss, static_cast<T*>(a.dz), a.lddz);
-    return hipGetLastError();
-  };
-  if (nvec <= 16) return go(std::integral_constant<int, 16>{});
-  if (nvec <= 256) return go(std::integral_constant<int, 64>{});
-  return go(std::integral_constant<int, 256>{});
+  const dim3 grid((unsigned)a.n, (nvec + per - 1) / per);
+  distill_grad_kernel<T><<<grid, 256, (size_t)entry_words(a.k) * 4, stream>>>(
+      static_cast<const T*>(a.z), a.ldz, a.V, per, static_cast<const f32x2*>(a.parts), count,
+      a.lse, a.ids, a.top, a.k, a.temp, a.weight, a.loss, static_cast<T*>(a.dz), a.lddz);
+  return hipGetLastError();
 }
 
 template <typename T>
@@ -423,11 +626,11 @@ hipError_t run_parts(const DistillArgs& a, int count, int* per, hipStream_t stre
 template <typename T>
 hipError_t run_forward(const DistillArgs& a, hipStream_t stream) {
   const int count = row_parts(a.n, vectors_of(a.V, sizeof(T) == 2));
-  if (count == 1) return run_rows<T, false>(a, stream);
+  if (count == 1) return run_rows<T, Pass::kForward>(a, stream);
   int per;
   const hipError_t e = run_parts<T>(a, count, &per, stream);
   if (e != hipSuccess) return e;
-  distill_join_kernel<T><<<(unsigned)a.n, 64, (size_t)2 * a.k * 4, stream>>>(
+  distill_join_kernel<T><<<(unsigned)a.n, 64, (size_t)entry_words(a.k) * 4, stream>>>(
       static_cast<const T*>(a.z), a.ldz, a.V, static_cast<const f32x2*>(a.parts), count, a.ids,
       a.top, a.k, a.temp, a.loss, a.lse);
   return hipGetLastError();
@@ -436,7 +639,7 @@ hipError_t run_forward(const DistillArgs& a, hipStream_t stream) {
 template <typename T>
 hipError_t run_step(const DistillArgs& a, hipStream_t stream) {
   const int count = row_parts(a.n, vectors_of(a.V, sizeof(T) == 2));
-  if (count == 1) return run_rows<T, true>(a, stream);
+  if (count == 1) return run_rows<T, Pass::kStep>(a, stream);
   int per;
   const hipError_t e = run_parts<T>(a, count, &per, stream);
   return e != hipSuccess ? e : run_grad<T>(a, count, per, stream);
@@ -444,28 +647,28 @@ hipError_t run_step(const DistillArgs& a, hipStream_t stream) {
 
 template <typename T>
 hipError_t run_backward(const DistillArgs& a, hipStream_t stream) {
-  // rows cut up only where there are too few to fill the chip
+  // elementwise but for the entries: long rows are cut up whatever their number
   const int nvec = vectors_of(a.V, sizeof(T) == 2);
-  const int64_t want = std::max<int64_t>(1, (2048 + a.n - 1) / a.n);
-  const int64_t most = std::max(1, nvec / 256);
-  const int count = (int)std::min<int64_t>(want, most);
-  return run_grad<T>(a, 0, (nvec + count - 1) / count, stream);
+  if (nvec <= 1024) return run_rows<T, Pass::kBackward>(a, stream);
+  const int per = 1024;
+  return run_grad<T>(a, 0, per, stream);
 }
 
 }  // namespace
 
 size_t distill_workspace_bytes(int64_t n, int32_t V) {
-  // parts of any count of rows up to n, in either dtype: at most 1024 + n, and
-  // at least two a row
+  // any count of rows up to n that is cut up, in either dtype: at most 1023 parts
+  // beside one a row
   const int nvec = std::max(vectors_of(V, 0), vectors_of(V, 1));
-  if (nvec <= 1024) return 0;
-  return (size_t)(std::max<int64_t>(1024 + n, 2 * n)) * sizeof(f32x2);
+  if (nvec <= kRowVectors) return 0;
+  return (size_t)(1024 + std::min<int64_t>(n, nvec / 192)) * sizeof(f32x2);
 }
 
 hipError_t launch_distill(const DistillArgs& a, DistillPass pass, int is_bf16,
                           hipStream_t stream) {
-  // a launch holds fewer than 2^32 threads: 2^21 rows of at most 1024
-  constexpr int64_t kMost = (int64_t)1 << 21;
+  // a launch holds fewer than 2^32 threads: 2^20 rows of at most 1024, or of
+  // 256 for each of a row's parts
+  constexpr int64_t kMost = (int64_t)1 << 20;
   for (int64_t r0 = 0; r0 < a.n; r0 += kMost) {
     DistillArgs c = a;
     const int64_t e = is_bf16 ? 2 : 4;

@@ -14,6 +14,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // or width that is no multiple of 16 bytes start anywhere.  One load or store
 // instruction all the same (global memory takes unaligned vectors).
 typedef int i32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef int int_a2 __attribute__((aligned(2)));  // a pair of bf16
 typedef int i32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -78,21 +79,28 @@ __device__ __forceinline__ i32x4 load_vec(const T* row, int v, int C, uint32_t f
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const uint32_t lo = 2 * e < left ? p[2 * e] : fill;
-      const uint32_t hi = 2 * e + 1 < left ? p[2 * e + 1] : fill;
-      out[e] = (int)(lo | (hi << 16));
+      out[e] = (int)(fill | (fill << 16));
+      if (2 * e + 1 < left)
+        out[e] = *reinterpret_cast<const int_a2*>(p + 2 * e);
+      else if (2 * e < left)
+        out[e] = (int)(p[2 * e] | (fill << 16));
     }
   }
   return out;
 }
 
-template <typename T>
+// NT: a non-temporal store, for rows that nothing reads soon.
+template <typename T, bool NT = false>
 __device__ __forceinline__ void store_vec(T* row, int v, int C, const i32x4& x) {
   constexpr int N = Row<T>::N;
+  typedef typename Row<T>::mem mem;
   T* p = row + (int64_t)v * N;
   const int left = C - v * N;
   if (left >= N) {
-    *reinterpret_cast<typename Row<T>::mem*>(p) = x;
+    if constexpr (NT)
+      __builtin_nontemporal_store((mem)x, reinterpret_cast<mem*>(p));
+    else
+      *reinterpret_cast<mem*>(p) = x;
     return;
   }
   if constexpr (N == 4) {
@@ -102,8 +110,10 @@ __device__ __forceinline__ void store_vec(T* row, int v, int C, const i32x4& x) 
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (2 * e < left) p[2 * e] = (uint16_t)(x[e] & 0xFFFF);
-      if (2 * e + 1 < left) p[2 * e + 1] = (uint16_t)((uint32_t)x[e] >> 16);
+      if (2 * e + 1 < left)
+        *reinterpret_cast<int_a2*>(p + 2 * e) = x[e];
+      else if (2 * e < left)
+        p[2 * e] = (uint16_t)(x[e] & 0xFFFF);
     }
   }
 }
@@ -139,7 +149,7 @@ __device__ __forceinline__ void store_channels(float* a, int v, int C, const flo
   }
 }
 
-// Reductions over aligned groups of G lanes, 16 <= G <= 64: quads and the two
+// Reductions over aligned groups of G lanes, 8 <= G <= 64: quads and the two
 // mirrors within 16 lanes by DPP, rows 16 apart and halves 32 apart by the
 // permlane swaps.  All VALU; every lane ends with the result.
 template <int CTRL>
@@ -148,11 +158,11 @@ __device__ __forceinline__ float dpp(float x) {
 }
 template <int G, typename Op>
 __device__ __forceinline__ float lanes_reduce(float x, Op op) {
-  static_assert(G == 16 || G == 32 || G == 64, "lanes that share a row");
+  static_assert(G == 8 || G == 16 || G == 32 || G == 64, "lanes that share a row");
   x = op(x, dpp<0xB1>(x));    // quad_perm [1, 0, 3, 2]
   x = op(x, dpp<0x4E>(x));    // quad_perm [2, 3, 0, 1]
   x = op(x, dpp<0x141>(x));   // row_half_mirror
-  x = op(x, dpp<0x140>(x));   // row_mirror
+  if constexpr (G >= 16) x = op(x, dpp<0x140>(x));  // row_mirror
   if constexpr (G >= 32) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
                                                     false);
