@@ -6,22 +6,23 @@
 // Forward: a gather bound by HBM.  G lanes share a row and walk its 16-byte
 // vectors, 256 / G rows a workgroup.
 //
-// Gradient: three launches.
-// 1. embed_sort_kernel orders the positions by id, stably, in one launch and
-//    without communication: workgroup p of P owns the ids that are p modulo P
-//    (frequent ids, often neighbours, then fall to different workgroups), reads
-//    all ids once to count its own per id and to count the ids of the workgroups
-//    before it (its first place in the order), and again to place the positions:
-//    a chunk of ids at a time goes to a queue in LDS, in order, and the
-//    workgroup's 16 wavefronts, each owning a sixteenth of the ids, hand out the
-//    places.  It also clears the table rows of its ids that have no position.
-// 2. embed_sum_kernel cuts the ordered positions into jobs of equal length,
-//    whatever the ids' frequencies; a group of lanes per job and column range
-//    adds the rows of each id in order.  An id that lies inside one job is
-//    final; the part of an id that continues in or from another job goes to the
-//    workspace.
-// 3. embed_join_kernel adds those parts, in order, at the job where the id
-//    begins.
+// Gradient: the positions are ordered by id, then added.
+// 1. embed_split_kernel (past kDirectRows positions) cuts the list of ids into
+//    chunks and orders each chunk's positions by bucket, id modulo 1024 (frequent
+//    ids, often neighbours, then fall to different buckets): every wavefront
+//    ranks 64 ids at a time by ten ballots over the bucket's bits.
+// 2. embed_order_kernel, a workgroup a bucket, takes its segments of all chunks in
+//    order (of few positions: the ids themselves), counts its ids and hands out
+//    the places: wavefronts take a queue in LDS in shares and rank 64 positions at a
+//    time by ballots over the ids' bits.  Its first place in the order is the number of positions in
+//    buckets before it, which the chunks' offsets give without communication.
+// 3. embed_sum_kernel cuts the order into jobs of J positions, whatever the ids'
+//    frequencies; lanes that share a job and a column range add each id's rows in
+//    order.  A job takes the ids that begin in it, to their end; ids of many
+//    positions are cut at the jobs' borders instead, their parts left in
+//    the workspace.  Other workgroups of the launch clear the table rows of ids
+//    without a position meanwhile.
+// 4. embed_join_kernel adds the parts, in order.
 // Every sum has an order that follows the ids and sizes alone: results repeat
 // bit for bit.
 #include <algorithm>
@@ -33,7 +34,6 @@ namespace shc {
 namespace {
 
 using namespace rowops;
-
 template <typename T, typename ID, int G>
 __global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ E, int64_t R,
                                                     int64_t ldE, const ID* __restrict__ ids,
@@ -64,174 +64,466 @@ __global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ E, int
   }
 }
 
-constexpr int kSortThreads = 1024;
+constexpr int kSortThreads = 256;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortPer = 8;                          // ids a thread takes from a chunk
-constexpr int kSortChunk = kSortThreads * kSortPer;  // ids of a chunk
+constexpr int kSplitPer = 4;                           // ids a thread of a chunk
+constexpr int kRoundPer = 4;                           // segments a thread of a round
+constexpr int kRound = kSortThreads * kRoundPer;       // segments of a round
+constexpr int kQueue = 1024;                           // positions in LDS at a time
+constexpr int kLogBuckets = 10, kBuckets = 1 << kLogBuckets;
+constexpr uint32_t kCut = 0x80000000u;  // in key_of: an id whose run is cut at jobs' borders
 
-// Ids of the sort's workgroup p of P = 1 << logP: id & (P - 1) == p, at most
-// keys = ceil(R / P) of them, local number id >> logP.
-// LDS: count[keys], then the queue (local number, position) of a chunk.
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
 template <typename ID>
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(
-    const ID* __restrict__ ids, int64_t id_stride, int n, int R, int pad, int logP, int keys,
-    int C, int clear, float* __restrict__ dE, int64_t ldE, int32_t* __restrict__ order,
-    int32_t* __restrict__ key_of, int32_t* __restrict__ total) {
-  extern __shared__ int smem[];
-  volatile int* count = smem;
-  int* queue_key = smem + keys;
-  int* queue_pos = queue_key + kSortChunk;
-  __shared__ int wave_sum[kSortWaves];
-  __shared__ int base_sh, queued;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int P = 1 << logP, p = blockIdx.x;
+__device__ __forceinline__ int valid_id(const ID* ids, int64_t id_stride, int64_t i, int R,
+                                        int pad) {
+  const int64_t id = (int64_t)ids[i * id_stride];
+  return id >= 0 && id < R && id != pad ? (int)id : -1;
+}
 
-  for (int k = tid; k < keys; k += kSortThreads) smem[k] = 0;
-  __syncthreads();
-  // counts of this workgroup's ids, and of the ids of the workgroups before it
-  int below = 0;
-  for (int i = tid; i < n; i += kSortThreads) {
-    const int64_t id = (int64_t)ids[(int64_t)i * id_stride];
-    if (id >= 0 && id < R && id != pad) {
-      const int b = (int)id & (P - 1);
-      below += b < p;
-      if (b == p) atomicAdd(&smem[(int)id >> logP], 1);
-    }
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) below += __shfl_xor(below, d, 64);
-  if (lane == 0) wave_sum[wave] = below;
-  __syncthreads();
-  if (tid == 0) {
-    int s = 0;
-    for (int w = 0; w < kSortWaves; ++w) s += wave_sum[w];
-    base_sh = s;
-  }
-  __syncthreads();
+__device__ __forceinline__ uint64_t lanes_below(int lane) { return (1ull << lane) - 1; }
 
-  // rows of ids without a position
-  if (clear) {
-    for (int k = wave; k < keys; k += kSortWaves) {
-      const int r = (k << logP) + p;
-      if (r < R && count[k] == 0)
-        for (int v = lane; 4 * v < C; v += 64) {
-          const float z[4] = {0.f, 0.f, 0.f, 0.f};
-          store_channels<4>(dE + (int64_t)r * ldE, v, C, z);
-        }
-    }
-  }
-  __syncthreads();
+// Inclusive sums over the lanes of a wavefront: shifts within 16 lanes, then the
+// last lanes of 16 and of 32 handed on, all by DPP.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int shifted(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x += shifted<0x111, 0xF>(x);  // row_shr 1, 2, 4, 8
+  x += shifted<0x112, 0xF>(x);
+  x += shifted<0x114, 0xF>(x);
+  x += shifted<0x118, 0xF>(x);
+  x += shifted<0x142, 0xA>(x);  // row_bcast 15, into rows 1 and 3
+  x += shifted<0x143, 0xC>(x);  // row_bcast 31, into rows 2 and 3
+  return x;
+}
 
-  // counts -> first places: consecutive keys per thread, their sums scanned
-  const int per = (keys + kSortThreads - 1) / kSortThreads;
-  int mine = 0;
-  for (int k = tid * per; k < min(keys, (tid + 1) * per); ++k) mine += count[k];
-  int inc = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int u = __shfl_up(inc, d, 64);
-    if (lane >= d) inc += u;
-  }
+// Exclusive sums over the threads of W wavefronts; *total their sum.  wave_sum [W]
+// is free on entry and on return.
+template <int W>
+__device__ __forceinline__ int block_scan(int mine, int* wave_sum, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int inc = wave_scan(mine);
   if (lane == 63) wave_sum[wave] = inc;
   __syncthreads();
-  int at = base_sh + inc - mine;
-  for (int w = 0; w < wave; ++w) at += wave_sum[w];
-  for (int k = tid * per; k < min(keys, (tid + 1) * per); ++k) {
-    const int c = count[k];
-    count[k] = at;
-    at += c;
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const int s = wave_sum[w];
+    before += w < wave ? s : 0;
+    all += s;
   }
-  // the last workgroup's last place is the number of ids that count
-  if (p == P - 1 && tid == kSortThreads - 1) *total = at;
+  __syncthreads();
+  *total = all;
+  return before + inc - mine;
+}
+
+// Chunk c's (id, position) by bucket, in order, to split[c * NT * kSplitPer + ...];
+// where each bucket begins to offs[c][kBuckets + 1].
+template <typename ID, int NT>
+__global__ __launch_bounds__(NT) void embed_split_kernel(
+    const ID* __restrict__ ids, int64_t id_stride, int64_t n, int R, int pad,
+    i32x2* __restrict__ split, int32_t* __restrict__ offs) {
+  constexpr int W = NT / 64, BPT = kBuckets / NT;  // wavefronts; buckets a thread
+  constexpr int64_t CHUNK = NT * kSplitPer;
+  extern __shared__ __align__(16) int hist[];  // [W][kBuckets]
+  __shared__ int wave_sum[W];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t w0 = blockIdx.x * CHUNK + (int64_t)wave * 64 * kSplitPer;
+  int id[kSplitPer], rank[kSplitPer];
+#pragma unroll
+  for (int u = 0; u < kSplitPer; ++u) {
+    const int64_t i = w0 + u * 64 + lane;
+    id[u] = i < n ? valid_id(ids, id_stride, i, R, pad) : -1;
+  }
+  volatile int* mine = hist + wave * kBuckets;
+  for (int b = lane; b < kBuckets / 4; b += 64)
+    reinterpret_cast<i32x4*>(hist + wave * kBuckets)[b] = i32x4{};
+  group_fence<64>();
+#pragma unroll
+  for (int u = 0; u < kSplitPer; ++u) {
+    const int b = id[u] & (kBuckets - 1);
+    uint64_t same = __ballot(id[u] >= 0);
+#pragma unroll
+    for (int k = 0; k < kLogBuckets; ++k) {
+      const uint64_t bit = __ballot((b >> k) & 1);
+      same &= ((b >> k) & 1) ? bit : ~bit;
+    }
+    if (id[u] >= 0) {
+      const int before = __popcll(same & lanes_below(lane));
+      const int start = mine[b];
+      rank[u] = start + before;
+      if (before == 0) mine[b] = start + __popcll(same);
+    }
+    group_fence<64>();
+  }
+  __syncthreads();
+  // bucket starts: a thread's BPT buckets, over the wavefronts
+  int h[W][BPT], sum[BPT], all = 0;
+#pragma unroll
+  for (int e = 0; e < BPT; ++e) {
+    sum[e] = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      h[w][e] = hist[w * kBuckets + tid * BPT + e];
+      sum[e] += h[w][e];
+    }
+    all += sum[e];
+  }
+  int total;
+  int at = block_scan<W>(all, wave_sum, &total);
+  int32_t* o = offs + (int64_t)blockIdx.x * (kBuckets + 1);
+  if (tid == 0) o[kBuckets] = total;
+#pragma unroll
+  for (int e = 0; e < BPT; ++e) {
+    o[tid * BPT + e] = at;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      hist[w * kBuckets + tid * BPT + e] = at;
+      at += h[w][e];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kSplitPer; ++u)
+    if (id[u] >= 0)
+      split[blockIdx.x * CHUNK + mine[id[u] & (kBuckets - 1)] + rank[u]] =
+          i32x2{id[u], (int)(w0 + u * 64 + lane)};
+}
+
+// Bucket p's positions by id.  Ids of the bucket: at most keys = ceil(R / kBuckets),
+// below 2^key_bits, local number id >> kLogBuckets.  order, key_of, run_end [n]:
+// position, id (with kCut where its positions are more than `most`) and the end of
+// the id's run, at its places; present [kBuckets][words]: a bit for every id with a
+// position; *total the number of positions with an id that counts.
+// LDS: place[keys], end[keys], at[kSortWaves][keys], the queue (local number,
+// position), a round of segments.
+template <typename ID, bool DIRECT>
+__global__ __launch_bounds__(kSortThreads) void embed_order_kernel(
+    const ID* __restrict__ ids, int64_t id_stride, int64_t n, int R, int pad, int keys,
+    int key_bits, int most, const i32x2* __restrict__ split, const int32_t* __restrict__ offs,
+    int chunks, int chunk, int32_t* __restrict__ order, uint32_t* __restrict__ key_of,
+    int32_t* __restrict__ run_end, uint32_t* __restrict__ present, int words,
+    int32_t* __restrict__ total) {
+  extern __shared__ int smem[];
+  constexpr int PER = kQueue / kSortThreads;  // entries of the queue a thread
+  int* place = smem;
+  int* end = place + keys;
+  int* at = end + keys;  // a wavefront's places, then its next ones
+  int* queue_key = at + kSortWaves * keys;
+  int* queue_pos = queue_key + kQueue;
+  int* seg_at = queue_pos + kQueue;  // [kRound]: a segment's first entry
+  int* seg_src = seg_at + kRound;    // and where it lies in its chunk
+  __shared__ int wave_sum[kSortWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int p = blockIdx.x;
+
+  // calls f(entries in the queue) for the bucket's entries, in order, a queue at
+  // a time; below: the thread's positions in the buckets before
+  int below = 0;
+  auto each_queue = [&](auto&& f) {
+    if constexpr (DIRECT) {
+      for (int64_t c0 = 0; c0 < n; c0 += kQueue) {
+        int key[PER];
+        uint64_t has[PER];
+        int found = 0;
+        const int64_t w0 = c0 + (int64_t)wave * 64 * PER;
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+          const int64_t i = w0 + u * 64 + lane;
+          const int id = i < n ? valid_id(ids, id_stride, i, R, pad) : -1;
+          const int b = id & (kBuckets - 1);
+          below += id >= 0 && b < p;
+          key[u] = id >= 0 && b == p ? id >> kLogBuckets : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+          has[u] = __ballot(key[u] >= 0);
+          found += __popcll(has[u]);
+        }
+        if (lane == 0) wave_sum[wave] = found;
+        __syncthreads();
+        int q = 0, entries = 0;
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) {
+          q += w < wave ? wave_sum[w] : 0;
+          entries += wave_sum[w];
+        }
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+          if (key[u] >= 0) {
+            const int s = q + __popcll(has[u] & lanes_below(lane));
+            queue_key[s] = key[u];
+            queue_pos[s] = (int)(w0 + u * 64 + lane);
+          }
+          q += __popcll(has[u]);
+        }
+        __syncthreads();
+        f(entries);
+        __syncthreads();
+      }
+    } else {
+      for (int c0 = 0; c0 < chunks; c0 += kRound) {
+        int from[kRoundPer], len[kRoundPer], sum = 0;
+#pragma unroll
+        for (int u = 0; u < kRoundPer; ++u) {
+          const int c = c0 + tid * kRoundPer + u;
+          from[u] = len[u] = 0;
+          if (c < chunks) {
+            const int32_t* o = offs + (int64_t)c * (kBuckets + 1) + p;
+            from[u] = o[0];
+            len[u] = o[1] - o[0];
+          }
+          below += from[u];
+          sum += len[u];
+        }
+        int entries;
+        int first = block_scan<kSortWaves>(sum, wave_sum, &entries);
+#pragma unroll
+        for (int u = 0; u < kRoundPer; ++u) {
+          seg_at[tid * kRoundPer + u] = first;
+          seg_src[tid * kRoundPer + u] = from[u];
+          first += len[u];
+        }
+        __syncthreads();
+        for (int q0 = 0; q0 < entries; q0 += kQueue) {
+          const int take = min(kQueue, entries - q0);
+          // a thread's entries together: the last segment that begins at or before
+          // each, by bisection, then their loads
+          int s[PER] = {};
+#pragma unroll
+          for (int d = kRound / 2; d > 0; d >>= 1)
+#pragma unroll
+            for (int u = 0; u < PER; ++u)
+              if (seg_at[s[u] + d] <= q0 + tid + u * kSortThreads) s[u] += d;
+          i32x2 e[PER];
+#pragma unroll
+          for (int u = 0; u < PER; ++u) {
+            const int i = tid + u * kSortThreads;
+            if (i < take)
+              e[u] = split[(int64_t)(c0 + s[u]) * chunk + seg_src[s[u]] + (q0 + i - seg_at[s[u]])];
+          }
+#pragma unroll
+          for (int u = 0; u < PER; ++u) {
+            const int i = tid + u * kSortThreads;
+            if (i < take) {
+              queue_key[i] = e[u][0] >> kLogBuckets;
+              queue_pos[i] = e[u][1];
+            }
+          }
+          __syncthreads();
+          f(take);
+          __syncthreads();
+        }
+      }
+    }
+  };
+  // a wavefront's share of a queue: consecutive blocks of 64
+  auto share = [&](int entries, int* lo, int* hi) {
+    const int blocks = (entries + 63) / 64, each = (blocks + kSortWaves - 1) / kSortWaves;
+    *lo = min(entries, wave * each * 64);
+    *hi = min(entries, (wave + 1) * each * 64);
+  };
+  auto count_queue = [&](int entries) {
+    int lo, hi;
+    share(entries, &lo, &hi);
+    for (int i = lo + lane; i < hi; i += 64) atomicAdd(&at[wave * keys + queue_key[i]], 1);
+  };
+
+  for (int k = tid; k < (2 + kSortWaves) * keys; k += kSortThreads) smem[k] = 0;
+  __syncthreads();
+  // counts, and the first place: positions of the buckets before
+  int held = 0, queues = 0;
+  each_queue([&](int entries) {
+    count_queue(entries);
+    held += entries;
+    ++queues;
+  });
+  int base;
+  block_scan<kSortWaves>(below, wave_sum, &base);
+  for (int k = tid; k < keys; k += kSortThreads)
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) place[k] += at[w * keys + k];
   __syncthreads();
 
-  for (int64_t c0 = 0; c0 < n; c0 += kSortChunk) {
-    // this chunk's ids of the workgroup, in order: wavefront w has the w-th
-    // part of the chunk
-    int key[kSortPer];
-    uint64_t has[kSortPer];
-    int found = 0;
-    const int64_t w0 = c0 + (int64_t)wave * 64 * kSortPer;
+  // ids present, 64 a wavefront at a time
+  for (int k0 = wave * 64; k0 < words * 32; k0 += kSortThreads) {
+    const uint64_t bits = __ballot(k0 + lane < keys && place[min(k0 + lane, keys - 1)] != 0);
+    if (lane < 2 && k0 / 32 + lane < words)
+      present[(int64_t)p * words + k0 / 32 + lane] = (uint32_t)(bits >> (32 * lane));
+  }
+  if (p == kBuckets - 1 && tid == 0) *total = base + held;
+  if (held == 0) return;  // the whole workgroup
+
+  // counts -> first places (with the cut bit where the id is long) and ends:
+  // consecutive ids per thread, their sums scanned
+  const int per = (keys + kSortThreads - 1) / kSortThreads;
+  const int k0 = min(keys, tid * per), k1 = min(keys, k0 + per);
+  __syncthreads();
+  int mine = 0, all;
+  for (int k = k0; k < k1; ++k) mine += place[k];
+  int next = base + block_scan<kSortWaves>(mine, wave_sum, &all);
+  for (int k = k0; k < k1; ++k) {
+    const int c = place[k];
+    place[k] = next | (c > most ? (int)kCut : 0);
+    next += c;
+    end[k] = next;
+  }
+  __syncthreads();
+
+  // places: a wavefront's blocks of 64 entries of the queue in order, every entry
+  // ranked among the block's of its id by ballots over the id's bits
+  auto hand_out = [&](int entries) {
+    // the wavefronts' counts -> their first places; place: the next queue's
+    for (int k = tid; k < keys; k += kSortThreads) {
+      int to = place[k];
 #pragma unroll
-    for (int u = 0; u < kSortPer; ++u) {
-      const int64_t i = w0 + u * 64 + lane;
-      key[u] = -1;
-      if (i < n) {
-        const int64_t id = (int64_t)ids[i * id_stride];
-        if (id >= 0 && id < R && id != pad && ((int)id & (P - 1)) == p) key[u] = (int)id >> logP;
+      for (int w = 0; w < kSortWaves; ++w) {
+        const int c = at[w * keys + k];
+        at[w * keys + k] = to;
+        to += c;
       }
-      has[u] = __ballot(key[u] >= 0);
-      found += __popcll(has[u]);
-    }
-    if (lane == 0) wave_sum[wave] = found;
-    __syncthreads();
-    int q = 0;
-    for (int w = 0; w < wave; ++w) q += wave_sum[w];
-    if (wave == kSortWaves - 1 && lane == 0) queued = q + found;
-#pragma unroll
-    for (int u = 0; u < kSortPer; ++u) {
-      if (key[u] >= 0) {
-        const int s = q + __popcll(has[u] & ((1ull << lane) - 1));
-        queue_key[s] = key[u];
-        queue_pos[s] = (int)(w0 + u * 64 + lane);
-      }
-      q += __popcll(has[u]);
+      place[k] = to;
     }
     __syncthreads();
-    // places: every wavefront walks the queue for the local numbers it owns
-    const int nq = queued;
-    for (int q0 = 0; q0 < nq; q0 += 64) {
-      const bool in = q0 + lane < nq;
+    int lo, hi;
+    share(entries, &lo, &hi);
+    volatile int* mine_at = at + wave * keys;
+    for (int q0 = lo; q0 < hi; q0 += 64) {
+      const bool in = q0 + lane < hi;
       const int k = in ? queue_key[q0 + lane] : 0;
-      uint64_t todo = __ballot(in && (k & (kSortWaves - 1)) == wave);
-      while (todo != 0) {
-        const int first = __ffsll((unsigned long long)todo) - 1;
-        const int kk = __shfl(k, first, 64);
-        const uint64_t same = __ballot(in && k == kk);
-        const int place = count[kk];
-        if (lane == first) count[kk] = place + __popcll(same);
-        if (in && k == kk) {
-          const int s = place + __popcll(same & ((1ull << lane) - 1));
-          order[s] = queue_pos[q0 + lane];
-          key_of[s] = (kk << logP) + p;
-        }
-        todo &= ~same;
+      uint64_t same = __ballot(in);
+      for (int b = 0; b < key_bits; ++b) {
+        const uint64_t bit = __ballot((k >> b) & 1);
+        same &= ((k >> b) & 1) ? bit : ~bit;
       }
+      if (in) {
+        const int to = mine_at[k];
+        const int before = __popcll(same & lanes_below(lane));
+        if (before == 0) mine_at[k] = to + __popcll(same);
+        const int s = (to & (int)~kCut) + before;
+        order[s] = queue_pos[q0 + lane];
+        key_of[s] = (uint32_t)((k << kLogBuckets) + p) | ((uint32_t)to & kCut);
+        run_end[s] = end[k];
+      }
+      group_fence<64>();
     }
-    __syncthreads();
+  };
+  if (queues == 1) {
+    hand_out(held);  // the queue and its counts are there
+  } else {
+    each_queue([&](int entries) {
+      for (int k = tid; k < kSortWaves * keys; k += kSortThreads) at[k] = 0;
+      __syncthreads();
+      count_queue(entries);
+      __syncthreads();
+      hand_out(entries);
+    });
   }
 }
 
-// Job j (J positions of the order) and columns [tile * G * N, + G * N): G lanes.
-// part [jobs][2][C]: what an id that began in an earlier job gets from this one
-// (slot 0), what an id that goes on in the next job gets from this one, where it
-// began here (slot 1).
-template <typename T, int G>
+// 4 zeros of a row, `past` the caches or not.
+__device__ __forceinline__ void clear_vec(float* row, int v, int C, int past) {
+  const float z[4] = {0.f, 0.f, 0.f, 0.f};
+  if (past)
+    store_channels<4, true>(row, v, C, z);
+  else
+    store_channels<4>(row, v, C, z);
+}
+
+// Workgroups [0, sums): jobs of J positions, G lanes each, by column ranges of
+// G vectors.  part [jobs][2][C]: of a cut id that began in an earlier job, what
+// this job adds (slot 0); of one that goes on in the next job, what this one, in
+// which it began, adds (slot 1).  A job takes fewer than 3 J positions: its own,
+// and the rest of an id that begins in it (of 2 J at most where it is not cut).
+// The others clear the table rows of the ids without a position.
+template <typename T, int G, int J>
 __global__ __launch_bounds__(256) void embed_sum_kernel(
-    const T* __restrict__ dY, int64_t lddy, const int32_t* __restrict__ order,
-    const int32_t* __restrict__ key_of, const int32_t* __restrict__ total, int J, int jobs, int C,
-    float scale, int accumulate, float* __restrict__ dE, int64_t ldE, float* __restrict__ part) {
-  constexpr int N = Row<T>::N, U = 8;
-  const int j = blockIdx.x * (256 / G) + threadIdx.x / G;
-  const int v = blockIdx.y * G + threadIdx.x % G;
-  const int m = *total;
+    const T* __restrict__ dY, int64_t lddy, int64_t n, const int32_t* __restrict__ order,
+    const uint32_t* __restrict__ key_of, const int32_t* __restrict__ run_end,
+    const uint32_t* __restrict__ present, int words, const int32_t* __restrict__ total, int jobs,
+    int sums, int clear, int past, int R, int C, float scale, int accumulate, float* __restrict__ dE,
+    int64_t ldE, float* __restrict__ part) {
+  constexpr int N = Row<T>::N, U = 8, TAKE = 3 * J;
+  __shared__ __align__(16) int pos_sh[256 / G][TAKE];
+  __shared__ __align__(16) uint32_t key_sh[256 / G][TAKE];
+  if ((int)blockIdx.x >= sums) {
+    // a wavefront clears `clear` rows at a time (up to 64), its lanes looking up
+    // one each; rows shorter than 64 vectors several together
+    const int lane = threadIdx.x & 63;
+    const int nv = (C + 3) / 4;
+    int wide = 64;
+    while (wide > 1 && wide / 2 >= nv) wide /= 2;
+    const int step = (gridDim.x - sums) * 4 * clear;
+    for (int r0 = ((blockIdx.x - sums) * 4 + (threadIdx.x >> 6)) * clear; r0 < R; r0 += step) {
+      const int r = r0 + lane, k = r >> kLogBuckets;
+      bool none = false;
+      if (lane < clear && r < R)
+        none = !((present[(int64_t)(r & (kBuckets - 1)) * words + (k >> 5)] >> (k & 31)) & 1);
+      const uint64_t rows = __ballot(none);
+      for (int i = lane / wide; i < clear; i += 64 / wide)
+        if ((rows >> i) & 1)
+          for (int v = lane % wide; v < nv; v += wide)
+            clear_vec(dE + (int64_t)(r0 + i) * ldE, v, C, past);
+    }
+    return;
+  }
+  const int tiles = ((C + N - 1) / N + G - 1) / G;
+  const int group = threadIdx.x / G, lane = threadIdx.x % G;
+  int j = (blockIdx.x / tiles) * (256 / G) + group;
+  if constexpr (G == 64) j = __builtin_amdgcn_readfirstlane(j);
+  const int v = (blockIdx.x % tiles) * G + lane;
   if (j >= jobs) return;
-  const int lo = j * J, hi = min(lo + J, m);
-  if (lo >= hi || v * N >= C) return;
-  const int before = lo > 0 ? key_of[lo - 1] : -1;
-  const int after = hi < m ? key_of[hi] : -1;
+  // everything the job may need at once: places past the total hold anything
+  int lo = j * J;
+  const int64_t next = min((int64_t)lo + J, n);
+  const int m = *total;
+  uint32_t key = key_of[lo];
+  const uint32_t before = lo > 0 ? key_of[lo - 1] : ~0u;
+  const int first_end = run_end[lo];
+  uint32_t last = key_of[next - 1];
+  int last_end = run_end[next - 1];
+  const uint32_t after = next < n ? key_of[next] : ~0u;
+  int* pos = pos_sh[group];
+  uint32_t* keys = key_sh[group];
+#pragma unroll
+  for (int i = 0; i < (TAKE + G - 1) / G; ++i) {
+    const int t = i * G + lane;
+    if (t < TAKE && lo + t < n) {
+      pos[t] = order[lo + t];
+      keys[t] = key_of[lo + t];
+    }
+  }
+  group_fence<64>();
+  if (lo >= m) return;
+  int hi = (int)next;
+  if (hi > m) {
+    hi = m;
+    last = key_of[m - 1];
+    last_end = run_end[m - 1];
+  }
+  const int lo0 = lo;
+  bool from_before = before == key;
+  if (from_before && !(key & kCut)) {  // an earlier job takes it to its end
+    lo = first_end;
+    if (lo >= hi) return;
+    key = keys[lo - lo0];
+    from_before = false;
+  }
+  const bool goes_on = (last & kCut) && hi < m && after == last;
+  if (!(last & kCut)) hi = last_end;
+  if (v * N >= C) return;
 
   float acc[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) acc[e] = 0.f;
-  bool from_before = key_of[lo] == before;
-  auto put = [&](int key, bool goes_on) {
-    if (from_before) {
-      store_channels<N>(part + ((int64_t)j * 2) * C, v, C, acc);
-    } else if (goes_on) {
-      store_channels<N>(part + ((int64_t)j * 2 + 1) * C, v, C, acc);
+  auto put = [&](bool to_next) {
+    if (from_before || to_next) {
+      store_channels<N>(part + ((int64_t)j * 2 + (from_before ? 0 : 1)) * C, v, C, acc);
     } else {
-      float* to = dE + (int64_t)key * ldE;
+      float* to = dE + (int64_t)(key & ~kCut) * ldE;
       float f[N];
       if (accumulate) load_channels<N>(to, v, C, f);
 #pragma unroll
@@ -242,24 +534,19 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] = 0.f;
   };
-  int key = key_of[lo];
-  for (int t0 = lo; t0 < hi; t0 += U) {
-    int pos[U], keys[U];
+  for (int t0 = lo - lo0; t0 < hi - lo0; t0 += U) {
     i32x4 raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int t = min(t0 + u, hi - 1);
-      pos[u] = order[t];
-      keys[u] = key_of[t];
+      const int t = min(t0 + u, hi - lo0 - 1);
+      raw[u] = load_vec(dY + (int64_t)pos[t] * lddy, v, C);
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = load_vec(dY + (int64_t)pos[u] * lddy, v, C);
-#pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (t0 + u < hi) {
-        if (keys[u] != key) {
-          put(key, false);
-          key = keys[u];
+      if (t0 + u < hi - lo0) {
+        if (keys[t0 + u] != key) {
+          put(false);
+          key = keys[t0 + u];
         }
         float f[N];
         Row<T>::widen(raw[u], f);
@@ -268,78 +555,121 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(
       }
     }
   }
-  put(key, key == after);
+  put(goes_on);
 }
 
-// The parts of the id that begins in job j and goes on in the next: slot 1 of
-// job j, then slot 0 of the jobs after it up to the last with that id.  The
-// workgroup's four quarters take every fourth of those, added in order.
-__global__ __launch_bounds__(256) void embed_join_kernel(
-    const int32_t* __restrict__ key_of, const int32_t* __restrict__ total, int J, int jobs, int C,
-    float scale, int accumulate, const float* __restrict__ part, float* __restrict__ dE,
-    int64_t ldE) {
-  __shared__ float sum[4][64][4];
+// The parts of the cut ids that begin in jobs [blockIdx.x * kJoinJobs, + kJoinJobs)
+// and go on in the next: slot 1 of the job, then slot 0 of the jobs after it up to
+// the last with that id.  L lanes hold four columns each; the workgroup's SHARES
+// groups of L take the parts in turn, each adding its own in order, and the groups
+// are added in order.
+constexpr int kJoinThreads = 512, kJoinJobs = 8;
+template <int L>
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(
+    const uint32_t* __restrict__ key_of, const int32_t* __restrict__ run_end,
+    const int32_t* __restrict__ total, int J, int jobs, int C, float scale, int accumulate,
+    const float* __restrict__ part, float* __restrict__ dE, int64_t ldE) {
+  constexpr int SHARES = kJoinThreads / L;
+  __shared__ f32x4 sum[SHARES][L];
   const int m = *total;
-  const int lane = threadIdx.x & 63, quarter = threadIdx.x >> 6;
-  const int v = blockIdx.y * 64 + lane;
-  for (int j = blockIdx.x; j < jobs; j += gridDim.x) {
-  const int lo = j * J, hi = lo + J;
-  if (hi >= m) return;  // the last job: nothing goes on
-  const int key = key_of[hi];
-  if (key_of[hi - 1] != key) continue;                                  // nothing goes on
-  if (key_of[lo] == key && lo > 0 && key_of[lo - 1] == key) continue;  // it began earlier
-  // the last job that has the id: it holds every position up to its last
-  int last = j + 1;
-  for (int b = (m - 1) / J; last < b;) {
-    const int mid = (last + b + 1) / 2;
-    if (key_of[mid * J] == key)
-      last = mid;
-    else
-      b = mid - 1;
-  }
-  float acc[4] = {0.f, 0.f, 0.f, 0.f}, f[4];
-  if (v * 4 < C) {
-    if (quarter == 0) load_channels<4>(part + ((int64_t)j * 2 + 1) * C, v, C, acc);
-    for (int q = j + 1 + quarter; q <= last; q += 4) {
-      load_channels<4>(part + ((int64_t)q * 2) * C, v, C, f);
+  const int wlane = threadIdx.x & 63, lane = threadIdx.x % L, share = threadIdx.x / L;
+  const int v = blockIdx.y * L + lane;
+  for (int64_t j0 = (int64_t)blockIdx.x * kJoinJobs; j0 < jobs;
+       j0 += (int64_t)gridDim.x * kJoinJobs) {
+    // every wavefront finds the jobs by itself, a lane each
+    bool begins = false;
+    const int64_t ji = j0 + wlane;
+    if (wlane < kJoinJobs && ji < jobs) {
+      const int64_t lo = ji * J, hi = lo + J;
+      if (hi < m) {
+        const uint32_t key = key_of[hi];
+        begins = (key & kCut) && key_of[hi - 1] == key &&
+                 !(lo > 0 && key_of[lo - 1] == key && key_of[lo] == key);
+      }
+    }
+    for (uint64_t todo = __ballot(begins); todo != 0; todo &= todo - 1) {
+      const int j = (int)j0 + __ffsll((unsigned long long)todo) - 1;
+      const int hi = (j + 1) * J;
+      const uint32_t key = key_of[hi];
+      const int last = (run_end[hi] - 1) / J;
+      float acc[4] = {0.f, 0.f, 0.f, 0.f}, f[4];
+      if (v * 4 < C) {
+        if (share == 0) load_channels<4>(part + ((int64_t)j * 2 + 1) * C, v, C, acc);
+#pragma unroll 8
+        for (int q = j + 1 + share; q <= last; q += SHARES) {
+          load_channels<4>(part + ((int64_t)q * 2) * C, v, C, f);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] += f[e];
+          for (int e = 0; e < 4; ++e) acc[e] += f[e];
+        }
+      }
+      sum[share][lane] = f32x4{acc[0], acc[1], acc[2], acc[3]};
+      __syncthreads();
+      if (share == 0 && v * 4 < C) {
+#pragma unroll 8
+        for (int q = 1; q < SHARES; ++q)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[e] += sum[q][lane][e];
+        float* to = dE + (int64_t)(key & ~kCut) * ldE;
+        if (accumulate) load_channels<4>(to, v, C, f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          f[e] = accumulate ? fmaf(acc[e], scale, f[e]) : acc[e] * scale;
+        store_channels<4>(to, v, C, f);
+      }
+      __syncthreads();
     }
   }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) sum[quarter][lane][e] = acc[e];
-  __syncthreads();
-  if (quarter == 0 && v * 4 < C) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += (sum[1][lane][e] + sum[2][lane][e]) + sum[3][lane][e];
-    float* to = dE + (int64_t)key * ldE;
-    if (accumulate) load_channels<4>(to, v, C, f);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = accumulate ? fmaf(acc[e], scale, f[e]) : acc[e] * scale;
-    store_channels<4>(to, v, C, f);
-  }
-  __syncthreads();
-  }
 }
 
+// Positions up to which every bucket reads the ids itself: one launch less (1,500
+// rows of 64 bf16: 23.0 us, 24.5 with the split; 3,000: 27.7, 26.4).
+constexpr int64_t kDirectRows = 2048;
+// Positions from which a chunk is split by 1024 threads: fewer, longer segments
+// (1,340,800 rows of 64 bf16: 133 us, 146 by 256 threads; 268,160: 33.6, 33.0).
+constexpr int64_t kWideRows = 524288;
+
+// Workspace: what the launches leave each other.
 struct EmbedPlan {
-  int logP, keys, J, jobs;
-  size_t lds, off_key, off_total, off_part, total;
+  int keys, key_bits, words, chunk, chunks, J, jobs;
+  size_t lds, off_key, off_end, off_present, off_total, off_split, off_offs, off_part, total;
 };
+
+// Positions of a job; an id of more than 2 J is cut.  Short jobs where there are
+// few wavefronts (16,384 rows of 64 bf16: 31 us with 8, 33 with 16, 43 with 32),
+// long ones where the parts' traffic counts (of 4,096: 160, 153, 150).
+[[nodiscard]] int job_rows(int64_t n, int32_t C) {
+  const int64_t w = n * C >> 9;  // about the wavefronts of one position each
+  return w >= 131072 ? 32 : w >= 32768 ? 16 : 8;
+}
 
 size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 void embed_plan(int64_t n, int64_t R, int32_t C, EmbedPlan* p) {
-  p->logP = 0;
-  while (p->logP < 8 && (1 << p->logP) < R) ++p->logP;
-  p->keys = (int)((R + (1 << p->logP) - 1) >> p->logP);
-  p->lds = ((size_t)p->keys + 2 * kSortChunk) * sizeof(int);
-  p->J = 32;
+  p->keys = (int)((R + kBuckets - 1) >> kLogBuckets);
+  p->words = (p->keys + 31) / 32;
+  p->chunk = kSplitPer * (n < kWideRows ? 256 : 1024);
+  p->chunks = n > kDirectRows ? (int)((n + p->chunk - 1) / p->chunk) : 0;
+  p->lds = ((2 + kSortWaves) * (size_t)p->keys + 2 * kQueue + 2 * kRound) * sizeof(int);
+  p->key_bits = 0;
+  while ((1 << p->key_bits) < p->keys) ++p->key_bits;
+  p->J = job_rows(n, C);
   p->jobs = (int)((n + p->J - 1) / p->J);
-  p->off_key = up256((size_t)n * 4);
-  p->off_total = p->off_key + up256((size_t)n * 4);
-  p->off_part = p->off_total + 256;
-  p->total = p->off_part + (size_t)p->jobs * 2 * (size_t)C * 4;
+  size_t at = 0;
+  auto place = [&](size_t bytes) {
+    const size_t here = at;
+    at += up256(bytes);
+    return here;
+  };
+  place((size_t)n * 4);  // order
+  p->off_key = place((size_t)n * 4);
+  p->off_end = place((size_t)n * 4);
+  p->off_present = place((size_t)kBuckets * p->words * 4);
+  p->off_total = place(4);
+  p->off_split = place((size_t)p->chunks * p->chunk * 8);
+  p->off_offs = place((size_t)p->chunks * (kBuckets + 1) * 4);
+  // only ids of more than 2 J positions have parts
+  p->off_part = place(n > 2 * p->J ? (size_t)p->jobs * 2 * (size_t)C * 4 : 0);
+  p->total = at;
 }
 
 template <typename T, typename ID>
@@ -360,41 +690,85 @@ hipError_t embed_rows(const void* E, int64_t R, int64_t ldE, const void* ids, in
   return go(std::integral_constant<int, 256>{});
 }
 
+struct EmbedWork {
+  EmbedPlan p;
+  int32_t *order, *run_end, *total, *offs;
+  uint32_t *key_of, *present;
+  i32x2* split;
+  float* part;
+};
+
 template <typename ID>
-hipError_t embed_sort(const void* ids, int64_t id_stride, int64_t n, int64_t R, int pad,
-                      const EmbedPlan& p, int32_t C, int clear, float* dE, int64_t ldE,
-                      int32_t* order, int32_t* key_of, int32_t* total, hipStream_t stream) {
+hipError_t embed_order(const void* ids, int64_t id_stride, int64_t n, int64_t R, int pad,
+                       const EmbedWork& w, hipStream_t stream) {
   // allow the large dynamic LDS allocation; once per instantiation
   static std::once_flag once;
   static hipError_t attr_err = hipSuccess;
+  constexpr int kMostLds =
+      (int)(((2 + kSortWaves) * (kMaxEmbedRows >> kLogBuckets) + 2 * kQueue + 2 * kRound) *
+            sizeof(int));
   std::call_once(once, [&] {
-    attr_err = hipFuncSetAttribute(
-        reinterpret_cast<const void*>(embed_sort_kernel<ID>),
-        hipFuncAttributeMaxDynamicSharedMemorySize,
-        (int)(((kMaxEmbedRows >> 8) + 2 * kSortChunk) * sizeof(int)));
+    attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(embed_split_kernel<ID, 1024>),
+                                   hipFuncAttributeMaxDynamicSharedMemorySize,
+                                   16 * kBuckets * sizeof(int));
+    for (const void* k : {reinterpret_cast<const void*>(embed_order_kernel<ID, true>),
+                          reinterpret_cast<const void*>(embed_order_kernel<ID, false>)})
+      if (attr_err == hipSuccess)
+        attr_err = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kMostLds);
   });
   if (attr_err != hipSuccess) return attr_err;
-  embed_sort_kernel<ID><<<1 << p.logP, kSortThreads, p.lds, stream>>>(
-      static_cast<const ID*>(ids), id_stride, (int)n, (int)R, pad, p.logP, p.keys, C, clear, dE,
-      ldE, order, key_of, total);
+  const ID* in = static_cast<const ID*>(ids);
+  if (w.p.chunks > 0) {
+    if (w.p.chunk == 256 * kSplitPer)
+      embed_split_kernel<ID, 256><<<w.p.chunks, 256, 4 * kBuckets * sizeof(int), stream>>>(
+          in, id_stride, n, (int)R, pad, w.split, w.offs);
+    else
+      embed_split_kernel<ID, 1024><<<w.p.chunks, 1024, 16 * kBuckets * sizeof(int), stream>>>(
+          in, id_stride, n, (int)R, pad, w.split, w.offs);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    embed_order_kernel<ID, false><<<kBuckets, kSortThreads, w.p.lds, stream>>>(
+        in, id_stride, n, (int)R, pad, w.p.keys, w.p.key_bits, 2 * w.p.J, w.split, w.offs, w.p.chunks,
+        w.p.chunk, w.order, w.key_of, w.run_end, w.present, w.p.words, w.total);
+  } else {
+    embed_order_kernel<ID, true><<<kBuckets, kSortThreads, w.p.lds, stream>>>(
+        in, id_stride, n, (int)R, pad, w.p.keys, w.p.key_bits, 2 * w.p.J, w.split, w.offs, 0, 0, w.order,
+        w.key_of, w.run_end, w.present, w.p.words, w.total);
+  }
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t embed_sum(const void* dY, int64_t lddy, const int32_t* order, const int32_t* key_of,
-                     const int32_t* total, const EmbedPlan& p, int32_t C, float scale,
-                     int accumulate, float* dE, int64_t ldE, float* part, hipStream_t stream) {
+hipError_t embed_sum(const void* dY, int64_t lddy, int64_t n, int64_t R, const EmbedWork& w,
+                     int32_t C, float scale, int accumulate, float* dE, int64_t ldE,
+                     hipStream_t stream) {
   const int nvec = (C + Row<T>::N - 1) / Row<T>::N;
-  auto go = [&](auto g) {
-    constexpr int G = decltype(g)::value;
-    const dim3 grid((p.jobs + 256 / G - 1) / (256 / G), (nvec + G - 1) / G);
-    embed_sum_kernel<T, G><<<grid, 256, 0, stream>>>(static_cast<const T*>(dY), lddy, order,
-                                                     key_of, total, p.J, p.jobs, C, scale,
-                                                     accumulate, dE, ldE, part);
+  auto go = [&](auto g, auto job) {
+    constexpr int G = decltype(g)::value, J = decltype(job)::value;
+    const int sums = (w.p.jobs + 256 / G - 1) / (256 / G) * ((nvec + G - 1) / G);
+    // about 16 KB a wavefront at a time; past the caches where the table does not
+    // fit the Infinity Cache, so that dY may stay there (4,096 rows, table of 32,768
+    // x 4,096: 113 us, 133 through the caches; of 64 rows: 107, 103)
+    const int clear = std::max(1, std::min(64, 4096 / C));
+    const int clears =
+        accumulate ? 0 : (int)std::min<int64_t>((R + 4 * clear - 1) / (4 * clear), 16384);
+    const int past = R * C >= (int64_t)1 << 26;
+    if (sums + clears == 0) return hipSuccess;
+    embed_sum_kernel<T, G, J><<<sums + clears, 256, 0, stream>>>(
+        static_cast<const T*>(dY), lddy, n, w.order, w.key_of, w.run_end, w.present, w.p.words,
+        w.total, w.p.jobs, sums, clear, past, (int)R, C, scale, accumulate, dE, ldE, w.part);
     return hipGetLastError();
   };
-  if (nvec <= 16) return go(std::integral_constant<int, 16>{});
-  return go(std::integral_constant<int, 64>{});
+  using std::integral_constant;
+  auto lanes = [&](auto job) {
+    if (nvec <= 8) return go(integral_constant<int, 8>{}, job);
+    if (nvec <= 16) return go(integral_constant<int, 16>{}, job);
+    if (nvec <= 32) return go(integral_constant<int, 32>{}, job);
+    return go(integral_constant<int, 64>{}, job);
+  };
+  if (w.p.J == 8) return lanes(integral_constant<int, 8>{});
+  if (w.p.J == 16) return lanes(integral_constant<int, 16>{});
+  return lanes(integral_constant<int, 32>{});
 }
 
 }  // namespace
@@ -430,24 +804,36 @@ hipError_t launch_embed_rows_backward(const void* dY, int64_t lddy, const void* 
                                       float scale, int64_t pad, int is_bf16, int accumulate,
                                       float* dE, int64_t ldE, void* ws, hipStream_t stream) {
   if (n == 0 && accumulate) return hipSuccess;
-  EmbedPlan p;
-  embed_plan(n, R, C, &p);
+  EmbedWork w;
+  embed_plan(n, R, C, &w.p);
   char* b = static_cast<char*>(ws);
-  int32_t* order = reinterpret_cast<int32_t*>(b);
-  int32_t* key_of = reinterpret_cast<int32_t*>(b + p.off_key);
-  int32_t* total = reinterpret_cast<int32_t*>(b + p.off_total);
-  float* part = reinterpret_cast<float*>(b + p.off_part);
+  w.order = reinterpret_cast<int32_t*>(b);
+  w.key_of = reinterpret_cast<uint32_t*>(b + w.p.off_key);
+  w.run_end = reinterpret_cast<int32_t*>(b + w.p.off_end);
+  w.present = reinterpret_cast<uint32_t*>(b + w.p.off_present);
+  w.total = reinterpret_cast<int32_t*>(b + w.p.off_total);
+  w.split = reinterpret_cast<i32x2*>(b + w.p.off_split);
+  w.offs = reinterpret_cast<int32_t*>(b + w.p.off_offs);
+  w.part = reinterpret_cast<float*>(b + w.p.off_part);
   const int pad32 = pad >= 0 && pad < R ? (int)pad : -1;
-  hipError_t e = (id64 ? embed_sort<int64_t> : embed_sort<int32_t>)(
-      ids, id_stride, n, R, pad32, p, C, !accumulate, dE, ldE, order, key_of, total, stream);
-  if (e != hipSuccess || n == 0) return e;
-  e = (is_bf16 ? embed_sum<uint16_t> : embed_sum<float>)(dY, lddy, order, key_of, total, p, C,
-                                                          scale, accumulate, dE, ldE, part, stream);
+  hipError_t e = (id64 ? embed_order<int64_t> : embed_order<int32_t>)(ids, id_stride, n, R, pad32,
+                                                                      w, stream);
   if (e != hipSuccess) return e;
-  const dim3 grid(std::min(p.jobs, 1 << 14), (C + 255) / 256);
-  embed_join_kernel<<<grid, 256, 0, stream>>>(key_of, total, p.J, p.jobs, C, scale, accumulate,
-                                              part, dE, ldE);
-  return hipGetLastError();
+  e = (is_bf16 ? embed_sum<uint16_t> : embed_sum<float>)(dY, lddy, n, R, w, C, scale, accumulate, dE,
+                                                          ldE, stream);
+  if (e != hipSuccess || n <= 2 * w.p.J) return e;  // no id is cut
+  auto join = [&](auto l) {
+    constexpr int L = decltype(l)::value;
+    const dim3 grid(std::min((w.p.jobs + kJoinJobs - 1) / kJoinJobs, 1 << 14),
+                    (C + 4 * L - 1) / (4 * L));
+    embed_join_kernel<L><<<grid, kJoinThreads, 0, stream>>>(w.key_of, w.run_end, w.total, w.p.J,
+                                                            w.p.jobs, C, scale, accumulate, w.part,
+                                                            dE, ldE);
+    return hipGetLastError();
+  };
+  if (C <= 64) return join(std::integral_constant<int, 16>{});
+  if (C <= 128) return join(std::integral_constant<int, 32>{});
+  return join(std::integral_constant<int, 64>{});
 }
 
 }  // namespace shc

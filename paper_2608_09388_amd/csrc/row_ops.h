@@ -134,14 +134,19 @@ __device__ __forceinline__ void load_channels(const float* a, int v, int C, floa
     for (int e = 0; e < N; ++e) f[e] = e < left ? a[(int64_t)v * N + e] : 0.f;
   }
 }
-template <int N>
+template <int N, bool NT = false>
 __device__ __forceinline__ void store_channels(float* a, int v, int C, const float* f) {
   const int left = C - v * N;
   if (left >= N) {
 #pragma unroll
-    for (int q = 0; q < N / 4; ++q)
-      *reinterpret_cast<f32x4_a4*>(a + (int64_t)v * N + 4 * q) =
-          f32x4_a4{f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]};
+    for (int q = 0; q < N / 4; ++q) {
+      f32x4_a4* to = reinterpret_cast<f32x4_a4*>(a + (int64_t)v * N + 4 * q);
+      const f32x4_a4 x = {f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]};
+      if constexpr (NT)
+        __builtin_nontemporal_store(x, to);
+      else
+        *to = x;
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < N; ++e)

@@ -108,7 +108,8 @@ def grad_case(r, n, R, kind):
     (5000, 3, 40, "zipf", 0, 0), (9000, 100003, 24, "zipf", 0, 3),
     (700, 300, 520, "uniform", 0, 0), (513, 50, 4099, "zipf", 5, 1),
     (20000, 257, 33, "outside", 0, 0), (70000, 655, 16, "runs", 0, 0),
-    (300, 1000, 16384, "zipf", 0, 0),
+    (300, 1000, 16384, "zipf", 0, 0), (4000, 2000003, 4, "uniform", 0, 0),
+    (530000, 700, 8, "zipf", 0, 0), (530001, 5, 3, "uniform", 0, 0),
 ])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_gradient(dtype, n, R, C, kind, extra, off, accumulate):
