@@ -133,6 +133,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_backward_kernel(
     for (int e = 0; e < N; ++e) ga[q][e] = 1.f, dg[q][e] = 0.f, db[q][e] = 0.f;
     if (v < nvec && gamma != nullptr) load_channels<N>(gamma, v, C, ga[q]);
   }
+  // the next row's vectors in flight, where the registers hold them
+  constexpr bool AHEAD = !(G == 1024 && NV == 4);
   const int64_t step = (int64_t)gridDim.x * R;
   int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / G;
   i32x4 cx[NV], cy[NV];
@@ -151,7 +153,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_backward_kernel(
   for (; row < n; row += step) {
     i32x4 nx[NV], ny[NV];
     float nmu = 0.f, nrs = 0.f;
-    if (row + step < n) fetch(row + step, nx, ny, &nmu, &nrs);
+    if (AHEAD && row + step < n) fetch(row + step, nx, ny, &nmu, &nrs);
     float sg = 0.f, sgh = 0.f;  // past the row's end dy = 0: nothing is added
 #pragma unroll
     for (int q = 0; q < NV; ++q) {
@@ -186,10 +188,14 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_backward_kernel(
         }
       }
     }
+    if constexpr (AHEAD) {
 #pragma unroll
-    for (int q = 0; q < NV; ++q) cx[q] = nx[q], cy[q] = ny[q];
-    cmu = nmu;
-    crs = nrs;
+      for (int q = 0; q < NV; ++q) cx[q] = nx[q], cy[q] = ny[q];
+      cmu = nmu;
+      crs = nrs;
+    } else if (row + step < n) {
+      fetch(row + step, cx, cy, &cmu, &crs);
+    }
   }
   if (col == nullptr) return;
   // the groups' sums, added one group after the other
@@ -230,31 +236,58 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_backward_kernel(
   }
 }
 
-// Adds `parts` partial rows of 2 C columns (dgamma, then dbeta): 32 columns a
-// workgroup, the rows in 32 interleaved shares added in order through LDS.
+// Adds `parts` partial rows of 2 C columns (dgamma, then dbeta): 16 lanes hold four
+// columns each, 64 threads a column take the rows in turn, and their sums are added
+// in two steps, all in a fixed order.
 __global__ __launch_bounds__(1024) void column_sum_kernel(const float* __restrict__ col, int parts,
                                                           int C, int accumulate,
                                                           float* __restrict__ dgamma,
                                                           float* __restrict__ dbeta) {
-  __shared__ float s[32][33];
-  const int c = threadIdx.x & 31, share = threadIdx.x >> 5;
-  const int at = blockIdx.x * 32 + c;
-  float a = 0.f;
-  if (at < 2 * C)
-    for (int p = share; p < parts; p += 32) a += col[(int64_t)p * 2 * C + at];
-  s[share][c] = a;
+  __shared__ f32x4 s[64][16];
+  const int lane = threadIdx.x & 15, share = threadIdx.x >> 4;
+  const int v = blockIdx.x * 16 + lane;
+  float a[4] = {0.f, 0.f, 0.f, 0.f}, f[4];
+  if (4 * v < 2 * C) {
+#pragma unroll 8
+    for (int p = share; p < parts; p += 64) {
+      load_channels<4>(col + (int64_t)p * 2 * C, v, 2 * C, f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[e] += f[e];
+    }
+  }
+  s[share][lane] = f32x4{a[0], a[1], a[2], a[3]};
   __syncthreads();
-  if (share != 0 || at >= 2 * C) return;
-  float* out = at < C ? dgamma : dbeta;
-  if (out == nullptr) return;
-  out += at < C ? at : at - C;
-  for (int q = 1; q < 32; ++q) a += s[q][c];
-  *out = accumulate ? *out + a : a;
+  if (share < 8) {
+#pragma unroll
+    for (int q = 1; q < 8; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[e] += s[share + 8 * q][lane][e];
+    s[share][lane] = f32x4{a[0], a[1], a[2], a[3]};  // read by no other until the barrier
+  }
+  __syncthreads();
+  if (share != 0) return;
+#pragma unroll
+  for (int q = 1; q < 8; ++q)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a[e] += s[q][lane][e];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int at = 4 * v + e;
+    float* out = at < C ? dgamma : dbeta;
+    if (at >= 2 * C || out == nullptr) continue;
+    out += at < C ? at : at - C;
+    *out = accumulate ? *out + a[e] : a[e];
+  }
 }
 
 // Calls f with the lanes of a row and the vectors a lane, as types, for rows of
-// nvec vectors (up to 16,384 channels).
-template <typename T, typename F>
+// nvec vectors (up to 16,384 channels).  The lanes fit the row within a third: at
+// 513 vectors (16,384 rows of 4,104 bf16) 256 lanes of three take 56 us forward and
+// 90 backward, 512 of two 70 and 125.  A row in one wavefront needs no barrier,
+// which the backward, with more registers a vector and fewer wavefronts, gains by
+// up to 256 vectors (16,384 rows of 2,048: 46 us, 54 with 256 lanes), the forward up
+// to 192 (of 2,048: 30, 27 with 256 lanes).
+template <typename T, bool BACKWARD, typename F>
 auto with_shape(int nvec, F&& f) {
   using std::integral_constant;
 #define SHC_SHAPE(limit, g, v) \
@@ -263,9 +296,20 @@ auto with_shape(int nvec, F&& f) {
   SHC_SHAPE(32, 32, 1);
   SHC_SHAPE(64, 64, 1);
   SHC_SHAPE(128, 64, 2);
-  SHC_SHAPE(256, 256, 1);
+  SHC_SHAPE(192, 64, 3);
+  if constexpr (BACKWARD) {
+    SHC_SHAPE(256, 64, 4);
+  } else {
+    SHC_SHAPE(256, 256, 1);
+  }
   SHC_SHAPE(512, 256, 2);
-  SHC_SHAPE(1024, 512, 2);
+  SHC_SHAPE(768, 256, 3);
+  if constexpr (BACKWARD) {
+    SHC_SHAPE(1024, 256, 4);
+  } else {
+    SHC_SHAPE(1024, 512, 2);
+  }
+  SHC_SHAPE(1536, 512, 3);
   if constexpr (sizeof(T) == 4) {
     SHC_SHAPE(2048, 1024, 2);
     return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
@@ -280,19 +324,22 @@ int vectors_of(int32_t C) {
   return (C + Row<T>::N - 1) / Row<T>::N;
 }
 
-// Workgroups of the row kernels: enough to fill the CUs several times over,
-// few enough that gamma is read (and a partial row of column sums written) once
-// per many rows.
+// Workgroups of the row kernels, per_cu to a CU: enough to keep HBM busy, few
+// enough that gamma is read once per many rows.
 int norm_blocks(int64_t n, int G, int per_cu) {
   const int rows = G > 256 ? 1 : 256 / G;
   const int64_t need = (n + rows - 1) / rows;
   return (int)std::min<int64_t>(need, 256 * per_cu);
 }
+// Of the backward, whose workgroups write a partial row of column sums each: two
+// (16,384 rows of 4,096 bf16: 87 us, 117 with one, 100 with four), three of short
+// rows (268,160 rows of 128: 47, 50 with two).
+int backward_per_cu(int G) { return G <= 32 ? 3 : 2; }
 
 template <typename T>
 int backward_blocks(int64_t n, int32_t C) {
-  return with_shape<T>(vectors_of<T>(C), [&](auto g, auto) {
-    return norm_blocks(n, decltype(g)::value, 2);
+  return with_shape<T, true>(vectors_of<T>(C), [&](auto g, auto) {
+    return norm_blocks(n, decltype(g)::value, backward_per_cu(decltype(g)::value));
   });
 }
 
@@ -300,7 +347,7 @@ template <typename T>
 hipError_t norm(const void* x, int64_t ldx, int64_t n, int32_t C, const float* gamma,
                 const float* beta, float eps, void* y, int64_t ldy, float* mean, float* rstd,
                 hipStream_t stream) {
-  return with_shape<T>(vectors_of<T>(C), [&](auto g, auto v) {
+  return with_shape<T, false>(vectors_of<T>(C), [&](auto g, auto v) {
     constexpr int G = decltype(g)::value, NV = decltype(v)::value;
     layer_norm_kernel<T, G, NV><<<norm_blocks(n, G, 4), G > 256 ? G : 256, 0, stream>>>(
         static_cast<const T*>(x), ldx, n, C, gamma, beta, eps, static_cast<T*>(y), ldy, mean,
@@ -313,10 +360,10 @@ template <typename T>
 hipError_t norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t n,
                          int32_t C, const float* gamma, const float* mean, const float* rstd,
                          void* dx, int64_t lddx, float* col, hipStream_t stream) {
-  return with_shape<T>(vectors_of<T>(C), [&](auto g, auto v) {
+  return with_shape<T, true>(vectors_of<T>(C), [&](auto g, auto v) {
     constexpr int G = decltype(g)::value, NV = decltype(v)::value;
     layer_norm_backward_kernel<T, G, NV>
-        <<<norm_blocks(n, G, 2), G > 256 ? G : 256, 0, stream>>>(
+        <<<norm_blocks(n, G, backward_per_cu(G)), G > 256 ? G : 256, 0, stream>>>(
             static_cast<const T*>(dy), lddy, static_cast<const T*>(x), ldx, n, C, gamma, mean,
             rstd, static_cast<T*>(dx), lddx, col);
     return hipGetLastError();
@@ -353,7 +400,7 @@ hipError_t launch_layer_norm_backward(const void* dy, int64_t lddy, const void* 
     if (e != hipSuccess) return e;
   }
   if (!want_cols || (n == 0 && accumulate)) return hipSuccess;
-  column_sum_kernel<<<(2 * C + 31) / 32, 1024, 0, stream>>>(col, blocks, C, accumulate, dgamma,
+  column_sum_kernel<<<(2 * C + 63) / 64, 1024, 0, stream>>>(col, blocks, C, accumulate, dgamma,
                                                            dbeta);
   return hipGetLastError();
 }
