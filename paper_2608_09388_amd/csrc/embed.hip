@@ -34,33 +34,48 @@ namespace shc {
 namespace {
 
 using namespace rowops;
-template <typename T, typename ID, int G>
+// G lanes share a row, with U vectors a lane in flight: of U rows where a row has at
+// most G vectors (SHORT), of one row otherwise.
+template <typename T, typename ID, int G, int U, bool SHORT>
 __global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ E, int64_t R,
                                                     int64_t ldE, const ID* __restrict__ ids,
                                                     int64_t id_stride, int64_t n, int C,
                                                     float scale, const T* __restrict__ add,
                                                     int64_t ldadd, T* __restrict__ out,
                                                     int64_t ldout) {
-  constexpr int N = Row<T>::N;
+  constexpr int N = Row<T>::N, ROWS = SHORT ? U : 1;
   const int lane = threadIdx.x % G;
-  const int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
-  if (row >= n) return;
-  const int64_t id = (int64_t)ids[row * id_stride];
-  const bool there = id >= 0 && id < R;
-  const T* e = E + (there ? id : 0) * ldE;
+  const int64_t row0 = ((int64_t)blockIdx.x * (256 / G) + threadIdx.x / G) * ROWS;
+  if (row0 >= n) return;
   const int nvec = (C + N - 1) / N;
-  for (int v = lane; v < nvec; v += G) {
-    float f[N], a[N];
-    Row<T>::widen(there ? load_vec(e, v, C) : i32x4{}, f);
-    if (add != nullptr) {
-      Row<T>::widen(load_vec(add + row * ldadd, v, C), a);
+  int64_t id[ROWS];
 #pragma unroll
-      for (int k = 0; k < N; ++k) f[k] = there ? fmaf(f[k], scale, a[k]) : a[k];
-    } else {
+  for (int u = 0; u < ROWS; ++u) id[u] = row0 + u < n ? (int64_t)ids[(row0 + u) * id_stride] : -1;
+  for (int v0 = lane; v0 < nvec; v0 += SHORT ? G : G * U) {
+    i32x4 e[U], a[U];
 #pragma unroll
-      for (int k = 0; k < N; ++k) f[k] *= scale;
+    for (int u = 0; u < U; ++u) {
+      const int r = SHORT ? u : 0, v = SHORT ? v0 : v0 + u * G;
+      e[u] = a[u] = i32x4{};
+      if (v < nvec && row0 + r < n) {
+        if (add != nullptr) a[u] = load_vec(add + (row0 + r) * ldadd, v, C);
+        if (id[r] >= 0 && id[r] < R) e[u] = load_vec(E + id[r] * ldE, v, C);
+      }
     }
-    store_vec(out + row * ldout, v, C, Row<T>::narrow(f));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = SHORT ? u : 0, v = SHORT ? v0 : v0 + u * G;
+      if (v < nvec && row0 + r < n) {
+        const bool there = id[r] >= 0 && id[r] < R;
+        float f[N], g[N];
+        Row<T>::widen(e[u], f);
+        Row<T>::widen(a[u], g);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+          f[k] = add == nullptr ? f[k] * scale : there ? fmaf(f[k], scale, g[k]) : g[k];
+        store_vec(out + (row0 + r) * ldout, v, C, Row<T>::narrow(f));
+      }
+    }
   }
 }
 
@@ -677,17 +692,25 @@ hipError_t embed_rows(const void* E, int64_t R, int64_t ldE, const void* ids, in
                       int64_t n, int32_t C, float scale, const void* add, int64_t ldadd, void* out,
                       int64_t ldout, hipStream_t stream) {
   const int nvec = (C + Row<T>::N - 1) / Row<T>::N;
-  auto go = [&](auto g) {
-    constexpr int G = decltype(g)::value;
-    const int64_t blocks = (n + 256 / G - 1) / (256 / G);
-    embed_kernel<T, ID, G><<<(unsigned)blocks, 256, 0, stream>>>(
+  auto go = [&](auto g, auto u, auto is_short) {
+    constexpr int G = decltype(g)::value, U = decltype(u)::value;
+    constexpr bool SHORT = decltype(is_short)::value;
+    constexpr int ROWS = 256 / G * (SHORT ? U : 1);
+    embed_kernel<T, ID, G, U, SHORT><<<(unsigned)((n + ROWS - 1) / ROWS), 256, 0, stream>>>(
         static_cast<const T*>(E), R, ldE, static_cast<const ID*>(ids), id_stride, n, C, scale,
         static_cast<const T*>(add), ldadd, static_cast<T*>(out), ldout);
     return hipGetLastError();
   };
-  if (nvec <= 16) return go(std::integral_constant<int, 16>{});
-  if (nvec <= 64) return go(std::integral_constant<int, 64>{});
-  return go(std::integral_constant<int, 256>{});
+  // two vectors a lane in flight (67,040 rows of 128 fp32 with an addend: 15.5 us;
+  // one 16.0, four 20.1)
+  using std::integral_constant;
+  integral_constant<int, 2> two;
+  if (nvec <= 8) return go(integral_constant<int, 8>{}, two, std::true_type{});
+  if (nvec <= 16) return go(integral_constant<int, 16>{}, two, std::true_type{});
+  if (nvec <= 32) return go(integral_constant<int, 32>{}, two, std::true_type{});
+  if (nvec <= 64) return go(integral_constant<int, 64>{}, two, std::true_type{});
+  if (nvec <= 128) return go(integral_constant<int, 64>{}, two, std::false_type{});
+  return go(integral_constant<int, 256>{}, two, std::false_type{});
 }
 
 struct EmbedWork {
