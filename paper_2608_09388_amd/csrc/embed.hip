@@ -652,23 +652,39 @@ struct EmbedPlan {
 // Positions of a job; an id of more than 2 J is cut.  Short jobs where there are
 // few wavefronts (16,384 rows of 64 bf16: 31 us with 8, 33 with 16, 43 with 32),
 // long ones where the parts' traffic counts (of 4,096: 160, 153, 150).
+constexpr int64_t kJobs16 = 32768, kJobs32 = 131072;  // wavefronts of one position each, about
 [[nodiscard]] int job_rows(int64_t n, int32_t C) {
-  const int64_t w = n * C >> 9;  // about the wavefronts of one position each
-  return w >= 131072 ? 32 : w >= 32768 ? 16 : 8;
+  const int64_t w = n * C >> 9;
+  return w >= kJobs32 ? 32 : w >= kJobs16 ? 16 : 8;
+}
+[[nodiscard]] int job_count(int64_t n, int32_t C) {
+  const int J = job_rows(n, C);
+  return (int)((n + J - 1) / J);
+}
+[[nodiscard]] int chunk_rows(int64_t n) { return kSplitPer * (n < kWideRows ? 256 : 1024); }
+[[nodiscard]] int chunk_count(int64_t n) {
+  return n > kDirectRows ? (int)((n + chunk_rows(n) - 1) / chunk_rows(n)) : 0;
 }
 
 size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
 
+// The workspace of n positions serves any smaller number too: every part of it has
+// the size that the number up to n with the most jobs, or chunks, needs.
 void embed_plan(int64_t n, int64_t R, int32_t C, EmbedPlan* p) {
   p->keys = (int)((R + kBuckets - 1) >> kLogBuckets);
-  p->words = (p->keys + 31) / 32;
-  p->chunk = kSplitPer * (n < kWideRows ? 256 : 1024);
-  p->chunks = n > kDirectRows ? (int)((n + p->chunk - 1) / p->chunk) : 0;
-  p->lds = ((2 + kSortWaves) * (size_t)p->keys + 2 * kQueue + 2 * kRound) * sizeof(int);
   p->key_bits = 0;
   while ((1 << p->key_bits) < p->keys) ++p->key_bits;
+  p->words = (p->keys + 31) / 32;
+  p->lds = ((2 + kSortWaves) * (size_t)p->keys + 2 * kQueue + 2 * kRound) * sizeof(int);
+  p->chunk = chunk_rows(n);
+  p->chunks = chunk_count(n);
   p->J = job_rows(n, C);
-  p->jobs = (int)((n + p->J - 1) / p->J);
+  p->jobs = job_count(n, C);
+  // the largest counts below the changes of rule
+  const int64_t most_chunks = std::max(p->chunks, chunk_count(std::min(n, kWideRows - 1)));
+  int64_t most_jobs = p->jobs;
+  for (const int64_t w : {kJobs16, kJobs32})
+    most_jobs = std::max<int64_t>(most_jobs, job_count(std::min(n, ((w << 9) - 1) / C), C));
   size_t at = 0;
   auto place = [&](size_t bytes) {
     const size_t here = at;
@@ -681,9 +697,8 @@ void embed_plan(int64_t n, int64_t R, int32_t C, EmbedPlan* p) {
   p->off_present = place((size_t)kBuckets * p->words * 4);
   p->off_total = place(4);
   p->off_split = place((size_t)p->chunks * p->chunk * 8);
-  p->off_offs = place((size_t)p->chunks * (kBuckets + 1) * 4);
-  // only ids of more than 2 J positions have parts
-  p->off_part = place(n > 2 * p->J ? (size_t)p->jobs * 2 * (size_t)C * 4 : 0);
+  p->off_offs = place((size_t)most_chunks * (kBuckets + 1) * 4);
+  p->off_part = place((size_t)most_jobs * 2 * (size_t)C * 4);
   p->total = at;
 }
 

@@ -153,6 +153,21 @@ def test_gradient_repeats_and_takes_fewer_rows():
     assert torch.equal(a, first)
 
 
+def test_gradient_of_fewer_rows_than_prepared():
+    """A prepared call's workspace serves smaller counts, also those that are cut
+    into shorter jobs (262,144 rows of 64 channels) or narrower chunks (524,288)."""
+    r = np.random.default_rng(2)
+    n, R, C = 530000, 300, 64
+    ids = torch.as_tensor(r.integers(0, R, n), dtype=torch.int32, device="cuda")
+    dY = torch.as_tensor(r.integers(-3, 4, (n, C)), dtype=torch.float32, device="cuda")
+    dE = torch.empty((R, C), device="cuda")
+    call = shc.prepare_embed_rows_backward(dY, ids, dE)
+    for m in (n, 524287, 262143, 3000, 17, 1):
+        call(m)
+        want = torch.zeros((R, C), device="cuda").index_add_(0, ids[:m].long(), dY[:m])
+        assert torch.equal(dE, want)         # whole numbers below 2^24: exact
+
+
 def test_gradient_of_a_table_past_32_bit_offsets():
     R, ld = 270_000, 16000                   # 4.3e9 fp32 elements, 17 GB
     buf = torch.full((R, ld), 1.0, dtype=torch.float32, device="cuda")
