@@ -840,7 +840,8 @@ int shc_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, in
  * but -inf every q is 0.  NaN and +inf make the row's own results NaN.  With
  * T < 1 the logits' maximum over T must be within fp32.
  *   logits, dlogits [n_rows] rows of V of `dtype`; top_ids [n_rows][k] int32,
- *   top_logits [n_rows][k] fp32; k in [1, 256]; temperature positive, finite.
+ *   top_logits [n_rows][k] fp32; k in [1, 256]; temperature positive and finite
+ *   (and not subnormal).
  *   loss [n_rows] fp32 out; row_weight [n_rows] fp32 = w, the upstream gradient
  *   of every row's loss, or NULL (1).
  *

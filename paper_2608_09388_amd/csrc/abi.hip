@@ -1276,8 +1276,8 @@ int check_distill(const void* logits, int64_t stride, int64_t n, int32_t V, cons
   SHC_TRY(check_dtype(dtype));
   SHC_TRY(check_width("V", V, kMaxLogits));
   SHC_TRY(check_width("k", k, kMaxTop));
-  if (!(temperature > 0.0f) || !std::isfinite(temperature))
-    return fail(SHC_ERR_INVALID_ARG, "temperature = %g must be positive and finite",
+  if (!std::isnormal(temperature) || temperature < 0.0f)
+    return fail(SHC_ERR_INVALID_ARG, "temperature = %g must be positive, normal and finite",
                 (double)temperature);
   SHC_TRY(check_row_tensor("logits", logits, n, V, stride, elem_size(dtype), false));
   SHC_TRY(check_array("top_ids", ids, n == 0));

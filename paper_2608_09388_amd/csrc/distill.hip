@@ -132,7 +132,8 @@ __device__ __forceinline__ float loss_terms(int k, float temp, const RowSoftmax&
     if (en.id[e] < 0 || p == 0.f) continue;
     const float zi = en.z[e];
     const float lq = zi == -INFINITY ? -INFINITY : (zi - r.m) / temp - kLn2 * r.l;
-    a += p * (kLn2 * log2_hw(p) - lq);
+    // (the hardware's logarithm takes a subnormal p as 0)
+    a += p * (kLn2 * log2_hw(fmaxf(p, 0x1p-126f)) - lq);
   }
   return lanes_reduce<L>(a, AddOp{});
 }

@@ -137,6 +137,19 @@ def test_a_bad_row_stays_alone(V):
     assert np.isnan(bad[5][3]).all()
 
 
+@pytest.mark.parametrize("V", [64, 3000])
+def test_entries_far_apart(V):
+    """Teacher's probabilities down to the subnormal range and below add nothing,
+    and no more."""
+    r = np.random.default_rng(V)
+    z = r.standard_normal((3, V))
+    ids = np.stack([r.permutation(V)[:8] for _ in range(3)])
+    top = np.array([[0, -1, -86.5, -87.3, -88, -95, -104, -300.0]] * 3)
+    top[1, :2] = 0.0                     # a sum of two: the rest move down once more
+    check(z, ids, top, 1.0, None, "f32")
+    check(z, ids, top * 3, 3.0, None, "bf16")
+
+
 def test_repeated_ids_share_their_probability():
     z = np.random.default_rng(0).standard_normal((2, 50))
     ids = np.array([[4, 4, 4, 9], [0, 49, 0, 49]])

@@ -1,6 +1,9 @@
 """The row operators' entry points without a GPU: arguments are refused on the
 host before any HIP call (as in test_abi_cpu.py, addresses are stand-ins that
 validation never follows)."""
+import math
+import random
+
 import pytest
 
 from paper_2608_09388_amd import binding as shc
@@ -94,6 +97,27 @@ def test_workspaces_grow_with_the_rows(lib):
             last = b
 
 
+def test_workspaces_grow_across_the_rules(lib):
+    """The counts at which a call changes its cutting need no more than larger ones."""
+    rng = random.Random(5)
+    for _ in range(300):
+        C = int(math.exp(rng.uniform(0, math.log(65536))))
+        n = int(math.exp(rng.uniform(0, math.log(1 << 22))))
+        sizes = [lib.shc_embed_rows_backward_workspace(m, 1000, C)
+                 for m in sorted({max(0, n - n // 3), n - 1, n, n + 1, n + n // 7})]
+        assert sizes == sorted(sizes), (n, C)
+    for C in (1, 64, 100, 4096):
+        for w in (32768, 131072):
+            edge = (w << 9) // C
+            sizes = [lib.shc_embed_rows_backward_workspace(m, 1000, C)
+                     for m in (edge // 2, edge - 1, edge, edge + 1, edge + 4096)]
+            assert sizes == sorted(sizes), C
+    for edge in (2048, 4096, 524288):
+        sizes = [lib.shc_embed_rows_backward_workspace(m, 1000, 16)
+                 for m in (edge - 1, edge, edge + 1, edge + 4096)]
+        assert sizes == sorted(sizes)
+
+
 def test_layer_norm(lib):
     call = caller(lib, "shc_layer_norm", dict(
         x=A, x_stride=64, n=10, C=64, gamma=A, beta=A, eps=1e-5, dtype=0, y=A, y_stride=64, mean=A,
@@ -132,7 +156,7 @@ def distill(extra):
 COMMON = [
     (dict(n=-1), -1, "n_rows"), (dict(V=0), -1, "V"), (dict(V=(1 << 24) + 1), -4, "V"),
     (dict(k=0), -1, "k"), (dict(k=257), -4, "k"), (dict(T=0.0), -1, "temperature"),
-    (dict(T=NAN), -1, "temperature"), (dict(T=INF), -1, "temperature"), (dict(dtype=5), -4, "dtype"),
+    (dict(T=1e-40), -1, "temperature"), (dict(T=NAN), -1, "temperature"), (dict(T=INF), -1, "temperature"), (dict(dtype=5), -4, "dtype"),
     (dict(z=None), -1, "logits"), (dict(z=ODD), -3, "logits"), (dict(stride=63), -1, "logits"),
     (dict(ids=None), -1, "top_ids"), (dict(top=None), -1, "top_logits"), (dict(top=ODD), -3, "top"),
 ]
