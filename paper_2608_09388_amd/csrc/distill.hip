@@ -58,46 +58,95 @@ __device__ __forceinline__ float prob(float z, const RowSoftmax& r, float c) {
 }
 
 // The teacher's entries of a row, in LDS: id (-1 where there is none), its own p,
-// the p of all the row's entries with that id, and the logit there.
+// the p of all the row's entries with that id, and the logit there.  Behind them,
+// for the gradient of rows of more than kPairs entries, a bit for each of the
+// `range` ids that it covers (modulo kMapBits): ids that are all different, the
+// usual case, are told by one pass over the entries, and only a row where a bit
+// was met twice compares every two entries.  30,000 rows of 1,000 bf16, step: 72 us
+// with 256 entries, 176 when all rows compare them; with up to 16 the two are
+// within 0.5 us of each other.
+constexpr int kPairs = 16;
+constexpr int kMapBits = 131072;
 __host__ __device__ constexpr int entry_slots(int k) { return (k + 3) & ~3; }
-__host__ __device__ constexpr int entry_words(int k) { return 4 * entry_slots(k); }
+__host__ __device__ constexpr int map_words(int k, int range) {
+  return k <= kPairs ? 0 : ((range < kMapBits ? range : kMapBits) + 127) / 128 * 4;
+}
+__host__ __device__ constexpr int entry_words(int k, int range) {
+  return 4 * entry_slots(k) + map_words(k, range);
+}
 struct Entries {
   int* id;
   float *p, *all, *z;
+  uint32_t* map;
   __device__ __forceinline__ Entries(int* lds, int k)
       : id(lds), p(reinterpret_cast<float*>(lds) + entry_slots(k)), all(p + entry_slots(k)),
-        z(all + entry_slots(k)) {}
+        z(all + entry_slots(k)),
+        map(reinterpret_cast<uint32_t*>(lds) + 4 * entry_slots(k)) {}
 };
 
-// Fills them, by L lanes of one wavefront; whether the row has any.  All of it,
+// Fills them, by L lanes of one wavefront; whether the row has any.  `all` is that
+// of the ids in [lo, lo + range).  All of it,
 // the logits' gather and the comparison of the ids too, is done before the
 // row's maximum is needed, beside the loads of the row.
 template <typename T, int L, bool GRAD>
 __device__ __forceinline__ bool teach(const T* __restrict__ z, const int32_t* __restrict__ ids,
                                       const float* __restrict__ top, int k, int V, float c,
-                                      int lane, const Entries& en) {
+                                      int lane, const Entries& en, int lo, int range) {
+  constexpr int U = 4;  // entries of a lane in flight
   float tm = -INFINITY, any = 0.f;
-  for (int e = lane; e < k; e += L) {
-    const int id = ids[e];
-    const float t = top[e];
-    const bool ok = id >= 0 && id < V && t != -INFINITY;
-    en.id[e] = ok ? id : -1;
-    en.p[e] = t;
-    if (ok) {
-      en.z[e] = Row<T>::get(z + id);
-      tm = fmaxf(tm, t);
-      any = 1.f;
+  for (int e0 = lane; e0 < k; e0 += U * L) {
+    int id[U];
+    float t[U], at[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int e = e0 + u * L;
+      id[u] = e < k ? ids[e] : -1;
+      t[u] = e < k ? top[e] : 0.f;
+      if (id[u] >= V || t[u] == -INFINITY) id[u] = -1;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) at[u] = id[u] >= 0 ? Row<T>::get(z + id[u]) : 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int e = e0 + u * L;
+      if (e >= k) break;
+      en.id[e] = max(id[u], -1);
+      en.p[e] = t[u];
+      en.z[e] = at[u];
+      if (id[u] >= 0) {
+        tm = fmaxf(tm, t[u]);
+        any = 1.f;
+      }
     }
   }
   tm = finite_max(lanes_reduce<L>(tm, MaxOp{}));
   if (lanes_reduce<L>(any, MaxOp{}) == 0.f) return false;
+  const int words = GRAD ? map_words(k, range) : 0;
+  for (int i = 4 * lane; i < words; i += 4 * L)
+    *reinterpret_cast<i32x4*>(en.map + i) = i32x4{};
   float s = 0.f;
-  for (int e = lane; e < k; e += L)
-    if (en.id[e] >= 0) s += exp2_hw((en.p[e] - tm) * c);
+  for (int e = lane; e < k; e += L) {
+    const float x = en.id[e] >= 0 ? exp2_hw((en.p[e] - tm) * c) : 0.f;
+    en.p[e] = x;
+    s += x;
+  }
   s = lanes_reduce<L>(s, AddOp{});
-  for (int e = lane; e < k; e += L)
-    en.p[e] = en.id[e] >= 0 ? exp2_hw((en.p[e] - tm) * c) / s : 0.f;
+  if (GRAD) group_fence<64>();
+  bool twice = false;
+  for (int e = lane; e < k; e += L) {
+    const float p = en.p[e] / s;
+    en.p[e] = p;
+    if (GRAD && words > 0) {
+      const unsigned at = (unsigned)(en.id[e] - lo);
+      en.all[e] = p;
+      if (at < (unsigned)range) {
+        const uint32_t bit = 1u << (at & 31);
+        twice |= atomicOr(en.map + ((at & (kMapBits - 1)) >> 5), bit) & bit;
+      }
+    }
+  }
   if constexpr (GRAD) {
+    if (words > 0 && lanes_reduce<L>(twice ? 1.f : 0.f, MaxOp{}) == 0.f) return true;
     const int slots = entry_slots(k);
     if (lane < slots - k) {  // the last four are whole: no id of the row's
       en.id[k + lane] = -2;
@@ -106,6 +155,7 @@ __device__ __forceinline__ bool teach(const T* __restrict__ z, const int32_t* __
     group_fence<64>();
     for (int e = lane; e < k; e += L) {
       const int id = en.id[e];
+      if ((unsigned)(id - lo) >= (unsigned)range) continue;
       float p = 0.f;
 #pragma unroll 4
       for (int o = 0; o < slots; o += 4) {
@@ -279,7 +329,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void distill_row_kernel(
   extern __shared__ __align__(16) int smem[];       // the groups' entries
   __shared__ GroupShare<G> sh;
   const int lane = threadIdx.x % G, group = threadIdx.x / G;
-  const Entries en(smem + group * entry_words(k), k);
+  const Entries en(
+      smem + group * (PASS == Pass::kForward ? entry_words(k, 0) : entry_words(k, V)), k);
   const int64_t row = (int64_t)blockIdx.x * R + group;
   if (row >= n) return;  // whole groups
   const float c = kLog2E / temp;
@@ -295,7 +346,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void distill_row_kernel(
   bool live = false;
   if (lane < L)
     live = teach<T, L, PASS != Pass::kForward>(zr, ids + row * k, top + row * k, k, V, c, lane,
-                                               en);
+                                               en, 0, V);
 
   // maximum; a row read twice has its sum over the running maximum too
   float m = -INFINITY, s = 0.f;
@@ -474,7 +525,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(
   const int lane = threadIdx.x;
   const float c = kLog2E / temp;
   const bool live =
-      teach<T, 64, false>(z + row * ldz, ids + row * k, top + row * k, k, V, c, lane, en);
+      teach<T, 64, false>(z + row * ldz, ids + row * k, top + row * k, k, V, c, lane, en, 0, 0);
   if (!live) {
     if (lane == 0) {
       loss[row] = 0.f;
@@ -519,7 +570,8 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(
     r = join_parts(parts + row * count, count, c, &s);
   }
   if (lane < 64) {
-    const bool live = teach<T, 64, true>(zr, ids + row * k, top + row * k, k, V, c, lane, en);
+    const bool live = teach<T, 64, true>(zr, ids + row * k, top + row * k, k, V, c, lane, en,
+                                         v0 * N, (v1 - v0) * N);
     if (loss != nullptr && blockIdx.y == 0) {
       const float a = live ? loss_terms<64>(k, temp, r, lane, en) : 0.f;
       if (lane == 0) loss[row] = temp * temp * a;
@@ -557,9 +609,11 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(
 
 int vectors_of(int32_t V, int is_bf16) { return is_bf16 ? (V + 7) / 8 : (V + 3) / 4; }
 
-// Entries a row up to which 32 (16) rows share a workgroup: theirs fill half of
-// the 64 KB of LDS that a launch has without asking.
-constexpr int kTop32 = 64, kTop16 = 128;
+// Entries a row up to which 32 (16) rows share a workgroup.  Above 32 a row of 8
+// lanes waits for its entries (121,924 rows of 128 bf16, 64 entries, step: 60 us,
+// with 16 lanes 50; of 24 entries 28, 33); above 128 those of 16 rows would fill
+// more than half of the 64 KB of LDS that a launch has without asking.
+constexpr int kTop32 = 32, kTop16 = 128;
 
 constexpr int kRowVectors = 4096;  // the longest row held in registers
 
@@ -581,7 +635,8 @@ hipError_t run_rows(const DistillArgs& a, hipStream_t stream) {
     constexpr int G = decltype(g)::value, NV = decltype(v)::value;
     constexpr int BLOCK = G > 256 ? G : 256, R = BLOCK / G;
     distill_row_kernel<T, G, NV, PASS>
-        <<<(unsigned)((a.n + R - 1) / R), BLOCK, (size_t)R * entry_words(a.k) * 4, stream>>>(
+        <<<(unsigned)((a.n + R - 1) / R), BLOCK, (size_t)R * entry_words(a.k, PASS == Pass::kForward ? 0 : a.V) * 4,
+           stream>>>(
             static_cast<const T*>(a.z), a.ldz, a.n, a.V, a.ids, a.top, a.k, a.temp, a.weight,
             a.loss, a.lse, static_cast<T*>(a.dz), a.lddz);
     return hipGetLastError();
@@ -608,7 +663,7 @@ template <typename T>
 hipError_t run_grad(const DistillArgs& a, int count, int per, hipStream_t stream) {
   const int nvec = vectors_of(a.V, sizeof(T) == 2);
   const dim3 grid((unsigned)a.n, (nvec + per - 1) / per);
-  distill_grad_kernel<T><<<grid, 256, (size_t)entry_words(a.k) * 4, stream>>>(
+  distill_grad_kernel<T><<<grid, 256, (size_t)entry_words(a.k, per * Row<T>::N) * 4, stream>>>(
       static_cast<const T*>(a.z), a.ldz, a.V, per, static_cast<const f32x2*>(a.parts), count,
       a.lse, a.ids, a.top, a.k, a.temp, a.weight, a.loss, static_cast<T*>(a.dz), a.lddz);
   return hipGetLastError();
@@ -631,7 +686,7 @@ hipError_t run_forward(const DistillArgs& a, hipStream_t stream) {
   int per;
   const hipError_t e = run_parts<T>(a, count, &per, stream);
   if (e != hipSuccess) return e;
-  distill_join_kernel<T><<<(unsigned)a.n, 64, (size_t)entry_words(a.k) * 4, stream>>>(
+  distill_join_kernel<T><<<(unsigned)a.n, 64, (size_t)entry_words(a.k, 0) * 4, stream>>>(
       static_cast<const T*>(a.z), a.ldz, a.V, static_cast<const f32x2*>(a.parts), count, a.ids,
       a.top, a.k, a.temp, a.loss, a.lse);
   return hipGetLastError();
@@ -648,10 +703,15 @@ hipError_t run_step(const DistillArgs& a, hipStream_t stream) {
 
 template <typename T>
 hipError_t run_backward(const DistillArgs& a, hipStream_t stream) {
-  // elementwise but for the entries: long rows are cut up whatever their number
+  // elementwise but for the entries, which every part of a row works out: rows in
+  // registers where there are enough of them (30,000 of bf16, 256 entries: 4,000 rows
+  // 115 us, in parts 138; 300 rows of 32 entries 10.8, 9.9), and longer parts where
+  // there are many entries (1,500 rows of 120,000, 256 entries: 175, in parts of 1024
+  // vectors 210; of 64 entries 147, 146)
   const int nvec = vectors_of(a.V, sizeof(T) == 2);
-  if (nvec <= 1024) return run_rows<T, Pass::kBackward>(a, stream);
-  const int per = 1024;
+  if (nvec <= 1024 || (nvec <= kRowVectors && a.n >= 512))
+    return run_rows<T, Pass::kBackward>(a, stream);
+  const int per = a.k > 128 ? 2048 : 1024;
   return run_grad<T>(a, 0, per, stream);
 }
 

@@ -157,6 +157,36 @@ def test_repeated_ids_share_their_probability():
     check(z, ids, top, 1.0, None, "f32")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,k", [(40, 16), (40, 17), (300, 33), (300, 200), (1000, 129),
+                                 (9000, 64), (33001, 256), (262145, 40), (300000, 256)])
+def test_rows_with_and_without_repeated_ids(dtype, V, k):
+    """Side by side: ids all different, one of them twice, ids that are equal in
+    their low bits only, one id throughout, and absent ones between."""
+    r = np.random.default_rng(V + k)
+    z = 2 * r.standard_normal((7, V))
+    ids = np.stack([r.permutation(V)[:k] for _ in range(7)])
+    ids[1, k - 1] = ids[1, 0]
+    ids[2, 1:4] = ids[2, 0]
+    ids[3] = V - 1
+    half = k // 2
+    ids[4, half:2 * half] = (ids[4, :half] + 131072) % V
+    ids[5, ::3] = -1
+    ids[6, ::2] = V
+    top = 3 * r.standard_normal((7, k))
+    np.put_along_axis(z, np.where((ids >= 0) & (ids < V), ids, 0),
+                      top + 0.5 * r.standard_normal((7, k)), 1)
+    check(z, ids, top, 1.5, r.random(7) + 0.5, dtype)
+
+
+def test_backward_of_many_long_rows():
+    r = np.random.default_rng(11)
+    z, ids, top = case(r, 513, 9000, 20, True)
+    check(z, ids, top, 1.0, None, "bf16")
+    z, ids, top = case(r, 512, 4200, 40, False)
+    check(z, ids, top, 1.0, None, "f32")
+
+
 def test_padding_rows_are_not_read():
     """A row without entries may hold anything."""
     z = np.zeros((4, 600))
