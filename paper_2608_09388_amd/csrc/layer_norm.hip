@@ -15,10 +15,10 @@
 // the two column sums) in registers and the next row's vectors in flight.
 //
 // The column sums dgamma and dbeta: every thread sums its columns over its
-// rows, the groups of a workgroup are added in LDS in order, every workgroup
-// writes one partial row to the workspace, and a second launch adds the
-// partial rows in a fixed order.  The number of workgroups follows the sizes
-// alone, so results repeat bit for bit.
+// rows, the groups of a wavefront are added across its lanes and the wavefronts of
+// a workgroup in LDS, every workgroup writes one partial row to the workspace, and a
+// second launch adds the partial rows, all in a fixed order.  The number of
+// workgroups follows the sizes alone, so results repeat bit for bit.
 #include <algorithm>
 
 #include "row_ops.h"
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_backward_kernel(
     const float* __restrict__ rstd, T* __restrict__ dx, int64_t lddx, float* __restrict__ col) {
   constexpr int N = Row<T>::N, BLOCK = G > 256 ? G : 256, R = BLOCK / G;
   __shared__ float part[G > 64 ? BLOCK / 64 : 1];
-  // column sums of the workgroup's groups (R > 1), one group's at a time
+  // column sums of the workgroup's wavefronts (R > 1), one's at a time
   __shared__ float cols[R > 1 ? 2 * G * NV * N : 1];
   const int lane = threadIdx.x % G;
   const int nvec = (C + N - 1) / N;
@@ -198,11 +198,20 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_backward_kernel(
     }
   }
   if (col == nullptr) return;
-  // the groups' sums, added one group after the other
+  // the sums of a wavefront's groups, then of the wavefronts, one after the other
   if constexpr (R > 1) {
-    for (int r = 1; r < R; ++r) {
+    constexpr int WAVES = BLOCK / 64;
+#pragma unroll
+    for (int q = 0; q < NV; ++q)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        dg[q][e] = groups_sum<G>(dg[q][e]);
+        db[q][e] = groups_sum<G>(db[q][e]);
+      }
+    const int first = threadIdx.x & 63;  // the lanes of a wavefront's first group
+    for (int w = 1; w < WAVES; ++w) {
       __syncthreads();
-      if (threadIdx.x / G == r) {
+      if (threadIdx.x >> 6 == w && first < G) {
 #pragma unroll
         for (int q = 0; q < NV; ++q)
 #pragma unroll
@@ -286,12 +295,15 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(const float* __restric
 // 90 backward, 512 of two 70 and 125.  A row in one wavefront needs no barrier,
 // which the backward, with more registers a vector and fewer wavefronts, gains by
 // up to 256 vectors (16,384 rows of 2,048: 46 us, 54 with 256 lanes), the forward up
-// to 192 (of 2,048: 30, 27 with 256 lanes).
+// to 192 (of 2,048: 30, 27 with 256 lanes).  Short rows are bound by the steps that a
+// group's lanes wait for: 200,000 rows of 64 bf16 take 10.6 and 20.4 us with 8 lanes,
+// 14.9 and 24.5 with 16.
 template <typename T, bool BACKWARD, typename F>
 auto with_shape(int nvec, F&& f) {
   using std::integral_constant;
 #define SHC_SHAPE(limit, g, v) \
   if (nvec <= limit) return f(integral_constant<int, g>{}, integral_constant<int, v>{})
+  SHC_SHAPE(8, 8, 1);
   SHC_SHAPE(16, 16, 1);
   SHC_SHAPE(32, 32, 1);
   SHC_SHAPE(64, 64, 1);

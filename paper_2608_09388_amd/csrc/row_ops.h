@@ -180,6 +180,22 @@ __device__ __forceinline__ float lanes_reduce(float x, Op op) {
   }
   return x;
 }
+// Sum over the lanes of a wavefront that have the same place in their groups of G.
+template <int G>
+__device__ __forceinline__ float groups_sum(float x) {
+  if constexpr (G <= 8) x += dpp<0x128>(x);  // row_ror 8
+  if constexpr (G <= 16) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  }
+  if constexpr (G <= 32) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  }
+  return x;
+}
 struct AddOp {
   __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
 };
