@@ -6,7 +6,9 @@
 // Forward: a gather bound by HBM.  G lanes share a row and walk its 16-byte
 // vectors, 256 / G rows a workgroup.
 //
-// Gradient: the positions are ordered by id, then added.
+// Gradient of up to 512 positions: one launch, embed_few_kernel; every position
+// looks through the list for its id.  Of more: the positions are ordered by id, then
+// added.
 // 1. embed_split_kernel (past kDirectRows positions) cuts the list of ids into
 //    chunks and orders each chunk's positions by bucket, id modulo 1024 (frequent
 //    ids, often neighbours, then fall to different buckets): every wavefront
@@ -14,8 +16,9 @@
 // 2. embed_order_kernel, a workgroup a bucket, takes its segments of all chunks in
 //    order (of few positions: the ids themselves), counts its ids and hands out
 //    the places: wavefronts take a queue in LDS in shares and rank 64 positions at a
-//    time by ballots over the ids' bits.  Its first place in the order is the number of positions in
-//    buckets before it, which the chunks' offsets give without communication.
+//    time by ballots over the ids' bits.  Its first place in the order is the number
+//    of positions in buckets before it, which the chunks' offsets give without
+//    communication.
 // 3. embed_sum_kernel cuts the order into jobs of J positions, whatever the ids'
 //    frequencies; lanes that share a job and a column range add each id's rows in
 //    order.  A job takes the ids that begin in it, to their end; ids of many
@@ -448,6 +451,101 @@ __device__ __forceinline__ void clear_vec(float* row, int v, int C, int past) {
     store_channels<4>(row, v, C, z);
 }
 
+// Up to kFew positions in one launch.  A workgroup of [0, sums) takes a position and
+// a range of 64 vectors, and wavefront w the positions [64 w, 64 w + 64) of the same
+// id, found by a ballot; where the position is the id's first, each adds its rows in
+// order, and their sums are added in order.  The others clear the table rows of ids
+// without a position, `rows` at a time.  Into a table of 5,000: 64 rows of 1,024 bf16
+// 6.4 us, by the launches below 13.8; 512 rows 8.4, 18.0 (one id throughout: 14.7,
+// 17.4); with 1,024 positions to a workgroup 1,024 rows 21.4, 18.5.
+constexpr int kFew = 512;
+template <typename T, typename ID>
+__global__ __launch_bounds__(kFew) void embed_few_kernel(
+    const T* __restrict__ dY, int64_t lddy, const ID* __restrict__ ids, int64_t id_stride, int n,
+    int R, int pad, int sums, int rows, int past, int C, float scale, int accumulate,
+    float* __restrict__ dE, int64_t ldE) {
+  constexpr int N = Row<T>::N, U = 8, W = kFew / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int mine = (int)threadIdx.x < n ? valid_id(ids, id_stride, threadIdx.x, R, pad) : -1;
+  if ((int)blockIdx.x >= sums) {
+    __shared__ uint32_t there[2 * W];  // a bit a row
+    const int nv = (C + 3) / 4;
+    int wide = 64;
+    while (wide > 1 && wide / 2 >= nv) wide /= 2;
+    const int step = (gridDim.x - sums) * rows;
+    for (int r0 = (blockIdx.x - sums) * rows; r0 < R; r0 += step) {
+      if (threadIdx.x < 2 * W) there[threadIdx.x] = 0;
+      __syncthreads();
+      const int at = mine - r0;
+      if (mine >= 0 && at >= 0 && at < rows) atomicOr(&there[at >> 5], 1u << (at & 31));
+      __syncthreads();
+      const int end = min(rows, R - r0);
+      for (int i = threadIdx.x / wide; i < end; i += kFew / wide)
+        if (!((there[i >> 5] >> (i & 31)) & 1))
+          for (int v = lane % wide; v < nv; v += wide)
+            clear_vec(dE + (int64_t)(r0 + i) * ldE, v, C, past);
+      __syncthreads();
+    }
+    return;
+  }
+  __shared__ int some[W];
+  __shared__ f32x4 sum[W > 1 ? W - 1 : 1][N / 4][64];
+  const int tiles = ((C + N - 1) / N + 63) / 64;
+  const int i = blockIdx.x / tiles, v = blockIdx.x % tiles * 64 + lane;
+  const int key = valid_id(ids, id_stride, i, R, pad);
+  uint64_t same = __ballot(mine >= 0 && mine == key);
+  if (lane == 0) some[wave] = same == 0 ? 64 : __ffsll((unsigned long long)same) - 1;
+  __syncthreads();
+  int first = -1;
+#pragma unroll
+  for (int w = W - 1; w >= 0; --w)
+    if (some[w] < 64) first = w * 64 + some[w];
+  if (first != i) return;  // the whole workgroup
+  float acc[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
+  while (same != 0) {
+    i32x4 raw[U];
+    int count = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      raw[u] = i32x4{};
+      if (same != 0) {
+        const int64_t at = wave * 64 + __ffsll((unsigned long long)same) - 1;
+        same &= same - 1;
+        if (v * N < C) raw[u] = load_vec(dY + at * lddy, v, C);
+        ++count;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float f[N];
+      Row<T>::widen(raw[u], f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] = u < count ? acc[e] + f[e] : acc[e];
+    }
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4)
+      sum[wave - 1][e / 4][lane] = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+  }
+  __syncthreads();
+  if (wave > 0 || v * N >= C) return;
+#pragma unroll
+  for (int w = 1; w < W; ++w)
+    if (some[w] < 64) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] += sum[w - 1][e / 4][lane][e % 4];
+    }
+  float* to = dE + (int64_t)key * ldE;
+  float f[N];
+  if (accumulate) load_channels<N>(to, v, C, f);
+#pragma unroll
+  for (int e = 0; e < N; ++e) f[e] = accumulate ? fmaf(acc[e], scale, f[e]) : acc[e] * scale;
+  store_channels<N>(to, v, C, f);
+}
+
 // Workgroups [0, sums): jobs of J positions, G lanes each, by column ranges of
 // G vectors.  part [jobs][2][C]: of a cut id that began in an earlier job, what
 // this job adds (slot 0); of one that goes on in the next job, what this one, in
@@ -459,8 +557,8 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(
     const T* __restrict__ dY, int64_t lddy, int64_t n, const int32_t* __restrict__ order,
     const uint32_t* __restrict__ key_of, const int32_t* __restrict__ run_end,
     const uint32_t* __restrict__ present, int words, const int32_t* __restrict__ total, int jobs,
-    int sums, int clear, int past, int R, int C, float scale, int accumulate, float* __restrict__ dE,
-    int64_t ldE, float* __restrict__ part) {
+    int sums, int clear, int past, int R, int C, float scale, int accumulate,
+    float* __restrict__ dE, int64_t ldE, float* __restrict__ part) {
   constexpr int N = Row<T>::N, U = 8, TAKE = 3 * J;
   __shared__ __align__(16) int pos_sh[256 / G][TAKE];
   __shared__ __align__(16) uint32_t key_sh[256 / G][TAKE];
@@ -766,13 +864,34 @@ hipError_t embed_order(const void* ids, int64_t id_stride, int64_t n, int64_t R,
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     embed_order_kernel<ID, false><<<kBuckets, kSortThreads, w.p.lds, stream>>>(
-        in, id_stride, n, (int)R, pad, w.p.keys, w.p.key_bits, 2 * w.p.J, w.split, w.offs, w.p.chunks,
-        w.p.chunk, w.order, w.key_of, w.run_end, w.present, w.p.words, w.total);
+        in, id_stride, n, (int)R, pad, w.p.keys, w.p.key_bits, 2 * w.p.J, w.split, w.offs,
+        w.p.chunks, w.p.chunk, w.order, w.key_of, w.run_end, w.present, w.p.words, w.total);
   } else {
     embed_order_kernel<ID, true><<<kBuckets, kSortThreads, w.p.lds, stream>>>(
-        in, id_stride, n, (int)R, pad, w.p.keys, w.p.key_bits, 2 * w.p.J, w.split, w.offs, 0, 0, w.order,
-        w.key_of, w.run_end, w.present, w.p.words, w.total);
+        in, id_stride, n, (int)R, pad, w.p.keys, w.p.key_bits, 2 * w.p.J, w.split, w.offs, 0, 0,
+        w.order, w.key_of, w.run_end, w.present, w.p.words, w.total);
   }
+  return hipGetLastError();
+}
+
+// Rows that a wavefront clears at a time, about 16 KB of them.
+int clear_rows(int32_t C) { return std::max(1, std::min(64, 4096 / C)); }
+// Whether the cleared rows go past the caches: where the table does not fit the
+// Infinity Cache, so that dY may stay there (4,096 rows, table of 32,768 x 4,096:
+// 113 us, 133 through the caches; of 64 rows: 107, 103).
+int clear_past(int64_t R, int32_t C) { return R * C >= (int64_t)1 << 26; }
+
+template <typename T, typename ID>
+hipError_t embed_few(const void* dY, int64_t lddy, const void* ids, int64_t id_stride, int64_t n,
+                     int64_t R, int pad, int32_t C, float scale, int accumulate, float* dE,
+                     int64_t ldE, hipStream_t stream) {
+  const int tiles = ((C + Row<T>::N - 1) / Row<T>::N + 63) / 64;
+  const int sums = (int)n * tiles, rows = kFew / 64 * clear_rows(C);
+  const int clears = accumulate ? 0 : (int)std::min<int64_t>((R + rows - 1) / rows, 16384);
+  if (sums + clears == 0) return hipSuccess;
+  embed_few_kernel<T, ID><<<sums + clears, kFew, 0, stream>>>(
+      static_cast<const T*>(dY), lddy, static_cast<const ID*>(ids), id_stride, (int)n, (int)R, pad,
+      sums, rows, clear_past(R, C), C, scale, accumulate, dE, ldE);
   return hipGetLastError();
 }
 
@@ -784,13 +903,10 @@ hipError_t embed_sum(const void* dY, int64_t lddy, int64_t n, int64_t R, const E
   auto go = [&](auto g, auto job) {
     constexpr int G = decltype(g)::value, J = decltype(job)::value;
     const int sums = (w.p.jobs + 256 / G - 1) / (256 / G) * ((nvec + G - 1) / G);
-    // about 16 KB a wavefront at a time; past the caches where the table does not
-    // fit the Infinity Cache, so that dY may stay there (4,096 rows, table of 32,768
-    // x 4,096: 113 us, 133 through the caches; of 64 rows: 107, 103)
-    const int clear = std::max(1, std::min(64, 4096 / C));
+    const int clear = clear_rows(C);
     const int clears =
         accumulate ? 0 : (int)std::min<int64_t>((R + 4 * clear - 1) / (4 * clear), 16384);
-    const int past = R * C >= (int64_t)1 << 26;
+    const int past = clear_past(R, C);
     if (sums + clears == 0) return hipSuccess;
     embed_sum_kernel<T, G, J><<<sums + clears, 256, 0, stream>>>(
         static_cast<const T*>(dY), lddy, n, w.order, w.key_of, w.run_end, w.present, w.p.words,
@@ -842,6 +958,12 @@ hipError_t launch_embed_rows_backward(const void* dY, int64_t lddy, const void* 
                                       float scale, int64_t pad, int is_bf16, int accumulate,
                                       float* dE, int64_t ldE, void* ws, hipStream_t stream) {
   if (n == 0 && accumulate) return hipSuccess;
+  const int pad32 = pad >= 0 && pad < R ? (int)pad : -1;
+  if (n <= kFew) {
+    auto few = is_bf16 ? (id64 ? embed_few<uint16_t, int64_t> : embed_few<uint16_t, int32_t>)
+                       : (id64 ? embed_few<float, int64_t> : embed_few<float, int32_t>);
+    return few(dY, lddy, ids, id_stride, n, R, pad32, C, scale, accumulate, dE, ldE, stream);
+  }
   EmbedWork w;
   embed_plan(n, R, C, &w.p);
   char* b = static_cast<char*>(ws);
@@ -853,13 +975,12 @@ hipError_t launch_embed_rows_backward(const void* dY, int64_t lddy, const void* 
   w.split = reinterpret_cast<i32x2*>(b + w.p.off_split);
   w.offs = reinterpret_cast<int32_t*>(b + w.p.off_offs);
   w.part = reinterpret_cast<float*>(b + w.p.off_part);
-  const int pad32 = pad >= 0 && pad < R ? (int)pad : -1;
   hipError_t e = (id64 ? embed_order<int64_t> : embed_order<int32_t>)(ids, id_stride, n, R, pad32,
                                                                       w, stream);
   if (e != hipSuccess) return e;
-  e = (is_bf16 ? embed_sum<uint16_t> : embed_sum<float>)(dY, lddy, n, R, w, C, scale, accumulate, dE,
-                                                          ldE, stream);
-  if (e != hipSuccess || n <= 2 * w.p.J) return e;  // no id is cut
+  e = (is_bf16 ? embed_sum<uint16_t> : embed_sum<float>)(dY, lddy, n, R, w, C, scale, accumulate,
+                                                         dE, ldE, stream);
+  if (e != hipSuccess) return e;
   auto join = [&](auto l) {
     constexpr int L = decltype(l)::value;
     const dim3 grid(std::min((w.p.jobs + kJoinJobs - 1) / kJoinJobs, 1 << 14),

@@ -100,6 +100,28 @@ def grad_case(r, n, R, kind):
     return r.integers(-3, R + 3, n)          # "outside"
 
 
+@pytest.mark.parametrize("kind", ["uniform", "zipf", "one", "runs", "outside"])
+@pytest.mark.parametrize("n", [63, 64, 65, 200, 511, 512, 513])
+@pytest.mark.parametrize("C,R,dtype", [(8, 600, "f32"), (521, 3, "bf16"), (300, 70, "f32")])
+def test_gradient_of_few_positions(kind, n, C, R, dtype):
+    """At the border between one launch and several; rows of ids that do not count
+    hold NaN."""
+    r = np.random.default_rng(n + C)
+    ids = grad_case(r, n, R, kind)
+    pad = int(ids[0]) if kind == "zipf" else -1
+    rows = r.standard_normal((n, C))
+    rows[(ids < 0) | (ids >= R) | (ids == pad)] = np.nan
+    dY, dE = Rows(n, C, dtype, 1, 1, rows), Rows(R, C, "f32", 2, 0)
+    shc.embed_rows_backward(dY.t, ids_tensor(ids, torch.int64, 1), dE.t, pad_id=pad)
+    clean = np.nan_to_num(dY.get())
+    ref = O.embed_backward(clean, ids, R, 1.0, pad)
+    size = O.embed_backward(np.abs(clean), ids, R, 1.0, pad)
+    count = O.embed_backward(np.ones((n, 1)), ids, R, 1.0, pad)
+    close(dE.get(), ref, 2 * ((count + 2) * u * size + u * np.abs(ref)), "dE")
+    assert np.all(dE.get()[count[:, 0] == 0] == 0)
+    dE.check_guard()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,R,C,kind,extra,off", [
     (0, 5, 8, "uniform", 0, 0), (1, 1, 1, "uniform", 0, 0), (2, 3, 7, "outside", 1, 1),
