@@ -6,7 +6,7 @@
 // Forward: a gather bound by HBM.  G lanes share a row and walk its 16-byte
 // vectors, 256 / G rows a workgroup.
 //
-// Gradient of up to 512 positions: one launch, embed_few_kernel; every position
+// Gradient of few positions (few_rows): one launch, embed_few_kernel; every position
 // looks through the list for its id.  Of more: the positions are ordered by id, then
 // added.
 // 1. embed_split_kernel (past kDirectRows positions) cuts the list of ids into
@@ -451,22 +451,27 @@ __device__ __forceinline__ void clear_vec(float* row, int v, int C, int past) {
     store_channels<4>(row, v, C, z);
 }
 
-// Up to kFew positions in one launch.  A workgroup of [0, sums) takes a position and
-// a range of 64 vectors, and wavefront w the positions [64 w, 64 w + 64) of the same
-// id, found by a ballot; where the position is the id's first, each adds its rows in
+// Few positions in one launch.  A workgroup of [0, sums) takes a position and a range
+// of 64 vectors, and wavefront w the positions [64 M w, 64 M (w + 1)) of the same id,
+// found by ballots; where the position is the id's first, each adds its rows in
 // order, and their sums are added in order.  The others clear the table rows of ids
 // without a position, `rows` at a time.  Into a table of 5,000: 64 rows of 1,024 bf16
-// 6.4 us, by the launches below 13.8; 512 rows 8.4, 18.0 (one id throughout: 14.7,
-// 17.4); with 1,024 positions to a workgroup 1,024 rows 21.4, 18.5.
-constexpr int kFew = 512;
-template <typename T, typename ID>
-__global__ __launch_bounds__(kFew) void embed_few_kernel(
+// 6.4 us, by the launches below 13.8; 512 rows 7.9, 18.0 (one id throughout: 13.9,
+// 17.4).
+constexpr int kFewThreads = 512;
+template <typename T, typename ID, int M>
+__global__ __launch_bounds__(kFewThreads) void embed_few_kernel(
     const T* __restrict__ dY, int64_t lddy, const ID* __restrict__ ids, int64_t id_stride, int n,
     int R, int pad, int sums, int rows, int past, int C, float scale, int accumulate,
     float* __restrict__ dE, int64_t ldE) {
-  constexpr int N = Row<T>::N, U = 8, W = kFew / 64;
+  constexpr int N = Row<T>::N, U = 8, W = kFewThreads / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int mine = (int)threadIdx.x < n ? valid_id(ids, id_stride, threadIdx.x, R, pad) : -1;
+  int mine[M];
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    const int i = (wave * M + m) * 64 + lane;
+    mine[m] = i < n ? valid_id(ids, id_stride, i, R, pad) : -1;
+  }
   if ((int)blockIdx.x >= sums) {
     __shared__ uint32_t there[2 * W];  // a bit a row
     const int nv = (C + 3) / 4;
@@ -476,11 +481,14 @@ __global__ __launch_bounds__(kFew) void embed_few_kernel(
     for (int r0 = (blockIdx.x - sums) * rows; r0 < R; r0 += step) {
       if (threadIdx.x < 2 * W) there[threadIdx.x] = 0;
       __syncthreads();
-      const int at = mine - r0;
-      if (mine >= 0 && at >= 0 && at < rows) atomicOr(&there[at >> 5], 1u << (at & 31));
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        const int at = mine[m] - r0;
+        if (mine[m] >= 0 && at >= 0 && at < rows) atomicOr(&there[at >> 5], 1u << (at & 31));
+      }
       __syncthreads();
       const int end = min(rows, R - r0);
-      for (int i = threadIdx.x / wide; i < end; i += kFew / wide)
+      for (int i = threadIdx.x / wide; i < end; i += kFewThreads / wide)
         if (!((there[i >> 5] >> (i & 31)) & 1))
           for (int v = lane % wide; v < nv; v += wide)
             clear_vec(dE + (int64_t)(r0 + i) * ldE, v, C, past);
@@ -493,36 +501,46 @@ __global__ __launch_bounds__(kFew) void embed_few_kernel(
   const int tiles = ((C + N - 1) / N + 63) / 64;
   const int i = blockIdx.x / tiles, v = blockIdx.x % tiles * 64 + lane;
   const int key = valid_id(ids, id_stride, i, R, pad);
-  uint64_t same = __ballot(mine >= 0 && mine == key);
-  if (lane == 0) some[wave] = same == 0 ? 64 : __ffsll((unsigned long long)same) - 1;
+  uint64_t same[M];
+  int begin = n;  // the wavefront's first position of that id
+#pragma unroll
+  for (int m = M - 1; m >= 0; --m) {
+    same[m] = __ballot(mine[m] >= 0 && mine[m] == key);
+    if (same[m] != 0)
+      begin = (wave * M + m) * 64 + __ffsll((unsigned long long)same[m]) - 1;
+  }
+  if (lane == 0) some[wave] = begin;
   __syncthreads();
-  int first = -1;
+  int first = n;
 #pragma unroll
   for (int w = W - 1; w >= 0; --w)
-    if (some[w] < 64) first = w * 64 + some[w];
+    if (some[w] < n) first = some[w];
   if (first != i) return;  // the whole workgroup
   float acc[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) acc[e] = 0.f;
-  while (same != 0) {
-    i32x4 raw[U];
-    int count = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      raw[u] = i32x4{};
-      if (same != 0) {
-        const int64_t at = wave * 64 + __ffsll((unsigned long long)same) - 1;
-        same &= same - 1;
-        if (v * N < C) raw[u] = load_vec(dY + at * lddy, v, C);
-        ++count;
+  for (int m = 0; m < M; ++m) {
+    while (same[m] != 0) {
+      i32x4 raw[U];
+      int count = 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        raw[u] = i32x4{};
+        if (same[m] != 0) {
+          const int64_t at = (wave * M + m) * 64 + __ffsll((unsigned long long)same[m]) - 1;
+          same[m] &= same[m] - 1;
+          if (v * N < C) raw[u] = load_vec(dY + at * lddy, v, C);
+          ++count;
+        }
       }
-    }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float f[N];
-      Row<T>::widen(raw[u], f);
+      for (int u = 0; u < U; ++u) {
+        float f[N];
+        Row<T>::widen(raw[u], f);
 #pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] = u < count ? acc[e] + f[e] : acc[e];
+        for (int e = 0; e < N; ++e) acc[e] = u < count ? acc[e] + f[e] : acc[e];
+      }
     }
   }
   if (wave > 0) {
@@ -534,7 +552,7 @@ __global__ __launch_bounds__(kFew) void embed_few_kernel(
   if (wave > 0 || v * N >= C) return;
 #pragma unroll
   for (int w = 1; w < W; ++w)
-    if (some[w] < 64) {
+    if (some[w] < n) {
 #pragma unroll
       for (int e = 0; e < N; ++e) acc[e] += sum[w - 1][e / 4][lane][e % 4];
     }
@@ -734,8 +752,8 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(
   }
 }
 
-// Positions up to which every bucket reads the ids itself: one launch less (1,500
-// rows of 64 bf16: 23.0 us, 24.5 with the split; 3,000: 27.7, 26.4).
+// Positions up to which every bucket reads the ids itself: one launch less (1,024
+// rows of 5,000 bf16: 34.8 us, 40.0 with the split; 2,048: 42.9, 45.6).
 constexpr int64_t kDirectRows = 2048;
 // Positions from which a chunk is split by 1024 threads: fewer, longer segments
 // (1,340,800 rows of 64 bf16: 133 us, 146 by 256 threads; 268,160: 33.6, 33.0).
@@ -881,18 +899,34 @@ int clear_rows(int32_t C) { return std::max(1, std::min(64, 4096 / C)); }
 // 113 us, 133 through the caches; of 64 rows: 107, 103).
 int clear_past(int64_t R, int32_t C) { return R * C >= (int64_t)1 << 26; }
 
+// Whether one launch does it: a position's workgroups, one for each range of columns,
+// look through the whole list, so that the work grows with the positions' square
+// (5,000 ids, bf16: 1,500 rows of 2,000 take 24.1 us, by the launches below 25.3; 2,048
+// rows 30.2, 25.3, of 500 10.6, 24.2).  One id throughout is the worst of it: 2,048 rows
+// of 64 take 40 us, 26.
+constexpr int kFewMost = 4 * kFewThreads;
+bool few_rows(int64_t n, int32_t C, int is_bf16) {
+  const int per = is_bf16 ? 512 : 256;
+  return n <= kFewThreads || (n <= kFewMost && n * ((C + per - 1) / per) <= 6144);
+}
+
 template <typename T, typename ID>
 hipError_t embed_few(const void* dY, int64_t lddy, const void* ids, int64_t id_stride, int64_t n,
                      int64_t R, int pad, int32_t C, float scale, int accumulate, float* dE,
                      int64_t ldE, hipStream_t stream) {
   const int tiles = ((C + Row<T>::N - 1) / Row<T>::N + 63) / 64;
-  const int sums = (int)n * tiles, rows = kFew / 64 * clear_rows(C);
+  const int sums = (int)n * tiles, rows = kFewThreads / 64 * clear_rows(C);
   const int clears = accumulate ? 0 : (int)std::min<int64_t>((R + rows - 1) / rows, 16384);
   if (sums + clears == 0) return hipSuccess;
-  embed_few_kernel<T, ID><<<sums + clears, kFew, 0, stream>>>(
-      static_cast<const T*>(dY), lddy, static_cast<const ID*>(ids), id_stride, (int)n, (int)R, pad,
-      sums, rows, clear_past(R, C), C, scale, accumulate, dE, ldE);
-  return hipGetLastError();
+  auto go = [&](auto m) {
+    embed_few_kernel<T, ID, decltype(m)::value><<<sums + clears, kFewThreads, 0, stream>>>(
+        static_cast<const T*>(dY), lddy, static_cast<const ID*>(ids), id_stride, (int)n, (int)R,
+        pad, sums, rows, clear_past(R, C), C, scale, accumulate, dE, ldE);
+    return hipGetLastError();
+  };
+  if (n <= kFewThreads) return go(std::integral_constant<int, 1>{});
+  if (n <= 2 * kFewThreads) return go(std::integral_constant<int, 2>{});
+  return go(std::integral_constant<int, 4>{});
 }
 
 template <typename T>
@@ -959,7 +993,7 @@ hipError_t launch_embed_rows_backward(const void* dY, int64_t lddy, const void* 
                                       float* dE, int64_t ldE, void* ws, hipStream_t stream) {
   if (n == 0 && accumulate) return hipSuccess;
   const int pad32 = pad >= 0 && pad < R ? (int)pad : -1;
-  if (n <= kFew) {
+  if (few_rows(n, C, is_bf16)) {
     auto few = is_bf16 ? (id64 ? embed_few<uint16_t, int64_t> : embed_few<uint16_t, int32_t>)
                        : (id64 ? embed_few<float, int64_t> : embed_few<float, int32_t>);
     return few(dY, lddy, ids, id_stride, n, R, pad32, C, scale, accumulate, dE, ldE, stream);

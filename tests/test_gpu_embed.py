@@ -101,8 +101,9 @@ def grad_case(r, n, R, kind):
 
 
 @pytest.mark.parametrize("kind", ["uniform", "zipf", "one", "runs", "outside"])
-@pytest.mark.parametrize("n", [63, 64, 65, 200, 511, 512, 513])
-@pytest.mark.parametrize("C,R,dtype", [(8, 600, "f32"), (521, 3, "bf16"), (300, 70, "f32")])
+@pytest.mark.parametrize("n", [63, 64, 65, 200, 511, 512, 513, 1024, 1025, 2047, 2048, 2049])
+@pytest.mark.parametrize("C,R,dtype", [(8, 600, "f32"), (521, 3, "bf16"), (300, 70, "f32"),
+                                       (1300, 900, "f32")])
 def test_gradient_of_few_positions(kind, n, C, R, dtype):
     """At the border between one launch and several; rows of ids that do not count
     hold NaN."""
