@@ -26,15 +26,15 @@
 //    positions are cut at the jobs' borders instead, their parts left in
 //    the workspace.  Other workgroups of the launch clear the table rows of ids
 //    without a position meanwhile.
-// 4. embed_join_kernel adds the parts, in order.
+// 4. embed_join_kernel adds the parts of the ids that the sums listed, in order.
 // Every sum has an order that follows the ids and sizes alone: results repeat
 // bit for bit.
 //
 // Measured: 16,384 rows of 4,096 bf16 into a table of 32,768, ids as frequent as
-// words: 148 us, 4.5 TB/s over all (6, 8, 127 and 7 us: the sums and the clearing are
-// bound by HBM, the rest by latency); 268,160 rows of 128 into 10,475: 37 us (6, 9, 17
-// and 4).  One id of very many positions is the worst: its bucket is one workgroup's
-// (65,536 rows of 1,024, one id: 600 us).
+// words: 146 us, 4.6 TB/s over all (6, 8, 127 and 5 us: the sums and the clearing are
+// bound by HBM, the rest by latency); 268,160 rows of 128 into 10,475: 34.5 us (6, 9,
+// 16 and 3).  One id of very many positions is the worst: its bucket is one workgroup's
+// (65,536 rows of 1,024, one id: 293 us).
 #include <algorithm>
 #include <mutex>
 
@@ -89,12 +89,9 @@ __global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ E, int
   }
 }
 
-constexpr int kSortThreads = 256;
-constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSplitPer = 4;                           // ids a thread of a chunk
-constexpr int kRoundPer = 4;                           // segments a thread of a round
-constexpr int kRound = kSortThreads * kRoundPer;       // segments of a round
-constexpr int kQueue = 1024;                           // positions in LDS at a time
+constexpr int kRound = 1024;                           // segments of a round
+constexpr int kQueuePer = 4;                           // positions a thread in LDS at a time
 constexpr int kLogBuckets = 10, kBuckets = 1 << kLogBuckets;
 constexpr uint32_t kCut = 0x80000000u;  // in key_of: an id whose run is cut at jobs' borders
 
@@ -222,26 +219,27 @@ __global__ __launch_bounds__(NT) void embed_split_kernel(
 // below 2^key_bits, local number id >> kLogBuckets.  order, key_of, run_end [n]:
 // position, id (with kCut where its positions are more than `most`) and the end of
 // the id's run, at its places; present [kBuckets][words]: a bit for every id with a
-// position; *total the number of positions with an id that counts.
-// LDS: place[keys], end[keys], at[kSortWaves][keys], the queue (local number,
+// position; total: the number of positions with an id that counts, and of cut ids,
+// none yet.
+// LDS: place[keys], end[keys], at[NT / 64][keys], the queue (local number,
 // position), a round of segments.
-template <typename ID, bool DIRECT>
-__global__ __launch_bounds__(kSortThreads) void embed_order_kernel(
+template <typename ID, int NT, bool DIRECT>
+__global__ __launch_bounds__(NT) void embed_order_kernel(
     const ID* __restrict__ ids, int64_t id_stride, int64_t n, int R, int pad, int keys,
     int key_bits, int most, const i32x2* __restrict__ split, const int32_t* __restrict__ offs,
     int chunks, int chunk, int32_t* __restrict__ order, uint32_t* __restrict__ key_of,
     int32_t* __restrict__ run_end, uint32_t* __restrict__ present, int words,
     int32_t* __restrict__ total) {
   extern __shared__ int smem[];
-  constexpr int PER = kQueue / kSortThreads;  // entries of the queue a thread
+  constexpr int W = NT / 64, PER = kQueuePer, QUEUE = NT * PER, SEGS = kRound / NT;
   int* place = smem;
   int* end = place + keys;
   int* at = end + keys;  // a wavefront's places, then its next ones
-  int* queue_key = at + kSortWaves * keys;
-  int* queue_pos = queue_key + kQueue;
-  int* seg_at = queue_pos + kQueue;  // [kRound]: a segment's first entry
+  int* queue_key = at + W * keys;
+  int* queue_pos = queue_key + QUEUE;
+  int* seg_at = queue_pos + QUEUE;  // [kRound]: a segment's first entry
   int* seg_src = seg_at + kRound;    // and where it lies in its chunk
-  __shared__ int wave_sum[kSortWaves];
+  __shared__ int wave_sum[W];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int p = blockIdx.x;
 
@@ -250,7 +248,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_order_kernel(
   int below = 0;
   auto each_queue = [&](auto&& f) {
     if constexpr (DIRECT) {
-      for (int64_t c0 = 0; c0 < n; c0 += kQueue) {
+      for (int64_t c0 = 0; c0 < n; c0 += QUEUE) {
         int key[PER];
         uint64_t has[PER];
         int found = 0;
@@ -272,7 +270,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_order_kernel(
         __syncthreads();
         int q = 0, entries = 0;
 #pragma unroll
-        for (int w = 0; w < kSortWaves; ++w) {
+        for (int w = 0; w < W; ++w) {
           q += w < wave ? wave_sum[w] : 0;
           entries += wave_sum[w];
         }
@@ -291,10 +289,10 @@ __global__ __launch_bounds__(kSortThreads) void embed_order_kernel(
       }
     } else {
       for (int c0 = 0; c0 < chunks; c0 += kRound) {
-        int from[kRoundPer], len[kRoundPer], sum = 0;
+        int from[SEGS], len[SEGS], sum = 0;
 #pragma unroll
-        for (int u = 0; u < kRoundPer; ++u) {
-          const int c = c0 + tid * kRoundPer + u;
+        for (int u = 0; u < SEGS; ++u) {
+          const int c = c0 + tid * SEGS + u;
           from[u] = len[u] = 0;
           if (c < chunks) {
             const int32_t* o = offs + (int64_t)c * (kBuckets + 1) + p;
@@ -305,16 +303,16 @@ __global__ __launch_bounds__(kSortThreads) void embed_order_kernel(
           sum += len[u];
         }
         int entries;
-        int first = block_scan<kSortWaves>(sum, wave_sum, &entries);
+        int first = block_scan<W>(sum, wave_sum, &entries);
 #pragma unroll
-        for (int u = 0; u < kRoundPer; ++u) {
-          seg_at[tid * kRoundPer + u] = first;
-          seg_src[tid * kRoundPer + u] = from[u];
+        for (int u = 0; u < SEGS; ++u) {
+          seg_at[tid * SEGS + u] = first;
+          seg_src[tid * SEGS + u] = from[u];
           first += len[u];
         }
         __syncthreads();
-        for (int q0 = 0; q0 < entries; q0 += kQueue) {
-          const int take = min(kQueue, entries - q0);
+        for (int q0 = 0; q0 < entries; q0 += QUEUE) {
+          const int take = min(QUEUE, entries - q0);
           // a thread's entries together: the last segment that begins at or before
           // each, by bisection, then their loads
           int s[PER] = {};
@@ -322,17 +320,17 @@ __global__ __launch_bounds__(kSortThreads) void embed_order_kernel(
           for (int d = kRound / 2; d > 0; d >>= 1)
 #pragma unroll
             for (int u = 0; u < PER; ++u)
-              if (seg_at[s[u] + d] <= q0 + tid + u * kSortThreads) s[u] += d;
+              if (seg_at[s[u] + d] <= q0 + tid + u * NT) s[u] += d;
           i32x2 e[PER];
 #pragma unroll
           for (int u = 0; u < PER; ++u) {
-            const int i = tid + u * kSortThreads;
+            const int i = tid + u * NT;
             if (i < take)
               e[u] = split[(int64_t)(c0 + s[u]) * chunk + seg_src[s[u]] + (q0 + i - seg_at[s[u]])];
           }
 #pragma unroll
           for (int u = 0; u < PER; ++u) {
-            const int i = tid + u * kSortThreads;
+            const int i = tid + u * NT;
             if (i < take) {
               queue_key[i] = e[u][0] >> kLogBuckets;
               queue_pos[i] = e[u][1];
@@ -347,17 +345,26 @@ __global__ __launch_bounds__(kSortThreads) void embed_order_kernel(
   };
   // a wavefront's share of a queue: consecutive blocks of 64
   auto share = [&](int entries, int* lo, int* hi) {
-    const int blocks = (entries + 63) / 64, each = (blocks + kSortWaves - 1) / kSortWaves;
+    const int blocks = (entries + 63) / 64, each = (blocks + W - 1) / W;
     *lo = min(entries, wave * each * 64);
     *hi = min(entries, (wave + 1) * each * 64);
   };
   auto count_queue = [&](int entries) {
     int lo, hi;
     share(entries, &lo, &hi);
-    for (int i = lo + lane; i < hi; i += 64) atomicAdd(&at[wave * keys + queue_key[i]], 1);
+    // lanes with the first one's id count as one: of a frequent id that is most, and
+    // additions to one address go one after the other
+    for (int i = lo + lane; i < hi; i += 64) {
+      const int k = queue_key[i], first = __builtin_amdgcn_readfirstlane(k);
+      const uint64_t same = __ballot(k == first);
+      if (k != first)
+        atomicAdd(&at[wave * keys + k], 1);
+      else if ((same & lanes_below(lane)) == 0)
+        atomicAdd(&at[wave * keys + k], __popcll(same));
+    }
   };
 
-  for (int k = tid; k < (2 + kSortWaves) * keys; k += kSortThreads) smem[k] = 0;
+  for (int k = tid; k < (2 + W) * keys; k += NT) smem[k] = 0;
   __syncthreads();
   // counts, and the first place: positions of the buckets before
   int held = 0, queues = 0;
@@ -367,29 +374,32 @@ __global__ __launch_bounds__(kSortThreads) void embed_order_kernel(
     ++queues;
   });
   int base;
-  block_scan<kSortWaves>(below, wave_sum, &base);
-  for (int k = tid; k < keys; k += kSortThreads)
+  block_scan<W>(below, wave_sum, &base);
+  for (int k = tid; k < keys; k += NT)
 #pragma unroll
-    for (int w = 0; w < kSortWaves; ++w) place[k] += at[w * keys + k];
+    for (int w = 0; w < W; ++w) place[k] += at[w * keys + k];
   __syncthreads();
 
   // ids present, 64 a wavefront at a time
-  for (int k0 = wave * 64; k0 < words * 32; k0 += kSortThreads) {
+  for (int k0 = wave * 64; k0 < words * 32; k0 += NT) {
     const uint64_t bits = __ballot(k0 + lane < keys && place[min(k0 + lane, keys - 1)] != 0);
     if (lane < 2 && k0 / 32 + lane < words)
       present[(int64_t)p * words + k0 / 32 + lane] = (uint32_t)(bits >> (32 * lane));
   }
-  if (p == kBuckets - 1 && tid == 0) *total = base + held;
+  if (p == kBuckets - 1 && tid == 0) {
+    total[0] = base + held;
+    total[1] = 0;
+  }
   if (held == 0) return;  // the whole workgroup
 
   // counts -> first places (with the cut bit where the id is long) and ends:
   // consecutive ids per thread, their sums scanned
-  const int per = (keys + kSortThreads - 1) / kSortThreads;
+  const int per = (keys + NT - 1) / NT;
   const int k0 = min(keys, tid * per), k1 = min(keys, k0 + per);
   __syncthreads();
   int mine = 0, all;
   for (int k = k0; k < k1; ++k) mine += place[k];
-  int next = base + block_scan<kSortWaves>(mine, wave_sum, &all);
+  int next = base + block_scan<W>(mine, wave_sum, &all);
   for (int k = k0; k < k1; ++k) {
     const int c = place[k];
     place[k] = next | (c > most ? (int)kCut : 0);
@@ -402,10 +412,10 @@ __global__ __launch_bounds__(kSortThreads) void embed_order_kernel(
   // ranked among the block's of its id by ballots over the id's bits
   auto hand_out = [&](int entries) {
     // the wavefronts' counts -> their first places; place: the next queue's
-    for (int k = tid; k < keys; k += kSortThreads) {
+    for (int k = tid; k < keys; k += NT) {
       int to = place[k];
 #pragma unroll
-      for (int w = 0; w < kSortWaves; ++w) {
+      for (int w = 0; w < W; ++w) {
         const int c = at[w * keys + k];
         at[w * keys + k] = to;
         to += c;
@@ -440,7 +450,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_order_kernel(
     hand_out(held);  // the queue and its counts are there
   } else {
     each_queue([&](int entries) {
-      for (int k = tid; k < kSortWaves * keys; k += kSortThreads) at[k] = 0;
+      for (int k = tid; k < W * keys; k += NT) at[k] = 0;
       __syncthreads();
       count_queue(entries);
       __syncthreads();
@@ -581,9 +591,9 @@ template <typename T, int G, int J>
 __global__ __launch_bounds__(256) void embed_sum_kernel(
     const T* __restrict__ dY, int64_t lddy, int64_t n, const int32_t* __restrict__ order,
     const uint32_t* __restrict__ key_of, const int32_t* __restrict__ run_end,
-    const uint32_t* __restrict__ present, int words, const int32_t* __restrict__ total, int jobs,
+    const uint32_t* __restrict__ present, int words, int32_t* __restrict__ total, int jobs,
     int sums, int clear, int past, int R, int C, float scale, int accumulate,
-    float* __restrict__ dE, int64_t ldE, float* __restrict__ part) {
+    float* __restrict__ dE, int64_t ldE, float* __restrict__ part, i32x4* __restrict__ cut) {
   constexpr int N = Row<T>::N, U = 8, TAKE = 3 * J;
   __shared__ __align__(16) int pos_sh[256 / G][TAKE];
   __shared__ __align__(16) uint32_t key_sh[256 / G][TAKE];
@@ -693,69 +703,71 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(
       }
     }
   }
+  if (goes_on && !from_before && v == 0)
+    cut[atomicAdd(total + 1, 1)] = i32x4{(int)(last & ~kCut), j, (last_end - 1) / J, 0};
   put(goes_on);
 }
 
-// The parts of the cut ids that begin in jobs [blockIdx.x * kJoinJobs, + kJoinJobs)
-// and go on in the next: slot 1 of the job, then slot 0 of the jobs after it up to
-// the last with that id.  L lanes hold four columns each; the workgroup's SHARES
-// groups of L take the parts in turn, each adding its own in order, and the groups
-// are added in order.
-constexpr int kJoinThreads = 512, kJoinJobs = 8;
+// The parts of the cut ids in the list, a range of 4 L columns of one after another:
+// slot 1 of the job in which it begins, then slot 0 of the jobs after it up to the
+// last with that id.  L lanes hold four columns each; the workgroup's SHARES groups of
+// L take the parts in turn, each adding its own in order, and the groups are added in
+// order.  The list's own order changes nothing.  16,384 rows of 4,096: 4.7 us (6.9
+// when workgroups looked through all jobs); 524,288 of 1,024, ids as frequent as
+// words: 21 us (53 with one part in flight a thread).
+constexpr int kJoinThreads = 512;
 template <int L>
 __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(
-    const uint32_t* __restrict__ key_of, const int32_t* __restrict__ run_end,
-    const int32_t* __restrict__ total, int J, int jobs, int C, float scale, int accumulate,
-    const float* __restrict__ part, float* __restrict__ dE, int64_t ldE) {
-  constexpr int SHARES = kJoinThreads / L;
+    const int32_t* __restrict__ total, const i32x4* __restrict__ cut, int C, float scale,
+    int accumulate, const float* __restrict__ part, float* __restrict__ dE, int64_t ldE) {
+  constexpr int SHARES = kJoinThreads / L, U = 8;
   __shared__ f32x4 sum[SHARES][L];
-  const int m = *total;
-  const int wlane = threadIdx.x & 63, lane = threadIdx.x % L, share = threadIdx.x / L;
-  const int v = blockIdx.y * L + lane;
-  for (int64_t j0 = (int64_t)blockIdx.x * kJoinJobs; j0 < jobs;
-       j0 += (int64_t)gridDim.x * kJoinJobs) {
-    // every wavefront finds the jobs by itself, a lane each
-    bool begins = false;
-    const int64_t ji = j0 + wlane;
-    if (wlane < kJoinJobs && ji < jobs) {
-      const int64_t lo = ji * J, hi = lo + J;
-      if (hi < m) {
-        const uint32_t key = key_of[hi];
-        begins = (key & kCut) && key_of[hi - 1] == key &&
-                 !(lo > 0 && key_of[lo - 1] == key && key_of[lo] == key);
-      }
-    }
-    for (uint64_t todo = __ballot(begins); todo != 0; todo &= todo - 1) {
-      const int j = (int)j0 + __ffsll((unsigned long long)todo) - 1;
-      const int hi = (j + 1) * J;
-      const uint32_t key = key_of[hi];
-      const int last = (run_end[hi] - 1) / J;
-      float acc[4] = {0.f, 0.f, 0.f, 0.f}, f[4];
-      if (v * 4 < C) {
-        if (share == 0) load_channels<4>(part + ((int64_t)j * 2 + 1) * C, v, C, acc);
-#pragma unroll 8
-        for (int q = j + 1 + share; q <= last; q += SHARES) {
-          load_channels<4>(part + ((int64_t)q * 2) * C, v, C, f);
+  const int lane = threadIdx.x % L, share = threadIdx.x / L;
+  const int tiles = (C + 4 * L - 1) / (4 * L);
+  const int64_t items = (int64_t)total[1] * tiles;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const i32x4 id = cut[item / tiles];
+    const int j = id[1], last = id[2], v = (int)(item % tiles) * L + lane;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f}, f[4];
+    if (v * 4 < C) {
+      if (share == 0) load_channels<4>(part + ((int64_t)j * 2 + 1) * C, v, C, acc);
+      const float* from = part + (int64_t)v * 4;
+      const int64_t step = (int64_t)2 * C;
+      int q = j + 1 + share;
+      if (v * 4 + 4 <= C) {  // U parts in flight
+        for (; q + (U - 1) * SHARES <= last; q += U * SHARES) {
+          f32x4_a4 x[U];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[e] += f[e];
+          for (int u = 0; u < U; ++u)
+            x[u] = *reinterpret_cast<const f32x4_a4*>(from + (q + u * SHARES) * step);
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += x[u][e];
         }
       }
-      sum[share][lane] = f32x4{acc[0], acc[1], acc[2], acc[3]};
-      __syncthreads();
-      if (share == 0 && v * 4 < C) {
-#pragma unroll 8
-        for (int q = 1; q < SHARES; ++q)
+#pragma unroll 4
+      for (; q <= last; q += SHARES) {
+        load_channels<4>(part + q * step, v, C, f);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[e] += sum[q][lane][e];
-        float* to = dE + (int64_t)(key & ~kCut) * ldE;
-        if (accumulate) load_channels<4>(to, v, C, f);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          f[e] = accumulate ? fmaf(acc[e], scale, f[e]) : acc[e] * scale;
-        store_channels<4>(to, v, C, f);
+        for (int e = 0; e < 4; ++e) acc[e] += f[e];
       }
-      __syncthreads();
     }
+    sum[share][lane] = f32x4{acc[0], acc[1], acc[2], acc[3]};
+    __syncthreads();
+    if (share == 0 && v * 4 < C) {
+#pragma unroll 8
+      for (int q = 1; q < SHARES; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += sum[q][lane][e];
+      float* to = dE + (int64_t)id[0] * ldE;
+      if (accumulate) load_channels<4>(to, v, C, f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        f[e] = accumulate ? fmaf(acc[e], scale, f[e]) : acc[e] * scale;
+      store_channels<4>(to, v, C, f);
+    }
+    __syncthreads();
   }
 }
 
@@ -766,10 +778,20 @@ constexpr int64_t kDirectRows = 2048;
 // (1,340,800 rows of 64 bf16: 133 us, 146 by 256 threads; 268,160: 33.6, 33.0).
 constexpr int64_t kWideRows = 524288;
 
+// Positions from which a bucket is ordered by 512 threads, a queue of 2,048 at a time:
+// frequent ids' buckets are the last to end (268,160 rows of 64 bf16, ids as frequent
+// as words: 75 us, 105 by 256 threads; evenly, 32.1, 33.2; 16,384: 30.6, 30.0 and 22.4,
+// 22.1).  Up to kWideKeys ids a bucket: the counts of each wavefront fit LDS.
+constexpr int64_t kWideOrder = 32768;
+constexpr int kWideThreads = 512, kWideKeys = 1024;
+constexpr size_t order_lds(int threads, int keys) {
+  return ((2 + threads / 64) * (size_t)keys + 2 * kQueuePer * threads + 2 * kRound) * sizeof(int);
+}
+
 // Workspace: what the launches leave each other.
 struct EmbedPlan {
-  int keys, key_bits, words, chunk, chunks, J, jobs;
-  size_t lds, off_key, off_end, off_present, off_total, off_split, off_offs, off_part, total;
+  int keys, key_bits, words, chunk, chunks, J, jobs, order_threads;
+  size_t off_key, off_end, off_present, off_total, off_cut, off_split, off_offs, off_part, total;
 };
 
 // Positions of a job; an id of more than 2 J is cut.  Short jobs where there are
@@ -798,7 +820,7 @@ void embed_plan(int64_t n, int64_t R, int32_t C, EmbedPlan* p) {
   p->key_bits = 0;
   while ((1 << p->key_bits) < p->keys) ++p->key_bits;
   p->words = (p->keys + 31) / 32;
-  p->lds = ((2 + kSortWaves) * (size_t)p->keys + 2 * kQueue + 2 * kRound) * sizeof(int);
+  p->order_threads = n >= kWideOrder && p->keys <= kWideKeys ? kWideThreads : 256;
   p->chunk = chunk_rows(n);
   p->chunks = chunk_count(n);
   p->J = job_rows(n, C);
@@ -818,7 +840,8 @@ void embed_plan(int64_t n, int64_t R, int32_t C, EmbedPlan* p) {
   p->off_key = place((size_t)n * 4);
   p->off_end = place((size_t)n * 4);
   p->off_present = place((size_t)kBuckets * p->words * 4);
-  p->off_total = place(4);
+  p->off_total = place(8);
+  p->off_cut = place((size_t)most_jobs * 16);
   p->off_split = place((size_t)p->chunks * p->chunk * 8);
   p->off_offs = place((size_t)most_chunks * (kBuckets + 1) * 4);
   p->off_part = place((size_t)most_jobs * 2 * (size_t)C * 4);
@@ -857,6 +880,7 @@ struct EmbedWork {
   uint32_t *key_of, *present;
   i32x2* split;
   float* part;
+  i32x4* cut;
 };
 
 template <typename ID>
@@ -865,17 +889,21 @@ hipError_t embed_order(const void* ids, int64_t id_stride, int64_t n, int64_t R,
   // allow the large dynamic LDS allocation; once per instantiation
   static std::once_flag once;
   static hipError_t attr_err = hipSuccess;
-  constexpr int kMostLds =
-      (int)(((2 + kSortWaves) * (kMaxEmbedRows >> kLogBuckets) + 2 * kQueue + 2 * kRound) *
-            sizeof(int));
+  constexpr int kMostKeys = kMaxEmbedRows >> kLogBuckets;
   std::call_once(once, [&] {
-    attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(embed_split_kernel<ID, 1024>),
-                                   hipFuncAttributeMaxDynamicSharedMemorySize,
-                                   16 * kBuckets * sizeof(int));
-    for (const void* k : {reinterpret_cast<const void*>(embed_order_kernel<ID, true>),
-                          reinterpret_cast<const void*>(embed_order_kernel<ID, false>)})
+    auto allow = [&](const void* kernel, size_t bytes) {
       if (attr_err == hipSuccess)
-        attr_err = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, kMostLds);
+        attr_err = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)bytes);
+    };
+    allow(reinterpret_cast<const void*>(embed_split_kernel<ID, 1024>),
+          16 * kBuckets * sizeof(int));
+    allow(reinterpret_cast<const void*>(embed_order_kernel<ID, 256, true>),
+          order_lds(256, kMostKeys));
+    allow(reinterpret_cast<const void*>(embed_order_kernel<ID, 256, false>),
+          order_lds(256, kMostKeys));
+    allow(reinterpret_cast<const void*>(embed_order_kernel<ID, kWideThreads, false>),
+          order_lds(kWideThreads, kWideKeys));
   });
   if (attr_err != hipSuccess) return attr_err;
   const ID* in = static_cast<const ID*>(ids);
@@ -888,15 +916,16 @@ hipError_t embed_order(const void* ids, int64_t id_stride, int64_t n, int64_t R,
           in, id_stride, n, (int)R, pad, w.split, w.offs);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    embed_order_kernel<ID, false><<<kBuckets, kSortThreads, w.p.lds, stream>>>(
+  }
+  auto order = [&](auto kernel) {
+    kernel<<<kBuckets, w.p.order_threads, order_lds(w.p.order_threads, w.p.keys), stream>>>(
         in, id_stride, n, (int)R, pad, w.p.keys, w.p.key_bits, 2 * w.p.J, w.split, w.offs,
         w.p.chunks, w.p.chunk, w.order, w.key_of, w.run_end, w.present, w.p.words, w.total);
-  } else {
-    embed_order_kernel<ID, true><<<kBuckets, kSortThreads, w.p.lds, stream>>>(
-        in, id_stride, n, (int)R, pad, w.p.keys, w.p.key_bits, 2 * w.p.J, w.split, w.offs, 0, 0,
-        w.order, w.key_of, w.run_end, w.present, w.p.words, w.total);
-  }
-  return hipGetLastError();
+    return hipGetLastError();
+  };
+  if (w.p.chunks == 0) return order(embed_order_kernel<ID, 256, true>);
+  return w.p.order_threads == 256 ? order(embed_order_kernel<ID, 256, false>)
+                                  : order(embed_order_kernel<ID, kWideThreads, false>);
 }
 
 // Rows that a wavefront clears at a time, about 16 KB of them.
@@ -951,7 +980,8 @@ hipError_t embed_sum(const void* dY, int64_t lddy, int64_t n, int64_t R, const E
     if (sums + clears == 0) return hipSuccess;
     embed_sum_kernel<T, G, J><<<sums + clears, 256, 0, stream>>>(
         static_cast<const T*>(dY), lddy, n, w.order, w.key_of, w.run_end, w.present, w.p.words,
-        w.total, w.p.jobs, sums, clear, past, (int)R, C, scale, accumulate, dE, ldE, w.part);
+        w.total, w.p.jobs, sums, clear, past, (int)R, C, scale, accumulate, dE, ldE, w.part,
+        w.cut);
     return hipGetLastError();
   };
   using std::integral_constant;
@@ -1016,6 +1046,7 @@ hipError_t launch_embed_rows_backward(const void* dY, int64_t lddy, const void* 
   w.split = reinterpret_cast<i32x2*>(b + w.p.off_split);
   w.offs = reinterpret_cast<int32_t*>(b + w.p.off_offs);
   w.part = reinterpret_cast<float*>(b + w.p.off_part);
+  w.cut = reinterpret_cast<i32x4*>(b + w.p.off_cut);
   hipError_t e = (id64 ? embed_order<int64_t> : embed_order<int32_t>)(ids, id_stride, n, R, pad32,
                                                                       w, stream);
   if (e != hipSuccess) return e;
@@ -1024,11 +1055,10 @@ hipError_t launch_embed_rows_backward(const void* dY, int64_t lddy, const void* 
   if (e != hipSuccess) return e;
   auto join = [&](auto l) {
     constexpr int L = decltype(l)::value;
-    const dim3 grid(std::min((w.p.jobs + kJoinJobs - 1) / kJoinJobs, 1 << 14),
-                    (C + 4 * L - 1) / (4 * L));
-    embed_join_kernel<L><<<grid, kJoinThreads, 0, stream>>>(w.key_of, w.run_end, w.total, w.p.J,
-                                                            w.p.jobs, C, scale, accumulate, w.part,
-                                                            dE, ldE);
+    // a workgroup for each range of columns of an id, if as many as can be are cut
+    const int64_t most = n / (2 * w.p.J + 1) * ((C + 4 * L - 1) / (4 * L));
+    embed_join_kernel<L><<<(int)std::min<int64_t>(most, 1024), kJoinThreads, 0, stream>>>(
+        w.total, w.cut, C, scale, accumulate, w.part, dE, ldE);
     return hipGetLastError();
   };
   if (C <= 64) return join(std::integral_constant<int, 16>{});

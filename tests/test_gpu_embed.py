@@ -123,6 +123,27 @@ def test_gradient_of_few_positions(kind, n, C, R, dtype):
     dE.check_guard()
 
 
+@pytest.mark.parametrize("n,R,C,kind", [
+    (32767, 40, 12, "zipf"), (32768, 40, 12, "zipf"), (50000, 300, 20, "one"),
+    (40001, 1 << 20, 3, "uniform"), (40001, (1 << 20) + 1, 3, "zipf"), (33000, 2, 131, "zipf"),
+])
+def test_gradient_of_many_positions(n, R, C, kind):
+    """Where the ordering takes more threads a bucket, and ids of thousands of
+    positions."""
+    r = np.random.default_rng(n + R)
+    ids = grad_case(r, n, R, kind)
+    dY, dE = Rows(n, C, "f32", 0, 0, r.standard_normal((n, C))), Rows(R, C, "f32", 1, 0)
+    shc.embed_rows_backward(dY.t, ids_tensor(ids, torch.int32, 2), dE.t)
+    first = dE.get().copy()
+    ref = O.embed_backward(dY.get(), ids, R, 1.0, -1)
+    size = O.embed_backward(np.abs(dY.get()), ids, R, 1.0, -1)
+    count = O.embed_backward(np.ones((n, 1)), ids, R, 1.0, -1)
+    close(first, ref, 2 * ((count + 2) * u * size + u * np.abs(ref)), "dE")
+    shc.embed_rows_backward(dY.t, ids_tensor(ids, torch.int32, 2), dE.t)
+    assert np.array_equal(dE.get(), first)      # bit for bit
+    dE.check_guard()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n,R,C,kind,extra,off", [
     (0, 5, 8, "uniform", 0, 0), (1, 1, 1, "uniform", 0, 0), (2, 3, 7, "outside", 1, 1),
