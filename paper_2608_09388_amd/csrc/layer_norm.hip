@@ -346,15 +346,21 @@ int norm_blocks(int64_t n, int G, int per_cu) {
   const int64_t need = (n + rows - 1) / rows;
   return (int)std::min<int64_t>(need, 256 * per_cu);
 }
-// Of the backward, whose workgroups write a partial row of column sums each: two
-// (16,384 rows of 4,096 bf16: 87 us, 117 with one, 100 with four), three of short
-// rows (268,160 rows of 128: 47, 50 with two).
-int backward_per_cu(int G) { return G <= 32 ? 3 : 2; }
+// Of the backward, whose workgroups write a partial row of column sums each: three to
+// a CU for short rows (268,160 rows of 128 bf16: 45 us, 48 with two), two up to 256
+// lanes (16,384 rows of 4,096: 80 us, 117 with one, 100 with four) and four rows or
+// more each past one to a CU (700 rows of 8,192: 18.4 us, 22.2 without), and one for
+// longer rows (1,110 rows of 9,280: 23.5 us, 32.4 with two; 12,000 of 16,384: 224, 242).
+int backward_groups(int64_t n, int G) {
+  if (G > 256) return norm_blocks(n, G, 1);
+  const int blocks = norm_blocks(n, G, G <= 32 ? 3 : 2);
+  return G < 256 ? blocks : (int)std::min<int64_t>(blocks, std::max<int64_t>(256, n / 4));
+}
 
 template <typename T>
 int backward_blocks(int64_t n, int32_t C) {
   return with_shape<T, true>(vectors_of<T>(C), [&](auto g, auto) {
-    return norm_blocks(n, decltype(g)::value, backward_per_cu(decltype(g)::value));
+    return backward_groups(n, decltype(g)::value);
   });
 }
 
@@ -378,7 +384,7 @@ hipError_t norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ld
   return with_shape<T, true>(vectors_of<T>(C), [&](auto g, auto v) {
     constexpr int G = decltype(g)::value, NV = decltype(v)::value;
     layer_norm_backward_kernel<T, G, NV>
-        <<<norm_blocks(n, G, backward_per_cu(G)), G > 256 ? G : 256, 0, stream>>>(
+        <<<backward_groups(n, G), G > 256 ? G : 256, 0, stream>>>(
             static_cast<const T*>(dy), lddy, static_cast<const T*>(x), ldx, n, C, gamma, mean,
             rstd, static_cast<T*>(dx), lddx, col);
     return hipGetLastError();
