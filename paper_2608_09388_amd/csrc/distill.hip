@@ -12,8 +12,9 @@
 // entries has loss 0 and gradient 0 and its logits are not read.
 //
 // Bound by HBM: V elements read, and V written by the gradient.
-// - Rows of up to 4096 vectors are read once, into the registers of the G threads
-//   that share them: maximum, sum, loss and gradient from there.
+// - Rows of up to 4096 vectors (of fp32 up to 16,384 for the step) are read once,
+//   into the registers of the G threads that share them: maximum, sum, loss and
+//   gradient from there.
 // - A workgroup of 1024 threads reads a longer row twice, the second time from
 //   the caches (256 rows in flight fit the Infinity Cache).
 // - Long rows of which there are few are cut into parts: a first launch leaves
@@ -619,7 +620,7 @@ int vectors_of(int32_t V, int is_bf16) { return is_bf16 ? (V + 7) / 8 : (V + 3) 
 // more than half of the 64 KB of LDS that a launch has without asking.
 constexpr int kTop32 = 32, kTop16 = 128;
 
-constexpr int kRowVectors = 4096;  // the longest row held in registers
+constexpr int kRowVectors = 4096;  // the longest row that is always held in registers
 
 // Parts of a row: 1 where a workgroup has a row to itself.  Rows in registers
 // always do: one launch, where two wait for the host (16 rows of 16,384 bf16,
@@ -659,6 +660,19 @@ hipError_t run_rows(const DistillArgs& a, hipStream_t stream) {
   SHC_ROW(1024, 256, 4);
   SHC_ROW(2048, 256, 8);
   SHC_ROW(kRowVectors, 512, 8);
+  // longer fp32 rows too for the step, whose second pass has as many bytes to store as
+  // to read, where there are two rows a CU or more (1,500 rows of 45,000: 113 us, read
+  // twice 126; 1,000 of 65,536: 116, 123; 3,000 of 17,000: 95, 93; 260 of 50,021: 33.4,
+  // 29.5).  bf16 rows, with twice the arithmetic a byte, gain nothing (2,000 of 65,536:
+  // 124, 119).
+  if constexpr (sizeof(T) == 4 && PASS == Pass::kStep) {
+    if (nvec > 5120 && a.n >= 512) {
+      SHC_ROW(8192, 1024, 8);
+      SHC_ROW(10240, 1024, 10);
+      SHC_ROW(13312, 1024, 13);
+      SHC_ROW(16384, 1024, 16);
+    }
+  }
 #undef SHC_ROW
   return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
 }

@@ -179,6 +179,28 @@ def test_rows_with_and_without_repeated_ids(dtype, V, k):
     check(z, ids, top, 1.5, r.random(7) + 0.5, dtype)
 
 
+@pytest.mark.parametrize("V", [20477, 20481, 32769, 41000, 53249, 65537])
+def test_step_of_many_long_rows(V):
+    r = np.random.default_rng(V)
+    n = 512
+    z, ids, top = case(r, n, V, 5, False)
+    z, ids, top = z.astype(np.float32), ids.astype(np.int32), top.astype(np.float32)
+    z[3, V // 2:] = LOWEST["f32"]
+    z[5, :-1] = -np.inf
+    ids[5], z[7] = -1, 1e6 + 20 * z[7]       # no entries; far from 0
+    ids[9, 1:] = ids[9, 0]
+    Z = torch.as_tensor(z, device="cuda")
+    loss, dz = shc.distill_top_step(Z, torch.as_tensor(ids, device="cuda"),
+                                    torch.as_tensor(top, device="cuda"))
+    rows = np.array([0, 1, 3, 5, 7, 9, n - 1])
+    z64, t64 = z[rows].astype(np.float64), top[rows].astype(np.float64)
+    rl, _, rdz = O.distill(z64, ids[rows], t64, 1.0)
+    b = DistillBounds(z64, ids[rows], t64, 1.0, None, O)
+    close(loss.double().cpu().numpy()[rows], rl, rounded(b.loss, rl, "f32"), "loss")
+    close(dz[torch.as_tensor(rows, device="cuda")].double().cpu().numpy(), rdz,
+          rounded(b.dz_step, rdz, "f32"), "step")
+
+
 def test_backward_of_many_long_rows():
     r = np.random.default_rng(11)
     z, ids, top = case(r, 513, 9000, 20, True)
