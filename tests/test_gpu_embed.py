@@ -123,6 +123,37 @@ def test_gradient_of_few_positions(kind, n, C, R, dtype):
     dE.check_guard()
 
 
+@pytest.mark.parametrize("n,R", [(400, 60), (5000, 60), (40000, 300)])
+def test_gradient_in_a_graph_and_on_another_stream(n, R):
+    """Each replay has ids of its own, with other ids long enough to be cut."""
+    r = np.random.default_rng(n)
+    C = 40
+    dY = Rows(n, C, "bf16", values=r.standard_normal((n, C)))
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    dE, want = (torch.empty((R, C), device="cuda") for _ in range(2))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        shc.embed_rows_backward(dY.t, ids, dE)
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        shc.embed_rows_backward(dY.t, ids, dE)
+    for k in range(4):
+        new = grad_case(r, n, R, ("zipf", "one", "uniform", "runs")[k])
+        ids.copy_(torch.as_tensor(new, dtype=torch.int32))
+        shc.embed_rows_backward(dY.t, ids, want)
+        torch.cuda.synchronize()
+        dE.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dE, want), k
+        ref = O.embed_backward(dY.get(), new, R, 1.0, -1)
+        size = O.embed_backward(np.abs(dY.get()), new, R, 1.0, -1)
+        count = O.embed_backward(np.ones((n, 1)), new, R, 1.0, -1)
+        close(want.double().cpu().numpy(), ref, 2 * (count + 2) * u * size, "dE")
+
+
 @pytest.mark.parametrize("n,R,C,kind", [
     (32767, 40, 12, "zipf"), (32768, 40, 12, "zipf"), (50000, 300, 20, "one"),
     (40001, 1 << 20, 3, "uniform"), (40001, (1 << 20) + 1, 3, "zipf"), (33000, 2, 131, "zipf"),
