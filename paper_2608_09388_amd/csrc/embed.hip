@@ -31,8 +31,8 @@
 // bit for bit.
 //
 // Measured: 16,384 rows of 4,096 bf16 into a table of 32,768, ids as frequent as
-// words: 146 us, 4.6 TB/s over all (6, 8, 127 and 5 us: the sums and the clearing are
-// bound by HBM, the rest by latency); 268,160 rows of 128 into 10,475: 34.5 us (6, 9,
+// words: 144 us, 4.7 TB/s over all (5, 8, 127 and 5 us: the sums and the clearing are
+// bound by HBM, the rest by latency); 268,160 rows of 128 into 10,475: 33 us (5, 10,
 // 16 and 3).  One id of very many positions is the worst: its bucket is one workgroup's
 // (65,536 rows of 1,024, one id: 293 us).
 #include <algorithm>
@@ -89,7 +89,6 @@ __global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ E, int
   }
 }
 
-constexpr int kSplitPer = 4;                           // ids a thread of a chunk
 constexpr int kRound = 1024;                           // segments of a round
 constexpr int kQueuePer = 4;                           // positions a thread in LDS at a time
 constexpr int kLogBuckets = 10, kBuckets = 1 << kLogBuckets;
@@ -142,21 +141,21 @@ __device__ __forceinline__ int block_scan(int mine, int* wave_sum, int* total) {
   return before + inc - mine;
 }
 
-// Chunk c's (id, position) by bucket, in order, to split[c * NT * kSplitPer + ...];
+// Chunk c's (id, position) by bucket, in order, to split[c * NT * PER + ...];
 // where each bucket begins to offs[c][kBuckets + 1].
-template <typename ID, int NT>
+template <typename ID, int NT, int PER>
 __global__ __launch_bounds__(NT) void embed_split_kernel(
     const ID* __restrict__ ids, int64_t id_stride, int64_t n, int R, int pad,
     i32x2* __restrict__ split, int32_t* __restrict__ offs) {
   constexpr int W = NT / 64, BPT = kBuckets / NT;  // wavefronts; buckets a thread
-  constexpr int64_t CHUNK = NT * kSplitPer;
+  constexpr int64_t CHUNK = NT * PER;
   extern __shared__ __align__(16) int hist[];  // [W][kBuckets]
   __shared__ int wave_sum[W];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t w0 = blockIdx.x * CHUNK + (int64_t)wave * 64 * kSplitPer;
-  int id[kSplitPer], rank[kSplitPer];
+  const int64_t w0 = blockIdx.x * CHUNK + (int64_t)wave * 64 * PER;
+  int id[PER], rank[PER];
 #pragma unroll
-  for (int u = 0; u < kSplitPer; ++u) {
+  for (int u = 0; u < PER; ++u) {
     const int64_t i = w0 + u * 64 + lane;
     id[u] = i < n ? valid_id(ids, id_stride, i, R, pad) : -1;
   }
@@ -165,7 +164,7 @@ __global__ __launch_bounds__(NT) void embed_split_kernel(
     reinterpret_cast<i32x4*>(hist + wave * kBuckets)[b] = i32x4{};
   group_fence<64>();
 #pragma unroll
-  for (int u = 0; u < kSplitPer; ++u) {
+  for (int u = 0; u < PER; ++u) {
     const int b = id[u] & (kBuckets - 1);
     uint64_t same = __ballot(id[u] >= 0);
 #pragma unroll
@@ -209,7 +208,7 @@ __global__ __launch_bounds__(NT) void embed_split_kernel(
   }
   __syncthreads();
 #pragma unroll
-  for (int u = 0; u < kSplitPer; ++u)
+  for (int u = 0; u < PER; ++u)
     if (id[u] >= 0)
       split[blockIdx.x * CHUNK + mine[id[u] & (kBuckets - 1)] + rank[u]] =
           i32x2{id[u], (int)(w0 + u * 64 + lane)};
@@ -774,8 +773,9 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(
 // Positions up to which every bucket reads the ids itself: one launch less (1,024
 // rows of 5,000 bf16: 34.8 us, 40.0 with the split; 2,048: 42.9, 45.6).
 constexpr int64_t kDirectRows = 2048;
-// Positions from which a chunk is split by 1024 threads: fewer, longer segments
-// (1,340,800 rows of 64 bf16: 133 us, 146 by 256 threads; 268,160: 33.6, 33.0).
+// Positions from which a chunk is 4096 of them, split by 1024 threads, not 1024 by 512:
+// fewer, longer segments (1,340,800 rows of 64 bf16: 133 us, 146 with short chunks;
+// 268,160: 33.6, 33.0).
 constexpr int64_t kWideRows = 524288;
 
 // Positions from which a bucket is ordered by 512 threads, a queue of 2,048 at a time:
@@ -806,7 +806,7 @@ constexpr int64_t kJobs16 = 32768, kJobs32 = 131072;  // wavefronts of one posit
   const int J = job_rows(n, C);
   return (int)((n + J - 1) / J);
 }
-[[nodiscard]] int chunk_rows(int64_t n) { return kSplitPer * (n < kWideRows ? 256 : 1024); }
+[[nodiscard]] int chunk_rows(int64_t n) { return n < kWideRows ? 1024 : 4096; }
 [[nodiscard]] int chunk_count(int64_t n) {
   return n > kDirectRows ? (int)((n + chunk_rows(n) - 1) / chunk_rows(n)) : 0;
 }
@@ -896,7 +896,7 @@ hipError_t embed_order(const void* ids, int64_t id_stride, int64_t n, int64_t R,
         attr_err = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
                                        (int)bytes);
     };
-    allow(reinterpret_cast<const void*>(embed_split_kernel<ID, 1024>),
+    allow(reinterpret_cast<const void*>(embed_split_kernel<ID, 1024, 4>),
           16 * kBuckets * sizeof(int));
     allow(reinterpret_cast<const void*>(embed_order_kernel<ID, 256, true>),
           order_lds(256, kMostKeys));
@@ -908,11 +908,12 @@ hipError_t embed_order(const void* ids, int64_t id_stride, int64_t n, int64_t R,
   if (attr_err != hipSuccess) return attr_err;
   const ID* in = static_cast<const ID*>(ids);
   if (w.p.chunks > 0) {
-    if (w.p.chunk == 256 * kSplitPer)
-      embed_split_kernel<ID, 256><<<w.p.chunks, 256, 4 * kBuckets * sizeof(int), stream>>>(
+    // two ids a thread of 512: 268,160 ids 5.3 us, four of 256 6.1
+    if (w.p.chunk == 1024)
+      embed_split_kernel<ID, 512, 2><<<w.p.chunks, 512, 8 * kBuckets * sizeof(int), stream>>>(
           in, id_stride, n, (int)R, pad, w.split, w.offs);
     else
-      embed_split_kernel<ID, 1024><<<w.p.chunks, 1024, 16 * kBuckets * sizeof(int), stream>>>(
+      embed_split_kernel<ID, 1024, 4><<<w.p.chunks, 1024, 16 * kBuckets * sizeof(int), stream>>>(
           in, id_stride, n, (int)R, pad, w.split, w.offs);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
