@@ -26,15 +26,15 @@
 //    positions are cut at the jobs' borders instead, their parts left in
 //    the workspace.  Other workgroups of the launch clear the table rows of ids
 //    without a position meanwhile.
-// 4. embed_join_kernel adds the parts of the ids that the sums listed, in order.
+// 4. embed_join_kernel adds the parts, in order.
 // Every sum has an order that follows the ids and sizes alone: results repeat
 // bit for bit.
 //
 // Measured: 16,384 rows of 4,096 bf16 into a table of 32,768, ids as frequent as
-// words: 144 us, 4.7 TB/s over all (5, 8, 127 and 5 us: the sums and the clearing are
+// words: 145 us, 4.6 TB/s over all (5, 8, 127 and 5 us: the sums and the clearing are
 // bound by HBM, the rest by latency); 268,160 rows of 128 into 10,475: 33 us (5, 10,
 // 16 and 3).  One id of very many positions is the worst: its bucket is one workgroup's
-// (65,536 rows of 1,024, one id: 293 us).
+// (65,536 rows of 1,024, one id: 315 us).
 #include <algorithm>
 #include <mutex>
 
@@ -218,8 +218,7 @@ __global__ __launch_bounds__(NT) void embed_split_kernel(
 // below 2^key_bits, local number id >> kLogBuckets.  order, key_of, run_end [n]:
 // position, id (with kCut where its positions are more than `most`) and the end of
 // the id's run, at its places; present [kBuckets][words]: a bit for every id with a
-// position; total: the number of positions with an id that counts, and of cut ids,
-// none yet.
+// position; *total the number of positions with an id that counts.
 // LDS: place[keys], end[keys], at[NT / 64][keys], the queue (local number,
 // position), a round of segments.
 template <typename ID, int NT, bool DIRECT>
@@ -385,10 +384,7 @@ __global__ __launch_bounds__(NT) void embed_order_kernel(
     if (lane < 2 && k0 / 32 + lane < words)
       present[(int64_t)p * words + k0 / 32 + lane] = (uint32_t)(bits >> (32 * lane));
   }
-  if (p == kBuckets - 1 && tid == 0) {
-    total[0] = base + held;
-    total[1] = 0;
-  }
+  if (p == kBuckets - 1 && tid == 0) *total = base + held;
   if (held == 0) return;  // the whole workgroup
 
   // counts -> first places (with the cut bit where the id is long) and ends:
@@ -590,9 +586,10 @@ template <typename T, int G, int J>
 __global__ __launch_bounds__(256) void embed_sum_kernel(
     const T* __restrict__ dY, int64_t lddy, int64_t n, const int32_t* __restrict__ order,
     const uint32_t* __restrict__ key_of, const int32_t* __restrict__ run_end,
-    const uint32_t* __restrict__ present, int words, int32_t* __restrict__ total, int jobs,
+    const uint32_t* __restrict__ present, int words, const int32_t* __restrict__ total, int jobs,
     int sums, int clear, int past, int R, int C, float scale, int accumulate,
-    float* __restrict__ dE, int64_t ldE, float* __restrict__ part, i32x4* __restrict__ cut) {
+    float* __restrict__ dE, int64_t ldE, float* __restrict__ part,
+    int32_t* __restrict__ begins) {
   constexpr int N = Row<T>::N, U = 8, TAKE = 3 * J;
   __shared__ __align__(16) int pos_sh[256 / G][TAKE];
   __shared__ __align__(16) uint32_t key_sh[256 / G][TAKE];
@@ -643,6 +640,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(
       keys[t] = key_of[lo + t];
     }
   }
+  if (v == 0) begins[j] = 0;  // the last job of a cut id that begins here; none yet
   group_fence<64>();
   if (lo >= m) return;
   int hi = (int)next;
@@ -702,55 +700,86 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(
       }
     }
   }
-  if (goes_on && !from_before && v == 0)
-    cut[atomicAdd(total + 1, 1)] = i32x4{(int)(last & ~kCut), j, (last_end - 1) / J, 0};
+  if (goes_on && !from_before && v == 0) begins[j] = (last_end - 1) / J;
   put(goes_on);
 }
 
-// The parts of the cut ids in the list, a range of 4 L columns of one after another:
-// slot 1 of the job in which it begins, then slot 0 of the jobs after it up to the
-// last with that id.  L lanes hold four columns each; the workgroup's SHARES groups of
-// L take the parts in turn, each adding its own in order, and the groups are added in
-// order.  The list's own order changes nothing.  16,384 rows of 4,096: 4.7 us (6.9
-// when workgroups looked through all jobs); 524,288 of 1,024, ids as frequent as
-// words: 21 us (53 with one part in flight a thread).
-constexpr int kJoinThreads = 512;
+// The parts of the cut ids that begin in jobs [blockIdx.x * range, + range): slot 1 of
+// the job, then slot 0 of the jobs after it up to the last with that id.  L lanes hold
+// four columns each.  Ids of up to kShortParts parts are taken by a group of L lanes
+// each, in order; of longer ones the workgroup's groups take the parts in turn, each
+// adding its own in order, and the groups are added in order.  16,384 rows of 4,096:
+// 4.7 us; 400,000 rows of 64 on 10,475 ids, all of which are cut in two or three: 43
+// us in all, 111 where a whole workgroup took each.
+constexpr int kJoinThreads = 512, kJoinRange = 64, kShortParts = 8;
 template <int L>
 __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(
-    const int32_t* __restrict__ total, const i32x4* __restrict__ cut, int C, float scale,
-    int accumulate, const float* __restrict__ part, float* __restrict__ dE, int64_t ldE) {
+    const uint32_t* __restrict__ key_of, const int32_t* __restrict__ begins, int J, int jobs,
+    int range, int C, float scale, int accumulate, const float* __restrict__ part,
+    float* __restrict__ dE, int64_t ldE) {
   constexpr int SHARES = kJoinThreads / L, U = 8;
   __shared__ f32x4 sum[SHARES][L];
+  __shared__ int from_job[2][kJoinRange], to_job[2][kJoinRange];
+  // every wavefront looks through the jobs, a lane each
+  const int wlane = threadIdx.x & 63, j0 = blockIdx.x * range;
+  const int last = wlane < range && j0 + wlane < jobs ? begins[j0 + wlane] : 0;
+  const bool is_long = last - (j0 + wlane) > kShortParts;
+  const uint64_t some[2] = {__ballot(last != 0 && !is_long), __ballot(last != 0 && is_long)};
+  if ((some[0] | some[1]) == 0) return;  // the whole workgroup
+  if (threadIdx.x < 64 && last != 0) {
+    const int at = __popcll((is_long ? some[1] : some[0]) & lanes_below(wlane));
+    from_job[is_long][at] = j0 + wlane;
+    to_job[is_long][at] = last;
+  }
+  __syncthreads();
   const int lane = threadIdx.x % L, share = threadIdx.x / L;
-  const int tiles = (C + 4 * L - 1) / (4 * L);
-  const int64_t items = (int64_t)total[1] * tiles;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const i32x4 id = cut[item / tiles];
-    const int j = id[1], last = id[2], v = (int)(item % tiles) * L + lane;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, f[4];
-    if (v * 4 < C) {
-      if (share == 0) load_channels<4>(part + ((int64_t)j * 2 + 1) * C, v, C, acc);
-      const float* from = part + (int64_t)v * 4;
-      const int64_t step = (int64_t)2 * C;
-      int q = j + 1 + share;
-      if (v * 4 + 4 <= C) {  // U parts in flight
-        for (; q + (U - 1) * SHARES <= last; q += U * SHARES) {
-          f32x4_a4 x[U];
+  const int v = blockIdx.y * L + lane;
+  const int64_t step = (int64_t)2 * C;
+  const float* from = part + (int64_t)v * 4;
+  float acc[4], f[4];
+  // acc += slot 0 of jobs q, q + by, ... up to the last
+  auto add = [&](int q, int to, int by) {
+    if (v * 4 + 4 <= C) {  // U parts in flight
+      for (; q + (U - 1) * by <= to; q += U * by) {
+        f32x4_a4 x[U];
 #pragma unroll
-          for (int u = 0; u < U; ++u)
-            x[u] = *reinterpret_cast<const f32x4_a4*>(from + (q + u * SHARES) * step);
+        for (int u = 0; u < U; ++u)
+          x[u] = *reinterpret_cast<const f32x4_a4*>(from + (q + u * by) * step);
 #pragma unroll
-          for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] += x[u][e];
-        }
+          for (int e = 0; e < 4; ++e) acc[e] += x[u][e];
       }
+    }
 #pragma unroll 4
-      for (; q <= last; q += SHARES) {
-        load_channels<4>(part + q * step, v, C, f);
+    for (; q <= to; q += by) {
+      load_channels<4>(part + q * step, v, C, f);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += f[e];
-      }
+      for (int e = 0; e < 4; ++e) acc[e] += f[e];
+    }
+  };
+  auto put = [&](int j) {
+    float* to = dE + (int64_t)(key_of[(int64_t)(j + 1) * J] & ~kCut) * ldE;
+    if (accumulate) load_channels<4>(to, v, C, f);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = accumulate ? fmaf(acc[e], scale, f[e]) : acc[e] * scale;
+    store_channels<4>(to, v, C, f);
+  };
+  if (v * 4 < C) {
+    for (int i = share; i < __popcll(some[0]); i += SHARES) {
+      const int j = from_job[0][i];
+      load_channels<4>(part + j * step + C, v, C, acc);
+      add(j + 1, to_job[0][i], 1);
+      put(j);
+    }
+  }
+  for (int i = 0; i < __popcll(some[1]); ++i) {
+    const int j = from_job[1][i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = 0.f;
+    if (v * 4 < C) {
+      if (share == 0) load_channels<4>(part + j * step + C, v, C, acc);
+      add(j + 1 + share, to_job[1][i], SHARES);
     }
     sum[share][lane] = f32x4{acc[0], acc[1], acc[2], acc[3]};
     __syncthreads();
@@ -759,12 +788,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(
       for (int q = 1; q < SHARES; ++q)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += sum[q][lane][e];
-      float* to = dE + (int64_t)id[0] * ldE;
-      if (accumulate) load_channels<4>(to, v, C, f);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        f[e] = accumulate ? fmaf(acc[e], scale, f[e]) : acc[e] * scale;
-      store_channels<4>(to, v, C, f);
+      put(j);
     }
     __syncthreads();
   }
@@ -774,8 +798,8 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(
 // rows of 5,000 bf16: 34.8 us, 40.0 with the split; 2,048: 42.9, 45.6).
 constexpr int64_t kDirectRows = 2048;
 // Positions from which a chunk is 4096 of them, split by 1024 threads, not 1024 by 512:
-// fewer, longer segments (1,340,800 rows of 64 bf16: 133 us, 146 with short chunks;
-// 268,160: 33.6, 33.0).
+// fewer, longer segments (1,340,800 rows of 64 bf16 took 20 us less; 268,160 29.4 us,
+// 32.3 with long chunks).
 constexpr int64_t kWideRows = 524288;
 
 // Positions from which a bucket is ordered by 512 threads, a queue of 2,048 at a time:
@@ -791,7 +815,7 @@ constexpr size_t order_lds(int threads, int keys) {
 // Workspace: what the launches leave each other.
 struct EmbedPlan {
   int keys, key_bits, words, chunk, chunks, J, jobs, order_threads;
-  size_t off_key, off_end, off_present, off_total, off_cut, off_split, off_offs, off_part, total;
+  size_t off_key, off_end, off_present, off_total, off_begins, off_split, off_offs, off_part, total;
 };
 
 // Positions of a job; an id of more than 2 J is cut.  Short jobs where there are
@@ -840,8 +864,8 @@ void embed_plan(int64_t n, int64_t R, int32_t C, EmbedPlan* p) {
   p->off_key = place((size_t)n * 4);
   p->off_end = place((size_t)n * 4);
   p->off_present = place((size_t)kBuckets * p->words * 4);
-  p->off_total = place(8);
-  p->off_cut = place((size_t)most_jobs * 16);
+  p->off_total = place(4);
+  p->off_begins = place((size_t)most_jobs * 4);
   p->off_split = place((size_t)p->chunks * p->chunk * 8);
   p->off_offs = place((size_t)most_chunks * (kBuckets + 1) * 4);
   p->off_part = place((size_t)most_jobs * 2 * (size_t)C * 4);
@@ -876,11 +900,10 @@ hipError_t embed_rows(const void* E, int64_t R, int64_t ldE, const void* ids, in
 
 struct EmbedWork {
   EmbedPlan p;
-  int32_t *order, *run_end, *total, *offs;
+  int32_t *order, *run_end, *total, *begins, *offs;
   uint32_t *key_of, *present;
   i32x2* split;
   float* part;
-  i32x4* cut;
 };
 
 template <typename ID>
@@ -982,7 +1005,7 @@ hipError_t embed_sum(const void* dY, int64_t lddy, int64_t n, int64_t R, const E
     embed_sum_kernel<T, G, J><<<sums + clears, 256, 0, stream>>>(
         static_cast<const T*>(dY), lddy, n, w.order, w.key_of, w.run_end, w.present, w.p.words,
         w.total, w.p.jobs, sums, clear, past, (int)R, C, scale, accumulate, dE, ldE, w.part,
-        w.cut);
+        w.begins);
     return hipGetLastError();
   };
   using std::integral_constant;
@@ -1044,10 +1067,10 @@ hipError_t launch_embed_rows_backward(const void* dY, int64_t lddy, const void* 
   w.run_end = reinterpret_cast<int32_t*>(b + w.p.off_end);
   w.present = reinterpret_cast<uint32_t*>(b + w.p.off_present);
   w.total = reinterpret_cast<int32_t*>(b + w.p.off_total);
+  w.begins = reinterpret_cast<int32_t*>(b + w.p.off_begins);
   w.split = reinterpret_cast<i32x2*>(b + w.p.off_split);
   w.offs = reinterpret_cast<int32_t*>(b + w.p.off_offs);
   w.part = reinterpret_cast<float*>(b + w.p.off_part);
-  w.cut = reinterpret_cast<i32x4*>(b + w.p.off_cut);
   hipError_t e = (id64 ? embed_order<int64_t> : embed_order<int32_t>)(ids, id_stride, n, R, pad32,
                                                                       w, stream);
   if (e != hipSuccess) return e;
@@ -1056,10 +1079,13 @@ hipError_t launch_embed_rows_backward(const void* dY, int64_t lddy, const void* 
   if (e != hipSuccess) return e;
   auto join = [&](auto l) {
     constexpr int L = decltype(l)::value;
-    // a workgroup for each range of columns of an id, if as many as can be are cut
-    const int64_t most = n / (2 * w.p.J + 1) * ((C + 4 * L - 1) / (4 * L));
-    embed_join_kernel<L><<<(int)std::min<int64_t>(most, 1024), kJoinThreads, 0, stream>>>(
-        w.total, w.cut, C, scale, accumulate, w.part, dE, ldE);
+    const int tiles = (C + 4 * L - 1) / (4 * L);
+    // few idle wavefronts, and few long ids one after the other: 2,048 workgroups
+    // (1,048,576 rows of 512: 425 us, with 512 of them 439), of 16 to 64 jobs
+    const int range = (int)std::clamp<int64_t>((int64_t)w.p.jobs * tiles / 2048, 16, kJoinRange);
+    const dim3 grid((unsigned)((w.p.jobs + range - 1) / range), tiles);
+    embed_join_kernel<L><<<grid, kJoinThreads, 0, stream>>>(
+        w.key_of, w.begins, w.p.J, w.p.jobs, range, C, scale, accumulate, w.part, dE, ldE);
     return hipGetLastError();
   };
   if (C <= 64) return join(std::integral_constant<int, 16>{});

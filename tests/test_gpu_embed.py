@@ -157,6 +157,7 @@ def test_gradient_in_a_graph_and_on_another_stream(n, R):
 @pytest.mark.parametrize("n,R,C,kind", [
     (32767, 40, 12, "zipf"), (32768, 40, 12, "zipf"), (50000, 300, 20, "one"),
     (40001, 1 << 20, 3, "uniform"), (40001, (1 << 20) + 1, 3, "zipf"), (33000, 2, 131, "zipf"),
+    (60000, 1500, 20, "uniform"), (60001, 1500, 70, "runs"),
 ])
 def test_gradient_of_many_positions(n, R, C, kind):
     """Where the ordering takes more threads a bucket, and ids of thousands of
