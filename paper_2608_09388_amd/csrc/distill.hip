@@ -722,12 +722,12 @@ hipError_t run_step(const DistillArgs& a, hipStream_t stream) {
 template <typename T>
 hipError_t run_backward(const DistillArgs& a, hipStream_t stream) {
   // elementwise but for the entries, which every part of a row works out: rows in
-  // registers where there are enough of them (30,000 of bf16, 256 entries: 4,000 rows
-  // 115 us, in parts 138; 300 rows of 32 entries 10.8, 9.9), and longer parts where
-  // there are many entries (1,500 rows of 120,000, 256 entries: 175, in parts of 1024
-  // vectors 210; of 64 entries 147, 146)
+  // registers where there are enough of them (31,424 of bf16, 8 entries: 3,000 rows
+  // 75.8 us, in parts 78.9, of 200 entries 91, 97; 800 rows 26.4, 23.3), and longer
+  // parts where there are many entries (1,500 rows of 120,000, 256 entries: 175, in
+  // parts of 1024 vectors 210; of 64 entries 147, 146)
   const int nvec = vectors_of(a.V, sizeof(T) == 2);
-  if (nvec <= 1024 || (nvec <= kRowVectors && a.n >= 512))
+  if (nvec <= 1024 || (nvec <= kRowVectors && a.n >= 1536))
     return run_rows<T, Pass::kBackward>(a, stream);
   const int per = a.k > 128 ? 2048 : 1024;
   return run_grad<T>(a, 0, per, stream);

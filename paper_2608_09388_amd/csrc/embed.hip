@@ -961,13 +961,13 @@ int clear_past(int64_t R, int32_t C) { return R * C >= (int64_t)1 << 26; }
 
 // Whether one launch does it: a position's workgroups, one for each range of columns,
 // look through the whole list, so that the work grows with the positions' square
-// (5,000 ids, bf16: 1,500 rows of 2,000 take 24.1 us, by the launches below 25.3; 2,048
-// rows 30.2, 25.3, of 500 10.6, 24.2).  One id throughout is the worst of it: 2,048 rows
+// (5,000 ids, bf16: 1,024 rows of 2,000 take 17.1 us, by the launches below 20.2; 2,048
+// rows of 500 10.6, 24.2, of 2,000 30.2, 25.3; 1,186 of 2,345 27.9, 24.6).  One id throughout is the worst of it: 2,048 rows
 // of 64 take 40 us, 26.
 constexpr int kFewMost = 4 * kFewThreads;
 bool few_rows(int64_t n, int32_t C, int is_bf16) {
   const int per = is_bf16 ? 512 : 256;
-  return n <= kFewThreads || (n <= kFewMost && n * ((C + per - 1) / per) <= 6144);
+  return n <= kFewThreads || (n <= kFewMost && n * ((C + per - 1) / per) <= 5120);
 }
 
 template <typename T, typename ID>

@@ -207,6 +207,10 @@ def test_backward_of_many_long_rows():
     check(z, ids, top, 1.0, None, "bf16")
     z, ids, top = case(r, 512, 4200, 40, False)
     check(z, ids, top, 1.0, None, "f32")
+    z, ids, top = case(r, 1536, 4200, 40, True)
+    check(z, ids, top, 1.0, None, "f32")
+    z, ids, top = case(r, 1537, 8300, 20, False)
+    check(z, ids, top, 1.0, None, "bf16")
 
 
 def test_padding_rows_are_not_read():
