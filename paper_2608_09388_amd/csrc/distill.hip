@@ -661,12 +661,13 @@ hipError_t run_rows(const DistillArgs& a, hipStream_t stream) {
   SHC_ROW(2048, 256, 8);
   SHC_ROW(kRowVectors, 512, 8);
   // longer fp32 rows too for the step, whose second pass has as many bytes to store as
-  // to read, where there are two rows a CU or more (1,500 rows of 45,000: 113 us, read
-  // twice 126; 1,000 of 65,536: 116, 123; 3,000 of 17,000: 95, 93; 260 of 50,021: 33.4,
-  // 29.5).  bf16 rows, with twice the arithmetic a byte, gain nothing (2,000 of 65,536:
+  // to read, from 112 MB of them on, when not all of it stays in the caches (1,500 rows
+  // of 45,000: 113 us, read twice 126; 1,000 of 65,536: 116, 123; 600 of 50,021: 57.9,
+  // 62.3; 600 of 32,768: 40.3, 39.1; of 24,000 2,000 rows 84.5, 89.7, but 1,300 62.4,
+  // 60.6).  bf16 rows, with twice the arithmetic a byte, gain nothing (2,000 of 65,536:
   // 124, 119).
   if constexpr (sizeof(T) == 4 && PASS == Pass::kStep) {
-    if (nvec > 5120 && a.n >= 512) {
+    if (nvec > 7168 && a.n * nvec >= 7000000) {
       SHC_ROW(8192, 1024, 8);
       SHC_ROW(10240, 1024, 10);
       SHC_ROW(13312, 1024, 13);

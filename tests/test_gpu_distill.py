@@ -201,6 +201,29 @@ def test_step_of_many_long_rows(V):
           rounded(b.dz_step, rdz, "f32"), "step")
 
 
+@pytest.mark.parametrize("V", [28669, 28673, 32769, 40961, 53248, 65535, 65537])
+def test_step_of_so_many_long_rows_that_registers_hold_them(V):
+    n, k = 1000, 9
+    g = torch.Generator(device="cuda")
+    g.manual_seed(V)
+    z = 2 * torch.randn((n, V), generator=g, device="cuda")
+    ids = torch.randint(0, V, (n, k), generator=g, device="cuda", dtype=torch.int32)
+    top = 3 * torch.randn((n, k), generator=g, device="cuda")
+    z[3, V // 2:] = LOWEST["f32"]
+    z[5, :-1] = -np.inf
+    ids[5], z[7] = -1, 1e6 + 20 * z[7]       # no entries; far from 0
+    ids[3] %= V // 2
+    ids[9, 1:] = ids[9, 0]
+    loss, dz = shc.distill_top_step(z, ids, top)
+    rows = [0, 1, 3, 5, 7, 9, 511, n - 1]
+    z64, t64 = z[rows].double().cpu().numpy(), top[rows].double().cpu().numpy()
+    picked = ids[rows].cpu().numpy()
+    rl, _, rdz = O.distill(z64, picked, t64, 1.0)
+    b = DistillBounds(z64, picked, t64, 1.0, None, O)
+    close(loss[rows].double().cpu().numpy(), rl, rounded(b.loss, rl, "f32"), "loss")
+    close(dz[rows].double().cpu().numpy(), rdz, rounded(b.dz_step, rdz, "f32"), "step")
+
+
 def test_backward_of_many_long_rows():
     r = np.random.default_rng(11)
     z, ids, top = case(r, 513, 9000, 20, True)
