@@ -507,9 +507,10 @@ __device__ __forceinline__ RowSoftmax join_parts(const f32x2* __restrict__ parts
   for (int i = lane + 64; i < count; i += 64) m = fmaxf(m, parts[i][0]);
   RowSoftmax r;
   r.m = finite_max(lanes_reduce<64>(m, MaxOp{}));
-  // a part without a logit but -inf has no sum; r.m may be far below its 0
+  // a part of nothing but -inf has the sum 0, and no maximum; one of NaN has none
+  // either, but a sum of NaN, which stays
   auto part = [&](const f32x2& p) {
-    return p[0] == -INFINITY ? 0.f : p[1] * exp2_hw((p[0] - r.m) * c);
+    return p[1] == 0.f ? 0.f : p[1] * exp2_hw((p[0] - r.m) * c);
   };
   float s = part(first);
   for (int i = lane + 64; i < count; i += 64) s += part(parts[i]);

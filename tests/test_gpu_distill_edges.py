@@ -1,0 +1,56 @@
+"""Distillation where values are far from the ordinary."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_09388_amd import binding as shc
+from tests.gpu_util import require_gpu
+from tests.row_util import TDT
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def dev():
+    return require_gpu()
+
+
+def run(z, ids, top, T=1.0, w=None):
+    """(loss, lse, dz of the backward, the step's loss, its dz) in fp64."""
+    n, V = z.shape
+    lse = torch.empty(n, device="cuda")
+    loss = shc.distill_top(z, ids, top, None, lse, T)
+    dz = shc.distill_top_backward(z, ids, top, lse, w, None, T)
+    loss2, dz2 = shc.distill_top_step(z, ids, top, w, None, None, T)
+    return [t.double().cpu().numpy() for t in (loss, lse, dz, loss2, dz2)]
+
+
+def entries(n, V, k, seed):
+    """Entries in a row's first quarter."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    z = torch.randn((n, V), generator=g, device="cuda")
+    ids = torch.randint(0, V // 4, (n, k), generator=g, device="cuda", dtype=torch.int32)
+    return z, ids, torch.randn((n, k), generator=g, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [600, 20000, 40000, 140001])
+@pytest.mark.parametrize("n", [6, 300])
+def test_nan_in_a_part_of_a_row(dtype, V, n):
+    """Runs of columns longer than a part of a row that is cut up; the answer does
+    not depend on the number of rows, and other rows' results stay."""
+    z, ids, top = entries(n, V, 5, V)
+    z = z.to(TDT[dtype])
+    good = run(z, ids, top)
+    z[1, V // 2:] = float("nan")
+    z[2, V // 2:] = -float("inf")
+    z[2, V - 1] = float("nan")               # nothing but -inf around it
+    z[3] = float("nan")
+    z[4, V // 2:] = torch.tensor(-1, dtype=torch.int32).view(torch.float32)  # sign bit set
+    bad = run(z, ids, top)
+    rows = [1, 2, 3, 4]
+    keep = np.setdiff1d(np.arange(n), rows)
+    for name, g, b in zip(("loss", "lse", "backward", "step's loss", "step"), good, bad):
+        assert np.isnan(b[rows]).all(), name
+        assert np.array_equal(g[keep], b[keep]), name
