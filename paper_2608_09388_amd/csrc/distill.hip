@@ -53,13 +53,14 @@ __device__ __forceinline__ i32x4 load_logits(const T* z, int v, int V) {
   return i32x4{b, b, b, b};
 }
 
-// Maximum and sum of a row: q_v = 2^((z_v - m) c - l).
+// Maximum and sum of a row: q_v = 2^((z_v - m) c - l).  m is not -inf, so that a
+// logit of -inf has q = 0, and q = NaN in a row with a NaN.
 struct RowSoftmax {
   float m, l;
 };
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ float prob(float z, const RowSoftmax& r, float c) {
-  return z == -INFINITY ? 0.f : exp2_hw((z - r.m) * c - r.l);
+  return exp2_hw((z - r.m) * c - r.l);
 }
 
 // The teacher's entries of a row, in LDS: id (-1 where there is none), its own p,
@@ -186,7 +187,9 @@ __device__ __forceinline__ float loss_terms(int k, float temp, const RowSoftmax&
     const float p = en.p[e];
     if (en.id[e] < 0 || p == 0.f) continue;
     const float zi = en.z[e];
-    const float lq = zi == -INFINITY ? -INFINITY : (zi - r.m) / temp - kLn2 * r.l;
+    // (l is -inf in a row of nothing but -inf, NaN in one with a NaN)
+    const bool none = zi == -INFINITY && r.l == r.l;
+    const float lq = none ? -INFINITY : (zi - r.m) / temp - kLn2 * r.l;
     // (the hardware's logarithm takes a subnormal p as 0)
     a += p * (kLn2 * log2_hw(fmaxf(p, 0x1p-126f)) - lq);
   }

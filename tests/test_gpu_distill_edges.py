@@ -54,3 +54,32 @@ def test_nan_in_a_part_of_a_row(dtype, V, n):
     for name, g, b in zip(("loss", "lse", "backward", "step's loss", "step"), good, bad):
         assert np.isnan(b[rows]).all(), name
         assert np.array_equal(g[keep], b[keep]), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [40, 3000, 20000, 40000, 140001])
+def test_nan_rows_with_entries_on_masked_logits(dtype, V):
+    """In a row with a NaN, loss and gradient are NaN at entries on -inf too; without
+    one they are +inf and -p there."""
+    z, ids, top = entries(3, V, 4, V)
+    z, ids = z.to(TDT[dtype]), torch.arange(4, dtype=torch.int32).repeat(3, 1).cuda()
+    z[:, 2] = -float("inf")
+    z[1, V - 1] = float("nan")
+    z[2, V - 1] = float("inf")
+    loss, lse, dz, loss2, dz2 = run(z, ids, top)
+    p = torch.softmax(top[0].double(), 0)[2].item()
+    for got in (dz, dz2):
+        assert np.isnan(got[1:]).all()
+        assert abs(got[0, 2] + p) <= 2.0 ** -8 * p
+    assert loss[0] == loss2[0] == np.inf
+    assert np.isnan(loss[1:]).all() and np.isnan(loss2[1:]).all()
+    # no other entry in the row
+    one = torch.full((3, 1), 2, dtype=torch.int32, device="cuda")
+    loss, lse, dz, loss2, dz2 = run(z, one, top[:, :1].contiguous())
+    for got in (loss, loss2):
+        assert got[0] == np.inf and np.isnan(got[1:]).all()
+    z[0] = -float("inf")                     # and no logit
+    loss, lse, dz, loss2, dz2 = run(z, one, top[:, :1].contiguous())
+    assert loss[0] == loss2[0] == np.inf and lse[0] == -np.inf
+    for got in (dz, dz2):
+        assert got[0, 2] == -1.0 and not np.delete(got[0], 2).any()
