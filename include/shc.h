@@ -848,7 +848,10 @@ int shc_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, in
  * shc_distill_top          -- loss, and lse = log of sum exp(z / T) [n_rows]
  *                             fp32 (may be NULL), for evaluation or a backward
  *                             whose w is not known yet.
- * shc_distill_top_backward -- dlogits from lse as shc_distill_top wrote it.
+ * shc_distill_top_backward -- dlogits from lse as shc_distill_top wrote it.  A row
+ *                             whose |lse| is above 64 (fp32) or 1024 (bf16), where
+ *                             lse keeps too little of the row's sum, is summed
+ *                             again.
  * shc_distill_top_step     -- loss and dlogits in one pass over the logits.
  * shc_distill_top and _step take a workspace of shc_distill_top_workspace
  * bytes (which may be 0; ws may then be NULL).

@@ -20,6 +20,8 @@
 // - Long rows of which there are few are cut into parts: a first launch leaves
 //   every part's maximum and sum in the workspace, the second joins them in order
 //   and computes the loss or its part of the gradient.
+// The backward takes q from the saved log-sum-exp, or sums the row again where 32 bits of
+// it do not keep the sum (keeps_sum).
 // The gradient writes w T q first; the k entries are corrected behind a fence,
 // entries of the same id all with the id's whole p, added in their order.
 //
@@ -305,6 +307,43 @@ struct RunningSum {
   }
 };
 
+// Maximum and sum of 2^((z - m) c) over vectors [v0, v1) of a row, by the G threads that
+// share it, U vectors a thread in flight; part: as of group_reduce.
+template <typename T, int G, int U>
+__device__ __forceinline__ float max_and_sum(const T* __restrict__ z, int V, int v0, int v1,
+                                             int lane, float c, float* part, float* sum) {
+  const int nvec = (V + Row<T>::N - 1) / Row<T>::N;
+  RunningSum<T> run;
+  for (int v = v0 + lane; v < v1; v += G * U) {
+    i32x4 in[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) in[u] = load_logits(z, v + G * u < v1 ? v + G * u : nvec, V);
+    run.take(in, c);
+  }
+  const float m = group_reduce<G>(run.m, MaxOp{}, part);
+  const Exponent x(finite_max(m), c);
+  float s = 0.f;
+  if (x.near) {
+    run.over(x.mc);
+    s = run.s;
+  } else {
+    for (int v = v0 + lane; v < v1; v += G) s = exp_sum<T, false>(load_logits(z, v, V), x, s);
+  }
+  s = group_reduce<G>(s, AddOp{}, part);
+  *sum = x.near ? s * exp2_hw(-fmaf(x.m, c, -x.mc)) : s;
+  return m;
+}
+
+// Whether the backward takes a row's q from its lse, which is m / T + ln S in fp32: the
+// rounding of the sum, of its two terms and of its product with T move every q by up to
+// 4 |lse| 2^-24, which is 2^-16 at 64, as much as the row's sum may be off, and 2^-12 at
+// 1,024, an eighth of bf16's own rounding.  Farther from 0 lse says less and less of S (of
+// a row of masks of the lowest value nothing), and the row's maximum and sum are taken again.
+template <typename T>
+__device__ __forceinline__ bool keeps_sum(float lse) {
+  return !(fabsf(lse) > (sizeof(T) == 2 ? 1024.f : 64.f));
+}
+
 // What the threads that share a row tell each other; one barrier a value.
 template <int G>
 struct GroupShare {
@@ -350,7 +389,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void distill_row_kernel(
 #pragma unroll
   for (int q = 0; q < NV; ++q) raw[q] = load_logits(zr, q * G + lane, V);
   const float w = PASS != Pass::kForward && weight != nullptr ? weight[row] : 1.f;
-  float saved = PASS == Pass::kBackward ? lse[row] : 0.f;
+  const float saved = PASS == Pass::kBackward ? lse[row] : 0.f;
   bool live = false;
   if (lane < L)
     live = teach<T, L, PASS != Pass::kForward>(zr, ids + row * k, top + row * k, k, V, c, lane,
@@ -398,11 +437,16 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void distill_row_kernel(
   // sum
   RowSoftmax r;
   if constexpr (PASS == Pass::kBackward) {
-    // z/T - lse: the saved lse takes the place of the maximum
-    saved *= temp;
-    r.m = finite_max(saved);
-    r.l = 0.f;
-    s = 1.f;
+    if (keeps_sum<T>(saved)) {  // z/T - lse: the saved lse takes the place of the maximum
+      r.m = saved * temp;
+      r.l = 0.f;
+      s = 1.f;
+    } else {
+      float* part = nullptr;
+      if constexpr (G > 64) part = sh.s;
+      r.m = finite_max(max_and_sum<T, G, 1>(zr, V, 0, nvec, lane, c, part, &s));
+      r.l = log2_hw(s);
+    }
   } else {
     r.m = finite_max(all);
   }
@@ -434,7 +478,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void distill_row_kernel(
       }
     }
   } else if (x.near) {
-    s = exp2_hw(fmaf(r.m, c, -x.mc));
+    s *= exp2_hw(fmaf(r.m, c, -x.mc));
   }
 
   if constexpr (PASS != Pass::kForward) {
@@ -471,32 +515,12 @@ template <typename T>
 __global__ __launch_bounds__(256) void distill_part_kernel(const T* __restrict__ z, int64_t ldz,
                                                            int V, int per, float temp,
                                                            f32x2* __restrict__ parts) {
-  constexpr int N = Row<T>::N, U = 4;
   __shared__ float part[4];
-  const T* zr = z + (int64_t)blockIdx.x * ldz;
-  const float c = kLog2E / temp;
-  const int nvec = (V + N - 1) / N;
+  const int nvec = (V + Row<T>::N - 1) / Row<T>::N;
   const int v0 = blockIdx.y * per, v1 = min(v0 + per, nvec);
-  RunningSum<T> run;
-  for (int v = v0 + threadIdx.x; v < v1; v += 256 * U) {
-    i32x4 in[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) in[u] = load_logits(zr, v + 256 * u < v1 ? v + 256 * u : nvec, V);
-    run.take(in, c);
-  }
-  const float m = group_reduce<256>(run.m, MaxOp{}, part);
-  const Exponent x(finite_max(m), c);
-  float s = 0.f;
-  if (x.near) {
-    run.over(x.mc);
-    s = run.s;
-  } else {
-    for (int v = v0 + threadIdx.x; v < v1; v += 256)
-      s = exp_sum<T, false>(load_logits(zr, v, V), x, s);
-  }
-  s = group_reduce<256>(s, AddOp{}, part);
-  // the sum of 2^((z - m) c)
-  if (x.near) s *= exp2_hw(-fmaf(x.m, c, -x.mc));
+  float s;
+  const float m = max_and_sum<T, 256, 4>(z + (int64_t)blockIdx.x * ldz, V, v0, v1, threadIdx.x,
+                                         kLog2E / temp, part, &s);
   if (threadIdx.x == 0) parts[(int64_t)blockIdx.x * gridDim.y + blockIdx.y] = f32x2{m, s};
 }
 
@@ -552,9 +576,12 @@ __global__ __launch_bounds__(64) void distill_join_kernel(
 }
 
 // Gradient of part blockIdx.y (per vectors) of row blockIdx.x, from lse (backward)
-// or from the row's parts (step: the first part also writes the loss).
+// or from the row's parts (step: the first part also writes the loss).  A row whose lse
+// does not keep its sum is taken whole by the first part's workgroup (1,024 rows of 131,072
+// bf16, all of them such: 164 us, 690 where every part sums the row; 64 rows 63, 40; no
+// such row: 106).  64 registers at most: 65, without the bound, cost 2%.
 template <typename T>
-__global__ __launch_bounds__(256) void distill_grad_kernel(
+__global__ __launch_bounds__(256, 8) void distill_grad_kernel(
     const T* __restrict__ z, int64_t ldz, int V, int per, const f32x2* __restrict__ parts,
     int count, const float* __restrict__ lse, const int32_t* __restrict__ ids,
     const float* __restrict__ top, int k, float temp, const float* __restrict__ weight,
@@ -562,6 +589,7 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(
   constexpr int N = Row<T>::N, U = 4;
   extern __shared__ __align__(16) int smem[];
   __shared__ int live_sh;
+  __shared__ float part[4];
   const int lane = threadIdx.x;
   const Entries en(smem, k);
   const int64_t row = blockIdx.x;
@@ -569,51 +597,62 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(
   const T* zr = z + row * ldz;
   T* dr = dz + row * lddz;
   const int nvec = (V + N - 1) / N;
-  const int v0 = blockIdx.y * per, v1 = min(v0 + per, nvec);
   RowSoftmax r;
   float s = 1.f;
-  if (lse != nullptr) {
-    r.m = finite_max(lse[row] * temp);  // z/T - lse: in the place of the maximum
+  bool whole = false;
+  if (lse == nullptr) {
+    r = join_parts(parts + row * count, count, c, &s);
+  } else if (keeps_sum<T>(lse[row])) {
+    r.m = lse[row] * temp;  // z/T - lse: in the place of the maximum
     r.l = 0.f;
   } else {
-    r = join_parts(parts + row * count, count, c, &s);
+    if (blockIdx.y > 0) return;
+    whole = true;
+    r.m = finite_max(max_and_sum<T, 256, U>(zr, V, 0, nvec, lane, c, part, &s));
+    r.l = log2_hw(s);
   }
-  if (lane < 64) {
-    const bool live = teach<T, 64, true>(zr, ids + row * k, top + row * k, k, V, c, lane, en,
-                                         v0 * N, (v1 - v0) * N);
-    if (loss != nullptr && blockIdx.y == 0) {
-      const float a = live ? loss_terms<64>(k, temp, r, lane, en) : 0.f;
-      if (lane == 0) loss[row] = temp * temp * a;
+  for (int v0 = blockIdx.y * per;;) {
+    const int v1 = min(v0 + per, nvec);
+    if (lane < 64) {
+      const bool live = teach<T, 64, true>(zr, ids + row * k, top + row * k, k, V, c, lane, en,
+                                           v0 * N, (v1 - v0) * N);
+      if (loss != nullptr && blockIdx.y == 0) {
+        const float a = live ? loss_terms<64>(k, temp, r, lane, en) : 0.f;
+        if (lane == 0) loss[row] = temp * temp * a;
+      }
+      if (lane == 0) live_sh = live;
     }
-    if (lane == 0) live_sh = live;
-  }
-  __syncthreads();
-  if (!live_sh) {
-    for (int v = v0 + lane; v < v1; v += 256) store_vec(dr, v, V, i32x4{});
-    return;
-  }
-  const float wt = (weight != nullptr ? weight[row] : 1.f) * temp;
-  if (s == 0.f) r.l = 0.f;  // no logit but -inf: every q is 0
-  const Exponent x(r.m, c);
-  if (x.near) s *= exp2_hw(fmaf(r.m, c, -x.mc));
-  const float by = s == 0.f ? 0.f : wt / s;
-  if (x.near) {
-    for (int v = v0 + lane; v < v1; v += 256 * U) {
-      i32x4 in[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        in[u] = load_logits(zr, v + 256 * u < v1 ? v + 256 * u : nvec, V);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (v + 256 * u < v1)
-          store_vec(dr, v + 256 * u, V, exp_scaled<T, true>(in[u], x, by));
+    __syncthreads();
+    if (!live_sh) {
+      for (int v = v0 + lane; v < (whole ? nvec : v1); v += 256) store_vec(dr, v, V, i32x4{});
+      return;
     }
-  } else {
-    for (int v = v0 + lane; v < v1; v += 256)
-      store_vec(dr, v, V, exp_scaled<T, false>(load_logits(zr, v, V), x, by));
+    const float wt = (weight != nullptr ? weight[row] : 1.f) * temp;
+    if (s == 0.f) r.l = 0.f;  // no logit but -inf: every q is 0
+    const Exponent x(r.m, c);
+    const float sum = x.near ? s * exp2_hw(fmaf(r.m, c, -x.mc)) : s;
+    const float by = s == 0.f ? 0.f : wt / sum;
+    if (x.near) {
+      for (int v = v0 + lane; v < v1; v += 256 * U) {
+        i32x4 in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          in[u] = load_logits(zr, v + 256 * u < v1 ? v + 256 * u : nvec, V);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (v + 256 * u < v1)
+            store_vec(dr, v + 256 * u, V, exp_scaled<T, true>(in[u], x, by));
+      }
+    } else {
+      for (int v = v0 + lane; v < v1; v += 256)
+        store_vec(dr, v, V, exp_scaled<T, false>(load_logits(zr, v, V), x, by));
+    }
+    __syncthreads();
+    if (lane < 64) fix_entries<T, 64>(dr, k, c, wt, r, lane, v0 * N, min(v1 * N, V), en);
+    v0 = v1;
+    if (!whole || v0 == nvec) return;
+    __syncthreads();  // live_sh and the entries are free again
   }
-  __syncthreads();
-  if (lane < 64) fix_entries<T, 64>(dr, k, c, wt, r, lane, v0 * N, min(v1 * N, V), en);
 }
 
 int vectors_of(int32_t V, int is_bf16) { return is_bf16 ? (V + 7) / 8 : (V + 3) / 4; }

@@ -3,11 +3,14 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import row_oracle as O
 from paper_2608_09388_amd import binding as shc
 from tests.gpu_util import require_gpu
-from tests.row_util import TDT
+from tests.row_util import TDT, DistillBounds, close, rounded
 
 pytestmark = pytest.mark.gpu
+
+LOWEST = {k: torch.finfo(t).min for k, t in TDT.items()}
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -83,3 +86,45 @@ def test_nan_rows_with_entries_on_masked_logits(dtype, V):
     assert loss[0] == loss2[0] == np.inf and lse[0] == -np.inf
     for got in (dz, dz2):
         assert got[0, 2] == -1.0 and not np.delete(got[0], 2).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,V,k", [(9, 40, 4), (9, 200, 40), (9, 500, 9), (9, 1000, 5),
+                                   (9, 2000, 5), (9, 4000, 5), (9, 9000, 20), (1600, 9000, 4),
+                                   (1540, 4200, 5), (9, 33001, 6), (9, 140001, 200)])
+def test_backward_of_rows_far_from_zero(dtype, n, V, k):
+    """lse in 32 bits says nothing of the sum where the maximum is large: the
+    backward is as near as the step is."""
+    z, ids, top = entries(n, V, k, n + V)
+    z *= 2
+    for row, at in enumerate((0.0, 70.0, -900.0, 4000.0, -3e5, 1e6, 1e9)):
+        z[row] += at
+    z[7] = LOWEST[dtype]                     # masks that leave nothing
+    z[8] = 6e4                               # equal logits
+    z[3, V // 2:] = LOWEST[dtype]
+    z = z.to(TDT[dtype])
+    w = torch.rand(n, device="cuda") + 0.5
+    dz = run(z[:9], ids[:9], top[:9], w=w[:9])[2] if n == 9 else run(z, ids, top, w=w)[2][:9]
+    Z, I, t, W = (a[:9].double().cpu().numpy() for a in (z, ids, top, w))
+    ref = O.distill(Z, I.astype(np.int64), t, 1.0, W)[2]
+    b = DistillBounds(Z, I.astype(np.int64), t, 1.0, W, O)
+    # row 0 is at 0, where lse keeps its digits; the others as the step's
+    bound = np.concatenate([b.dz_back[:1], b.dz_step[1:]])
+    if dtype == "bf16":                      # up to 1,024 the saved lse serves bf16
+        bound[1:3] = b.dz_back[1:3]
+    close(dz, ref, rounded(bound, ref, dtype), "backward")
+
+
+@pytest.mark.parametrize("T", [0.01, 30.0])
+@pytest.mark.parametrize("V", [300, 5000, 40000])
+def test_backward_far_from_zero_at_other_temperatures(T, V):
+    z, ids, top = entries(4, V, 6, V)
+    z += torch.tensor([[0.0], [50.0], [-2000.0], [1e5]], device="cuda")
+    dz = run(z, ids, top, T)[2]
+    Z, I, t = (a.double().cpu().numpy() for a in (z, ids, top))
+    T = float(np.float32(T))
+    ref = O.distill(Z, I.astype(np.int64), t, T)[2]
+    b = DistillBounds(Z, I.astype(np.int64), t, T, None, O)
+    far = np.abs(Z.max(1, keepdims=True) / T) > 80
+    bound = np.where(far, b.dz_step, b.dz_back)
+    close(dz, ref, rounded(bound, ref, "f32"), "backward")
