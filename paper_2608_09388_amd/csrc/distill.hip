@@ -473,7 +473,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void distill_row_kernel(
     if (lane < L) {
       const float a = loss_terms<L>(k, temp, r, lane, en);
       if (lane == 0) {
-        loss[row] = temp * temp * a;
+        loss[row] = temp * (temp * a);
         if (PASS == Pass::kForward && lse != nullptr) lse[row] = r.m / temp + kLn2 * r.l;
       }
     }
@@ -570,7 +570,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(
   const RowSoftmax r = join_parts(parts + row * count, count, c, &s);
   const float a = loss_terms<64>(k, temp, r, lane, en);
   if (lane == 0) {
-    loss[row] = temp * temp * a;
+    loss[row] = temp * (temp * a);
     if (lse != nullptr) lse[row] = r.m / temp + kLn2 * r.l;
   }
 }
@@ -618,7 +618,7 @@ __global__ __launch_bounds__(256, 8) void distill_grad_kernel(
                                            v0 * N, (v1 - v0) * N);
       if (loss != nullptr && blockIdx.y == 0) {
         const float a = live ? loss_terms<64>(k, temp, r, lane, en) : 0.f;
-        if (lane == 0) loss[row] = temp * temp * a;
+        if (lane == 0) loss[row] = temp * (temp * a);
       }
       if (lane == 0) live_sh = live;
     }

@@ -128,3 +128,28 @@ def test_backward_far_from_zero_at_other_temperatures(T, V):
     far = np.abs(Z.max(1, keepdims=True) / T) > 80
     bound = np.where(far, b.dz_step, b.dz_back)
     close(dz, ref, rounded(bound, ref, "f32"), "backward")
+
+
+@pytest.mark.parametrize("T", [1e-25, 2e-20, 1e-12, 1e18])
+@pytest.mark.parametrize("V", [30, 2000, 40000])
+def test_loss_at_the_ends_of_the_temperatures(T, V):
+    """T^2 leaves the range of fp32 long before T^2 times the sum does."""
+    z, ids, top = entries(3, V, 5, V)
+    loss, lse, dz, loss2, dz2 = run(z, ids, top, T)
+    Z, I, t = (a.double().cpu().numpy() for a in (z, ids, top))
+    T = float(np.float32(T))
+    ref = O.distill(Z, I.astype(np.int64), t, T)[0]
+    b = DistillBounds(Z, I.astype(np.int64), t, T, None, O)
+    close(loss, ref, rounded(b.loss, ref, "f32"), "loss")
+    close(loss2, ref, rounded(b.loss, ref, "f32"), "loss of the step")
+
+
+def test_loss_of_equal_distributions_at_a_large_temperature():
+    """T^2 is past fp32, T^2 times the rounding of the sum is not."""
+    z, ids = torch.full((2, 1), 3.0, device="cuda"), torch.zeros((2, 1), device="cuda").int()
+    T = float(np.float32(1e20))
+    loss, lse, dz, loss2, dz2 = run(z, ids, z, T)
+    b = DistillBounds(np.full((2, 1), 3.0), np.zeros((2, 1), np.int64), np.full((2, 1), 3.0), T,
+                      None, O)
+    for got in (loss, loss2):
+        close(got, np.zeros(2), rounded(b.loss, np.zeros(2), "f32"), "loss")
