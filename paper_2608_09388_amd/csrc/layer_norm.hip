@@ -157,7 +157,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_backward_kernel(
     i32x4 nx[NV], ny[NV];
     float nmu = 0.f, nrs = 0.f;
     if (AHEAD && row + step < n) fetch(row + step, nx, ny, &nmu, &nrs);
-    float sg = 0.f, sgh = 0.f;  // past the row's end dy = 0: nothing is added
+    float sg = 0.f, sgh = 0.f;  // past the row's end x = dy = 0
 #pragma unroll
     for (int q = 0; q < NV; ++q) {
       float fx[N], fy[N];
@@ -173,6 +173,21 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_backward_kernel(
       }
     }
     if (dx != nullptr) {
+      // past the row's end h = -mean rstd: 0 times that is nothing unless it is past fp32
+      // (a row of 1e37 throughout), when the sum is taken over the row's own channels
+      if (__builtin_expect(!(fabsf(cmu * crs) < INFINITY), 0)) {
+        sgh = 0.f;
+#pragma unroll
+        for (int q = 0; q < NV; ++q) {
+          const int left = C - (q * G + lane) * N;
+          float fx[N], fy[N];
+          Row<T>::widen(cx[q], fx);
+          Row<T>::widen(cy[q], fy);
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (e < left) sgh = fmaf(fy[e] * ga[q][e], (fx[e] - cmu) * crs, sgh);
+        }
+      }
       const float mg = group_reduce<G>(sg, AddOp{}, my_part) * inv_c;
       const float mgh = group_reduce<G>(sgh, AddOp{}, my_part) * inv_c;
 #pragma unroll
