@@ -39,6 +39,7 @@ class VertexHead:
                  temperature: float = 2.0, dtype: str = "bf16", seed: int = 0,
                  device: str = "cuda"):
         self.B, self.V, self.C, self.classes, self.T = B, V, C, classes, temperature
+        self.top = top  # entries a row that it asks of its teacher
         dt, f32 = DTYPE[dtype], torch.float32
         g = torch.Generator(device=device)
         g.manual_seed(seed)
@@ -134,13 +135,13 @@ def main():
     ap.add_argument("--lr", type=float, default=0.5)
     ap.add_argument("--dtype", choices=sorted(DTYPE), default="bf16")
     a = ap.parse_args()
-    B, V, k = a.bodies, a.vertices, 8
-    head = VertexHead(B, V, a.channels, a.classes, k, dtype=a.dtype)
+    B, V = a.bodies, a.vertices
+    head = VertexHead(B, V, a.channels, a.classes, dtype=a.dtype)
     g = torch.Generator(device="cuda")
     g.manual_seed(1)
     # the teacher prefers the same classes at a vertex in every body
     table = 3.0 * torch.randn((V, a.classes), generator=g, device="cuda")
-    top_logits, top_ids = table.topk(k, dim=1)
+    top_logits, top_ids = table.topk(head.top, dim=1)
     top_ids = top_ids.to(torch.int32)
 
     def teacher(coords):
