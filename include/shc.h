@@ -835,7 +835,7 @@ int shc_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x, in
  *
  * An entry whose id is outside [0, V), or whose t is -inf, is absent; ids may
  * repeat.  A row without entries (padding) has loss 0, lse 0 and gradient 0,
- * and its logits are not read.  A logit of -inf has q = 0 (an entry with p > 0
+ * whatever its logits hold.  A logit of -inf has q = 0 (an entry with p > 0
  * there makes the loss +inf; the gradient stays finite), in a row of nothing
  * but -inf every q is 0.  NaN and +inf make the row's own results NaN.  With
  * T < 1 the logits' maximum over T must be within fp32.

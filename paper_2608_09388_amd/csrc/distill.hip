@@ -9,12 +9,13 @@
 // and S = sum 2^((z - m) c), q = 2^((z - m) c - log2 S).  The difference is
 // taken before the factor, so masks of the type's lowest value stay finite.
 // A logit of -inf has q = 0, also in a row that has no other; a row without
-// entries has loss 0 and gradient 0 and its logits are not read.
+// entries has loss 0 and gradient 0 whatever its logits are (they are read: the
+// loads do not wait for the entries).
 //
 // Bound by HBM: V elements read, and V written by the gradient.
-// - Rows of up to 4096 vectors (of fp32 up to 16,384 for the step) are read once,
-//   into the registers of the G threads that share them: maximum, sum, loss and
-//   gradient from there.
+// - Rows of up to 4096 vectors are read once, into the registers of the G threads
+//   that share them: maximum, sum, loss and gradient from there.  So are, by the step,
+//   many fp32 rows of 7,169 to 16,384 vectors (run_rows).
 // - A workgroup of 1024 threads reads a longer row twice, the second time from
 //   the caches (256 rows in flight fit the Infinity Cache).
 // - Long rows of which there are few are cut into parts: a first launch leaves
@@ -682,11 +683,10 @@ hipError_t run_rows(const DistillArgs& a, hipStream_t stream) {
   auto go = [&](auto g, auto v) {
     constexpr int G = decltype(g)::value, NV = decltype(v)::value;
     constexpr int BLOCK = G > 256 ? G : 256, R = BLOCK / G;
-    distill_row_kernel<T, G, NV, PASS>
-        <<<(unsigned)((a.n + R - 1) / R), BLOCK, (size_t)R * entry_words(a.k, PASS == Pass::kForward ? 0 : a.V) * 4,
-           stream>>>(
-            static_cast<const T*>(a.z), a.ldz, a.n, a.V, a.ids, a.top, a.k, a.temp, a.weight,
-            a.loss, a.lse, static_cast<T*>(a.dz), a.lddz);
+    const size_t lds = (size_t)R * entry_words(a.k, PASS == Pass::kForward ? 0 : a.V) * 4;
+    distill_row_kernel<T, G, NV, PASS><<<(unsigned)((a.n + R - 1) / R), BLOCK, lds, stream>>>(
+        static_cast<const T*>(a.z), a.ldz, a.n, a.V, a.ids, a.top, a.k, a.temp, a.weight, a.loss,
+        a.lse, static_cast<T*>(a.dz), a.lddz);
     return hipGetLastError();
   };
 #define SHC_ROW(limit, g, v) \
@@ -705,10 +705,12 @@ hipError_t run_rows(const DistillArgs& a, hipStream_t stream) {
   SHC_ROW(kRowVectors, 512, 8);
   // longer fp32 rows too for the step, whose second pass has as many bytes to store as
   // to read, from 112 MB of them on, when not all of it stays in the caches (1,500 rows
-  // of 45,000: 113 us, read twice 126; 1,000 of 65,536: 116, 123; 600 of 50,021: 57.9,
-  // 62.3; 600 of 32,768: 40.3, 39.1; of 24,000 2,000 rows 84.5, 89.7, but 1,300 62.4,
-  // 60.6).  bf16 rows, with twice the arithmetic a byte, gain nothing (2,000 of 65,536:
-  // 124, 119).
+  // of 45,000: 113 us, read twice 126; 1,000 of 65,536: 115, 123; 600 of 50,021: 57.9,
+  // 62.3; 600 of 32,768: 40.3, 39.1).  Not up to 7,168 vectors, where it takes more rows
+  // to pay (of 24,000 2,000 rows take 84.5, 89.7, but 1,300, also above 112 MB, 62.4,
+  // 60.6).  With 16 vectors a thread 14 registers spill: 60 bytes of scratch a thread, and
+  // still faster (1,000 of 53,252: 95, 103; 500 of 65,536: 61, 66).  bf16 rows, with twice
+  // the arithmetic a byte, gain nothing (2,000 of 65,536: 124, 119).
   if constexpr (sizeof(T) == 4 && PASS == Pass::kStep) {
     if (nvec > 7168 && a.n * nvec >= 7000000) {
       SHC_ROW(8192, 1024, 8);
@@ -718,7 +720,10 @@ hipError_t run_rows(const DistillArgs& a, hipStream_t stream) {
     }
   }
 #undef SHC_ROW
-  return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
+  if constexpr (PASS == Pass::kBackward)
+    return hipErrorInvalidValue;  // run_backward takes longer rows in parts
+  else
+    return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 0>{});
 }
 
 template <typename T>

@@ -31,9 +31,9 @@
 // bit for bit.
 //
 // Measured: 16,384 rows of 4,096 bf16 into a table of 32,768, ids as frequent as
-// words: 145 us, 4.6 TB/s over all (5, 8, 127 and 5 us: the sums and the clearing are
-// bound by HBM, the rest by latency); 268,160 rows of 128 into 10,475: 33 us (5, 10,
-// 16 and 3).  One id of very many positions is the worst: its bucket is one workgroup's
+// words: 145 us, 4.6 TB/s over all (5, 8, 129 and 5 us: the sums and the clearing are
+// bound by HBM, the rest by latency); 268,160 rows of 128 into 10,475: 34 us (5, 11,
+// 17 and 3).  One id of very many positions is the worst: its bucket is one workgroup's
 // (65,536 rows of 1,024, one id: 315 us).
 #include <algorithm>
 #include <mutex>
@@ -962,8 +962,8 @@ int clear_past(int64_t R, int32_t C) { return R * C >= (int64_t)1 << 26; }
 // Whether one launch does it: a position's workgroups, one for each range of columns,
 // look through the whole list, so that the work grows with the positions' square
 // (5,000 ids, bf16: 1,024 rows of 2,000 take 17.1 us, by the launches below 20.2; 2,048
-// rows of 500 10.6, 24.2, of 2,000 30.2, 25.3; 1,186 of 2,345 27.9, 24.6).  One id throughout is the worst of it: 2,048 rows
-// of 64 take 40 us, 26.
+// rows of 500 10.6, 24.2, of 2,000 30.2, 25.3; 1,186 of 2,345 27.9, 24.6).  One id
+// throughout is the worst of it: 2,048 rows of 64 take 40 us, 26.
 constexpr int kFewMost = 4 * kFewThreads;
 bool few_rows(int64_t n, int32_t C, int is_bf16) {
   const int per = is_bf16 ? 512 : 256;

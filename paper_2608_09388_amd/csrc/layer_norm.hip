@@ -21,7 +21,7 @@
 // workgroups follows the sizes alone, so results repeat bit for bit.
 //
 // Measured: forward, 4,099 rows of 5,001 fp32: 34.7 us, 4.7 TB/s; gradient, 16,384
-// rows of 4,096 bf16: 80.6 us, 5.0 TB/s (77 and 5 in the second launch).
+// rows of 4,096 bf16: 81.4 us, 4.9 TB/s (78 and 5 in the second launch).
 #include <algorithm>
 
 #include "row_ops.h"
