@@ -39,8 +39,9 @@
  *   inv entry outside [-1, n_rows), a coordinate outside [0, B) x [0, V)) are
  *   treated as absent rows, never dereferenced.
  * - Inputs and outputs of one call must not overlap.
- * - The row operators (embedding rows, layer norm, distillation) take rows of
- *   any width at any stride: their comment block states their own rules.
+ * - The row operators (embedding rows, layer norm, distillation) and the dense
+ *   operators (linear layer, its cross entropy, clipping) take rows of any
+ *   width at any stride: their comment blocks state their own rules.
  * - Return value: SHC_OK (0) or a negative SHC_ERR_* code.  Nothing is
  *   launched when validation fails.  SHC_ERR_HIP reports a HIP runtime or
  *   launch failure; shc_last_error() then holds the message (thread-local).
@@ -64,6 +65,8 @@ extern "C" {
 /* activation codes (Eq. 10) */
 #define SHC_ACT_NONE 0
 #define SHC_ACT_RELU 1 /* y if y > 0 else 0 */
+#define SHC_ACT_GELU 2 /* y Phi(y), Phi the normal distribution (shc_linear only) */
+#define SHC_ACT_SILU 3 /* y / (1 + exp(-y)) (shc_linear only) */
 
 /* status codes */
 #define SHC_OK 0
@@ -871,6 +874,154 @@ int shc_distill_top_step(const void* logits, int64_t logits_stride, int64_t n_ro
                          float temperature, const float* row_weight, int32_t dtype, float* loss,
                          void* dlogits, int64_t dlogits_stride, void* ws, size_t ws_bytes,
                          hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Dense layers, the loss over a large vocabulary, and clipping             */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * The layers of a network on active rows beyond the sparse linear layer's shapes,
+ * the loss of its last one, and what stands before the optimizer.  Rules, where
+ * they differ from the row operators':
+ * - Widths Cin, Cout and C are in [1, 65536], V in [1, 2^24], n_rows below 2^27,
+ *   row strides below 2^40 / n_rows; a product of sizes may not pass 2^22 tiles
+ *   of 128 x 128 (SHC_ERR_UNSUPPORTED).
+ * - Inputs, weights, outputs and the gradients of weights are of `dtype`; biases,
+ *   their gradients, losses and statistics are fp32.
+ * - bf16 products are exact and summed in fp32; fp32 products are formed from
+ *   three bf16 terms of each operand (six products, 2^-23 of a product left out
+ *   at most), sums that are not finite or beyond 2^80 again on the fp32 matrix
+ *   cores.  Every output is rounded once, but for dz (below), which is rounded to
+ *   `dtype` before the products of a backward take it.
+ * - Sums have a fixed order that follows the sizes and alignments: results repeat
+ *   bit for bit.
+ * - A workspace query takes `aligned`: 1 where every row tensor that the call
+ *   reads starts at a multiple of 16 bytes, with rows a multiple of 16 bytes and
+ *   less than 2^21 elements apart; 0 always suffices.  A call whose tensors are
+ *   not so needs the larger size (SHC_ERR_CAPACITY); rows of a multiple of 8
+ *   elements at such places are read as they are, others are packed first.  The
+ *   workspace for n rows serves every smaller count.  Calls that share a
+ *   workspace must not overlap.
+ * - With `accumulate` 1 the gradients of weights and biases are added to what the
+ *   outputs hold.
+ */
+
+/*
+ * Dense linear layer with bias, activation and residual:
+ *
+ *   z = x W + bias,   out = act(z) + residual
+ *
+ *   x [n_rows] rows of Cin, W [Cin] rows of Cout, residual, pre, out [n_rows] rows
+ *   of Cout; bias [Cout] or NULL; residual NULL for none, and may be out itself.
+ *   pre: z (rounded), for the backward, or NULL.   act: any SHC_ACT_*.
+ */
+size_t shc_linear_workspace(int64_t n_rows, int32_t Cin, int32_t Cout, int32_t dtype,
+                            int32_t aligned);
+int shc_linear(const void* x, int64_t x_stride, int64_t n_rows, int32_t Cin, const void* W,
+               int64_t W_stride, int32_t Cout, const float* bias, int32_t act,
+               const void* residual, int64_t residual_stride, int32_t dtype, void* pre,
+               int64_t pre_stride, void* out, int64_t out_stride, void* ws, size_t ws_bytes,
+               hipStream_t stream);
+
+/*
+ * Gradients of the dense linear layer from z as shc_linear wrote it to pre:
+ *
+ *   dz = dout act'(z),   dx = dz W^T,   dW = x^T dz,   db = sum over rows of dz
+ *
+ * (act' of SHC_ACT_RELU is 0 at 0; the residual's gradient is dout itself).
+ *   dout, pre [n_rows] rows of Cout (pre may be NULL with SHC_ACT_NONE); dx
+ *   [n_rows] rows of Cin, dW [Cin] rows of Cout, db [Cout] fp32; each output may
+ *   be NULL.  db sums dz before it is rounded.
+ */
+size_t shc_linear_backward_workspace(int64_t n_rows, int32_t Cin, int32_t Cout, int32_t dtype,
+                                     int32_t act, int32_t aligned);
+int shc_linear_backward(const void* dout, int64_t dout_stride, const void* x, int64_t x_stride,
+                        int64_t n_rows, int32_t Cin, const void* W, int64_t W_stride,
+                        int32_t Cout, const void* pre, int64_t pre_stride, int32_t act,
+                        int32_t dtype, int32_t accumulate, void* dx, int64_t dx_stride, void* dW,
+                        int64_t dW_stride, float* db, void* ws, size_t ws_bytes,
+                        hipStream_t stream);
+
+/*
+ * Cross entropy of a linear layer's logits over V classes, none of which is
+ * written to memory, with W the table of V rows of C that shc_embed_rows reads too:
+ *
+ *   z_v = x . W_v + bias_v,   lse = log of sum exp z,   loss = lse - z_label
+ *   dz_v = w (exp(z_v - lse) - [v = label])
+ *   dx = dz W,   dW = dz^T x,   db = sum over rows of dz
+ *
+ *   x, dx [n_rows] rows of C; W, dW [V] rows of C; bias, db [V] fp32, each may be
+ *   NULL.  labels [n_rows] int32 or int64 (id_type), label_stride elements apart
+ *   (>= 0).  A row whose label is outside [0, V) is padding: loss, lse and dx are
+ *   0 and it reaches no other gradient, whatever x holds there; its products are
+ *   left out.
+ *   loss, lse [n_rows] fp32, row_weight [n_rows] fp32 = w, the upstream gradient of
+ *   every row's loss, or NULL (1).  dx, dW and db may each be NULL.
+ *   A logit of -inf (by its bias) has probability 0; a label there makes the loss
+ *   +inf, the gradient stays finite; in a row of nothing but -inf every probability
+ *   is 0.  NaN, +inf or a sum without end in a row makes its results NaN, and those
+ *   of dW and db that it reaches.
+ *
+ * shc_linear_cross_entropy          -- loss, and lse (may be NULL) for a backward.
+ * shc_linear_cross_entropy_backward -- gradients from lse as written.
+ * shc_linear_cross_entropy_step     -- loss and gradients.
+ * The backward and the step hold dz for up to 2^30 (bf16) or 2^28 (fp32) pairs of
+ * row and class at a time in the workspace.  `pass` of the workspace query: 0
+ * forward, 1 backward, 2 step; `aligned` speaks of W alone.
+ */
+#define SHC_XENT_FORWARD 0
+#define SHC_XENT_BACKWARD 1
+#define SHC_XENT_STEP 2
+size_t shc_linear_cross_entropy_workspace(int64_t n_rows, int32_t C, int32_t V, int32_t dtype,
+                                          int32_t pass, int32_t aligned);
+int shc_linear_cross_entropy(const void* x, int64_t x_stride, int64_t n_rows, int32_t C,
+                             const void* W, int64_t W_stride, int32_t V, const float* bias,
+                             const void* labels, int32_t id_type, int64_t label_stride,
+                             int32_t dtype, float* loss, float* lse, void* ws, size_t ws_bytes,
+                             hipStream_t stream);
+int shc_linear_cross_entropy_backward(const void* x, int64_t x_stride, int64_t n_rows, int32_t C,
+                                      const void* W, int64_t W_stride, int32_t V,
+                                      const float* bias, const void* labels, int32_t id_type,
+                                      int64_t label_stride, const float* lse,
+                                      const float* row_weight, int32_t dtype, int32_t accumulate,
+                                      void* dx, int64_t dx_stride, void* dW, int64_t dW_stride,
+                                      float* db, void* ws, size_t ws_bytes, hipStream_t stream);
+int shc_linear_cross_entropy_step(const void* x, int64_t x_stride, int64_t n_rows, int32_t C,
+                                  const void* W, int64_t W_stride, int32_t V, const float* bias,
+                                  const void* labels, int32_t id_type, int64_t label_stride,
+                                  const float* row_weight, int32_t dtype, int32_t accumulate,
+                                  float* loss, void* dx, int64_t dx_stride, void* dW,
+                                  int64_t dW_stride, float* db, void* ws, size_t ws_bytes,
+                                  hipStream_t stream);
+
+/*
+ * Norm of all gradients together, and their clipping to it:
+ *
+ *   norm = sqrt(sum over every element of every tensor of g^2)
+ *   factor = 1 where norm <= max_norm, else max_norm / norm;   out = factor g
+ *
+ *   grads: host array of `count` tensors (0 to 65,536), read during the call: numel
+ *   elements (below 2^40) of dtype at `data`, contiguous, aligned to their elements;
+ *   data may be NULL where numel is 0.  shc_clip_grads writes every tensor's `out`,
+ *   which may be its own data, and may overlap no other region of the call
+ *   (SHC_ERR_INVALID_ARG); shc_grad_norm ignores it.
+ *   norm: one fp32 on the device; squares are summed in fp64, in a fixed order.
+ *   max_norm not negative, not NaN; an infinity never clips.
+ * An infinite norm makes the factor 0 and an infinite element NaN, a NaN norm makes
+ * every element NaN.  The norm of several devices' shards is the root of the sum of
+ * their squares: combine *norm between the two calls.
+ */
+typedef struct shc_grad {
+  const void* data;
+  void* out;
+  int64_t numel;
+  int32_t dtype;
+} shc_grad;
+size_t shc_grad_norm_workspace(const shc_grad* grads, int64_t count);
+int shc_grad_norm(const shc_grad* grads, int64_t count, float* norm, void* ws, size_t ws_bytes,
+                  hipStream_t stream);
+int shc_clip_grads(const shc_grad* grads, int64_t count, const float* norm, float max_norm,
+                   hipStream_t stream);
 
 /*
  * Stream-ordering events -- a runtime helper, not an operator of the paper.

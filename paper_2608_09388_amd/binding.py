@@ -21,7 +21,8 @@ LIB_PATH = os.path.join(HERE, "libshc.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "shc.h")
 
 SHC_F32, SHC_BF16 = 0, 1
-SHC_ACT_NONE, SHC_ACT_RELU = 0, 1
+SHC_ACT_NONE, SHC_ACT_RELU, SHC_ACT_GELU, SHC_ACT_SILU = 0, 1, 2, 3
+SHC_XENT_FORWARD, SHC_XENT_BACKWARD, SHC_XENT_STEP = 0, 1, 2
 SHC_COMBINE_SUM, SHC_COMBINE_MEAN, SHC_COMBINE_MAX = 0, 1, 2
 # largest V shc_compact_mask_table_start takes
 COMPACT_TABLE_MAX_V = 19456
@@ -69,6 +70,10 @@ class StackDesc(ctypes.Structure):
                 ("pooled", _c_ptr), ("pool_empty", _c_f), ("n_sets", _c_i32),
                 ("sets", StackIndexSet * 3), ("side", _c_ptr), ("tail", _c_ptr),
                 ("split_ws", _c_ptr), ("split_ws_bytes", _c_sz)]
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("data", _c_ptr), ("out", _c_ptr), ("numel", _c_i64), ("dtype", _c_i32)]
 
 
 STACK_FEED_FN = ctypes.CFUNCTYPE(ctypes.c_int, _c_ptr, _c_i64, _c_ptr)
@@ -188,6 +193,32 @@ _SIGS = {
     "shc_distill_top_step": (ctypes.c_int, [_c_ptr, _c_i64, _c_i64, _c_i32, _c_ptr, _c_ptr,
                                             _c_i32, _c_f, _c_ptr, _c_i32, _c_ptr, _c_ptr, _c_i64,
                                             _c_ptr, _c_sz, _c_ptr]),
+    "shc_linear_workspace": (_c_sz, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32]),
+    "shc_linear": (ctypes.c_int, [_c_ptr, _c_i64, _c_i64, _c_i32, _c_ptr, _c_i64, _c_i32, _c_ptr,
+                                  _c_i32, _c_ptr, _c_i64, _c_i32, _c_ptr, _c_i64, _c_ptr, _c_i64,
+                                  _c_ptr, _c_sz, _c_ptr]),
+    "shc_linear_backward_workspace": (_c_sz, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_i32]),
+    "shc_linear_backward": (ctypes.c_int, [_c_ptr, _c_i64, _c_ptr, _c_i64, _c_i64, _c_i32, _c_ptr,
+                                           _c_i64, _c_i32, _c_ptr, _c_i64, _c_i32, _c_i32, _c_i32,
+                                           _c_ptr, _c_i64, _c_ptr, _c_i64, _c_ptr, _c_ptr, _c_sz,
+                                           _c_ptr]),
+    "shc_linear_cross_entropy_workspace": (_c_sz, [_c_i64, _c_i32, _c_i32, _c_i32, _c_i32,
+                                                   _c_i32]),
+    "shc_linear_cross_entropy": (ctypes.c_int, [_c_ptr, _c_i64, _c_i64, _c_i32, _c_ptr, _c_i64,
+                                                _c_i32, _c_ptr, _c_ptr, _c_i32, _c_i64, _c_i32,
+                                                _c_ptr, _c_ptr, _c_ptr, _c_sz, _c_ptr]),
+    "shc_linear_cross_entropy_backward": (ctypes.c_int, [
+        _c_ptr, _c_i64, _c_i64, _c_i32, _c_ptr, _c_i64, _c_i32, _c_ptr, _c_ptr, _c_i32, _c_i64,
+        _c_ptr, _c_ptr, _c_i32, _c_i32, _c_ptr, _c_i64, _c_ptr, _c_i64, _c_ptr, _c_ptr, _c_sz,
+        _c_ptr]),
+    "shc_linear_cross_entropy_step": (ctypes.c_int, [
+        _c_ptr, _c_i64, _c_i64, _c_i32, _c_ptr, _c_i64, _c_i32, _c_ptr, _c_ptr, _c_i32, _c_i64,
+        _c_ptr, _c_i32, _c_i32, _c_ptr, _c_ptr, _c_i64, _c_ptr, _c_i64, _c_ptr, _c_ptr, _c_sz,
+        _c_ptr]),
+    "shc_grad_norm_workspace": (_c_sz, [ctypes.POINTER(Grad), _c_i64]),
+    "shc_grad_norm": (ctypes.c_int, [ctypes.POINTER(Grad), _c_i64, _c_ptr, _c_ptr, _c_sz,
+                                     _c_ptr]),
+    "shc_clip_grads": (ctypes.c_int, [ctypes.POINTER(Grad), _c_i64, _c_ptr, _c_f, _c_ptr]),
     "shc_event_create": (ctypes.c_int, [ctypes.POINTER(_c_ptr)]),
     "shc_event_record": (ctypes.c_int, [_c_ptr, _c_ptr]),
     "shc_stream_wait_event": (ctypes.c_int, [_c_ptr, _c_ptr]),
@@ -1244,13 +1275,13 @@ class _Operands:
             raise ValueError(f"{name} holds {t.numel()} elements, needs {numel}")
         return t.data_ptr()
 
-    def ids(self, t):
+    def ids(self, t, name="ids"):
         """(pointer, type code, stride, count) of a list of ids."""
-        self._place(t, "ids")
+        self._place(t, name)
         if t.dtype not in (torch.int32, torch.int64):
-            raise TypeError(f"ids must be int32 or int64, got {t.dtype}")
+            raise TypeError(f"{name} must be int32 or int64, got {t.dtype}")
         if t.dim() != 1:
-            raise ValueError(f"ids must be one-dimensional, got {tuple(t.shape)}")
+            raise ValueError(f"{name} must be one-dimensional, got {tuple(t.shape)}")
         code = SHC_IDS_I64 if t.dtype == torch.int64 else SHC_IDS_I32
         return t.data_ptr(), code, t.stride(0) if t.numel() > 1 else 1, t.numel()
 
@@ -1480,3 +1511,265 @@ def distill_top_step(logits, top_ids, top_logits, row_weight=None, loss=None, dl
                                     temperature, ws, stream)
     call(logits.shape[0])
     return loss, dlogits
+
+
+# ----------------------------------------------------------------------------
+# dense layers, the loss over a large vocabulary, and clipping.  Row tensors as
+# the row operators'; W of the linear layer is [Cin][Cout], of the cross entropy
+# [V][C].  Each operator as a prepared call, for any row count up to its tensors',
+# and as a plain one over the tensors' rows.
+# ----------------------------------------------------------------------------
+
+
+def _aligned(*rows) -> int:
+    """Whether row tensors start and step by 16 bytes."""
+    def fits(t):
+        stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]  # as _Operands.rows
+        return t.data_ptr() % 16 == 0 and stride % 8 == 0 and stride < 1 << 21
+    return int(all(fits(t) for t in rows))
+
+
+def linear_workspace(n_rows: int, Cin: int, Cout: int, dtype: int, aligned: bool = False) -> int:
+    """shc_linear_workspace."""
+    return int(load().shc_linear_workspace(n_rows, Cin, Cout, dtype, int(aligned)))
+
+
+def linear_backward_workspace(n_rows: int, Cin: int, Cout: int, dtype: int,
+                              act: int = SHC_ACT_NONE, aligned: bool = False) -> int:
+    """shc_linear_backward_workspace."""
+    return int(load().shc_linear_backward_workspace(n_rows, Cin, Cout, dtype, act, int(aligned)))
+
+
+def linear_cross_entropy_workspace(n_rows: int, C: int, V: int, dtype: int,
+                                   which: int = SHC_XENT_STEP, aligned: bool = False) -> int:
+    """shc_linear_cross_entropy_workspace."""
+    return int(load().shc_linear_cross_entropy_workspace(n_rows, C, V, dtype, which,
+                                                         int(aligned)))
+
+
+def prepare_linear(x, W, bias, out, act: int = SHC_ACT_NONE, residual=None, pre=None, ws=None,
+                   stream=None) -> Prepared:
+    """shc_linear: out = act(x W + bias) + residual; residual may be out, pre [n][Cout]
+    keeps x W + bias for the backward."""
+    o = _Operands()
+    x_ptr, x_ld, n, Cin = o.rows(x, "x")
+    dt = _dtype_code(x)
+    w_ptr, w_ld, rows, Cout = o.rows(W, "W", x.dtype)
+    if rows != Cin:
+        raise ValueError(f"W has {rows} rows, x rows of {Cin}")
+    o_ptr, o_ld, n_out, _ = o.rows(out, "out", x.dtype, Cout)
+    n_max = min(n, n_out)
+    r_ptr, r_ld, p_ptr, p_ld = None, Cout, None, Cout
+    if residual is not None:
+        r_ptr, r_ld, n_r, _ = o.rows(residual, "residual", x.dtype, Cout)
+        n_max = min(n_max, n_r)
+    if pre is not None:
+        p_ptr, p_ld, n_p, _ = o.rows(pre, "pre", x.dtype, Cout)
+        n_max = min(n_max, n_p)
+    need = linear_workspace(n_max, Cin, Cout, dt, _aligned(x, W))
+    ws, ws_ptr, ws_bytes = o.workspace(ws, need, stream)
+    args = [x_ptr, x_ld, 0, Cin, w_ptr, w_ld, Cout,
+            o.array(bias, "bias", torch.float32, Cout, True), act, r_ptr, r_ld, dt, p_ptr, p_ld,
+            o_ptr, o_ld, ws_ptr, ws_bytes, _stream(stream)]
+    return Prepared("shc_linear", args, 2, n_max, (x, W, bias, out, residual, pre, ws))
+
+
+def linear(x, W, bias=None, out=None, act: int = SHC_ACT_NONE, residual=None, pre=None, ws=None,
+           stream=None):
+    """shc_linear over all rows of x; returns out (made here when None)."""
+    if out is None:
+        out = _new((x.shape[0], W.shape[-1]), x.dtype, x.device, stream)
+    prepare_linear(x, W, bias, out, act, residual, pre, ws, stream)(x.shape[0])
+    return out
+
+
+def prepare_linear_backward(dout, x, W, pre, dx=None, dW=None, db=None, act: int = SHC_ACT_NONE,
+                            accumulate: bool = False, ws=None, stream=None) -> Prepared:
+    """shc_linear_backward; pre as the forward wrote it (None with SHC_ACT_NONE); dx [n][Cin],
+    dW [Cin][Cout], db [Cout] fp32, each or None."""
+    o = _Operands()
+    g_ptr, g_ld, n_g, Cout = o.rows(dout, "dout")
+    dt = _dtype_code(dout)
+    x_ptr, x_ld, n, Cin = o.rows(x, "x", dout.dtype)
+    w_ptr, w_ld, rows, _ = o.rows(W, "W", dout.dtype, Cout)
+    if rows != Cin:
+        raise ValueError(f"W has {rows} rows, x rows of {Cin}")
+    n_max = min(n, n_g)
+    p_ptr, p_ld, d_ptr, d_ld, dw_ptr, dw_ld = None, Cout, None, Cin, None, Cout
+    if pre is not None:
+        p_ptr, p_ld, n_p, _ = o.rows(pre, "pre", dout.dtype, Cout)
+        n_max = min(n_max, n_p)
+    if dx is not None:
+        d_ptr, d_ld, n_d, _ = o.rows(dx, "dx", dout.dtype, Cin)
+        n_max = min(n_max, n_d)
+    if dW is not None:
+        dw_ptr, dw_ld, rows, _ = o.rows(dW, "dW", dout.dtype, Cout)
+        if rows != Cin:
+            raise ValueError(f"dW has {rows} rows, not {Cin}")
+    need = linear_backward_workspace(n_max, Cin, Cout, dt, act, _aligned(x, W, dout))
+    ws, ws_ptr, ws_bytes = o.workspace(ws, need, stream)
+    args = [g_ptr, g_ld, x_ptr, x_ld, 0, Cin, w_ptr, w_ld, Cout, p_ptr, p_ld, act, dt,
+            int(bool(accumulate)), d_ptr, d_ld, dw_ptr, dw_ld,
+            o.array(db, "db", torch.float32, Cout, True), ws_ptr, ws_bytes, _stream(stream)]
+    return Prepared("shc_linear_backward", args, 4, n_max, (dout, x, W, pre, dx, dW, db, ws))
+
+
+def linear_backward(dout, x, W, pre=None, dx=None, dW=None, db=None, act: int = SHC_ACT_NONE,
+                    accumulate: bool = False, ws=None, stream=None):
+    """shc_linear_backward over all rows of dout; writes those of dx, dW and db that are given."""
+    prepare_linear_backward(dout, x, W, pre, dx, dW, db, act, accumulate, ws,
+                            stream)(dout.shape[0])
+
+
+def _xent(o, x, W, bias, labels):
+    x_ptr, x_ld, n, C = o.rows(x, "x")
+    dt = _dtype_code(x)
+    w_ptr, w_ld, V, _ = o.rows(W, "W", x.dtype, C)
+    l_ptr, code, l_ld, n_l = o.ids(labels, "labels")
+    args = [x_ptr, x_ld, 0, C, w_ptr, w_ld, V, o.array(bias, "bias", torch.float32, V, True),
+            l_ptr, code, l_ld]
+    return args, dt, min(n, n_l), C, V
+
+
+def _xent_grads(o, args, x, dx, dW, db, n_max, C, V):
+    """The gradients' arguments, and the rows that dx has."""
+    d_ptr, d_ld, dw_ptr, dw_ld = None, C, None, C
+    if dx is not None:
+        d_ptr, d_ld, n_d, _ = o.rows(dx, "dx", x.dtype, C)
+        n_max = min(n_max, n_d)
+    if dW is not None:
+        dw_ptr, dw_ld, rows, _ = o.rows(dW, "dW", x.dtype, C)
+        if rows != V:
+            raise ValueError(f"dW has {rows} rows, not {V}")
+    return [d_ptr, d_ld, dw_ptr, dw_ld, o.array(db, "db", torch.float32, V, True)], n_max
+
+
+def prepare_linear_cross_entropy(x, W, bias, labels, loss, lse=None, ws=None,
+                                 stream=None) -> Prepared:
+    """shc_linear_cross_entropy: loss [n] (and lse [n]) fp32 of the logits x W^T + bias against
+    labels [n]; W [V][C]; a label outside [0, V) marks padding."""
+    o = _Operands()
+    args, dt, n_max, C, V = _xent(o, x, W, bias, labels)
+    f32 = torch.float32
+    args += [dt, o.array(loss, "loss", f32, n_max), o.array(lse, "lse", f32, n_max, True)]
+    need = linear_cross_entropy_workspace(n_max, C, V, dt, SHC_XENT_FORWARD, _aligned(W))
+    ws, ws_ptr, ws_bytes = o.workspace(ws, need, stream)
+    args += [ws_ptr, ws_bytes, _stream(stream)]
+    return Prepared("shc_linear_cross_entropy", args, 2, n_max,
+                    (x, W, bias, labels, loss, lse, ws))
+
+
+def linear_cross_entropy(x, W, labels, bias=None, loss=None, lse=None, ws=None, stream=None):
+    """shc_linear_cross_entropy over all rows of x; returns loss (made here when None)."""
+    if loss is None:
+        loss = _new(x.shape[0], torch.float32, x.device, stream)
+    prepare_linear_cross_entropy(x, W, bias, labels, loss, lse, ws, stream)(x.shape[0])
+    return loss
+
+
+def prepare_linear_cross_entropy_backward(x, W, bias, labels, lse, row_weight, dx=None, dW=None,
+                                          db=None, accumulate: bool = False, ws=None,
+                                          stream=None) -> Prepared:
+    """shc_linear_cross_entropy_backward from lse [n]; dx [n][C], dW [V][C], db [V] fp32, each
+    or None."""
+    o = _Operands()
+    args, dt, n_max, C, V = _xent(o, x, W, bias, labels)
+    f32 = torch.float32
+    grads, n_max = _xent_grads(o, args, x, dx, dW, db, n_max, C, V)
+    args += [o.array(lse, "lse", f32, n_max), o.array(row_weight, "row_weight", f32, n_max, True),
+             dt, int(bool(accumulate))] + grads
+    need = linear_cross_entropy_workspace(n_max, C, V, dt, SHC_XENT_BACKWARD, _aligned(W))
+    ws, ws_ptr, ws_bytes = o.workspace(ws, need, stream)
+    args += [ws_ptr, ws_bytes, _stream(stream)]
+    return Prepared("shc_linear_cross_entropy_backward", args, 2, n_max,
+                    (x, W, bias, labels, lse, row_weight, dx, dW, db, ws))
+
+
+def linear_cross_entropy_backward(x, W, labels, lse, row_weight=None, bias=None, dx=None, dW=None,
+                                  db=None, accumulate: bool = False, ws=None, stream=None):
+    """shc_linear_cross_entropy_backward over all rows of x."""
+    prepare_linear_cross_entropy_backward(x, W, bias, labels, lse, row_weight, dx, dW, db,
+                                          accumulate, ws, stream)(x.shape[0])
+
+
+def prepare_linear_cross_entropy_step(x, W, bias, labels, row_weight, loss, dx=None, dW=None,
+                                      db=None, accumulate: bool = False, ws=None,
+                                      stream=None) -> Prepared:
+    """shc_linear_cross_entropy_step: loss [n], and the gradients that are given."""
+    o = _Operands()
+    args, dt, n_max, C, V = _xent(o, x, W, bias, labels)
+    f32 = torch.float32
+    grads, n_max = _xent_grads(o, args, x, dx, dW, db, n_max, C, V)
+    args += [o.array(row_weight, "row_weight", f32, n_max, True), dt, int(bool(accumulate)),
+             o.array(loss, "loss", f32, n_max)] + grads
+    need = linear_cross_entropy_workspace(n_max, C, V, dt, SHC_XENT_STEP, _aligned(W))
+    ws, ws_ptr, ws_bytes = o.workspace(ws, need, stream)
+    args += [ws_ptr, ws_bytes, _stream(stream)]
+    return Prepared("shc_linear_cross_entropy_step", args, 2, n_max,
+                    (x, W, bias, labels, row_weight, loss, dx, dW, db, ws))
+
+
+def linear_cross_entropy_step(x, W, labels, row_weight=None, bias=None, loss=None, dx=None,
+                              dW=None, db=None, accumulate: bool = False, ws=None, stream=None):
+    """shc_linear_cross_entropy_step over all rows of x; returns loss (made here when None)."""
+    if loss is None:
+        loss = _new(x.shape[0], torch.float32, x.device, stream)
+    prepare_linear_cross_entropy_step(x, W, bias, labels, row_weight, loss, dx, dW, db,
+                                      accumulate, ws, stream)(x.shape[0])
+    return loss
+
+
+def _grad_list(o, grads, outs):
+    grads = list(grads)
+    outs = grads if outs is None else list(outs)
+    if len(outs) != len(grads):
+        raise ValueError(f"{len(grads)} gradients, {len(outs)} outputs")
+    table = (Grad * max(1, len(grads)))()
+    for i, (g, out) in enumerate(zip(grads, outs)):
+        if not isinstance(g, torch.Tensor):
+            raise TypeError(f"grads[{i}] must be a torch.Tensor")
+        table[i] = Grad(o.array(g, f"grads[{i}]", g.dtype, 0),
+                        o.array(out, f"outs[{i}]", g.dtype, 0), g.numel(), _dtype_code(g))
+        if out.numel() != g.numel():
+            raise ValueError(f"outs[{i}] holds {out.numel()} elements, grads[{i}] {g.numel()}")
+    return table, len(grads), grads, outs
+
+
+def grad_norm_workspace(grads) -> int:
+    """shc_grad_norm_workspace of a list of tensors."""
+    table, count, _, _ = _grad_list(_Operands(), grads, None)
+    return int(load().shc_grad_norm_workspace(table, count))
+
+
+def prepare_grad_norm(grads, norm, ws=None, stream=None) -> Prepared:
+    """shc_grad_norm: norm [1] fp32 of all the tensors together (contiguous, fp32 or bf16)."""
+    o = _Operands()
+    n_ptr = o.array(norm, "norm", torch.float32, 1)
+    table, count, grads, _ = _grad_list(o, grads, None)
+    ws, ws_ptr, ws_bytes = o.workspace(ws, int(load().shc_grad_norm_workspace(table, count)),
+                                       stream)
+    return Prepared("shc_grad_norm", [table, count, n_ptr, ws_ptr, ws_bytes, _stream(stream)],
+                    None, 0, (grads, norm, ws))
+
+
+def grad_norm(grads, norm=None, ws=None, stream=None):
+    """shc_grad_norm; returns norm ([1] fp32, made here when None)."""
+    grads = list(grads)
+    if norm is None:
+        norm = _new(1, torch.float32, grads[0].device if grads else "cuda", stream)
+    prepare_grad_norm(grads, norm, ws, stream)()
+    return norm
+
+
+def prepare_clip_grads(grads, norm, max_norm: float, outs=None, stream=None) -> Prepared:
+    """shc_clip_grads: the tensors times min(1, max_norm / norm), in place or into outs."""
+    o = _Operands()
+    n_ptr = o.array(norm, "norm", torch.float32, 1)
+    table, count, grads, outs = _grad_list(o, grads, outs)
+    return Prepared("shc_clip_grads", [table, count, n_ptr, float(max_norm), _stream(stream)],
+                    None, 0, (grads, norm, outs))
+
+
+def clip_grads(grads, norm, max_norm: float, outs=None, stream=None):
+    """shc_clip_grads."""
+    prepare_clip_grads(grads, norm, max_norm, outs, stream)()

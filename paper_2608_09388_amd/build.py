@@ -19,7 +19,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libshc.so")
 SOURCES = ["compact.hip", "neighbors.hip", "rows.hip", "norm.hip", "scores.hip", "backward.hip",
            "gemm.hip", "conv_walk.hip", "conv_ws.hip", "conv_sm.hip", "conv_split.hip",
-           "conv_packed.hip", "embed.hip", "layer_norm.hip", "distill.hip", "abi.hip", "stack.hip"]
+           "conv_packed.hip", "embed.hip", "layer_norm.hip", "distill.hip", "dense.hip",
+           "linear.hip", "xent.hip", "clip.hip", "abi.hip", "stack.hip"]
 ARCH = os.environ.get("SHC_OFFLOAD_ARCH", "gfx950")
 
 # Packed fp32 VALU instructions are disabled for all device code.

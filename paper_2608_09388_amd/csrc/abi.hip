@@ -3,9 +3,11 @@
 // without a GPU.
 #include <stdarg.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include "../../include/shc.h"
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 
@@ -1454,6 +1456,354 @@ int shc_distill_top_step(const void* logits, int64_t logits_stride, int64_t n_ro
                            row_weight, loss, nullptr, dlogits, dlogits_stride, ws};
   return hip_status(shc::launch_distill(a, shc::DistillPass::kStep, dtype == SHC_BF16, stream),
                     "distill_top_step launch");
+}
+
+// -- dense layers, cross entropy, clipping ---------------------------------------
+
+namespace {
+
+constexpr int32_t kMaxDenseChannels = 65536;
+constexpr int64_t kMaxDenseRows = ((int64_t)1 << 27) - 1;
+constexpr int64_t kMaxTiles = (int64_t)1 << 22;
+constexpr int64_t kMaxGrads = 65536;
+
+int check_dense_rows(int64_t n) {
+  SHC_TRY(check_rows(n));
+  if (n > kMaxDenseRows)
+    return fail(SHC_ERR_UNSUPPORTED, "n_rows = %lld is not below 2^27", (long long)n);
+  return SHC_OK;
+}
+
+bool tiles_fit(int64_t M, int64_t N) {
+  return ((M + 127) / 128) * ((N + 127) / 128) < kMaxTiles;
+}
+int check_tiles(int64_t M, int64_t N) {
+  if (!tiles_fit(M, N))
+    return fail(SHC_ERR_UNSUPPORTED, "%lld x %lld is not below 2^22 tiles of 128 x 128",
+                (long long)M, (long long)N);
+  return SHC_OK;
+}
+
+int check_linear(const shc::LinearArgs& a, int32_t dtype, bool backward) {
+  const size_t e = elem_size(dtype);
+  SHC_TRY(check_row_tensor("x", a.x, a.n, a.Cin, a.ldx, e, false));
+  SHC_TRY(check_row_tensor("W", a.W, a.n > 0 ? a.Cin : 0, a.Cout, a.ldw, e, false));
+  const bool pre = backward && a.act != SHC_ACT_NONE;
+  if (!backward || pre) SHC_TRY(check_row_tensor("pre", a.pre, a.n, a.Cout, a.ldpre, e, !pre));
+  SHC_TRY(check_tiles(a.n, a.Cout));
+  SHC_TRY(check_tiles(a.n, a.Cin));
+  return check_tiles(a.Cin, a.Cout);
+}
+
+int check_linear_sizes(int64_t n, int32_t Cin, int32_t Cout, int32_t dtype, int32_t act) {
+  SHC_TRY(check_dense_rows(n));
+  SHC_TRY(check_dtype(dtype));
+  SHC_TRY(check_width("Cin", Cin, kMaxDenseChannels));
+  SHC_TRY(check_width("Cout", Cout, kMaxDenseChannels));
+  if (act < SHC_ACT_NONE || act > SHC_ACT_SILU)
+    return fail(SHC_ERR_UNSUPPORTED, "unknown activation code %d", act);
+  return SHC_OK;
+}
+
+bool dense_sizes(int64_t n, int32_t a, int32_t most_a, int32_t b, int32_t most_b, int32_t dtype) {
+  return n >= 0 && n <= kMaxDenseRows && a > 0 && a <= most_a && b > 0 && b <= most_b &&
+         (dtype == SHC_F32 || dtype == SHC_BF16);
+}
+
+int check_xent(const shc::XentArgs& a, int32_t dtype, int32_t id_type) {
+  SHC_TRY(check_dense_rows(a.n));
+  SHC_TRY(check_dtype(dtype));
+  SHC_TRY(check_width("C", a.C, kMaxDenseChannels));
+  SHC_TRY(check_width("V", a.V, kMaxLogits));
+  SHC_TRY(check_tiles(a.n, a.V));
+  SHC_TRY(check_tiles(a.n, a.C));
+  SHC_TRY(check_tiles(a.V, a.C));
+  const size_t e = elem_size(dtype);
+  SHC_TRY(check_row_tensor("x", a.x, a.n, a.C, a.ldx, e, false));
+  SHC_TRY(check_row_tensor("W", a.W, a.n > 0 ? a.V : 0, a.C, a.ldw, e, false));
+  SHC_TRY(check_array("bias", a.bias, true));
+  if (id_type != SHC_IDS_I32 && id_type != SHC_IDS_I64)
+    return fail(SHC_ERR_UNSUPPORTED, "unknown id type code %d", id_type);
+  if (a.label_stride < 0 || a.label_stride > kMaxElements ||
+      (a.n > 0 && a.label_stride > kMaxElements / a.n))
+    return fail(SHC_ERR_INVALID_ARG, "label_stride = %lld outside [0, 2^40 / n_rows]",
+                (long long)a.label_stride);
+  if (a.n == 0) return SHC_OK;
+  if (a.labels == nullptr) return fail(SHC_ERR_INVALID_ARG, "labels is NULL");
+  const size_t id = id_type == SHC_IDS_I64 ? 8 : 4;
+  if (reinterpret_cast<uintptr_t>(a.labels) % id != 0)
+    return fail(SHC_ERR_MISALIGNED, "labels is not aligned to its elements of %zu bytes", id);
+  return SHC_OK;
+}
+
+int check_xent_grads(const shc::XentArgs& a, int32_t dtype, int32_t accumulate) {
+  const size_t e = elem_size(dtype);
+  SHC_TRY(check_flag("accumulate", accumulate));
+  SHC_TRY(check_array("row_weight", a.weight, true));
+  SHC_TRY(check_row_tensor("dx", a.dx, a.n, a.C, a.lddx, e, true));
+  SHC_TRY(check_row_tensor("dW", a.dW, a.V, a.C, a.lddW, e, true));
+  return check_array("db", a.db, true);
+}
+
+int run_xent(const shc::XentArgs& a, shc::XentPass pass, size_t ws_bytes, hipStream_t stream,
+             const char* what) {
+  if (a.n > 0)
+    SHC_TRY(check_ws(a.ws, ws_bytes, shc::xent_workspace_bytes(a.n, a.C, a.V, a.bf16,
+                                                               shc::xent_aligned(a), pass)));
+  return hip_status(shc::launch_xent(a, pass, stream), what);
+}
+
+// The caller's list as the launchers take it; NULL with an error set.  freed by the caller.
+shc::ClipTensor* clip_list(const shc_grad* grads, int64_t count, bool outs, int* status) {
+  *status = SHC_OK;
+  const auto refuse = [&](int rc) {
+    *status = rc;
+    return nullptr;
+  };
+  if (count < 0 || count > kMaxGrads)
+    return refuse(fail(SHC_ERR_INVALID_ARG, "count = %lld outside [0, 65536]", (long long)count));
+  if (count > 0 && grads == nullptr)
+    return refuse(fail(SHC_ERR_INVALID_ARG, "grads is NULL"));
+  for (int64_t i = 0; i < count; ++i) {
+    const shc_grad& g = grads[i];
+    if (g.dtype != SHC_F32 && g.dtype != SHC_BF16)
+      return refuse(fail(SHC_ERR_UNSUPPORTED, "grads[%lld]: unknown dtype code %d", (long long)i,
+                         g.dtype));
+    if (g.numel < 0 || g.numel >= kMaxElements)
+      return refuse(fail(SHC_ERR_INVALID_ARG, "grads[%lld]: numel = %lld outside [0, 2^40)",
+                         (long long)i, (long long)g.numel));
+    if (g.numel == 0) continue;
+    if (g.data == nullptr || (outs && g.out == nullptr))
+      return refuse(fail(SHC_ERR_INVALID_ARG, "grads[%lld]: %s is NULL", (long long)i,
+                         g.data == nullptr ? "data" : "out"));
+    const size_t e = elem_size(g.dtype);
+    if (reinterpret_cast<uintptr_t>(g.data) % e != 0 ||
+        (outs && reinterpret_cast<uintptr_t>(g.out) % e != 0))
+      return refuse(fail(SHC_ERR_MISALIGNED, "grads[%lld] is not aligned to its elements of %zu "
+                         "bytes", (long long)i, e));
+  }
+  auto* t = static_cast<shc::ClipTensor*>(malloc((size_t)(count + 1) * sizeof(shc::ClipTensor)));
+  if (t == nullptr) return refuse(fail(SHC_ERR_CAPACITY, "out of host memory"));
+  for (int64_t i = 0; i < count; ++i)
+    t[i] = {grads[i].data, outs ? grads[i].out : nullptr, grads[i].numel,
+            grads[i].dtype == SHC_BF16};
+  return t;
+}
+
+// No output overlaps another region, but for its own data as a whole.
+int check_outs(const shc::ClipTensor* t, int64_t count) {
+  struct Region {
+    uintptr_t first, end;
+    int64_t tensor;
+    bool out;
+  };
+  auto* r = static_cast<Region*>(malloc((size_t)(2 * count + 1) * sizeof(Region)));
+  if (r == nullptr) return fail(SHC_ERR_CAPACITY, "out of host memory");
+  int64_t n = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    if (t[i].numel == 0) continue;
+    const uintptr_t bytes = (uintptr_t)t[i].numel * (t[i].bf16 ? 2 : 4);
+    const uintptr_t d = reinterpret_cast<uintptr_t>(t[i].data);
+    const uintptr_t o = reinterpret_cast<uintptr_t>(t[i].out);
+    if (o != d) r[n++] = {d, d + bytes, i, false};
+    r[n++] = {o, o + bytes, i, true};
+  }
+  std::sort(r, r + n, [](const Region& a, const Region& b) { return a.first < b.first; });
+  // the farthest ends so far, of outputs and of all regions
+  uintptr_t out_end = 0, any_end = 0;
+  int64_t bad = -1;
+  for (int64_t i = 0; i < n && bad < 0; ++i) {
+    if (r[i].first < out_end || (r[i].out && r[i].first < any_end)) bad = r[i].tensor;
+    if (r[i].out) out_end = std::max(out_end, r[i].end);
+    any_end = std::max(any_end, r[i].end);
+  }
+  free(r);
+  if (bad >= 0)
+    return fail(SHC_ERR_INVALID_ARG, "grads[%lld]: an output overlaps another tensor",
+                (long long)bad);
+  return SHC_OK;
+}
+
+}  // namespace
+
+size_t shc_linear_workspace(int64_t n_rows, int32_t Cin, int32_t Cout, int32_t dtype,
+                            int32_t aligned) {
+  if (!dense_sizes(n_rows, Cin, kMaxDenseChannels, Cout, kMaxDenseChannels, dtype)) return 0;
+  return shc::linear_workspace_bytes(n_rows, Cin, Cout, dtype == SHC_BF16, aligned == 1);
+}
+
+int shc_linear(const void* x, int64_t x_stride, int64_t n_rows, int32_t Cin, const void* W,
+               int64_t W_stride, int32_t Cout, const float* bias, int32_t act,
+               const void* residual, int64_t residual_stride, int32_t dtype, void* pre,
+               int64_t pre_stride, void* out, int64_t out_stride, void* ws, size_t ws_bytes,
+               hipStream_t stream) {
+  g_last_error[0] = 0;
+  SHC_TRY(check_linear_sizes(n_rows, Cin, Cout, dtype, act));
+  shc::LinearArgs a{};
+  a.x = x, a.ldx = x_stride, a.n = n_rows, a.Cin = Cin, a.Cout = Cout;
+  a.W = W, a.ldw = W_stride, a.bias = bias, a.act = act, a.bf16 = dtype == SHC_BF16;
+  a.res = residual, a.ldres = residual_stride, a.pre = pre, a.ldpre = pre_stride;
+  a.out = out, a.ldout = out_stride, a.ws = ws;
+  SHC_TRY(check_linear(a, dtype, false));
+  const size_t e = elem_size(dtype);
+  SHC_TRY(check_array("bias", bias, true));
+  SHC_TRY(check_row_tensor("residual", residual, n_rows, Cout, residual_stride, e, true));
+  SHC_TRY(check_row_tensor("out", out, n_rows, Cout, out_stride, e, false));
+  if (n_rows == 0) return SHC_OK;
+  if (residual != nullptr && residual == out && residual_stride != out_stride)
+    return fail(SHC_ERR_INVALID_ARG, "residual is out with another stride");
+  SHC_TRY(check_ws(ws, ws_bytes, shc::linear_workspace_bytes(n_rows, Cin, Cout, a.bf16,
+                                                             shc::linear_aligned(a, false))));
+  return hip_status(shc::launch_linear(a, stream), "linear launch");
+}
+
+size_t shc_linear_backward_workspace(int64_t n_rows, int32_t Cin, int32_t Cout, int32_t dtype,
+                                     int32_t act, int32_t aligned) {
+  if (!dense_sizes(n_rows, Cin, kMaxDenseChannels, Cout, kMaxDenseChannels, dtype) ||
+      act < SHC_ACT_NONE || act > SHC_ACT_SILU)
+    return 0;
+  return shc::linear_backward_workspace_bytes(n_rows, Cin, Cout, dtype == SHC_BF16, aligned == 1,
+                                              act);
+}
+
+int shc_linear_backward(const void* dout, int64_t dout_stride, const void* x, int64_t x_stride,
+                        int64_t n_rows, int32_t Cin, const void* W, int64_t W_stride,
+                        int32_t Cout, const void* pre, int64_t pre_stride, int32_t act,
+                        int32_t dtype, int32_t accumulate, void* dx, int64_t dx_stride, void* dW,
+                        int64_t dW_stride, float* db, void* ws, size_t ws_bytes,
+                        hipStream_t stream) {
+  g_last_error[0] = 0;
+  SHC_TRY(check_linear_sizes(n_rows, Cin, Cout, dtype, act));
+  SHC_TRY(check_flag("accumulate", accumulate));
+  shc::LinearArgs a{};
+  a.x = x, a.ldx = x_stride, a.n = n_rows, a.Cin = Cin, a.Cout = Cout;
+  a.W = W, a.ldw = W_stride, a.act = act, a.bf16 = dtype == SHC_BF16;
+  a.pre = const_cast<void*>(pre), a.ldpre = pre_stride;
+  a.dout = dout, a.lddout = dout_stride, a.dx = dx, a.lddx = dx_stride;
+  a.dW = dW, a.lddW = dW_stride, a.db = db, a.accumulate = accumulate, a.ws = ws;
+  SHC_TRY(check_linear(a, dtype, true));
+  const size_t e = elem_size(dtype);
+  SHC_TRY(check_row_tensor("dout", dout, n_rows, Cout, dout_stride, e, false));
+  SHC_TRY(check_row_tensor("dx", dx, n_rows, Cin, dx_stride, e, true));
+  SHC_TRY(check_row_tensor("dW", dW, Cin, Cout, dW_stride, e, true));
+  SHC_TRY(check_array("db", db, true));
+  if (n_rows > 0)
+    SHC_TRY(check_ws(ws, ws_bytes,
+                     shc::linear_backward_workspace_bytes(n_rows, Cin, Cout, a.bf16,
+                                                          shc::linear_aligned(a, true), act)));
+  return hip_status(shc::launch_linear_backward(a, stream), "linear_backward launch");
+}
+
+size_t shc_linear_cross_entropy_workspace(int64_t n_rows, int32_t C, int32_t V, int32_t dtype,
+                                          int32_t pass, int32_t aligned) {
+  if (!dense_sizes(n_rows, C, kMaxDenseChannels, V, kMaxLogits, dtype) ||
+      pass < SHC_XENT_FORWARD || pass > SHC_XENT_STEP)
+    return 0;
+  return shc::xent_workspace_bytes(n_rows, C, V, dtype == SHC_BF16, aligned == 1,
+                                   static_cast<shc::XentPass>(pass));
+}
+
+static shc::XentArgs xent_args(const void* x, int64_t x_stride, int64_t n_rows, int32_t C,
+                               const void* W, int64_t W_stride, int32_t V, const float* bias,
+                               const void* labels, int32_t id_type, int64_t label_stride,
+                               int32_t dtype, void* ws) {
+  shc::XentArgs a{};
+  a.x = x, a.ldx = x_stride, a.n = n_rows, a.C = C, a.V = V, a.W = W, a.ldw = W_stride;
+  a.bias = bias, a.labels = labels, a.id64 = id_type == SHC_IDS_I64;
+  a.label_stride = label_stride, a.bf16 = dtype == SHC_BF16, a.ws = ws;
+  return a;
+}
+
+int shc_linear_cross_entropy(const void* x, int64_t x_stride, int64_t n_rows, int32_t C,
+                             const void* W, int64_t W_stride, int32_t V, const float* bias,
+                             const void* labels, int32_t id_type, int64_t label_stride,
+                             int32_t dtype, float* loss, float* lse, void* ws, size_t ws_bytes,
+                             hipStream_t stream) {
+  g_last_error[0] = 0;
+  shc::XentArgs a = xent_args(x, x_stride, n_rows, C, W, W_stride, V, bias, labels, id_type,
+                              label_stride, dtype, ws);
+  a.loss = loss, a.lse = lse;
+  SHC_TRY(check_xent(a, dtype, id_type));
+  SHC_TRY(check_array("loss", loss, n_rows == 0));
+  SHC_TRY(check_array("lse", lse, true));
+  return run_xent(a, shc::XentPass::kForward, ws_bytes, stream, "linear_cross_entropy launch");
+}
+
+int shc_linear_cross_entropy_backward(const void* x, int64_t x_stride, int64_t n_rows, int32_t C,
+                                      const void* W, int64_t W_stride, int32_t V,
+                                      const float* bias, const void* labels, int32_t id_type,
+                                      int64_t label_stride, const float* lse,
+                                      const float* row_weight, int32_t dtype, int32_t accumulate,
+                                      void* dx, int64_t dx_stride, void* dW, int64_t dW_stride,
+                                      float* db, void* ws, size_t ws_bytes, hipStream_t stream) {
+  g_last_error[0] = 0;
+  shc::XentArgs a = xent_args(x, x_stride, n_rows, C, W, W_stride, V, bias, labels, id_type,
+                              label_stride, dtype, ws);
+  a.lse = const_cast<float*>(lse), a.weight = row_weight, a.accumulate = accumulate;
+  a.dx = dx, a.lddx = dx_stride, a.dW = dW, a.lddW = dW_stride, a.db = db;
+  SHC_TRY(check_xent(a, dtype, id_type));
+  SHC_TRY(check_array("lse", lse, n_rows == 0));
+  SHC_TRY(check_xent_grads(a, dtype, accumulate));
+  return run_xent(a, shc::XentPass::kBackward, ws_bytes, stream,
+                  "linear_cross_entropy_backward launch");
+}
+
+int shc_linear_cross_entropy_step(const void* x, int64_t x_stride, int64_t n_rows, int32_t C,
+                                  const void* W, int64_t W_stride, int32_t V, const float* bias,
+                                  const void* labels, int32_t id_type, int64_t label_stride,
+                                  const float* row_weight, int32_t dtype, int32_t accumulate,
+                                  float* loss, void* dx, int64_t dx_stride, void* dW,
+                                  int64_t dW_stride, float* db, void* ws, size_t ws_bytes,
+                                  hipStream_t stream) {
+  g_last_error[0] = 0;
+  shc::XentArgs a = xent_args(x, x_stride, n_rows, C, W, W_stride, V, bias, labels, id_type,
+                              label_stride, dtype, ws);
+  a.loss = loss, a.weight = row_weight, a.accumulate = accumulate;
+  a.dx = dx, a.lddx = dx_stride, a.dW = dW, a.lddW = dW_stride, a.db = db;
+  SHC_TRY(check_xent(a, dtype, id_type));
+  SHC_TRY(check_array("loss", loss, n_rows == 0));
+  SHC_TRY(check_xent_grads(a, dtype, accumulate));
+  return run_xent(a, shc::XentPass::kStep, ws_bytes, stream, "linear_cross_entropy_step launch");
+}
+
+size_t shc_grad_norm_workspace(const shc_grad* grads, int64_t count) {
+  int rc;
+  shc::ClipTensor* t = clip_list(grads, count, false, &rc);
+  if (t == nullptr) return 0;
+  const size_t bytes = shc::grad_norm_workspace_bytes(t, count);
+  free(t);
+  return bytes;
+}
+
+int shc_grad_norm(const shc_grad* grads, int64_t count, float* norm, void* ws, size_t ws_bytes,
+                  hipStream_t stream) {
+  g_last_error[0] = 0;
+  SHC_TRY(check_array("norm", norm, false));
+  int rc;
+  shc::ClipTensor* t = clip_list(grads, count, false, &rc);
+  if (t == nullptr) return rc;
+  rc = check_ws(ws, ws_bytes, shc::grad_norm_workspace_bytes(t, count));
+  if (rc == SHC_OK)
+    rc = hip_status(shc::launch_grad_norm(t, count, norm, ws, stream), "grad_norm launch");
+  free(t);
+  return rc;
+}
+
+int shc_clip_grads(const shc_grad* grads, int64_t count, const float* norm, float max_norm,
+                   hipStream_t stream) {
+  g_last_error[0] = 0;
+  SHC_TRY(check_array("norm", norm, false));
+  if (!(max_norm >= 0.0f))
+    return fail(SHC_ERR_INVALID_ARG, "max_norm = %g must not be negative", (double)max_norm);
+  int rc;
+  shc::ClipTensor* t = clip_list(grads, count, true, &rc);
+  if (t == nullptr) return rc;
+  rc = check_outs(t, count);
+  if (rc == SHC_OK)
+    rc = hip_status(shc::launch_clip_grads(t, count, norm, max_norm, stream),
+                    "clip_grads launch");
+  free(t);
+  return rc;
 }
 
 // -- stream-ordering events ---------------------------------------------------

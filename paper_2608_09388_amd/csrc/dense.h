@@ -1,0 +1,117 @@
+// Host interface of the matrix products (dense.hip) behind the dense linear layer
+// (linear.hip) and the cross entropy of a linear layer (xent.hip).
+#pragma once
+
+#include "dense_tile.h"
+
+namespace shc {
+namespace dense {
+
+// Activations: the layer's SHC_ACT_* codes.
+constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3;
+
+// What becomes of a product's element v at (row, col), in this order:
+//   v += add32[row][col];  out32[row][col] = v, and nothing else, where out32 is set
+//   v += bias[col];  pre[row][col] = v;  v = act(v);
+//   v += res[to[row]][col];  out[to[row]][col] = v
+// res, pre and out are bf16, or fp32 of a split product; res may be out itself.
+struct Store {
+  const float* add32;
+  float* out32;  // both [M][N], N apart
+  const float* bias;
+  int act;
+  const void* res;
+  int64_t ld_res;
+  void* pre;
+  int64_t ld_pre;
+  void* out;
+  int64_t ld_out;
+  const int32_t* to;  // NULL: row
+};
+
+struct Product {
+  Operand A, B;
+  bool a_rows, b_rows;  // the order of each operand (see dense_tile.h)
+  bool split;           // fp32 as three bf16 terms
+  int64_t M, N, K;
+  // the device count of live rows, from row0 on, bounds M (rows of D) or K; NULL: all
+  const int32_t* count;
+  int64_t row0;
+  bool count_is_k;
+  int64_t full;  // the count at which an operand's `alt` is not needed
+  Store store;
+  float* partials;  // where K is cut into parts: their sums
+  size_t partial_bytes;
+};
+
+// Bytes of partial sums with which a product of up to M x N x K may be cut along K;
+// grows with each of the sizes.
+size_t partial_bytes(int64_t M, int64_t N, int64_t K);
+hipError_t launch_product(const Product& p, hipStream_t stream);
+
+// Whether rows of C elements, ld apart, can be read as they are (bf16).
+inline bool direct(const void* p, int64_t ld, int64_t C) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && C % 8 == 0 &&
+         ld < ((int64_t)1 << 21);
+}
+// Rows of a packed copy are a multiple of this many elements long, zeros at the end.
+inline int64_t packed_width(int64_t C) { return C <= 64 ? (C + 7) / 8 * 8 : (C + 63) / 64 * 64; }
+inline size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+inline size_t packed_bytes(int64_t rows, int64_t C, bool split) {
+  return align256((size_t)rows * packed_width(C) * 2 * (split ? 3 : 1));
+}
+
+// Packs n rows of C elements into rows of packed_width(C) bf16: copies of bf16, or
+// the three terms of fp32, `rows` * packed_width(C) elements from term to term.
+// Packed row r is row idx[r] (NULL: r) for r below *count - row0 (NULL: n); with
+// `unless_full`, nothing is written where *count is that number.
+struct Pack {
+  const void* src;
+  int64_t ld;
+  int64_t n, rows;
+  int32_t C;
+  int split;
+  const int32_t* idx;
+  const int32_t* count;
+  int64_t row0;
+  int64_t unless_full;  // -1: none
+  uint16_t* dst;
+};
+hipError_t launch_pack(const Pack& p, hipStream_t stream);
+
+// out[c] (+)= sum over `rows` partial rows of C, `ld` apart, in ascending order.
+hipError_t launch_sum_rows(const float* parts, int64_t rows, int64_t ld, int32_t C, int accumulate,
+                           float* out, hipStream_t stream);
+
+// Shape of the workgroups' tiles and parts along K for a product.
+enum class TileKind { k256, k128, k64, k16 };
+struct Plan {
+  TileKind kind;
+  int parts;
+};
+// few_rows: tiles of fewer than 128 rows too (operand A in rows).
+Plan plan_product(int64_t M, int64_t N, int64_t K, int pairs, bool few_rows,
+                  size_t partial_bytes);
+
+using Shape256 = Shape<8, 1, 2, 4>;
+using Shape128 = Shape<4, 1, 2, 2>;
+using Shape64 = Shape<4, 1, 1, 4>;
+using Shape16 = Shape<1, 1, 1, 4>;
+inline int tile_m(TileKind k) {
+  return k == TileKind::k256 ? 256 : k == TileKind::k128 ? 128 : k == TileKind::k64 ? 64 : 16;
+}
+inline int tile_n(TileKind k) { return k == TileKind::k128 ? 128 : 256; }
+
+// Calls f(shape) for the kind.
+template <typename F>
+hipError_t with_tile(TileKind kind, F&& f) {
+  switch (kind) {
+    case TileKind::k256: return f(Shape256{});
+    case TileKind::k128: return f(Shape128{});
+    case TileKind::k64: return f(Shape64{});
+    default: return f(Shape16{});
+  }
+}
+
+}  // namespace dense
+}  // namespace shc

@@ -1,0 +1,274 @@
+// Matrix products of the dense layers: D = A B^T over the tile of dense_tile.h, with
+// bias, activation, residual, row scatter and rounding in the epilogue; and the packing
+// of operands that the tile cannot read as they are.
+//
+// Which tile, and how many parts K is cut into, follows from the sizes by a model of
+// the time, `plan_product`: rounds of workgroups over the CUs times the steps of one,
+// plus what parts cost (their fp32 sums written and read back, a second launch).
+#include <algorithm>
+#include <mutex>
+
+#include "dense.h"
+#include "dense_epilogue.h"
+
+namespace shc {
+namespace dense {
+namespace {
+
+struct Args {
+  Operand A, B;
+  int64_t M, N, K;
+  const int32_t* count;
+  int64_t row0, full;
+  int count_is_k;
+  Store store;
+  float* partials;
+  int parts, tm, tn;
+};
+
+template <class S, bool AROWS, bool BROWS, int PAIRS>
+__global__ __launch_bounds__(S::THREADS) void product_kernel(Args a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  int tm, tn;
+  tile_of(blockIdx.x, a.tm, a.tn, &tm, &tn);
+  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+  int64_t M = a.M, K = a.K;
+  if (a.count != nullptr) {
+    const int64_t left = rows_left(a.count, a.row0, a.count_is_k ? a.K : a.M);
+    if (a.count_is_k) {
+      K = a.A.k = a.B.k = left;
+    } else {
+      M = a.A.extent = left;
+      if (m0 >= M) return;
+    }
+    if (*a.count != a.full) {
+      if (a.A.alt != nullptr) a.A.p = a.A.alt, a.A.ld = a.A.alt_ld;
+      if (a.B.alt != nullptr) a.B.p = a.B.alt, a.B.ld = a.B.alt_ld;
+    }
+  }
+  const int KT = (int)((K + BK - 1) / BK), per = (KT + a.parts - 1) / a.parts;
+  const int t0 = min(KT, (int)blockIdx.y * per), t1 = min(KT, t0 + per);
+  Tile<S, AROWS, BROWS, PAIRS> tile;
+  tile.run(a.A, a.B, M, a.N, K, m0, n0, t0, t1, smem);
+  if (a.parts > 1) {
+    float* to = a.partials + (int64_t)blockIdx.y * a.M * a.N;
+    tile.each(m0, n0, [&](int64_t row, int64_t col, const float* v) {
+      if (row >= M) return;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (col + 8 * h < a.N)
+          rowops::store_channels<8>(to + row * a.N, (int)(col / 8) + h, (int)a.N, v + 8 * h);
+    });
+    return;
+  }
+  tile.each(m0, n0, [&](int64_t row, int64_t col, const float* v) {
+    if (row >= M) return;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (col + 8 * h < a.N) store8<PAIRS == 1>(a.store, row, (int)(col / 8) + h, (int)a.N,
+                                                v + 8 * h);
+  });
+}
+
+// Sums the parts in order and stores: a thread to 8 columns of a row.
+template <bool BF16>
+__global__ __launch_bounds__(256) void join_kernel(const float* parts, int n, int64_t M, int N,
+                                                   const int32_t* count, int64_t row0, Store st) {
+  const int nv = (N + 7) / 8;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = at / nv;
+  if (row >= rows_left(count, row0, M)) return;
+  const int v = (int)(at - row * nv);
+  float sum[8], f[8];
+  const float* from = parts + row * N;
+  rowops::load_channels<8>(from, v, N, sum);
+  for (int p = 1; p < n; ++p) {
+    rowops::load_channels<8>(from + p * M * N, v, N, f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += f[e];
+  }
+  store8<BF16>(st, row, v, N, sum);
+}
+
+// 8 elements of a packed row to a thread.
+template <typename T, bool SPLIT>
+__global__ __launch_bounds__(256) void pack_kernel(Pack p, int width) {
+  using namespace rowops;
+  if (p.unless_full >= 0 && *p.count == p.unless_full) return;
+  const int nv = width / 8;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = at / nv;
+  if (row >= rows_left(p.count, p.row0, p.n)) return;
+  const int v = (int)(at - row * nv);
+  const T* from = static_cast<const T*>(p.src) +
+                  (p.idx != nullptr ? (int64_t)p.idx[row] : row) * p.ld;
+  uint16_t* to = p.dst + row * width + 8 * v;
+  if constexpr (!SPLIT) {
+    i32x4 x = {0, 0, 0, 0};
+    if (8 * v < p.C) x = load_vec<T>(from, v, p.C);
+    *reinterpret_cast<i32x4*>(to) = x;
+  } else {
+    float x[8], t[8], r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+    if (8 * v < p.C) load_channels<8>(from, v, p.C, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= kSplitScale;
+    // each term is the nearest bf16 to what is left: 8 + 8 + 8 significand bits
+    for (int term = 0; term < 3; ++term) {
+      const i32x4 h = Row<uint16_t>::narrow(x);
+      Row<uint16_t>::widen(h, t);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e] = x[e] - t[e], x[e] = r[e];
+      *reinterpret_cast<i32x4*>(to + term * p.rows * width) = h;
+    }
+  }
+}
+
+__global__ __launch_bounds__(1024) void sum_rows_kernel(const float* parts, int64_t rows,
+                                                        int64_t ld, int C, int accumulate,
+                                                        float* out) {
+  __shared__ float part[16][64];
+  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+  const int c = blockIdx.x * 64 + x;
+  const int64_t per = (rows + 15) / 16, r0 = y * per, r1 = r0 + per < rows ? r0 + per : rows;
+  float s = 0.f;
+  if (c < C)
+    for (int64_t r = r0; r < r1; ++r) s += parts[r * ld + c];
+  part[y][x] = s;
+  __syncthreads();
+  if (y != 0 || c >= C) return;
+  for (int q = 1; q < 16; ++q) s += part[q][x];
+  out[c] = accumulate ? out[c] + s : s;
+}
+
+constexpr int64_t kMostPartial = (int64_t)64 << 20;
+
+template <class S, bool AROWS, bool BROWS, int PAIRS>
+hipError_t run(const Args& a, hipStream_t stream) {
+  auto kern = product_kernel<S, AROWS, BROWS, PAIRS>;
+  static std::once_flag once;
+  static hipError_t attr = hipSuccess;
+  std::call_once(once, [&] {
+    attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+  });
+  if (attr != hipSuccess) return attr;
+  kern<<<dim3(a.tm * a.tn, a.parts), S::THREADS, S::LDS, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <class S, int PAIRS>
+hipError_t run_orders(const Args& a, bool ar, bool br, hipStream_t stream) {
+  if constexpr (S::BM >= 128)
+    if (!ar && !br) return run<S, false, false, PAIRS>(a, stream);
+  if (ar && br) return run<S, true, true, PAIRS>(a, stream);
+  if (ar && !br) return run<S, true, false, PAIRS>(a, stream);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+size_t partial_bytes(int64_t M, int64_t N, int64_t K) {
+  // at most a part to two steps of K, and at most kMostPartial
+  const int64_t parts = K / (2 * BK);
+  if (parts <= 1) return 0;
+  const int64_t mn = M * N * 4;
+  return (size_t)(mn > kMostPartial / parts ? kMostPartial : mn * parts);
+}
+
+// Times in us.  A step is 64 of K in one workgroup's tile; workgroups of 256 x 256
+// have a CU to themselves, the others share it with one more.
+Plan plan_product(int64_t M, int64_t N, int64_t K, int pairs, bool few_rows,
+                  size_t partial_bytes) {
+  struct Kind {
+    TileKind kind;
+    int slots;
+    double step;
+  };
+  static constexpr Kind kinds[] = {{TileKind::k256, 256, 1.9},
+                                   {TileKind::k128, 512, 1.2},
+                                   {TileKind::k64, 512, 1.4},
+                                   {TileKind::k16, 512, 1.2}};
+  const int64_t KT = (K + BK - 1) / BK;
+  Plan best{TileKind::k128, 1};
+  double least = 1e300;
+  for (const Kind& k : kinds) {
+    if (!few_rows && tile_m(k.kind) < 128) continue;
+    const int64_t tiles = ((M + tile_m(k.kind) - 1) / tile_m(k.kind)) *
+                          ((N + tile_n(k.kind) - 1) / tile_n(k.kind));
+    for (int parts = 1; parts <= 64; parts = parts < 4 ? parts + 1 : parts + parts / 2) {
+      if (parts > 1 && (KT < 2 * parts || (double)parts * M * N * 4 > (double)partial_bytes)) break;
+      const double rounds = (double)((tiles * parts + k.slots - 1) / k.slots);
+      const double steps = (double)((KT + parts - 1) / parts) * pairs;
+      double t = rounds * (steps * k.step + 2.0);
+      if (parts > 1) t += 4.0 + (double)parts * M * N * 8 / 4e6;
+      if (t < least) least = t, best = {k.kind, parts};
+    }
+  }
+  return best;
+}
+
+hipError_t launch_product(const Product& p, hipStream_t stream) {
+  if (p.M <= 0 || p.N <= 0) return hipSuccess;
+  Plan plan = plan_product(p.M, p.N, p.K, p.split ? kPairs : 1, p.a_rows,
+                           p.partials != nullptr ? p.partial_bytes : 0);
+  Args a;
+  a.A = p.A, a.B = p.B;
+  a.M = p.M, a.N = p.N, a.K = p.K;
+  a.count = p.count, a.row0 = p.row0, a.full = p.full, a.count_is_k = p.count_is_k;
+  a.store = p.store;
+  a.partials = p.partials;
+  a.parts = plan.parts;
+  const int64_t tm = (p.M + tile_m(plan.kind) - 1) / tile_m(plan.kind);
+  const int64_t tn = (p.N + tile_n(plan.kind) - 1) / tile_n(plan.kind);
+  if (tm * tn >= (int64_t)1 << 22) return hipErrorInvalidConfiguration;
+  a.tm = (int)tm, a.tn = (int)tn;
+  hipError_t e = with_tile(plan.kind, [&](auto shape) {
+    using S = decltype(shape);
+    return p.split ? run_orders<S, kPairs>(a, p.a_rows, p.b_rows, stream)
+                   : run_orders<S, 1>(a, p.a_rows, p.b_rows, stream);
+  });
+  if (e != hipSuccess || plan.parts == 1) return e;
+  const int64_t threads = p.M * ((p.N + 7) / 8);
+  const int blocks = (int)((threads + 255) / 256);
+  const int32_t* rows = p.count_is_k ? nullptr : p.count;
+  if (p.split)
+    join_kernel<false><<<blocks, 256, 0, stream>>>(p.partials, plan.parts, p.M, (int)p.N, rows,
+                                                   p.row0, p.store);
+  else
+    join_kernel<true><<<blocks, 256, 0, stream>>>(p.partials, plan.parts, p.M, (int)p.N, rows,
+                                                  p.row0, p.store);
+  return hipGetLastError();
+}
+
+hipError_t launch_pack(const Pack& p, hipStream_t stream) {
+  const int width = (int)packed_width(p.C);
+  const int64_t blocks = (p.n * (width / 8) + 255) / 256;
+  if (blocks == 0) return hipSuccess;
+  if (blocks >= (int64_t)1 << 24) {  // a launch has fewer than 2^32 threads
+    Pack a = p, b = p;
+    a.n = p.n / 2, b.n = p.n - a.n, b.row0 += a.n;
+    if (p.idx != nullptr)
+      b.idx += a.n;
+    else
+      b.src = static_cast<const char*>(p.src) + a.n * p.ld * (p.split ? 4 : 2);
+    b.dst += a.n * width;
+    const hipError_t e = launch_pack(a, stream);
+    return e != hipSuccess ? e : launch_pack(b, stream);
+  }
+  if (p.split)
+    pack_kernel<float, true><<<(int)blocks, 256, 0, stream>>>(p, width);
+  else
+    pack_kernel<uint16_t, false><<<(int)blocks, 256, 0, stream>>>(p, width);
+  return hipGetLastError();
+}
+
+hipError_t launch_sum_rows(const float* parts, int64_t rows, int64_t ld, int32_t C, int accumulate,
+                           float* out, hipStream_t stream) {
+  sum_rows_kernel<<<(C + 63) / 64, 1024, 0, stream>>>(parts, rows, ld, C, accumulate, out);
+  return hipGetLastError();
+}
+
+}  // namespace dense
+}  // namespace shc

@@ -340,4 +340,82 @@ size_t distill_workspace_bytes(int64_t n, int32_t V);
 hipError_t launch_distill(const DistillArgs& a, DistillPass pass, int is_bf16,
                           hipStream_t stream);
 
+// dense linear layer with bias, activation and residual, and its gradients
+// (linear.hip); strides in elements
+struct LinearArgs {
+  const void* x;
+  int64_t ldx, n;
+  int32_t Cin, Cout;
+  const void* W;  // [Cin] rows of Cout
+  int64_t ldw;
+  const float* bias;
+  int act;
+  bool bf16;
+  const void* res;
+  int64_t ldres;
+  void* pre;  // forward: out; backward: in
+  int64_t ldpre;
+  void* out;
+  int64_t ldout;
+  // backward
+  const void* dout;
+  int64_t lddout;
+  void* dx;
+  int64_t lddx;
+  void* dW;
+  int64_t lddW;
+  float* db;
+  int accumulate;
+  void* ws;
+};
+// whether the tensors that the products read start and step by 16 bytes
+bool linear_aligned(const LinearArgs& a, bool backward);
+size_t linear_workspace_bytes(int64_t n, int32_t Cin, int32_t Cout, bool bf16, bool aligned);
+size_t linear_backward_workspace_bytes(int64_t n, int32_t Cin, int32_t Cout, bool bf16,
+                                       bool aligned, int act);
+hipError_t launch_linear(const LinearArgs& a, hipStream_t stream);
+hipError_t launch_linear_backward(const LinearArgs& a, hipStream_t stream);
+
+// cross entropy of a linear layer's logits, and its gradients (xent.hip)
+struct XentArgs {
+  const void* x;
+  int64_t ldx, n;
+  int32_t C, V;
+  const void* W;  // [V] rows of C
+  int64_t ldw;
+  const float* bias;
+  const void* labels;
+  int id64;
+  int64_t label_stride;
+  bool bf16;
+  float* loss;
+  float* lse;  // forward: out; backward: in
+  const float* weight;
+  void* dx;
+  int64_t lddx;
+  void* dW;
+  int64_t lddW;
+  float* db;
+  int accumulate;
+  void* ws;
+};
+enum class XentPass { kForward, kBackward, kStep };
+bool xent_aligned(const XentArgs& a);
+size_t xent_workspace_bytes(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned,
+                            XentPass pass);
+hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream);
+
+// norm of all gradients and their clipping (clip.hip)
+struct ClipTensor {
+  const void* data;
+  void* out;
+  int64_t numel;
+  bool bf16;
+};
+size_t grad_norm_workspace_bytes(const ClipTensor* t, int64_t count);
+hipError_t launch_grad_norm(const ClipTensor* t, int64_t count, float* norm, void* ws,
+                            hipStream_t stream);
+hipError_t launch_clip_grads(const ClipTensor* t, int64_t count, const float* norm,
+                             float max_norm, hipStream_t stream);
+
 }  // namespace shc

@@ -1,0 +1,570 @@
+// Cross entropy of a linear layer's logits, without keeping them, and its gradients.
+// For a row x_i with label y_i in [0, V) and the table W [V][C]:
+//
+//   z_v = x_i . W_v + b_v,  lse_i = log sum exp z_v,  loss_i = lse_i - z_{y_i}
+//   dz_v = w_i (exp(z_v - lse_i) - [v = y_i])
+//   dx_i = sum over v of dz_v W_v,  dW_v = sum over i of dz_v x_i,  db_v = sum of dz_v
+//
+// Rows whose label is outside of [0, V) are padding.  A first pass over the labels
+// lists the others; where any is left out, the rows of x that count are packed, so
+// that padding costs no products and whatever it holds reaches no sum.  How many they
+// are stays on the device: workgroups past them end at once.
+//
+// Forward: one product over all of V whose epilogue takes every row's maximum and sum
+// of exponentials over the tile's columns and the label's logit; a second launch joins
+// the tiles.  Nothing of size rows x V is written.
+//
+// Backward: for a piece of rows at a time, the logits again, turned in the epilogue
+// into dz [rows][V] (bf16, rounded once from fp32, or fp32), and the products dz W and
+// dz^T x over it; db from the unrounded dz, summed per tile.  A piece is at most 2^30
+// (bf16) or 2^28 (fp32) elements of dz, so most calls have one; with more, dW is summed
+// over them in fp32.
+#include <algorithm>
+#include <mutex>
+
+#include "dense.h"
+#include "dense_epilogue.h"
+
+namespace shc {
+
+using namespace dense;
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int kLabelsPerBlock = 4096;  // 256 threads, 16 each
+
+__device__ __forceinline__ int64_t label_at(const void* labels, int id64, int64_t stride,
+                                            int64_t i) {
+  return id64 ? static_cast<const int64_t*>(labels)[i * stride]
+              : (int64_t)static_cast<const int32_t*>(labels)[i * stride];
+}
+
+struct Labels {
+  const void* p;
+  int id64;
+  int64_t stride;
+  int32_t V;
+  __device__ __forceinline__ int64_t get(int64_t i) const { return label_at(p, id64, stride, i); }
+  __device__ __forceinline__ bool live(int64_t i) const {
+    const int64_t y = get(i);
+    return y >= 0 && y < V;
+  }
+};
+
+// Live rows of every block of labels.
+__global__ __launch_bounds__(256) void count_labels_kernel(Labels l, int64_t n, int32_t* counts) {
+  __shared__ int total;
+  if (threadIdx.x == 0) total = 0;
+  __syncthreads();
+  int c = 0;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    const int64_t i = (int64_t)blockIdx.x * kLabelsPerBlock + q * 256 + threadIdx.x;
+    c += __popcll(__ballot(i < n && l.live(i)));
+  }
+  if ((threadIdx.x & 63) == 0) atomicAdd(&total, c);  // whole numbers: any order
+  __syncthreads();
+  if (threadIdx.x == 0) counts[blockIdx.x] = total;
+}
+
+// The live rows in ascending order, their number, and the results of the others.
+__global__ __launch_bounds__(256) void list_rows_kernel(Labels l, int64_t n, const int32_t* counts,
+                                                        int32_t* idx, int32_t* count, float* loss,
+                                                        float* lse) {
+  __shared__ int wave[4], before[4];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int c = 0;
+  for (int b = threadIdx.x; b < (int)blockIdx.x; b += 256) c += counts[b];
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) c += __shfl_xor(c, d, 64);
+  if (lane == 0) before[w] = c;
+  __syncthreads();
+  int base = before[0] + before[1] + before[2] + before[3];
+  for (int q = 0; q < 16; ++q) {
+    const int64_t i = (int64_t)blockIdx.x * kLabelsPerBlock + q * 256 + threadIdx.x;
+    const bool live = i < n && l.live(i);
+    const uint64_t mask = __ballot(live);
+    __syncthreads();
+    if (lane == 0) wave[w] = __popcll(mask);
+    __syncthreads();
+    int at = base + __popcll(mask & ((1ull << lane) - 1));
+    for (int p = 0; p < w; ++p) at += wave[p];
+    if (live) {
+      idx[at] = (int32_t)i;
+    } else if (i < n) {
+      if (loss != nullptr) loss[i] = 0.f;
+      if (lse != nullptr) lse[i] = 0.f;
+    }
+    base += wave[0] + wave[1] + wave[2] + wave[3];
+  }
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *count = base;
+}
+
+struct Logits {
+  Operand A, B;       // rows of x from row0 on, the table
+  int64_t rows, C;    // rows of the piece, channels
+  const int32_t* count;
+  int64_t row0, full;
+  const float* bias;
+  Labels labels;
+  const int32_t* idx;  // of the piece
+  int tm, tn;
+  // statistics
+  float2* parts;  // [tn][rows]: maximum and sum over a tile's columns
+  float* at_label;
+  // gradient
+  const float* lse;
+  const float* weight;
+  void* dz;
+  int64_t ld_dz;
+  int width;
+  float* sums;  // [tm * WM][V] or NULL
+};
+
+// The logits of a tile: M rows are live.  False where none is.
+template <class S, int PAIRS>
+__device__ __forceinline__ bool logits_tile(Logits& a, Tile<S, true, true, PAIRS>& tile,
+                                            int64_t* m0, int64_t* n0, int64_t* M, int* tn,
+                                            char* smem) {
+  int tm;
+  tile_of(blockIdx.x, a.tm, a.tn, &tm, tn);
+  *m0 = (int64_t)tm * S::BM, *n0 = (int64_t)*tn * S::BN;
+  *M = a.A.extent = rows_left(a.count, a.row0, a.rows);
+  if (*m0 >= *M) return false;
+  if (a.A.alt != nullptr && *a.count != a.full) a.A.p = a.A.alt, a.A.ld = a.A.alt_ld;
+  tile.run(a.A, a.B, *M, a.labels.V, a.C, *m0, *n0, 0, (int)((a.C + BK - 1) / BK), smem);
+  return true;
+}
+
+// Over the four lanes that hold a row.
+template <typename Op>
+__device__ __forceinline__ float row_reduce(float x, Op op) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  x = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// 16 columns' logits in place: bias added, -inf past the last.
+__device__ __forceinline__ void finish_logits(float* z, const float* bias, int64_t col, int V) {
+  if (bias != nullptr) {
+    float b[16];
+    if (col + 16 <= V) {
+      rowops::load_channels<8>(bias + col, 0, 8, b);
+      rowops::load_channels<8>(bias + col, 1, 16, b + 8);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) b[e] = col + e < V ? bias[col + e] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] += b[e];
+  }
+  if (col + 16 > V) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (col + e >= V) z[e] = -__builtin_inff();
+  }
+}
+
+// (m, s) with s = sum of e^(z - m): a maximum of -inf stands for 0 in the differences, so
+// that a row of nothing but -inf has s = 0, and a NaN stays in s whatever its maximum.
+__device__ __forceinline__ float finite_or_0(float m) { return m == -__builtin_inff() ? 0.f : m; }
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+  const float m = fmaxf(a.x, b.x), f = finite_or_0(m);
+  return float2{m, a.y * __builtin_amdgcn_exp2f((a.x - f) * kLog2e) +
+                       b.y * __builtin_amdgcn_exp2f((b.x - f) * kLog2e)};
+}
+
+template <class S, int PAIRS>
+__global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  Tile<S, true, true, PAIRS> tile;
+  int64_t m0, n0, M;
+  int tn;
+  if (!logits_tile<S, PAIRS>(a, tile, &m0, &n0, &M, &tn, smem)) return;
+  // LDS is free: the last step's reads are behind the tile's last barrier
+  float2* red = reinterpret_cast<float2*>(smem);  // [WN][BM]
+  const int wn = (threadIdx.x >> 6) % S::WN;
+  const bool first = (threadIdx.x & 63) < 16;
+  tile.each(m0, n0, [&](int64_t row, int64_t col, float* z) {
+    finish_logits(z, a.bias, col, a.labels.V);
+    float m = z[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) m = fmaxf(m, z[e]);
+    m = row_reduce(m, rowops::MaxOp{});
+    const float f = finite_or_0(m);
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f((z[e] - f) * kLog2e);
+    s = row_reduce(s, rowops::AddOp{});
+    if (first) red[wn * S::BM + (int)(row - m0)] = float2{m, s};
+    if (row < M) {
+      const int64_t y = a.labels.get(a.idx[row]) - col;
+      if (y >= 0 && y < 16) {
+        float at = z[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) at = y == e ? z[e] : at;
+        a.at_label[row] = at;
+      }
+    }
+  });
+  __syncthreads();
+  for (int r = threadIdx.x; r < S::BM && m0 + r < M; r += S::THREADS) {
+    float2 t = red[r];
+#pragma unroll
+    for (int w = 1; w < S::WN; ++w) t = join(t, red[w * S::BM + r]);
+    a.parts[(int64_t)tn * a.rows + m0 + r] = t;
+  }
+}
+
+// 16 rows to a workgroup, 16 threads to a row.
+__global__ __launch_bounds__(256) void join_stats_kernel(const float2* parts, int tiles,
+                                                         int64_t rows, const int32_t* count,
+                                                         const int32_t* idx, const float* at_label,
+                                                         float* loss, float* lse) {
+  __shared__ float2 part[16][16];
+  const int r = threadIdx.x & 15, p = threadIdx.x >> 4;
+  const int64_t row = (int64_t)blockIdx.x * 16 + r;
+  const int64_t live = *count;
+  if ((int64_t)blockIdx.x * 16 >= live) return;
+  float2 t = {-__builtin_inff(), 0.f};
+  if (row < live)
+#pragma unroll 4
+    for (int q = p; q < tiles; q += 16) t = join(t, parts[(int64_t)q * rows + row]);
+  part[p][r] = t;
+  __syncthreads();
+  if (p != 0 || row >= live) return;
+  for (int q = 1; q < 16; ++q) t = join(t, part[q][r]);
+  const float l = t.x + __logf(t.y), z = at_label[row];
+  const int64_t to = idx[row];
+  if (lse != nullptr) lse[to] = l;
+  // a label on a logit of -inf, in a row of nothing but -inf too
+  if (loss != nullptr) loss[to] = z == -__builtin_inff() && l == l ? -z : l - z;
+}
+
+template <class S, int PAIRS>
+__global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  Tile<S, true, true, PAIRS> tile;
+  int64_t m0, n0, M;
+  int tn;
+  if (!logits_tile<S, PAIRS>(a, tile, &m0, &n0, &M, &tn, smem)) return;
+  float sum[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) sum[e] = 0.f;
+  tile.each(m0, n0, [&](int64_t row, int64_t col, float* z) {
+    if (row >= M) return;
+    finish_logits(z, a.bias, col, a.labels.V);
+    const int64_t i = a.idx[row];
+    const int64_t y = a.labels.get(i) - col;
+    const float lse = a.lse[i], w = a.weight != nullptr ? a.weight[i] : 1.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float q = z[e] == -__builtin_inff()
+                          ? 0.f
+                          : __builtin_amdgcn_exp2f((z[e] - lse) * kLog2e);
+      z[e] = w * (y == e ? q - 1.f : q);
+      if (col + e >= a.labels.V) z[e] = 0.f;
+      sum[e] += z[e];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (col + 8 * h < a.width)
+        put8<PAIRS == 1>(a.dz, row, a.ld_dz, (int)(col / 8) + h, a.width, z + 8 * h);
+  });
+  if (a.sums == nullptr) return;
+  // over the tile's rows: the lane's, then the 16 lanes' of the same columns
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  float mine = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const float s = rowops::lanes_reduce<16>(sum[e], rowops::AddOp{});
+    mine = (lane & 15) == e ? s : mine;
+  }
+  const int64_t col = n0 + (w % S::WN) * 64 + lane;
+  const int64_t part = m0 / S::BM * S::WM + w / S::WN;
+  if (col < a.labels.V) a.sums[part * a.labels.V + col] = mine;
+}
+
+// Column sums over the parts of the live rows, in order, added to what the pieces
+// before gave (`first` 0) or to what db holds (`accumulate`).
+__global__ __launch_bounds__(1024) void join_sums_kernel(const float* sums, int rows_per_part,
+                                                         int64_t rows, const int32_t* count,
+                                                         int64_t row0, int V, int add, float* db) {
+  __shared__ float part[16][64];
+  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + x;
+  const int64_t parts =
+      (rows_left(count, row0, rows) + rows_per_part - 1) / rows_per_part;
+  const int64_t per = (parts + 15) / 16, p0 = y * per, p1 = p0 + per < parts ? p0 + per : parts;
+  float s = 0.f;
+  if (c < V)
+    for (int64_t p = p0; p < p1; ++p) s += sums[p * V + c];
+  part[y][x] = s;
+  __syncthreads();
+  if (y != 0 || c >= V) return;
+  for (int q = 1; q < 16; ++q) s += part[q][x];
+  db[c] = add ? db[c] + s : s;
+}
+
+// The gradient of rows of padding: zeros.
+template <typename T>
+__global__ __launch_bounds__(256) void zero_rows_kernel(Labels l, int64_t n, const int32_t* count,
+                                                        T* dx, int64_t ld, int C) {
+  using namespace rowops;
+  if (*count == n) return;
+  const int lane = threadIdx.x & 63;
+  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < n;
+       i += (int64_t)gridDim.x * 4) {
+    if (l.live(i)) continue;
+    for (int v = lane; v * Row<T>::N < C; v += 64) store_vec<T>(dx + i * ld, v, C, i32x4{0, 0, 0, 0});
+  }
+}
+
+struct Layout {
+  int64_t width, rows, pieces;  // columns of dz, rows and number of the pieces
+  size_t idx, count, counts, x, W, parts, at_label, lse, dz, dz32, sums, acc, partials,
+      partial_bytes, total;
+};
+
+Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass pass) {
+  Layout w{};
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += align256(bytes);
+    return here;
+  };
+  w.width = packed_width(V);
+  const int64_t most = (int64_t)1 << (bf16 ? 30 : 28);
+  w.rows = std::min<int64_t>(n, std::max<int64_t>(256, most / w.width / 256 * 256));
+  w.pieces = n == 0 ? 0 : (n + w.rows - 1) / w.rows;
+  w.idx = take((size_t)n * 4);
+  w.count = take(4);
+  w.counts = take((size_t)((n + kLabelsPerBlock - 1) / kLabelsPerBlock) * 4);
+  w.x = take(packed_bytes(n, C, !bf16));
+  w.W = take(bf16 && aligned && C % 8 == 0 ? 0 : packed_bytes(V, C, !bf16));
+  if (pass != XentPass::kBackward) {
+    w.parts = take((size_t)((V + 127) / 128) * n * 8);
+    w.at_label = take((size_t)n * 4);
+    w.lse = take(pass == XentPass::kStep ? (size_t)n * 4 : 0);
+  }
+  if (pass != XentPass::kForward) {
+    w.dz = take(packed_bytes(w.rows, V, !bf16));
+    w.dz32 = take(bf16 ? 0 : (size_t)w.rows * V * 4);
+    w.sums = take((size_t)(w.rows / 64 + 4) * V * 4);
+    w.acc = take(w.pieces > 1 ? (size_t)V * C * 4 : 0);
+    w.partial_bytes = std::max(partial_bytes(w.rows, C, V), partial_bytes(V, C, w.rows));
+    w.partials = take(w.partial_bytes);
+  }
+  w.total = at;
+  return w;
+}
+
+char* byte(void* ws, size_t at) { return static_cast<char*>(ws) + at; }
+
+#define SHC_LAUNCH(expr)                   \
+  do {                                     \
+    const hipError_t _e = (expr);          \
+    if (_e != hipSuccess) return _e;       \
+  } while (0)
+
+template <class S, int PAIRS, bool GRAD>
+hipError_t run_logits(const Logits& a, hipStream_t stream) {
+  auto kern = GRAD ? logit_grad_kernel<S, PAIRS> : logit_stats_kernel<S, PAIRS>;
+  static std::once_flag once;
+  static hipError_t attr = hipSuccess;
+  std::call_once(once, [&] {
+    attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+  });
+  if (attr != hipSuccess) return attr;
+  kern<<<a.tm * a.tn, S::THREADS, S::LDS, stream>>>(a);
+  return hipGetLastError();
+}
+
+// `kind` receives the tile that was taken.
+template <bool GRAD>
+hipError_t launch_logits(Logits a, bool bf16, TileKind* kind, hipStream_t stream) {
+  TileKind k = plan_product(a.rows, a.labels.V, a.C, bf16 ? 1 : kPairs, true, 0).kind;
+  if (k == TileKind::k16 && a.rows > 64) k = TileKind::k64;  // sums: 64 rows to a part
+  *kind = k;
+  const int64_t tm = (a.rows + tile_m(k) - 1) / tile_m(k);
+  const int64_t tn = (a.labels.V + tile_n(k) - 1) / tile_n(k);
+  if (tm * tn >= (int64_t)1 << 22) return hipErrorInvalidConfiguration;
+  a.tm = (int)tm, a.tn = (int)tn;
+  return with_tile(k, [&](auto shape) {
+    using S = decltype(shape);
+    return bf16 ? run_logits<S, 1, GRAD>(a, stream) : run_logits<S, kPairs, GRAD>(a, stream);
+  });
+}
+
+}  // namespace
+
+bool xent_aligned(const XentArgs& a) { return !a.bf16 || direct(a.W, a.ldw, 8); }
+
+size_t xent_workspace_bytes(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned,
+                            XentPass pass) {
+  return layout(n, C, V, bf16, aligned, pass).total;
+}
+
+hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
+  const Layout w = layout(a.n, a.C, a.V, a.bf16, xent_aligned(a), pass);
+  const bool grads = pass != XentPass::kForward;
+  const Labels labels{a.labels, a.id64, a.label_stride, a.V};
+  int32_t* idx = reinterpret_cast<int32_t*>(byte(a.ws, w.idx));
+  int32_t* count = reinterpret_cast<int32_t*>(byte(a.ws, w.count));
+  if (a.n == 0) {  // the parameters' gradients of no rows
+    if (grads && !a.accumulate) {
+      if (a.db != nullptr) SHC_LAUNCH(launch_sum_rows(nullptr, 0, 0, a.V, 0, a.db, stream));
+      if (a.dW != nullptr) {
+        Product p{};
+        p.split = !a.bf16;
+        p.M = a.V, p.N = a.C;
+        p.store.out = a.dW, p.store.ld_out = a.lddW;
+        SHC_LAUNCH(launch_product(p, stream));
+      }
+    }
+    return hipSuccess;
+  }
+  // 1. the live rows
+  const int blocks = (int)((a.n + kLabelsPerBlock - 1) / kLabelsPerBlock);
+  int32_t* counts = reinterpret_cast<int32_t*>(byte(a.ws, w.counts));
+  float* lse = pass == XentPass::kStep ? reinterpret_cast<float*>(byte(a.ws, w.lse)) : a.lse;
+  count_labels_kernel<<<blocks, 256, 0, stream>>>(labels, a.n, counts);
+  SHC_LAUNCH(hipGetLastError());
+  list_rows_kernel<<<blocks, 256, 0, stream>>>(labels, a.n, counts, idx, count,
+                                               pass == XentPass::kBackward ? nullptr : a.loss,
+                                               pass == XentPass::kForward ? a.lse : nullptr);
+  SHC_LAUNCH(hipGetLastError());
+  const bool as_is = a.bf16 && direct(a.x, a.ldx, a.C);
+  const int64_t xwidth = packed_width(a.C);
+  uint16_t* xs = reinterpret_cast<uint16_t*>(byte(a.ws, w.x));
+  SHC_LAUNCH(launch_pack(Pack{a.x, a.ldx, a.n, a.n, a.C, !a.bf16, idx, count, 0,
+                              as_is ? a.n : -1, xs}, stream));
+  // rows of x from row0 on, along the rows or across
+  const auto x_of = [&](int64_t row0, int64_t rows, bool along) {
+    Operand o{};
+    o.ld = as_is ? a.ldx : xwidth;
+    o.p = as_is ? static_cast<const uint16_t*>(a.x) + row0 * a.ldx : xs + row0 * xwidth;
+    if (as_is) o.alt = xs + row0 * xwidth, o.alt_ld = xwidth;
+    const int64_t width = as_is ? a.C : xwidth;
+    o.extent = along ? rows : width;
+    o.k = along ? width : rows;
+    o.plane = a.n * xwidth;
+    if (!a.bf16) o.f32 = static_cast<const float*>(a.x), o.f32_ld = a.ldx, o.idx = idx + row0;
+    return o;
+  };
+  // 2. the table
+  const bool W_as_is = a.bf16 && direct(a.W, a.ldw, a.C);
+  const int64_t Wwidth = W_as_is ? a.C : packed_width(a.C);
+  const uint16_t* Wp = static_cast<const uint16_t*>(a.W);
+  int64_t Wld = a.ldw;
+  if (!W_as_is) {
+    uint16_t* to = reinterpret_cast<uint16_t*>(byte(a.ws, w.W));
+    SHC_LAUNCH(launch_pack(Pack{a.W, a.ldw, a.V, a.V, a.C, !a.bf16, nullptr, nullptr, 0, -1, to},
+                           stream));
+    Wp = to, Wld = Wwidth;
+  }
+  const auto W_of = [&](bool along) {
+    Operand o{};
+    o.p = Wp, o.ld = Wld;
+    o.extent = along ? a.V : Wwidth;
+    o.k = along ? Wwidth : a.V;
+    o.plane = (int64_t)a.V * Wwidth;
+    if (!a.bf16) o.f32 = static_cast<const float*>(a.W), o.f32_ld = a.ldw;
+    return o;
+  };
+  Logits g{};
+  g.B = W_of(true);
+  g.C = a.C;
+  g.count = count, g.full = a.n;
+  g.bias = a.bias;
+  g.labels = labels;
+  TileKind kind;
+  if (pass != XentPass::kBackward) {  // 3. statistics, loss and lse
+    g.A = x_of(0, a.n, true);
+    g.rows = a.n, g.row0 = 0, g.idx = idx;
+    g.parts = reinterpret_cast<float2*>(byte(a.ws, w.parts));
+    g.at_label = reinterpret_cast<float*>(byte(a.ws, w.at_label));
+    SHC_LAUNCH(launch_logits<false>(g, a.bf16, &kind, stream));
+    join_stats_kernel<<<(int)((a.n + 15) / 16), 256, 0, stream>>>(
+        g.parts, (a.V + tile_n(kind) - 1) / tile_n(kind), a.n, count, idx, g.at_label, a.loss,
+        lse);
+    SHC_LAUNCH(hipGetLastError());
+  }
+  if (!grads) return hipSuccess;
+  // 4. gradients, a piece of the live rows at a time
+  g.lse = lse, g.weight = a.weight;
+  const int64_t dz_ld = a.bf16 ? w.width : a.V;
+  uint16_t* dz = reinterpret_cast<uint16_t*>(byte(a.ws, w.dz));
+  float* acc = reinterpret_cast<float*>(byte(a.ws, w.acc));
+  for (int64_t piece = 0; piece < w.pieces; ++piece) {
+    const int64_t row0 = piece * w.rows, rows = std::min(w.rows, a.n - row0);
+    g.A = x_of(row0, rows, true);
+    g.rows = rows, g.row0 = row0, g.idx = idx + row0;
+    g.dz = a.bf16 ? static_cast<void*>(dz) : byte(a.ws, w.dz32);
+    g.ld_dz = dz_ld;
+    g.width = (int)dz_ld;
+    g.sums = a.db != nullptr ? reinterpret_cast<float*>(byte(a.ws, w.sums)) : nullptr;
+    SHC_LAUNCH(launch_logits<true>(g, a.bf16, &kind, stream));
+    if (a.db != nullptr) {
+      const int per = kind == TileKind::k256 ? 128 : kind == TileKind::k16 ? 16 : 64;
+      join_sums_kernel<<<(a.V + 63) / 64, 1024, 0, stream>>>(g.sums, per, rows, count, row0, a.V,
+                                                             piece > 0 || a.accumulate, a.db);
+      SHC_LAUNCH(hipGetLastError());
+    }
+    if (a.dx == nullptr && a.dW == nullptr) continue;
+    if (!a.bf16)
+      SHC_LAUNCH(launch_pack(Pack{g.dz, dz_ld, rows, rows, a.V, 1, nullptr, count, row0, -1, dz},
+                             stream));
+    Operand d{};
+    d.p = dz, d.ld = w.width, d.plane = rows * w.width;
+    if (!a.bf16) d.f32 = static_cast<const float*>(g.dz), d.f32_ld = dz_ld;
+    Product p{};
+    p.split = !a.bf16;
+    p.count = count, p.row0 = row0, p.full = a.n;
+    p.partials = reinterpret_cast<float*>(byte(a.ws, w.partials));
+    p.partial_bytes = w.partial_bytes;
+    if (a.dx != nullptr) {
+      p.A = d, p.A.extent = rows, p.A.k = w.width;
+      p.B = W_of(false);
+      p.a_rows = true, p.b_rows = false;
+      p.M = rows, p.N = a.C, p.K = a.V;
+      p.store.out = a.dx, p.store.ld_out = a.lddx, p.store.to = idx + row0;
+      SHC_LAUNCH(launch_product(p, stream));
+    }
+    if (a.dW != nullptr) {
+      p.A = d, p.A.extent = w.width, p.A.k = rows;
+      p.B = x_of(row0, rows, false);
+      p.a_rows = p.b_rows = false;
+      p.M = a.V, p.N = a.C, p.K = rows;
+      p.count_is_k = true;
+      p.store = Store{};
+      p.store.add32 = piece > 0 ? acc : nullptr;
+      if (piece + 1 < w.pieces) {
+        p.store.out32 = acc;
+      } else {
+        p.store.out = a.dW, p.store.ld_out = a.lddW;
+        if (a.accumulate) p.store.res = a.dW, p.store.ld_res = a.lddW;
+      }
+      SHC_LAUNCH(launch_product(p, stream));
+    }
+  }
+  if (a.dx != nullptr) {
+    const int zero_blocks = (int)std::min<int64_t>((a.n + 3) / 4, 2048);
+    if (a.bf16)
+      zero_rows_kernel<uint16_t><<<zero_blocks, 256, 0, stream>>>(
+          labels, a.n, count, static_cast<uint16_t*>(a.dx), a.lddx, a.C);
+    else
+      zero_rows_kernel<float><<<zero_blocks, 256, 0, stream>>>(
+          labels, a.n, count, static_cast<float*>(a.dx), a.lddx, a.C);
+    SHC_LAUNCH(hipGetLastError());
+  }
+  return hipSuccess;
+}
+
+}  // namespace shc
