@@ -278,20 +278,7 @@ struct Tile {
       if (t + 1 < steps) read(a0, b0, buf, 0);
       multiply(a1, b1);
     }
-    if constexpr (PAIRS > 1) {
-      bool fine = true;
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) fine &= __builtin_isfinite(acc[i][j][e]);
-          acc[i][j] *= kSplitBack;
-        }
-      // An infinity, a NaN, a value of 2^104 or a sum of 2^80: the wavefront's
-      // part of the tile again, on the fp32 matrix cores from the values
-      if (__any(!fine)) again(A, B, M, N, K, m0 + wm * 16 * MI, n0 + wn * 64 * S::NG, t0, t1);
-    }
+    if constexpr (PAIRS > 1) again(A, B, M, N, K, m0 + wm * 16 * MI, n0 + wn * 64 * S::NG, t0, t1);
   }
 
   __device__ __forceinline__ void clear() {
@@ -301,27 +288,36 @@ struct Tile {
       for (int j = 0; j < 4 * S::NG; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  // Scales the sums of split products back.  Sums that are not finite (an infinity, a
+  // NaN, a value of 2^104 or more, a sum of 2^80) are taken again on the fp32 matrix
+  // cores from the values, 16 x 16 at a time, and replaced; the others stay.
   __device__ __forceinline__ void again(const Operand& A, const Operand& B, int64_t M, int64_t N,
                                         int64_t K, int64_t m0, int64_t n0, int t0, int t1) {
-    constexpr int MI = S::MI, NJ = 4 * S::NG;
     const int i16 = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
     const int64_t end = (int64_t)t1 * BK < K ? (int64_t)t1 * BK : K;
-    clear();
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+      for (int j = 0; j < 4 * S::NG; ++j) {
+        bool fine = true;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) fine &= __builtin_isfinite(acc[i][j][e]);
+        if (__any(!fine)) {
+          const int64_t m = m0 + i * 16 + i16;
+          const int64_t n = n0 + (j >> 2) * 64 + (i16 >> 2) * 16 + (j & 3) * 4 + (i16 & 3);
+          f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-    for (int64_t k = (int64_t)t0 * BK; k < end; k += 4) {
-      float a[MI], b[NJ];
+          for (int64_t k = (int64_t)t0 * BK; k < end; k += 4)
+            sum = __builtin_amdgcn_mfma_f32_16x16x4f32(original<BROWS>(B, n, k + g, N, end),
+                                                       original<AROWS>(A, m, k + g, M, end), sum,
+                                                       0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < MI; ++i) a[i] = original<AROWS>(A, m0 + i * 16 + i16, k + g, M, end);
-#pragma unroll
-      for (int j = 0; j < NJ; ++j)
-        b[j] = original<BROWS>(
-            B, n0 + (j >> 2) * 64 + (i16 >> 2) * 16 + (j & 3) * 4 + (i16 & 3), k + g, N, end);
-#pragma unroll
-      for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j], a[i], acc[i][j], 0, 0, 0);
-    }
+          for (int e = 0; e < 4; ++e)
+            acc[i][j][e] = __builtin_isfinite(acc[i][j][e]) ? acc[i][j][e] * kSplitBack : sum[e];
+        } else {
+          acc[i][j] *= kSplitBack;
+        }
+      }
   }
 
   // f(row of D, first column, 16 adjacent values) for what the lane holds.

@@ -263,9 +263,9 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
     const float lse = a.lse[i], w = a.weight != nullptr ? a.weight[i] : 1.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float q = z[e] == -__builtin_inff()
-                          ? 0.f
-                          : __builtin_amdgcn_exp2f((z[e] - lse) * kLog2e);
+      // lse = -inf: a row of nothing but -inf
+      const float q =
+          lse == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((z[e] - lse) * kLog2e);
       z[e] = w * (y == e ? q - 1.f : q);
       if (col + e >= a.labels.V) z[e] = 0.f;
       sum[e] += z[e];
