@@ -84,7 +84,7 @@ hipError_t launch_sum_rows(const float* parts, int64_t rows, int64_t ld, int32_t
                            float* out, hipStream_t stream);
 
 // Shape of the workgroups' tiles and parts along K for a product.
-enum class TileKind { k256, k128, k64, k16 };
+enum class TileKind { k256, k128, k64, k32 };
 struct Plan {
   TileKind kind;
   int parts;
@@ -93,12 +93,12 @@ struct Plan {
 Plan plan_product(int64_t M, int64_t N, int64_t K, int pairs, bool few_rows,
                   size_t partial_bytes);
 
-using Shape256 = Shape<8, 1, 2, 4>;
-using Shape128 = Shape<4, 1, 2, 2>;
-using Shape64 = Shape<4, 1, 1, 4>;
-using Shape16 = Shape<1, 1, 1, 4>;
+using Shape256 = Shape<4, 2, 2, 4>;
+using Shape128 = Shape<2, 2, 2, 2>;
+using Shape64 = Shape<2, 2, 1, 4>;
+using Shape32 = Shape<1, 2, 1, 4>;
 inline int tile_m(TileKind k) {
-  return k == TileKind::k256 ? 256 : k == TileKind::k128 ? 128 : k == TileKind::k64 ? 64 : 16;
+  return k == TileKind::k256 ? 256 : k == TileKind::k128 ? 128 : k == TileKind::k64 ? 64 : 32;
 }
 inline int tile_n(TileKind k) { return k == TileKind::k128 ? 128 : 256; }
 
@@ -109,7 +109,7 @@ hipError_t with_tile(TileKind kind, F&& f) {
     case TileKind::k256: return f(Shape256{});
     case TileKind::k128: return f(Shape128{});
     case TileKind::k64: return f(Shape64{});
-    default: return f(Shape16{});
+    default: return f(Shape32{});
   }
 }
 

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(Args a) {
   tile.run(a.A, a.B, M, a.N, K, m0, n0, t0, t1, smem);
   if (a.parts > 1) {
     float* to = a.partials + (int64_t)blockIdx.y * a.M * a.N;
-    tile.each(m0, n0, [&](int64_t row, int64_t col, const float* v) {
+    tile.each(m0, n0, [&](int64_t row, int64_t col, const float* v, int) {
       if (row >= M) return;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(Args a) {
     });
     return;
   }
-  tile.each(m0, n0, [&](int64_t row, int64_t col, const float* v) {
+  tile.each(m0, n0, [&](int64_t row, int64_t col, const float* v, int) {
     if (row >= M) return;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -189,7 +189,7 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, int pairs, bool few_rows,
   static constexpr Kind kinds[] = {{TileKind::k256, 256, 1.9},
                                    {TileKind::k128, 512, 1.2},
                                    {TileKind::k64, 512, 1.4},
-                                   {TileKind::k16, 512, 1.2}};
+                                   {TileKind::k32, 512, 1.2}};
   const int64_t KT = (K + BK - 1) / BK;
   Plan best{TileKind::k128, 1};
   double least = 1e300;

@@ -8,12 +8,14 @@
 // k * ld + r ("cols": it runs across rows), so that x W, dz W^T and x^T dz read
 // their tensors as they are.
 //
-// A tile of BM x BN is WM x WN wavefronts of (16 MI) x (64 NG).  Its operands pass
-// through LDS in steps of 64 along k, in two buffers, brought by loads that write
-// LDS directly.  A step is two halves of 32; each half's fragments are read into
-// registers while the matrix instructions of the half before run, so that they
-// wait neither for LDS nor, with a whole step between a load and its first use,
-// for memory, and there is one barrier to a step:
+// A tile of BM x BN is WM x WN wavefronts of (32 MB) x (32 NB), in 32 x 32 x 16 matrix
+// instructions: half as many operand registers are read per product as with 16 x 16
+// x 32, and the large products run at the power limit.  The tile's operands pass
+// through LDS in steps of 64 along k, in two buffers, brought by loads that write LDS
+// directly.  A step is two halves of 32; each half's fragments are read into registers
+// while the matrix instructions of the half before run, so that they wait neither for
+// LDS nor, with a whole step between a load and its first use, for memory, and there
+// is one barrier to a step:
 //
 //   read half 1 of step t;  multiply half 0 of t;
 //   wait for those reads and for step t + 1 in LDS;  barrier;
@@ -26,15 +28,14 @@
 // contiguous kilobyte.  Fragments of a cols operand come from the transposing LDS
 // read: 16 lanes give the addresses of 4 x 16 elements and each gets a column.
 //
-// The products run transposed (D^T = B A^T), and the rows of B that a fragment
-// takes are chosen so that a lane ends with 16 adjacent columns of one row of D:
-// row lane % 16, columns 16 (lane / 16) + 4 j + i of the 64, in register i of
-// fragment j.
+// The products run transposed (D^T = B A^T): a lane holds columns 8 b + 4 (lane / 32)
+// + e of row lane % 32 of a 32 x 32 block; the halves of the wavefront exchange them at
+// the end, after which a lane has 16 adjacent columns.
 //
 // Loads past the ends give zeros: a buffer descriptor covers exactly the rows that
 // are there, and chunks past a row's end get an offset outside of it.  Operands
 // start at multiples of 16 bytes, with rows of a multiple of 8 elements, a
-// multiple of 8 elements and less than 2^22 apart (see `direct`).
+// multiple of 8 elements and less than 2^21 apart (see `direct`).
 #pragma once
 
 #include "row_ops.h"
@@ -47,6 +48,7 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr int BK = 64;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct Operand {
   const uint16_t* p;
@@ -69,30 +71,22 @@ constexpr int kPairs = 6;
 __device__ __forceinline__ int pair_a(int p) { return (0x012010 >> (4 * (5 - p))) & 0xF; }
 __device__ __forceinline__ int pair_b(int p) { return (0x210100 >> (4 * (5 - p))) & 0xF; }
 
-template <int MI_, int NG_, int WM_, int WN_>
+template <int MB_, int NB_, int WM_, int WN_>
 struct Shape {
-  static constexpr int MI = MI_, NG = NG_, WM = WM_, WN = WN_;
-  static constexpr int BM = 16 * MI * WM, BN = 64 * NG * WN, NW = WM * WN, THREADS = 64 * NW;
+  static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_;
+  static constexpr int BM = 32 * MB * WM, BN = 32 * NB * WN, NW = WM * WN, THREADS = 64 * NW;
   static constexpr int LDS_A = BM * BK * 2, LDS_B = BN * BK * 2, STAGE = LDS_A + LDS_B;
   static constexpr int LDS = 2 * STAGE;
 };
 
-// The place of chunk c of a row in LDS.  PERM: the fragments take rows
-// 16 q + 4 j + i of 64 (operand B), else 16 adjacent rows (operand A).
-// rows operand: R rows of 8 chunks, key from the row; cols operand: 64 rows (k)
-// of R / 8 chunks, key from k.
-template <bool PERM>
-__device__ __forceinline__ int rows_key(int r) {
-  return PERM ? (r & 3) | ((r >> 2) & 4) : r & 7;
-}
-template <int R, bool PERM>
-__device__ __forceinline__ int cols_key(int k) {
-  if constexpr (R == 64) return PERM ? (k >> 1) & 1 : k & 2;
-  return PERM ? (k & 1) | ((k & 2) << 2) : (k & 3) << 1;
-}
+// What the place of a chunk in its row of LDS is XORed with: rows operand, 8 chunks
+// to row r (a read takes 16 rows at a time, two of them 256 bytes of banks); cols
+// operand, 16 or more chunks to row k (32 lanes have 64 bytes of 4 rows).
+__device__ __forceinline__ int rows_key(int r) { return (r >> 1) & 7; }
+__device__ __forceinline__ int cols_key(int k) { return (k & 3) << 2; }
 
 // One operand's side of the tile.
-template <int R, bool ROWS, bool PERM, int NW>
+template <int R, bool ROWS, int NW>
 struct Side {
   static constexpr int INSTR = R * BK * 2 / 1024;          // loads of a kilobyte
   static constexpr int PER_WAVE = (INSTR + NW - 1) / NW;
@@ -111,7 +105,7 @@ struct Side {
       bytes = ((left - 1) * o.ld + o.k) * 2;
       step = BK * 2;
       const int r = w * 8 + (lane >> 3);
-      kl = ((lane & 7) ^ rows_key<PERM>(r)) * 8;
+      kl = ((lane & 7) ^ rows_key(r)) * 8;
       off = (uint32_t)((r * o.ld + kl) * 2);
       inc = (int32_t)(8 * NW * o.ld * 2);
     } else {
@@ -121,7 +115,8 @@ struct Side {
       bytes = ((o.k - 1) * o.ld + left) * 2;
       step = o.ld * BK * 2;
       kl = w * KR + lane / S;
-      const int c = (lane % S) ^ cols_key<R, PERM>(kl);
+      static_assert(R >= 128, "16 chunks to a row");
+      const int c = (lane % S) ^ cols_key(kl);
       off = c * 8 < left ? (uint32_t)((kl * o.ld + c * 8) * 2) : 0xFFFFFFF0u;
       inc = (int32_t)(KR * NW * o.ld * 2);
     }
@@ -138,14 +133,7 @@ struct Side {
       if (INSTR % NW != 0 && i * NW + w >= INSTR) break;
       uint32_t o = off == 0xFFFFFFF0u ? off : off + i * inc;
       if constexpr (ROWS) {
-        // the key of PERM rows changes with the load only through bit 4 of the row
-        int k = kl;
-        if constexpr (PERM && (8 * NW) % 32 != 0) {
-          const int flip = (rows_key<PERM>(i * NW * 8 + w * 8) ^ rows_key<PERM>(w * 8)) * 8;
-          o += ((kl ^ flip) - kl) * 2;
-          k = kl ^ flip;
-        }
-        if ((int64_t)kt * BK + k >= K) o = 0xFFFFFFF0u;
+        if ((int64_t)kt * BK + kl >= K) o = 0xFFFFFFF0u;
       } else {
         static_assert((64 / (R / 8) * NW) % 4 == 0 || INSTR <= NW, "the key repeats");
       }
@@ -155,46 +143,45 @@ struct Side {
   }
 };
 
-// Fragments of one half step: F of 16 rows by 32 k.
-template <int R, bool ROWS, bool PERM, int F>
-struct Frags {
-  static constexpr int BASES = ROWS ? 2 : PERM ? 2 : (R == 64 ? 2 : 4);
-  int at[BASES];  // LDS byte offsets of the lane
+// The transposing read.  `restrict` gives it the alias information without which the
+// compiler waits, at every such read, for all loads into LDS that are under way; here
+// the steps' own waits and barriers order them.
+__device__ __forceinline__ s16x4 read_transposed(const char* __restrict__ p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+}
 
-  // r0: the wave's first row (a multiple of 64 with PERM)
+// Fragments of 32 rows by 16 k: lane l has row l % 32, k 8 (l / 32) to 8 (l / 32) + 7.
+template <int R, bool ROWS>
+struct Frags {
+  int at;  // LDS byte offset of the lane in the first fragment; others by XOR
+
+  // r0: the wave's first row, a multiple of 32
   __device__ __forceinline__ void init(int r0, int lane) {
-    const int i = lane & 15, g = lane >> 4;
+    const int h = lane >> 5;
     if constexpr (ROWS) {
-      const int r = r0 + (PERM ? 16 * (i >> 2) + (i & 3) : i);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) at[h] = r * 128 + (((4 * h + g) ^ rows_key<PERM>(r)) * 16);
+      const int r = r0 + (lane & 31);
+      at = r * 128 + ((h ^ rows_key(r)) * 16);
     } else {
-      const int k = 8 * g + (i >> 2), q = i & 3, key = cols_key<R, PERM>(k);
-#pragma unroll
-      for (int b = 0; b < BASES; ++b) {
-        // PERM: fragment j = 2 b (+ 1: 8 bytes on); else fragment f = b modulo BASES
-        const int c = r0 / 8 + (PERM ? 2 * q + b : 2 * b + (q >> 1));
-        at[b] = k * (R * 2) + ((c ^ key) * 16) + (PERM ? 0 : (q & 1) * 8);
-      }
+      const int i = lane & 15, k = 8 * h + (i >> 2);
+      const int c = r0 / 8 + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
+      at = k * (R * 2) + ((c ^ cols_key(k)) * 16) + (i & 1) * 8;
     }
   }
-  __device__ __forceinline__ bf16x8 get(const char* lds, int f, int h) const {
+  // rows 32 f on, k 16 s on
+  __device__ __forceinline__ bf16x8 get(const char* lds, int f, int s) const {
     if constexpr (ROWS) {
-      const int add = PERM ? (f >> 2) * 64 * 128 + (f & 3) * 4 * 128 : f * 16 * 128;
-      return *reinterpret_cast<const bf16x8*>(lds + at[h] + add);
+      return *reinterpret_cast<const bf16x8*>(lds + (at ^ (s * 32)) + f * 32 * 128);
     } else {
-      const int b = PERM ? (f >> 1) & 1 : f % BASES;
-      const int add = (PERM ? (f >> 2) * 128 + (f & 1) * 8 : f / BASES * (BASES * 32)) +
-                      h * 32 * R * 2;
+      // 64 bytes a fragment; f & 3 meets the key's bits (r0 is a multiple of 32 MB or NB)
+      const char* p = lds + (at ^ ((f & 3) * 64)) + (f >> 2) * 256 + s * 16 * R * 2;
       union {
-        s16x4 s[2];
-        bf16x8 v;
+        s16x4 v[2];
+        bf16x8 all;
       } u;
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        u.s[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_s16x4*)(lds + at[b] + add + e * 4 * R * 2));
-      return u.v;
+        u.v[e] = read_transposed(p + e * 4 * R * 2);
+      return u.all;
     }
   }
 };
@@ -215,26 +202,31 @@ constexpr float kSplitScale = 0x1p24f, kSplitBack = 0x1p-48f;
 
 template <class S, bool AROWS, bool BROWS, int PAIRS>
 struct Tile {
-  f32x4 acc[S::MI][4 * S::NG];
+  static constexpr int MB = S::MB, NB = S::NB;
+  f32x16 acc[MB][NB];
 
   // The tile at (m0, n0) of the M x N of which both operands hold enough rows,
   // over steps [t0, t1) of 64 along K.  smem: S::LDS bytes at a multiple of 1024.
   __device__ __forceinline__ void run(const Operand& A, const Operand& B, int64_t M, int64_t N,
                                       int64_t K, int64_t m0, int64_t n0, int t0, int t1,
                                       char* smem) {
-    constexpr int MI = S::MI, NJ = 4 * S::NG;
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = w / S::WN, wn = w % S::WN;
-    Side<S::BM, AROWS, false, S::NW> sa;
-    Side<S::BN, BROWS, true, S::NW> sb;
+    Side<S::BM, AROWS, S::NW> sa;
+    Side<S::BN, BROWS, S::NW> sb;
     sa.init(A, m0, w, lane);
     sb.init(B, n0, w, lane);
-    Frags<S::BM, AROWS, false, MI> fa;
-    Frags<S::BN, BROWS, true, NJ> fb;
-    fa.init(wm * 16 * MI, lane);
-    fb.init(wn * 64 * S::NG, lane);
-    clear();
+    Frags<S::BM, AROWS> fa;
+    Frags<S::BN, BROWS> fb;
+    fa.init(wm * 32 * MB, lane);
+    fb.init(wn * 32 * NB, lane);
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     if (t0 >= t1) return;
 
     int lp = 0, lk = t0;  // the next step to load: its pair, and its place along K
@@ -247,20 +239,26 @@ struct Tile {
       sb.load(to + S::LDS_A, pb, lk, kb, w);
       if (++lk == t1 && PAIRS > 1) lk = t0, ++lp;
     };
-    bf16x8 a0[MI], b0[NJ], a1[MI], b1[NJ];
-    const auto read = [&](bf16x8(&a)[MI], bf16x8(&b)[NJ], int buf, int h) {
+    bf16x8 a0[MB][2], b0[NB][2], a1[MB][2], b1[NB][2];
+    const auto read = [&](bf16x8(&a)[MB][2], bf16x8(&b)[NB][2], int buf, int h) {
       const char* from = smem + buf * S::STAGE;
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) b[j] = fb.get(from + S::LDS_A, j, h);
+      for (int s = 0; s < 2; ++s) {
 #pragma unroll
-      for (int i = 0; i < MI; ++i) a[i] = fa.get(from, i, h);
+        for (int j = 0; j < NB; ++j) b[j][s] = fb.get(from + S::LDS_A, j, 2 * h + s);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) a[i][s] = fa.get(from, i, 2 * h + s);
+      }
     };
-    const auto multiply = [&](const bf16x8(&a)[MI], const bf16x8(&b)[NJ]) {
+    const auto multiply = [&](const bf16x8(&a)[MB][2], const bf16x8(&b)[NB][2]) {
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j][s], a[i][s], acc[i][j], 0, 0,
+                                                                0);
     };
     // Waits and barriers in one asm block each: no access to LDS moves across.
     const int steps = PAIRS * (t1 - t0);
@@ -272,47 +270,42 @@ struct Tile {
     for (int t = 0; t < steps; ++t) {
       read(a1, b1, buf, 1);
       multiply(a0, b0);
+      __builtin_amdgcn_sched_barrier(0);  // the products are not moved behind the wait
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
       if (t + 2 < steps) load(buf);
       buf ^= 1;
       if (t + 1 < steps) read(a0, b0, buf, 0);
       multiply(a1, b1);
     }
-    if constexpr (PAIRS > 1) again(A, B, M, N, K, m0 + wm * 16 * MI, n0 + wn * 64 * S::NG, t0, t1);
-  }
-
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-      for (int j = 0; j < 4 * S::NG; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (PAIRS > 1)
+      again(A, B, M, N, K, m0 + wm * 32 * MB, n0 + wn * 32 * NB, t0, t1);
   }
 
   // Scales the sums of split products back.  Sums that are not finite (an infinity, a
   // NaN, a value of 2^104 or more, a sum of 2^80) are taken again on the fp32 matrix
-  // cores from the values, 16 x 16 at a time, and replaced; the others stay.
+  // cores from the values, 32 x 32 at a time, and replaced; the others stay.
   __device__ __forceinline__ void again(const Operand& A, const Operand& B, int64_t M, int64_t N,
                                         int64_t K, int64_t m0, int64_t n0, int t0, int t1) {
-    const int i16 = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+    const int r = threadIdx.x & 31, h = (threadIdx.x >> 5) & 1;
     const int64_t end = (int64_t)t1 * BK < K ? (int64_t)t1 * BK : K;
 #pragma unroll
-    for (int i = 0; i < S::MI; ++i)
+    for (int i = 0; i < MB; ++i)
 #pragma unroll
-      for (int j = 0; j < 4 * S::NG; ++j) {
+      for (int j = 0; j < NB; ++j) {
         bool fine = true;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) fine &= __builtin_isfinite(acc[i][j][e]);
+        for (int e = 0; e < 16; ++e) fine &= __builtin_isfinite(acc[i][j][e]);
         if (__any(!fine)) {
-          const int64_t m = m0 + i * 16 + i16;
-          const int64_t n = n0 + (j >> 2) * 64 + (i16 >> 2) * 16 + (j & 3) * 4 + (i16 & 3);
-          f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-          for (int64_t k = (int64_t)t0 * BK; k < end; k += 4)
-            sum = __builtin_amdgcn_mfma_f32_16x16x4f32(original<BROWS>(B, n, k + g, N, end),
-                                                       original<AROWS>(A, m, k + g, M, end), sum,
-                                                       0, 0, 0);
+          f32x16 sum;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
+          for (int e = 0; e < 16; ++e) sum[e] = 0.f;
+#pragma unroll 1
+          for (int64_t k = (int64_t)t0 * BK; k < end; k += 2)
+            sum = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                original<BROWS>(B, n0 + j * 32 + r, k + h, N, end),
+                original<AROWS>(A, m0 + i * 32 + r, k + h, M, end), sum, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
             acc[i][j][e] = __builtin_isfinite(acc[i][j][e]) ? acc[i][j][e] * kSplitBack : sum[e];
         } else {
           acc[i][j] *= kSplitBack;
@@ -320,22 +313,30 @@ struct Tile {
       }
   }
 
-  // f(row of D, first column, 16 adjacent values) for what the lane holds.
+  // f(row of D, first column, 16 adjacent values, block of columns) for what the lane holds.
   template <typename F>
   __device__ __forceinline__ void each(int64_t m0, int64_t n0, F&& f) const {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t row = m0 + (w / S::WN) * 16 * S::MI + (lane & 15);
-    const int64_t col = n0 + (w % S::WN) * 64 * S::NG + (lane >> 4) * 16;
+    const int64_t row = m0 + (w / S::WN) * 32 * MB + (lane & 31);
+    const int64_t col = n0 + (w % S::WN) * 32 * NB + (lane >> 5) * 16;
 #pragma unroll
-    for (int i = 0; i < S::MI; ++i)
+    for (int i = 0; i < MB; ++i)
 #pragma unroll
-      for (int q = 0; q < S::NG; ++q) {
+      for (int j = 0; j < NB; ++j) {
+        // register 4 b + e: column 8 b + 4 (lane / 32) + e.  The upper half's columns of
+        // b = 0, 1 for the lower half's of b = 2, 3.
         float v[16];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[4 * j + e] = acc[i][4 * q + j][e];
-        f(row + 16 * i, col + 64 * q, v);
+          for (int e = 0; e < 4; ++e) {
+            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][4 * b + e]),
+                                                            __float_as_uint(acc[i][j][4 * b + 8 + e]),
+                                                            false, false);
+            v[8 * b + e] = __uint_as_float(x[0]);
+            v[8 * b + 4 + e] = __uint_as_float(x[1]);
+          }
+        f(row + 32 * i, col + 32 * j, v, j);
       }
   }
 };

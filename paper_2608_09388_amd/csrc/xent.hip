@@ -137,15 +137,12 @@ __device__ __forceinline__ bool logits_tile(Logits& a, Tile<S, true, true, PAIRS
   return true;
 }
 
-// Over the four lanes that hold a row.
+// Over the two lanes that hold a row.
 template <typename Op>
 __device__ __forceinline__ float row_reduce(float x, Op op) {
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
                                                   false);
-  x = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                  false);
-  return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+  return op(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 
 // 16 columns' logits in place: bias added, -inf past the last.
@@ -186,10 +183,9 @@ __global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
   int tn;
   if (!logits_tile<S, PAIRS>(a, tile, &m0, &n0, &M, &tn, smem)) return;
   // LDS is free: the last step's reads are behind the tile's last barrier
-  float2* red = reinterpret_cast<float2*>(smem);  // [WN][BM]
-  const int wn = (threadIdx.x >> 6) % S::WN;
-  const bool first = (threadIdx.x & 63) < 16;
-  tile.each(m0, n0, [&](int64_t row, int64_t col, float* z) {
+  float2* red = reinterpret_cast<float2*>(smem);  // [BN / 32][BM]
+  const bool first = (threadIdx.x & 63) < 32;
+  tile.each(m0, n0, [&](int64_t row, int64_t col, float* z, int) {
     finish_logits(z, a.bias, col, a.labels.V);
     float m = z[0];
 #pragma unroll
@@ -200,7 +196,7 @@ __global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f((z[e] - f) * kLog2e);
     s = row_reduce(s, rowops::AddOp{});
-    if (first) red[wn * S::BM + (int)(row - m0)] = float2{m, s};
+    if (first) red[(int)(col - n0) / 32 * S::BM + (int)(row - m0)] = float2{m, s};
     if (row < M) {
       const int64_t y = a.labels.get(a.idx[row]) - col;
       if (y >= 0 && y < 16) {
@@ -215,7 +211,7 @@ __global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
   for (int r = threadIdx.x; r < S::BM && m0 + r < M; r += S::THREADS) {
     float2 t = red[r];
 #pragma unroll
-    for (int w = 1; w < S::WN; ++w) t = join(t, red[w * S::BM + r]);
+    for (int b = 1; b < S::BN / 32; ++b) t = join(t, red[b * S::BM + r]);
     a.parts[(int64_t)tn * a.rows + m0 + r] = t;
   }
 }
@@ -252,10 +248,10 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
   int64_t m0, n0, M;
   int tn;
   if (!logits_tile<S, PAIRS>(a, tile, &m0, &n0, &M, &tn, smem)) return;
-  float sum[16];
+  float sum[S::NB][16];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) sum[e] = 0.f;
-  tile.each(m0, n0, [&](int64_t row, int64_t col, float* z) {
+  for (int e = 0; e < 16 * S::NB; ++e) sum[e / 16][e % 16] = 0.f;
+  tile.each(m0, n0, [&](int64_t row, int64_t col, float* z, int j) {
     if (row >= M) return;
     finish_logits(z, a.bias, col, a.labels.V);
     const int64_t i = a.idx[row];
@@ -268,7 +264,7 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
           lse == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((z[e] - lse) * kLog2e);
       z[e] = w * (y == e ? q - 1.f : q);
       if (col + e >= a.labels.V) z[e] = 0.f;
-      sum[e] += z[e];
+      sum[j][e] += z[e];
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -276,17 +272,20 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
         put8<PAIRS == 1>(a.dz, row, a.ld_dz, (int)(col / 8) + h, a.width, z + 8 * h);
   });
   if (a.sums == nullptr) return;
-  // over the tile's rows: the lane's, then the 16 lanes' of the same columns
+  // over the tile's rows: the lane's, then the 32 lanes' of the same columns
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  float mine = 0.f;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const float s = rowops::lanes_reduce<16>(sum[e], rowops::AddOp{});
-    mine = (lane & 15) == e ? s : mine;
-  }
-  const int64_t col = n0 + (w % S::WN) * 64 + lane;
   const int64_t part = m0 / S::BM * S::WM + w / S::WN;
-  if (col < a.labels.V) a.sums[part * a.labels.V + col] = mine;
+#pragma unroll
+  for (int j = 0; j < S::NB; ++j) {
+    float mine = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float s = rowops::lanes_reduce<32>(sum[j][e], rowops::AddOp{});
+      mine = (lane & 31) == e ? s : mine;
+    }
+    const int64_t col = n0 + (w % S::WN * S::NB + j) * 32 + (lane >> 5) * 16 + (lane & 31);
+    if ((lane & 31) < 16 && col < a.labels.V) a.sums[part * a.labels.V + col] = mine;
+  }
 }
 
 // Column sums over the parts of the live rows, in order, added to what the pieces
@@ -390,7 +389,7 @@ hipError_t run_logits(const Logits& a, hipStream_t stream) {
 template <bool GRAD>
 hipError_t launch_logits(Logits a, bool bf16, TileKind* kind, hipStream_t stream) {
   TileKind k = plan_product(a.rows, a.labels.V, a.C, bf16 ? 1 : kPairs, true, 0).kind;
-  if (k == TileKind::k16 && a.rows > 64) k = TileKind::k64;  // sums: 64 rows to a part
+  if (k == TileKind::k32 && a.rows > 64) k = TileKind::k64;  // sums: 64 rows to a part
   *kind = k;
   const int64_t tm = (a.rows + tile_m(k) - 1) / tile_m(k);
   const int64_t tn = (a.labels.V + tile_n(k) - 1) / tile_n(k);
@@ -512,7 +511,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
     g.sums = a.db != nullptr ? reinterpret_cast<float*>(byte(a.ws, w.sums)) : nullptr;
     SHC_LAUNCH(launch_logits<true>(g, a.bf16, &kind, stream));
     if (a.db != nullptr) {
-      const int per = kind == TileKind::k256 ? 128 : kind == TileKind::k16 ? 16 : 64;
+      const int per = kind == TileKind::k256 ? 128 : kind == TileKind::k32 ? 32 : 64;
       join_sums_kernel<<<(a.V + 63) / 64, 1024, 0, stream>>>(g.sums, per, rows, count, row0, a.V,
                                                              piece > 0 || a.accumulate, a.db);
       SHC_LAUNCH(hipGetLastError());
