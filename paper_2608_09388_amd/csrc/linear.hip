@@ -171,9 +171,9 @@ hipError_t operand(const void* p, int64_t ld, int64_t n, int32_t C, bool bf16, b
                      stream);
 }
 
-#define SHC_LAUNCH(expr)                   \
+#define SHC_LAUNCH(...)                    \
   do {                                     \
-    const hipError_t _e = (expr);          \
+    const hipError_t _e = (__VA_ARGS__);   \
     if (_e != hipSuccess) return _e;       \
   } while (0)
 

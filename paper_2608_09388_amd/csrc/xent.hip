@@ -14,11 +14,18 @@
 // of exponentials over the tile's columns and the label's logit; a second launch joins
 // the tiles.  Nothing of size rows x V is written.
 //
-// Backward: for a piece of rows at a time, the logits again, turned in the epilogue
-// into dz [rows][V] (bf16, rounded once from fp32, or fp32), and the products dz W and
-// dz^T x over it; db from the unrounded dz, summed per tile.  A piece is at most 2^30
-// (bf16) or 2^28 (fp32) elements of dz, so most calls have one; with more, dW is summed
-// over them in fp32.
+// Gradients: for a piece of rows at a time dz [rows][V] (bf16, rounded once from fp32, or
+// fp32), and the products dz W and dz^T x over it; db from the unrounded dz, summed
+// over 64 rows or a tile's, then over these.  A piece is at most 2^30 (bf16) or 2^28
+// (fp32) elements of dz, so most calls have one; with more, dW is summed over them in
+// fp32.  dz comes
+// - in the backward, from the logits again, in the epilogue of their product;
+// - in the step, from what its forward kept of the piece: bf16 without db, the
+//   exponentials relative to the maximum of their tile's columns, in fp16 times 2^15
+//   (off by 2^-12 of their value, 2^-40 of the tile's largest at the small end: next to
+//   the rounding of dz to bf16, nothing); fp32, or with db, the logits in fp32.  One pass
+//   over them gives dz.  For short rows the product is cheaper than that pass
+//   (`keeps`).
 #include <algorithm>
 #include <mutex>
 
@@ -113,6 +120,7 @@ struct Logits {
   // statistics
   float2* parts;  // [tn][rows]: maximum and sum over a tile's columns
   float* at_label;
+  void* kept;  // [rows][width]
   // gradient
   const float* lse;
   const float* weight;
@@ -175,7 +183,11 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
                        b.y * __builtin_amdgcn_exp2f((b.x - f) * kLog2e)};
 }
 
-template <class S, int PAIRS>
+// What the forward of a step keeps of the logits.
+enum Keep { kNothing, kExps, kLogits };
+constexpr float kExpScale = 32768.f;
+
+template <class S, int PAIRS, Keep KEEP>
 __global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   Tile<S, true, true, PAIRS> tile;
@@ -183,7 +195,9 @@ __global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
   int tn;
   if (!logits_tile<S, PAIRS>(a, tile, &m0, &n0, &M, &tn, smem)) return;
   // LDS is free: the last step's reads are behind the tile's last barrier
-  float2* red = reinterpret_cast<float2*>(smem);  // [BN / 32][BM]
+  constexpr int BLOCKS = S::BN / 32;
+  float* most = reinterpret_cast<float*>(smem);  // [BLOCKS][BM]
+  float* sums = most + BLOCKS * S::BM;
   const bool first = (threadIdx.x & 63) < 32;
   tile.each(m0, n0, [&](int64_t row, int64_t col, float* z, int) {
     finish_logits(z, a.bias, col, a.labels.V);
@@ -191,12 +205,7 @@ __global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
 #pragma unroll
     for (int e = 1; e < 16; ++e) m = fmaxf(m, z[e]);
     m = row_reduce(m, rowops::MaxOp{});
-    const float f = finite_or_0(m);
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f((z[e] - f) * kLog2e);
-    s = row_reduce(s, rowops::AddOp{});
-    if (first) red[(int)(col - n0) / 32 * S::BM + (int)(row - m0)] = float2{m, s};
+    if (first) most[(int)(col - n0) / 32 * S::BM + (int)(row - m0)] = m;
     if (row < M) {
       const int64_t y = a.labels.get(a.idx[row]) - col;
       if (y >= 0 && y < 16) {
@@ -208,23 +217,137 @@ __global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
     }
   });
   __syncthreads();
-  for (int r = threadIdx.x; r < S::BM && m0 + r < M; r += S::THREADS) {
-    float2 t = red[r];
+  const auto row_most = [&](int r) {
+    float m = most[r];
 #pragma unroll
-    for (int b = 1; b < S::BN / 32; ++b) t = join(t, red[b * S::BM + r]);
-    a.parts[(int64_t)tn * a.rows + m0 + r] = t;
+    for (int b = 1; b < BLOCKS; ++b) m = fmaxf(m, most[b * S::BM + r]);
+    return m;
+  };
+  tile.each(m0, n0, [&](int64_t row, int64_t col, float* z, int) {
+    finish_logits(z, a.bias, col, a.labels.V);
+    if constexpr (KEEP == kLogits) {
+      float* to = static_cast<float*>(a.kept) + row * a.width;
+      if (row < M && col < a.width) {
+        rowops::store_channels<8>(to + col, 0, a.width - (int)col, z);
+        if (col + 8 < a.width) rowops::store_channels<8>(to + col, 1, a.width - (int)col, z + 8);
+      }
+    }
+    const float f = finite_or_0(row_most((int)(row - m0)));
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      z[e] = __builtin_amdgcn_exp2f((z[e] - f) * kLog2e);
+      s += z[e];
+    }
+    s = row_reduce(s, rowops::AddOp{});
+    if (first) sums[(int)(col - n0) / 32 * S::BM + (int)(row - m0)] = s;
+    if constexpr (KEEP == kExps) {
+      typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+      _Float16* to = static_cast<_Float16*>(a.kept) + row * a.width + col;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        half8 x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (_Float16)(z[8 * h + e] * kExpScale);
+        if (row < M && col + 8 * h < a.width) *reinterpret_cast<half8*>(to + 8 * h) = x;
+      }
+    }
+  });
+  __syncthreads();
+  for (int r = threadIdx.x; r < S::BM && m0 + r < M; r += S::THREADS) {
+    float s = sums[r];
+#pragma unroll
+    for (int b = 1; b < BLOCKS; ++b) s += sums[b * S::BM + r];
+    a.parts[(int64_t)tn * a.rows + m0 + r] = float2{row_most(r), s};
   }
+}
+
+// dz of the live rows from what was kept: 64 rows by 512 columns to a workgroup, 16 rows
+// of 8 columns to a thread.
+struct FromKept {
+  const void* kept;
+  int64_t rows;
+  const int32_t* count;
+  int64_t row0;
+  const float2* parts;
+  int tile;  // columns of a tile of parts
+  Labels labels;
+  const int32_t* idx;
+  const float* lse;
+  const float* weight;
+  void* dz;
+  int width, dz_width;
+  float* sums;  // [ceil(rows / 64)][V] or NULL
+};
+template <bool BF16, Keep KEEP>
+__global__ __launch_bounds__(256) void from_kept_kernel(FromKept a) {
+  __shared__ float part[3][64 * 8];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t live = rows_left(a.count, a.row0, a.rows);
+  const int64_t r0 = (int64_t)blockIdx.x * 64;
+  if (r0 >= live) return;
+  const int64_t r1 = r0 + 64 < live ? r0 + 64 : live;
+  const int v = blockIdx.y * 64 + lane, col = 8 * v;
+  const int V = a.labels.V;
+  float sum[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+  if (col < a.dz_width) {
+#pragma unroll 2
+    for (int64_t row = r0 + w; row < r1; row += 4) {
+      const int64_t i = a.idx[row];
+      const float lse = a.lse[i], wt = a.weight != nullptr ? a.weight[i] : 1.f;
+      const int64_t y = a.labels.get(i) - col;
+      float z[8];
+      if constexpr (KEEP == kExps) {
+        typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+        const half8 x = *reinterpret_cast<const half8*>(static_cast<const _Float16*>(a.kept) +
+                                                        row * a.width + col);
+        const float m = finite_or_0(a.parts[(int64_t)(col / a.tile) * a.rows + row].x);
+        const float f = lse == -__builtin_inff()
+                            ? 0.f
+                            : __builtin_amdgcn_exp2f((m - lse) * kLog2e) * (1.f / kExpScale);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = (float)x[e] * f;
+      } else {
+        rowops::load_channels<8>(static_cast<const float*>(a.kept) + row * a.width, v, a.width, z);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          z[e] = lse == -__builtin_inff() ? 0.f
+                                          : __builtin_amdgcn_exp2f((z[e] - lse) * kLog2e);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        z[e] = wt * (y == e ? z[e] - 1.f : z[e]);
+        if (col + e >= V) z[e] = 0.f;
+        sum[e] += z[e];
+      }
+      put8<BF16>(a.dz, row, a.dz_width, v, a.dz_width, z);
+    }
+  }
+  if (a.sums == nullptr) return;
+  if (w > 0)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[w - 1][e * 64 + lane] = sum[e];
+  __syncthreads();
+  if (w > 0 || col >= V) return;
+#pragma unroll
+  for (int q = 0; q < 3; ++q)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += part[q][e * 64 + lane];
+  rowops::store_channels<8>(a.sums + (int64_t)blockIdx.x * V, v, V, sum);
 }
 
 // 16 rows to a workgroup, 16 threads to a row.
 __global__ __launch_bounds__(256) void join_stats_kernel(const float2* parts, int tiles,
                                                          int64_t rows, const int32_t* count,
-                                                         const int32_t* idx, const float* at_label,
-                                                         float* loss, float* lse) {
+                                                         int64_t row0, const int32_t* idx,
+                                                         const float* at_label, float* loss,
+                                                         float* lse) {
   __shared__ float2 part[16][16];
   const int r = threadIdx.x & 15, p = threadIdx.x >> 4;
   const int64_t row = (int64_t)blockIdx.x * 16 + r;
-  const int64_t live = *count;
+  const int64_t live = rows_left(count, row0, rows);
   if ((int64_t)blockIdx.x * 16 >= live) return;
   float2 t = {-__builtin_inff(), 0.f};
   if (row < live)
@@ -325,9 +448,12 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(Labels l, int64_t n, con
 
 struct Layout {
   int64_t width, rows, pieces;  // columns of dz, rows and number of the pieces
-  size_t idx, count, counts, x, W, parts, at_label, lse, dz, dz32, sums, acc, partials,
+  size_t idx, count, counts, x, W, parts, at_label, lse, kept, dz, dz32, sums, acc, partials,
       partial_bytes, total;
 };
+
+// Whether the step keeps the logits or their exponentials.
+bool keeps(int32_t C, bool bf16) { return C >= (bf16 ? 512 : 128); }
 
 Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass pass) {
   Layout w{};
@@ -352,8 +478,11 @@ Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass
     w.lse = take(pass == XentPass::kStep ? (size_t)n * 4 : 0);
   }
   if (pass != XentPass::kForward) {
+    // fp32 logits become dz where they are; bf16 exponentials too (a step without db)
+    const bool kept = pass == XentPass::kStep && keeps(C, bf16);
     w.dz = take(packed_bytes(w.rows, V, !bf16));
     w.dz32 = take(bf16 ? 0 : (size_t)w.rows * V * 4);
+    w.kept = take(bf16 && kept ? (size_t)w.rows * w.width * 4 : 0);
     w.sums = take((size_t)(w.rows / 64 + 4) * V * 4);
     w.acc = take(w.pieces > 1 ? (size_t)V * C * 4 : 0);
     w.partial_bytes = std::max(partial_bytes(w.rows, C, V), partial_bytes(V, C, w.rows));
@@ -365,15 +494,23 @@ Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass
 
 char* byte(void* ws, size_t at) { return static_cast<char*>(ws) + at; }
 
-#define SHC_LAUNCH(expr)                   \
+#define SHC_LAUNCH(...)                    \
   do {                                     \
-    const hipError_t _e = (expr);          \
+    const hipError_t _e = (__VA_ARGS__);   \
     if (_e != hipSuccess) return _e;       \
   } while (0)
 
-template <class S, int PAIRS, bool GRAD>
+enum class Logit { kStats, kStatsExps, kStatsLogits, kGrad };
+template <class S, int PAIRS, Logit WHAT>
 hipError_t run_logits(const Logits& a, hipStream_t stream) {
-  auto kern = GRAD ? logit_grad_kernel<S, PAIRS> : logit_stats_kernel<S, PAIRS>;
+  constexpr Keep keep = WHAT == Logit::kStatsExps     ? kExps
+                        : WHAT == Logit::kStatsLogits ? kLogits
+                                                      : kNothing;
+  void (*kern)(Logits);
+  if constexpr (WHAT == Logit::kGrad)
+    kern = logit_grad_kernel<S, PAIRS>;
+  else
+    kern = logit_stats_kernel<S, PAIRS, keep>;
   static std::once_flag once;
   static hipError_t attr = hipSuccess;
   std::call_once(once, [&] {
@@ -386,7 +523,7 @@ hipError_t run_logits(const Logits& a, hipStream_t stream) {
 }
 
 // `kind` receives the tile that was taken.
-template <bool GRAD>
+template <Logit WHAT>
 hipError_t launch_logits(Logits a, bool bf16, TileKind* kind, hipStream_t stream) {
   TileKind k = plan_product(a.rows, a.labels.V, a.C, bf16 ? 1 : kPairs, true, 0).kind;
   if (k == TileKind::k32 && a.rows > 64) k = TileKind::k64;  // sums: 64 rows to a part
@@ -397,8 +534,18 @@ hipError_t launch_logits(Logits a, bool bf16, TileKind* kind, hipStream_t stream
   a.tm = (int)tm, a.tn = (int)tn;
   return with_tile(k, [&](auto shape) {
     using S = decltype(shape);
-    return bf16 ? run_logits<S, 1, GRAD>(a, stream) : run_logits<S, kPairs, GRAD>(a, stream);
+    if constexpr (WHAT == Logit::kStatsExps)
+      return run_logits<S, 1, WHAT>(a, stream);
+    else
+      return bf16 ? run_logits<S, 1, WHAT>(a, stream) : run_logits<S, kPairs, WHAT>(a, stream);
   });
+}
+
+template <bool BF16, Keep KEEP>
+hipError_t launch_from_kept(const FromKept& a, hipStream_t stream) {
+  const dim3 grid((unsigned)((a.rows + 63) / 64), (a.dz_width + 511) / 512);
+  from_kept_kernel<BF16, KEEP><<<grid, 256, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -484,16 +631,22 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
   g.bias = a.bias;
   g.labels = labels;
   TileKind kind;
-  if (pass != XentPass::kBackward) {  // 3. statistics, loss and lse
+  g.parts = reinterpret_cast<float2*>(byte(a.ws, w.parts));
+  g.at_label = reinterpret_cast<float*>(byte(a.ws, w.at_label));
+  const auto join = [&](int64_t row0, int64_t rows) {
+    join_stats_kernel<<<(int)((rows + 15) / 16), 256, 0, stream>>>(
+        g.parts, (a.V + tile_n(kind) - 1) / tile_n(kind), rows, count, row0, idx + row0,
+        g.at_label, a.loss, lse);
+    return hipGetLastError();
+  };
+  const bool products = a.dx != nullptr || a.dW != nullptr;
+  const bool keep =
+      pass == XentPass::kStep && keeps(a.C, a.bf16) && (products || a.db != nullptr);
+  if (pass != XentPass::kBackward && !keep) {  // 3. statistics, loss and lse
     g.A = x_of(0, a.n, true);
     g.rows = a.n, g.row0 = 0, g.idx = idx;
-    g.parts = reinterpret_cast<float2*>(byte(a.ws, w.parts));
-    g.at_label = reinterpret_cast<float*>(byte(a.ws, w.at_label));
-    SHC_LAUNCH(launch_logits<false>(g, a.bf16, &kind, stream));
-    join_stats_kernel<<<(int)((a.n + 15) / 16), 256, 0, stream>>>(
-        g.parts, (a.V + tile_n(kind) - 1) / tile_n(kind), a.n, count, idx, g.at_label, a.loss,
-        lse);
-    SHC_LAUNCH(hipGetLastError());
+    SHC_LAUNCH(launch_logits<Logit::kStats>(g, a.bf16, &kind, stream));
+    SHC_LAUNCH(join(0, a.n));
   }
   if (!grads) return hipSuccess;
   // 4. gradients, a piece of the live rows at a time
@@ -509,14 +662,28 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
     g.ld_dz = dz_ld;
     g.width = (int)dz_ld;
     g.sums = a.db != nullptr ? reinterpret_cast<float*>(byte(a.ws, w.sums)) : nullptr;
-    SHC_LAUNCH(launch_logits<true>(g, a.bf16, &kind, stream));
+    int per = 64;  // rows to a part of the sums
+    if (keep) {
+      const bool exps = a.bf16 && a.db == nullptr;
+      g.kept = a.bf16 && !exps ? byte(a.ws, w.kept) : g.dz;
+      SHC_LAUNCH(exps ? launch_logits<Logit::kStatsExps>(g, a.bf16, &kind, stream)
+                      : launch_logits<Logit::kStatsLogits>(g, a.bf16, &kind, stream));
+      SHC_LAUNCH(join(row0, rows));
+      const FromKept f{g.kept, rows, count, row0, g.parts, tile_n(kind), labels, g.idx, lse,
+                       a.weight, g.dz, (int)dz_ld, (int)dz_ld, g.sums};
+      SHC_LAUNCH(exps     ? launch_from_kept<true, kExps>(f, stream)
+                 : a.bf16 ? launch_from_kept<true, kLogits>(f, stream)
+                          : launch_from_kept<false, kLogits>(f, stream));
+    } else {
+      SHC_LAUNCH(launch_logits<Logit::kGrad>(g, a.bf16, &kind, stream));
+      per = kind == TileKind::k256 ? 128 : kind == TileKind::k32 ? 32 : 64;
+    }
     if (a.db != nullptr) {
-      const int per = kind == TileKind::k256 ? 128 : kind == TileKind::k32 ? 32 : 64;
       join_sums_kernel<<<(a.V + 63) / 64, 1024, 0, stream>>>(g.sums, per, rows, count, row0, a.V,
                                                              piece > 0 || a.accumulate, a.db);
       SHC_LAUNCH(hipGetLastError());
     }
-    if (a.dx == nullptr && a.dW == nullptr) continue;
+    if (!products) continue;
     if (!a.bf16)
       SHC_LAUNCH(launch_pack(Pack{g.dz, dz_ld, rows, rows, a.V, 1, nullptr, count, row0, -1, dz},
                              stream));
