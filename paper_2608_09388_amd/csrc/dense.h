@@ -84,7 +84,7 @@ hipError_t launch_sum_rows(const float* parts, int64_t rows, int64_t ld, int32_t
                            float* out, hipStream_t stream);
 
 // Shape of the workgroups' tiles and parts along K for a product.
-enum class TileKind { k256, k128, k64, k32 };
+enum class TileKind { k256, k128, k64x128, k64, k32 };
 struct Plan {
   TileKind kind;
   int parts;
@@ -95,12 +95,18 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, int pairs, bool few_rows,
 
 using Shape256 = Shape<4, 2, 2, 4>;
 using Shape128 = Shape<2, 2, 2, 2>;
+using Shape64x128 = Shape<1, 2, 2, 2>;
 using Shape64 = Shape<2, 2, 1, 4>;
 using Shape32 = Shape<1, 2, 1, 4>;
-inline int tile_m(TileKind k) {
-  return k == TileKind::k256 ? 256 : k == TileKind::k128 ? 128 : k == TileKind::k64 ? 64 : 32;
+constexpr int tile_m(TileKind k) {
+  return k == TileKind::k256   ? Shape256::BM
+         : k == TileKind::k128 ? Shape128::BM
+         : k == TileKind::k32  ? Shape32::BM
+                               : Shape64::BM;
 }
-inline int tile_n(TileKind k) { return k == TileKind::k128 ? 128 : 256; }
+constexpr int tile_n(TileKind k) {
+  return k == TileKind::k128 || k == TileKind::k64x128 ? Shape128::BN : Shape256::BN;
+}
 
 // Calls f(shape) for the kind.
 template <typename F>
@@ -108,6 +114,7 @@ hipError_t with_tile(TileKind kind, F&& f) {
   switch (kind) {
     case TileKind::k256: return f(Shape256{});
     case TileKind::k128: return f(Shape128{});
+    case TileKind::k64x128: return f(Shape64x128{});
     case TileKind::k64: return f(Shape64{});
     default: return f(Shape32{});
   }

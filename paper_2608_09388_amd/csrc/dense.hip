@@ -7,6 +7,7 @@
 // plus what parts cost (their fp32 sums written and read back, a second launch).
 #include <algorithm>
 #include <mutex>
+#include <cstdlib>
 
 #include "dense.h"
 #include "dense_epilogue.h"
@@ -48,26 +49,34 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(Args a) {
   }
   const int KT = (int)((K + BK - 1) / BK), per = (KT + a.parts - 1) / a.parts;
   const int t0 = min(KT, (int)blockIdx.y * per), t1 = min(KT, t0 + per);
+  constexpr bool BF16 = PAIRS == 1;
   Tile<S, AROWS, BROWS, PAIRS> tile;
+  const auto fetch = [&](int64_t row, int64_t col) {
+    Fetched<BF16> g{};
+    if (a.parts == 1 && row < M && col < a.N)
+      g = fetch8<BF16>(a.store, row, (int)(col / 8), (int)a.N);
+    return g;
+  };
+  // small tiles have registers to fetch what the store needs before the product
+  Fetched<BF16> got[4];
+  if constexpr (S::MB == 1) tile.fetch_block(m0, n0, 0, got, fetch);
   tile.run(a.A, a.B, M, a.N, K, m0, n0, t0, t1, smem);
   if (a.parts > 1) {
     float* to = a.partials + (int64_t)blockIdx.y * a.M * a.N;
-    tile.each(m0, n0, [&](int64_t row, int64_t col, const float* v, int) {
-      if (row >= M) return;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (col + 8 * h < a.N)
-          rowops::store_channels<8>(to + row * a.N, (int)(col / 8) + h, (int)a.N, v + 8 * h);
+    tile.each(m0, n0, smem, [&](int64_t row, int64_t col, const float (&v)[8]) {
+      if (row < M && col < a.N)
+        rowops::store_channels<8>(to + row * a.N, (int)(col / 8), (int)a.N, v);
     });
     return;
   }
-  tile.each(m0, n0, [&](int64_t row, int64_t col, const float* v, int) {
-    if (row >= M) return;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (col + 8 * h < a.N) store8<PAIRS == 1>(a.store, row, (int)(col / 8) + h, (int)a.N,
-                                                v + 8 * h);
-  });
+  if constexpr (S::MB > 1) tile.fetch_block(m0, n0, 0, got, fetch);
+  float bias[8];
+  if (tile.col_of(n0) < a.N) bias8(a.store, (int)(tile.col_of(n0) / 8), (int)a.N, bias);
+  tile.each(m0, n0, smem, got, fetch,
+            [&](int64_t row, int64_t col, const float (&v)[8], const Fetched<BF16>& g) {
+              if (row < M && col < a.N)
+                store8<BF16>(a.store, row, (int)(col / 8), (int)a.N, v, bias, g);
+            });
 }
 
 // Sums the parts in order and stores: a thread to 8 columns of a row.
@@ -79,7 +88,9 @@ __global__ __launch_bounds__(256) void join_kernel(const float* parts, int n, in
   const int64_t row = at / nv;
   if (row >= rows_left(count, row0, M)) return;
   const int v = (int)(at - row * nv);
-  float sum[8], f[8];
+  float sum[8], f[8], bias[8];
+  bias8(st, v, N, bias);
+  const Fetched<BF16> g = fetch8<BF16>(st, row, v, N);
   const float* from = parts + row * N;
   rowops::load_channels<8>(from, v, N, sum);
   for (int p = 1; p < n; ++p) {
@@ -87,7 +98,7 @@ __global__ __launch_bounds__(256) void join_kernel(const float* parts, int n, in
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += f[e];
   }
-  store8<BF16>(st, row, v, N, sum);
+  store8<BF16>(st, row, v, N, sum, bias, g);
 }
 
 // 8 elements of a packed row to a thread.
@@ -188,9 +199,11 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, int pairs, bool few_rows,
   };
   static constexpr Kind kinds[] = {{TileKind::k256, 256, 1.9},
                                    {TileKind::k128, 512, 1.2},
+                                   {TileKind::k64x128, 768, 1.2},
                                    {TileKind::k64, 512, 1.4},
                                    {TileKind::k32, 512, 1.2}};
   const int64_t KT = (K + BK - 1) / BK;
+  if (const char* e = getenv("SHC_TILE")) { int v = atoi(e); return Plan{(TileKind)(v % 10), v / 10 > 0 ? v / 10 : 1}; }
   Plan best{TileKind::k128, 1};
   double least = 1e300;
   for (const Kind& k : kinds) {

@@ -1,6 +1,8 @@
 // Activations of the dense layers, their slopes, and the store of a product's values.
 #pragma once
 
+#include <type_traits>
+
 #include "dense.h"
 
 namespace shc {
@@ -71,9 +73,34 @@ __device__ __forceinline__ void put8(void* base, int64_t row, int64_t ld, int v,
     store_channels<8>(static_cast<float*>(base) + row * ld, v, N, f);
 }
 
+// What a store of 8 values of a row needs from memory, loaded ahead of it.
+template <bool BF16>
+struct Fetched {
+  typedef typename std::conditional<BF16, i32x4, float[8]>::type Raw;
+  Raw res;
+  int64_t to;
+};
+template <bool BF16>
+__device__ __forceinline__ Fetched<BF16> fetch8(const Store& s, int64_t row, int v, int N) {
+  Fetched<BF16> g;
+  g.to = s.to != nullptr ? (int64_t)s.to[row] : row;
+  if (s.res != nullptr) {
+    if constexpr (BF16)
+      g.res = rowops::load_vec<uint16_t>(
+          static_cast<const uint16_t*>(s.res) + g.to * s.ld_res, v, N);
+    else
+      rowops::load_channels<8>(static_cast<const float*>(s.res) + g.to * s.ld_res, v, N, g.res);
+  }
+  return g;
+}
+__device__ __forceinline__ void bias8(const Store& s, int v, int N, float (&b)[8]) {
+  if (s.bias != nullptr) rowops::load_channels<8>(s.bias, v, N, b);
+}
+
 template <bool BF16>
 __device__ __forceinline__ void store8(const Store& s, int64_t row, int v, int N,
-                                       const float* values) {
+                                       const float (&values)[8], const float (&bias)[8],
+                                       const Fetched<BF16>& g) {
   float f[8], x[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) f[e] = values[e];
@@ -87,22 +114,25 @@ __device__ __forceinline__ void store8(const Store& s, int64_t row, int v, int N
     return;
   }
   if (s.bias != nullptr) {
-    rowops::load_channels<8>(s.bias, v, N, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] += x[e];
+    for (int e = 0; e < 8; ++e) f[e] += bias[e];
   }
   if (s.pre != nullptr) put8<BF16>(s.pre, row, s.ld_pre, v, N, f);
   if (s.act != kActNone) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = act_of(s.act, f[e]);
   }
-  const int64_t to = s.to != nullptr ? (int64_t)s.to[row] : row;
   if (s.res != nullptr) {
-    load8<BF16>(s.res, to, s.ld_res, v, N, x);
+    if constexpr (BF16) {
+      rowops::Row<uint16_t>::widen(g.res, x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = g.res[e];
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] += x[e];
   }
-  put8<BF16>(s.out, to, s.ld_out, v, N, f);
+  put8<BF16>(s.out, g.to, s.ld_out, v, N, f);
 }
 
 }  // namespace dense

@@ -29,8 +29,9 @@
 // read: 16 lanes give the addresses of 4 x 16 elements and each gets a column.
 //
 // The products run transposed (D^T = B A^T): a lane holds columns 8 b + 4 (lane / 32)
-// + e of row lane % 32 of a 32 x 32 block; the halves of the wavefront exchange them at
-// the end, after which a lane has 16 adjacent columns.
+// + e of row lane % 32 of a 32 x 32 block.  At the end they pass through LDS, 32 rows of
+// the wavefront's 64 columns at a time, so that 8 lanes have 64 adjacent columns of a
+// row: stores, and loads of a residual, are of whole 128 bytes.
 //
 // Loads past the ends give zeros: a buffer descriptor covers exactly the rows that
 // are there, and chunks past a row's end get an offset outside of it.  Operands
@@ -263,8 +264,8 @@ struct Tile {
     // Waits and barriers in one asm block each: no access to LDS moves across.
     const int steps = PAIRS * (t1 - t0);
     load(0);
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     if (steps > 1) load(1);
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     read(a0, b0, 0, 0);
     int buf = 0;
     for (int t = 0; t < steps; ++t) {
@@ -313,31 +314,73 @@ struct Tile {
       }
   }
 
-  // f(row of D, first column, 16 adjacent values, block of columns) for what the lane holds.
-  template <typename F>
-  __device__ __forceinline__ void each(int64_t m0, int64_t n0, F&& f) const {
+  // What the lane stores of block i: rows of D and first column of row t of 4.
+  static __device__ __forceinline__ int64_t row_of(int64_t m0, int i, int t) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t row = m0 + (w / S::WN) * 32 * MB + (lane & 31);
-    const int64_t col = n0 + (w % S::WN) * 32 * NB + (lane >> 5) * 16;
+    return m0 + (w / S::WN) * 32 * MB + 32 * i + 8 * t + (lane >> 3);
+  }
+  static __device__ __forceinline__ int64_t col_of(int64_t n0) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    return n0 + (w % S::WN) * 64 + (lane & 7) * 8;
+  }
+  // g[t] = fetch(row, column) of block i
+  template <typename G, typename Fetch>
+  static __device__ __forceinline__ void fetch_block(int64_t m0, int64_t n0, int i, G (&g)[4],
+                                                     Fetch&& fetch) {
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+    for (int t = 0; t < 4; ++t) g[t] = fetch(row_of(m0, i, t), col_of(n0));
+  }
+  // f(row of D, first column, 8 adjacent values, what was fetched for them): lane l has
+  // 8 (l % 8) of the wavefront's 64 columns, rows l / 8 and 8 on.  Through 8 KB of smem
+  // a wavefront, 16 chunks of 16 bytes to a row, placed by the row's number.  `got` is
+  // block 0's; each next block's is fetched before the block at hand is stored, where
+  // there are registers for both.
+  template <typename G, typename Fetch, typename F>
+  __device__ __forceinline__ void each(int64_t m0, int64_t n0, char* smem, G (&got)[4],
+                                       Fetch&& fetch, F&& f) const {
+    static_assert(NB == 2 && S::NW * 8192 <= S::LDS, "64 columns to a wavefront");
+    const int lane = threadIdx.x & 63;
+    char* mine = smem + (threadIdx.x >> 6) * 8192;
+    const int r = lane & 31, h = lane >> 5, r8 = lane >> 3, q = lane & 7;
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        // register 4 b + e: column 8 b + 4 (lane / 32) + e.  The upper half's columns of
-        // b = 0, 1 for the lower half's of b = 2, 3.
-        float v[16];
+    for (int i = 0; i < MB; ++i) {
+      constexpr bool kAhead = sizeof(G) <= 24;
+      G next[4];
+      if (kAhead && i + 1 < MB) fetch_block(m0, n0, i + 1, next, fetch);
+      if (!kAhead && i > 0) fetch_block(m0, n0, i, got, fetch);
+      rowops::group_fence<64>();  // the reads of the rows before are over
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+      for (int j = 0; j < NB; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[i][j][4 * b + e]),
-                                                            __float_as_uint(acc[i][j][4 * b + 8 + e]),
-                                                            false, false);
-            v[8 * b + e] = __uint_as_float(x[0]);
-            v[8 * b + 4 + e] = __uint_as_float(x[1]);
-          }
-        f(row + 32 * i, col + 32 * j, v, j);
+        for (int b = 0; b < 4; ++b)
+          *reinterpret_cast<f32x4*>(mine + r * 256 + (((8 * j + 2 * b + h) ^ (r & 15)) * 16)) =
+              f32x4{acc[i][j][4 * b], acc[i][j][4 * b + 1], acc[i][j][4 * b + 2],
+                    acc[i][j][4 * b + 3]};
+      rowops::group_fence<64>();
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int at = 8 * t + r8;
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const f32x4 x =
+              *reinterpret_cast<const f32x4*>(mine + at * 256 + (((2 * q + u) ^ (at & 15)) * 16));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[4 * u + e] = x[e];
+        }
+        f(row_of(m0, i, t), col_of(n0), v, got[t]);
       }
+      if (kAhead && i + 1 < MB) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) got[t] = next[t];
+      }
+    }
+  }
+  template <typename F>  // with nothing to fetch
+  __device__ __forceinline__ void each(int64_t m0, int64_t n0, char* smem, F&& f) const {
+    int none[4];
+    each(m0, n0, smem, none, [](int64_t, int64_t) { return 0; },
+         [&](int64_t row, int64_t col, float (&v)[8], int) { f(row, col, v); });
   }
 };
 

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(GradRows a) {
 }
 
 // Lanes to a row and chunks of rows: up to 64 lanes, about four workgroups to a CU,
-// 64 rows to a chunk at least.
+// 16 rows to a chunk at least.
 struct GradShape {
   int G, cols;
   int64_t chunks, chunk;
@@ -90,7 +90,7 @@ GradShape grad_shape(int64_t n, int32_t C) {
   s.G = 8;
   while (s.G < 64 && s.G < nv) s.G *= 2;
   s.cols = (nv + s.G - 1) / s.G;
-  s.chunks = std::max<int64_t>(1, std::min<int64_t>((n + 63) / 64, std::max(1, 1024 / s.cols)));
+  s.chunks = std::max<int64_t>(1, std::min<int64_t>((n + 15) / 16, std::max(1, 1024 / s.cols)));
   s.chunk = std::max<int64_t>(1, (n + s.chunks - 1) / s.chunks);
   return s;
 }

@@ -75,10 +75,19 @@ __global__ __launch_bounds__(256) void count_labels_kernel(Labels l, int64_t n, 
   if (threadIdx.x == 0) counts[blockIdx.x] = total;
 }
 
+// What the epilogues need of the live rows, in their order.
+struct LiveRows {
+  int32_t* idx;
+  int32_t* label;
+  float* weight;
+  float* lse;
+};
+
 // The live rows in ascending order, their number, and the results of the others.
 __global__ __launch_bounds__(256) void list_rows_kernel(Labels l, int64_t n, const int32_t* counts,
-                                                        int32_t* idx, int32_t* count, float* loss,
-                                                        float* lse) {
+                                                        LiveRows rows, int32_t* count,
+                                                        const float* weight, const float* lse_in,
+                                                        float* loss, float* lse) {
   __shared__ int wave[4], before[4];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   int c = 0;
@@ -98,7 +107,10 @@ __global__ __launch_bounds__(256) void list_rows_kernel(Labels l, int64_t n, con
     int at = base + __popcll(mask & ((1ull << lane) - 1));
     for (int p = 0; p < w; ++p) at += wave[p];
     if (live) {
-      idx[at] = (int32_t)i;
+      rows.idx[at] = (int32_t)i;
+      rows.label[at] = (int32_t)l.get(i);
+      rows.weight[at] = weight != nullptr ? weight[i] : 1.f;
+      if (lse_in != nullptr) rows.lse[at] = lse_in[i];
     } else if (i < n) {
       if (loss != nullptr) loss[i] = 0.f;
       if (lse != nullptr) lse[i] = 0.f;
@@ -114,16 +126,14 @@ struct Logits {
   const int32_t* count;
   int64_t row0, full;
   const float* bias;
-  Labels labels;
-  const int32_t* idx;  // of the piece
+  int V;
+  LiveRows live;  // of the piece
   int tm, tn;
   // statistics
   float2* parts;  // [tn][rows]: maximum and sum over a tile's columns
   float* at_label;
   void* kept;  // [rows][width]
   // gradient
-  const float* lse;
-  const float* weight;
   void* dz;
   int64_t ld_dz;
   int width;
@@ -141,37 +151,52 @@ __device__ __forceinline__ bool logits_tile(Logits& a, Tile<S, true, true, PAIRS
   *M = a.A.extent = rows_left(a.count, a.row0, a.rows);
   if (*m0 >= *M) return false;
   if (a.A.alt != nullptr && *a.count != a.full) a.A.p = a.A.alt, a.A.ld = a.A.alt_ld;
-  tile.run(a.A, a.B, *M, a.labels.V, a.C, *m0, *n0, 0, (int)((a.C + BK - 1) / BK), smem);
+  tile.run(a.A, a.B, *M, a.V, a.C, *m0, *n0, 0, (int)((a.C + BK - 1) / BK), smem);
   return true;
 }
 
-// Over the two lanes that hold a row.
-template <typename Op>
-__device__ __forceinline__ float row_reduce(float x, Op op) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                  false);
-  return op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+// What is added to the products of 8 columns: the bias, -inf past the last.
+__device__ __forceinline__ void load_bias(float (&b)[8], const float* bias, int64_t col, int V) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) b[e] = col + e < V ? 0.f : -__builtin_inff();
+  if (bias != nullptr) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (col + e < V) b[e] = bias[col + e];
+  }
 }
 
-// 16 columns' logits in place: bias added, -inf past the last.
-__device__ __forceinline__ void finish_logits(float* z, const float* bias, int64_t col, int V) {
-  if (bias != nullptr) {
-    float b[16];
-    if (col + 16 <= V) {
-      rowops::load_channels<8>(bias + col, 0, 8, b);
-      rowops::load_channels<8>(bias + col, 1, 16, b + 8);
-    } else {
+// e^(z - by) of N logits in place, as one multiplication and addition before the
+// power of two: the rounding of by log2(e) is below that of by itself.  Past 2^100 (masks
+// of the type's lowest value) the difference is taken first.
+template <int N>
+__device__ __forceinline__ void exps_less(float (&z)[N], float by) {
+  if (fabsf(by) < 0x1p100f) {
+    const float scaled = -by * kLog2e;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) b[e] = col + e < V ? bias[col + e] : 0.f;
-    }
+    for (int e = 0; e < N; ++e) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], kLog2e, scaled));
+  } else {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) z[e] += b[e];
+    for (int e = 0; e < N; ++e) z[e] = __builtin_amdgcn_exp2f((z[e] - by) * kLog2e);
   }
-  if (col + 16 > V) {
+}
+
+// dz of N logits, y the label less the first one's column.  lse = -inf: a row of nothing
+// but -inf, whose probabilities are 0.
+template <int N>
+__device__ __forceinline__ void grad_of(float (&z)[N], int y, float lse, float w) {
+  if (lse == -__builtin_inff()) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (col + e >= V) z[e] = -__builtin_inff();
+    for (int e = 0; e < N; ++e) z[e] = 0.f;
+  } else {
+    exps_less(z, lse);
   }
+  if (y >= 0 && y < N) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] = y == e ? z[e] - 1.f : z[e];
+  }
+#pragma unroll
+  for (int e = 0; e < N; ++e) z[e] *= w;
 }
 
 // (m, s) with s = sum of e^(z - m): a maximum of -inf stands for 0 in the differences, so
@@ -194,26 +219,32 @@ __global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
   int64_t m0, n0, M;
   int tn;
   if (!logits_tile<S, PAIRS>(a, tile, &m0, &n0, &M, &tn, smem)) return;
-  // LDS is free: the last step's reads are behind the tile's last barrier
-  constexpr int BLOCKS = S::BN / 32;
-  float* most = reinterpret_cast<float*>(smem);  // [BLOCKS][BM]
+  // per row and 64 columns, behind what the tile passes its sums through
+  constexpr int BLOCKS = S::BN / 64;
+  static_assert(S::NW * 8192 + (2 * BLOCKS + 1) * S::BM * 4 <= S::LDS, "fits the tile's LDS");
+  float* most = reinterpret_cast<float*>(smem + S::NW * 8192);  // [BLOCKS][BM]
   float* sums = most + BLOCKS * S::BM;
-  const bool first = (threadIdx.x & 63) < 32;
-  tile.each(m0, n0, [&](int64_t row, int64_t col, float* z, int) {
-    finish_logits(z, a.bias, col, a.labels.V);
+  int32_t* label = reinterpret_cast<int32_t*>(sums + BLOCKS * S::BM);  // [BM]
+  for (int r = threadIdx.x; r < S::BM; r += S::THREADS)
+    label[r] = m0 + r < M ? a.live.label[m0 + r] : -1;
+  __syncthreads();
+  const bool first = (threadIdx.x & 7) == 0;
+  float bias[8];
+  load_bias(bias, a.bias, tile.col_of(n0), a.V);
+  tile.each(m0, n0, smem, [&](int64_t row, int64_t col, float (&z)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] += bias[e];
     float m = z[0];
 #pragma unroll
-    for (int e = 1; e < 16; ++e) m = fmaxf(m, z[e]);
-    m = row_reduce(m, rowops::MaxOp{});
-    if (first) most[(int)(col - n0) / 32 * S::BM + (int)(row - m0)] = m;
-    if (row < M) {
-      const int64_t y = a.labels.get(a.idx[row]) - col;
-      if (y >= 0 && y < 16) {
-        float at = z[0];
+    for (int e = 1; e < 8; ++e) m = fmaxf(m, z[e]);
+    m = rowops::lanes_reduce<8>(m, rowops::MaxOp{});
+    if (first) most[(int)(col - n0) / 64 * S::BM + (int)(row - m0)] = m;
+    const int y = label[(int)(row - m0)] - (int)col;
+    if (y >= 0 && y < 8) {
+      float at = z[0];
 #pragma unroll
-        for (int e = 1; e < 16; ++e) at = y == e ? z[e] : at;
-        a.at_label[row] = at;
-      }
+      for (int e = 1; e < 8; ++e) at = y == e ? z[e] : at;
+      a.at_label[row] = at;
     }
   });
   __syncthreads();
@@ -223,34 +254,27 @@ __global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
     for (int b = 1; b < BLOCKS; ++b) m = fmaxf(m, most[b * S::BM + r]);
     return m;
   };
-  tile.each(m0, n0, [&](int64_t row, int64_t col, float* z, int) {
-    finish_logits(z, a.bias, col, a.labels.V);
-    if constexpr (KEEP == kLogits) {
-      float* to = static_cast<float*>(a.kept) + row * a.width;
-      if (row < M && col < a.width) {
-        rowops::store_channels<8>(to + col, 0, a.width - (int)col, z);
-        if (col + 8 < a.width) rowops::store_channels<8>(to + col, 1, a.width - (int)col, z + 8);
-      }
-    }
-    const float f = finite_or_0(row_most((int)(row - m0)));
+  tile.each(m0, n0, smem, [&](int64_t row, int64_t col, float (&z)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] += bias[e];
+    const bool store = row < M && col < a.width;
+    if constexpr (KEEP == kLogits)
+      if (store)
+        rowops::store_channels<8>(static_cast<float*>(a.kept) + row * a.width, (int)(col / 8),
+                                  a.width, z);
+    exps_less(z, finite_or_0(row_most((int)(row - m0))));
     float s = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      z[e] = __builtin_amdgcn_exp2f((z[e] - f) * kLog2e);
-      s += z[e];
-    }
-    s = row_reduce(s, rowops::AddOp{});
-    if (first) sums[(int)(col - n0) / 32 * S::BM + (int)(row - m0)] = s;
+    for (int e = 0; e < 8; ++e) s += z[e];
+    s = rowops::lanes_reduce<8>(s, rowops::AddOp{});
+    if (first) sums[(int)(col - n0) / 64 * S::BM + (int)(row - m0)] = s;
     if constexpr (KEEP == kExps) {
       typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-      _Float16* to = static_cast<_Float16*>(a.kept) + row * a.width + col;
+      half8 x;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        half8 x;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (_Float16)(z[8 * h + e] * kExpScale);
-        if (row < M && col + 8 * h < a.width) *reinterpret_cast<half8*>(to + 8 * h) = x;
-      }
+      for (int e = 0; e < 8; ++e) x[e] = (_Float16)(z[e] * kExpScale);
+      if (store)
+        *reinterpret_cast<half8*>(static_cast<_Float16*>(a.kept) + row * a.width + col) = x;
     }
   });
   __syncthreads();
@@ -271,10 +295,8 @@ struct FromKept {
   int64_t row0;
   const float2* parts;
   int tile;  // columns of a tile of parts
-  Labels labels;
-  const int32_t* idx;
-  const float* lse;
-  const float* weight;
+  int V;
+  LiveRows live;
   void* dz;
   int width, dz_width;
   float* sums;  // [ceil(rows / 64)][V] or NULL
@@ -288,16 +310,15 @@ __global__ __launch_bounds__(256) void from_kept_kernel(FromKept a) {
   if (r0 >= live) return;
   const int64_t r1 = r0 + 64 < live ? r0 + 64 : live;
   const int v = blockIdx.y * 64 + lane, col = 8 * v;
-  const int V = a.labels.V;
+  const int V = a.V;
   float sum[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) sum[e] = 0.f;
   if (col < a.dz_width) {
 #pragma unroll 2
     for (int64_t row = r0 + w; row < r1; row += 4) {
-      const int64_t i = a.idx[row];
-      const float lse = a.lse[i], wt = a.weight != nullptr ? a.weight[i] : 1.f;
-      const int64_t y = a.labels.get(i) - col;
+      const float lse = a.live.lse[row], wt = a.live.weight[row];
+      const int y = a.live.label[row] - col;
       float z[8];
       if constexpr (KEEP == kExps) {
         typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -309,19 +330,23 @@ __global__ __launch_bounds__(256) void from_kept_kernel(FromKept a) {
                             : __builtin_amdgcn_exp2f((m - lse) * kLog2e) * (1.f / kExpScale);
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] = (float)x[e] * f;
+        if (y >= 0 && y < 8) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) z[e] = y == e ? z[e] - 1.f : z[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] *= wt;
       } else {
         rowops::load_channels<8>(static_cast<const float*>(a.kept) + row * a.width, v, a.width, z);
+        grad_of(z, y, lse, wt);
+      }
+      if (col + 8 > V) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          z[e] = lse == -__builtin_inff() ? 0.f
-                                          : __builtin_amdgcn_exp2f((z[e] - lse) * kLog2e);
+          if (col + e >= V) z[e] = 0.f;
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        z[e] = wt * (y == e ? z[e] - 1.f : z[e]);
-        if (col + e >= V) z[e] = 0.f;
-        sum[e] += z[e];
-      }
+      for (int e = 0; e < 8; ++e) sum[e] += z[e];
       put8<BF16>(a.dz, row, a.dz_width, v, a.dz_width, z);
     }
   }
@@ -341,7 +366,7 @@ __global__ __launch_bounds__(256) void from_kept_kernel(FromKept a) {
 // 16 rows to a workgroup, 16 threads to a row.
 __global__ __launch_bounds__(256) void join_stats_kernel(const float2* parts, int tiles,
                                                          int64_t rows, const int32_t* count,
-                                                         int64_t row0, const int32_t* idx,
+                                                         int64_t row0, LiveRows rows_live,
                                                          const float* at_label, float* loss,
                                                          float* lse) {
   __shared__ float2 part[16][16];
@@ -358,7 +383,8 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const float2* parts, in
   if (p != 0 || row >= live) return;
   for (int q = 1; q < 16; ++q) t = join(t, part[q][r]);
   const float l = t.x + __logf(t.y), z = at_label[row];
-  const int64_t to = idx[row];
+  const int64_t to = rows_live.idx[row];
+  rows_live.lse[row] = l;
   if (lse != nullptr) lse[to] = l;
   // a label on a logit of -inf, in a row of nothing but -inf too
   if (loss != nullptr) loss[to] = z == -__builtin_inff() && l == l ? -z : l - z;
@@ -371,44 +397,41 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
   int64_t m0, n0, M;
   int tn;
   if (!logits_tile<S, PAIRS>(a, tile, &m0, &n0, &M, &tn, smem)) return;
-  float sum[S::NB][16];
-#pragma unroll
-  for (int e = 0; e < 16 * S::NB; ++e) sum[e / 16][e % 16] = 0.f;
-  tile.each(m0, n0, [&](int64_t row, int64_t col, float* z, int j) {
-    if (row >= M) return;
-    finish_logits(z, a.bias, col, a.labels.V);
-    const int64_t i = a.idx[row];
-    const int64_t y = a.labels.get(i) - col;
-    const float lse = a.lse[i], w = a.weight != nullptr ? a.weight[i] : 1.f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      // lse = -inf: a row of nothing but -inf
-      const float q =
-          lse == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f((z[e] - lse) * kLog2e);
-      z[e] = w * (y == e ? q - 1.f : q);
-      if (col + e >= a.labels.V) z[e] = 0.f;
-      sum[j][e] += z[e];
+  // the rows' label, lse and weight, behind what the tile passes its sums through
+  static_assert(S::NW * 8192 + 3 * S::BM * 4 <= S::LDS, "fits the tile's LDS");
+  int32_t* label = reinterpret_cast<int32_t*>(smem + S::NW * 8192);
+  float* lse = reinterpret_cast<float*>(label + S::BM);
+  float* weight = lse + S::BM;
+  for (int r = threadIdx.x; r < S::BM; r += S::THREADS)
+    if (m0 + r < M) {
+      label[r] = a.live.label[m0 + r];
+      lse[r] = a.live.lse[m0 + r];
+      weight[r] = a.live.weight[m0 + r];
     }
+  __syncthreads();
+  float sum[8], bias[8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (col + 8 * h < a.width)
-        put8<PAIRS == 1>(a.dz, row, a.ld_dz, (int)(col / 8) + h, a.width, z + 8 * h);
+  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+  load_bias(bias, a.bias, tile.col_of(n0), a.V);
+  tile.each(m0, n0, smem, [&](int64_t row, int64_t col, float (&z)[8]) {
+    if (row >= M) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z[e] += bias[e];
+    const int r = (int)(row - m0);
+    grad_of(z, label[r] - (int)col, lse[r], weight[r]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += z[e];
+    if (col < a.width) put8<PAIRS == 1>(a.dz, row, a.ld_dz, (int)(col / 8), a.width, z);
   });
   if (a.sums == nullptr) return;
-  // over the tile's rows: the lane's, then the 32 lanes' of the same columns
+  // over the wavefront's rows: the lane's, then the lanes' of the same columns
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int64_t part = m0 / S::BM * S::WM + w / S::WN;
 #pragma unroll
-  for (int j = 0; j < S::NB; ++j) {
-    float mine = 0.f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float s = rowops::lanes_reduce<32>(sum[j][e], rowops::AddOp{});
-      mine = (lane & 31) == e ? s : mine;
-    }
-    const int64_t col = n0 + (w % S::WN * S::NB + j) * 32 + (lane >> 5) * 16 + (lane & 31);
-    if ((lane & 31) < 16 && col < a.labels.V) a.sums[part * a.labels.V + col] = mine;
-  }
+  for (int e = 0; e < 8; ++e) sum[e] = rowops::groups_sum<8>(sum[e]);
+  const int64_t col = n0 + (w % S::WN) * 64 + lane * 8;
+  if (lane < 8 && col < a.V)
+    rowops::store_channels<8>(a.sums + part * a.V, (int)(col / 8), a.V, sum);
 }
 
 // Column sums over the parts of the live rows, in order, added to what the pieces
@@ -448,7 +471,7 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(Labels l, int64_t n, con
 
 struct Layout {
   int64_t width, rows, pieces;  // columns of dz, rows and number of the pieces
-  size_t idx, count, counts, x, W, parts, at_label, lse, kept, dz, dz32, sums, acc, partials,
+  size_t idx, label, weight, lse, count, counts, x, W, parts, at_label, kept, dz, dz32, sums, acc, partials,
       partial_bytes, total;
 };
 
@@ -468,6 +491,9 @@ Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass
   w.rows = std::min<int64_t>(n, std::max<int64_t>(256, most / w.width / 256 * 256));
   w.pieces = n == 0 ? 0 : (n + w.rows - 1) / w.rows;
   w.idx = take((size_t)n * 4);
+  w.label = take((size_t)n * 4);
+  w.weight = take((size_t)n * 4);
+  w.lse = take((size_t)n * 4);
   w.count = take(4);
   w.counts = take((size_t)((n + kLabelsPerBlock - 1) / kLabelsPerBlock) * 4);
   w.x = take(packed_bytes(n, C, !bf16));
@@ -475,7 +501,6 @@ Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass
   if (pass != XentPass::kBackward) {
     w.parts = take((size_t)((V + 127) / 128) * n * 8);
     w.at_label = take((size_t)n * 4);
-    w.lse = take(pass == XentPass::kStep ? (size_t)n * 4 : 0);
   }
   if (pass != XentPass::kForward) {
     // fp32 logits become dz where they are; bf16 exponentials too (a step without db)
@@ -525,11 +550,11 @@ hipError_t run_logits(const Logits& a, hipStream_t stream) {
 // `kind` receives the tile that was taken.
 template <Logit WHAT>
 hipError_t launch_logits(Logits a, bool bf16, TileKind* kind, hipStream_t stream) {
-  TileKind k = plan_product(a.rows, a.labels.V, a.C, bf16 ? 1 : kPairs, true, 0).kind;
+  TileKind k = plan_product(a.rows, a.V, a.C, bf16 ? 1 : kPairs, true, 0).kind;
   if (k == TileKind::k32 && a.rows > 64) k = TileKind::k64;  // sums: 64 rows to a part
   *kind = k;
   const int64_t tm = (a.rows + tile_m(k) - 1) / tile_m(k);
-  const int64_t tn = (a.labels.V + tile_n(k) - 1) / tile_n(k);
+  const int64_t tn = (a.V + tile_n(k) - 1) / tile_n(k);
   if (tm * tn >= (int64_t)1 << 22) return hipErrorInvalidConfiguration;
   a.tm = (int)tm, a.tn = (int)tn;
   return with_tile(k, [&](auto shape) {
@@ -562,6 +587,11 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
   const bool grads = pass != XentPass::kForward;
   const Labels labels{a.labels, a.id64, a.label_stride, a.V};
   int32_t* idx = reinterpret_cast<int32_t*>(byte(a.ws, w.idx));
+  const auto live_from = [&](int64_t row0) {
+    return LiveRows{idx + row0, reinterpret_cast<int32_t*>(byte(a.ws, w.label)) + row0,
+                    reinterpret_cast<float*>(byte(a.ws, w.weight)) + row0,
+                    reinterpret_cast<float*>(byte(a.ws, w.lse)) + row0};
+  };
   int32_t* count = reinterpret_cast<int32_t*>(byte(a.ws, w.count));
   if (a.n == 0) {  // the parameters' gradients of no rows
     if (grads && !a.accumulate) {
@@ -579,12 +609,14 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
   // 1. the live rows
   const int blocks = (int)((a.n + kLabelsPerBlock - 1) / kLabelsPerBlock);
   int32_t* counts = reinterpret_cast<int32_t*>(byte(a.ws, w.counts));
-  float* lse = pass == XentPass::kStep ? reinterpret_cast<float*>(byte(a.ws, w.lse)) : a.lse;
-  count_labels_kernel<<<blocks, 256, 0, stream>>>(labels, a.n, counts);
-  SHC_LAUNCH(hipGetLastError());
-  list_rows_kernel<<<blocks, 256, 0, stream>>>(labels, a.n, counts, idx, count,
-                                               pass == XentPass::kBackward ? nullptr : a.loss,
-                                               pass == XentPass::kForward ? a.lse : nullptr);
+  if (blocks > 1) {
+    count_labels_kernel<<<blocks, 256, 0, stream>>>(labels, a.n, counts);
+    SHC_LAUNCH(hipGetLastError());
+  }
+  const bool back = pass == XentPass::kBackward;
+  list_rows_kernel<<<blocks, 256, 0, stream>>>(
+      labels, a.n, counts, live_from(0), count, a.weight, back ? a.lse : nullptr,
+      back ? nullptr : a.loss, pass == XentPass::kForward ? a.lse : nullptr);
   SHC_LAUNCH(hipGetLastError());
   const bool as_is = a.bf16 && direct(a.x, a.ldx, a.C);
   const int64_t xwidth = packed_width(a.C);
@@ -629,14 +661,14 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
   g.C = a.C;
   g.count = count, g.full = a.n;
   g.bias = a.bias;
-  g.labels = labels;
+  g.V = a.V;
   TileKind kind;
   g.parts = reinterpret_cast<float2*>(byte(a.ws, w.parts));
   g.at_label = reinterpret_cast<float*>(byte(a.ws, w.at_label));
   const auto join = [&](int64_t row0, int64_t rows) {
     join_stats_kernel<<<(int)((rows + 15) / 16), 256, 0, stream>>>(
-        g.parts, (a.V + tile_n(kind) - 1) / tile_n(kind), rows, count, row0, idx + row0,
-        g.at_label, a.loss, lse);
+        g.parts, (a.V + tile_n(kind) - 1) / tile_n(kind), rows, count, row0,
+        live_from(row0), g.at_label, a.loss, pass == XentPass::kForward ? a.lse : nullptr);
     return hipGetLastError();
   };
   const bool products = a.dx != nullptr || a.dW != nullptr;
@@ -644,20 +676,19 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
       pass == XentPass::kStep && keeps(a.C, a.bf16) && (products || a.db != nullptr);
   if (pass != XentPass::kBackward && !keep) {  // 3. statistics, loss and lse
     g.A = x_of(0, a.n, true);
-    g.rows = a.n, g.row0 = 0, g.idx = idx;
+    g.rows = a.n, g.row0 = 0, g.live = live_from(0);
     SHC_LAUNCH(launch_logits<Logit::kStats>(g, a.bf16, &kind, stream));
     SHC_LAUNCH(join(0, a.n));
   }
   if (!grads) return hipSuccess;
   // 4. gradients, a piece of the live rows at a time
-  g.lse = lse, g.weight = a.weight;
   const int64_t dz_ld = a.bf16 ? w.width : a.V;
   uint16_t* dz = reinterpret_cast<uint16_t*>(byte(a.ws, w.dz));
   float* acc = reinterpret_cast<float*>(byte(a.ws, w.acc));
   for (int64_t piece = 0; piece < w.pieces; ++piece) {
     const int64_t row0 = piece * w.rows, rows = std::min(w.rows, a.n - row0);
     g.A = x_of(row0, rows, true);
-    g.rows = rows, g.row0 = row0, g.idx = idx + row0;
+    g.rows = rows, g.row0 = row0, g.live = live_from(row0);
     g.dz = a.bf16 ? static_cast<void*>(dz) : byte(a.ws, w.dz32);
     g.ld_dz = dz_ld;
     g.width = (int)dz_ld;
@@ -669,8 +700,8 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
       SHC_LAUNCH(exps ? launch_logits<Logit::kStatsExps>(g, a.bf16, &kind, stream)
                       : launch_logits<Logit::kStatsLogits>(g, a.bf16, &kind, stream));
       SHC_LAUNCH(join(row0, rows));
-      const FromKept f{g.kept, rows, count, row0, g.parts, tile_n(kind), labels, g.idx, lse,
-                       a.weight, g.dz, (int)dz_ld, (int)dz_ld, g.sums};
+      const FromKept f{g.kept, rows, count, row0, g.parts, tile_n(kind), a.V, g.live, g.dz,
+                       (int)dz_ld, (int)dz_ld, g.sums};
       SHC_LAUNCH(exps     ? launch_from_kept<true, kExps>(f, stream)
                  : a.bf16 ? launch_from_kept<true, kLogits>(f, stream)
                           : launch_from_kept<false, kLogits>(f, stream));
