@@ -84,29 +84,26 @@ hipError_t launch_sum_rows(const float* parts, int64_t rows, int64_t ld, int32_t
                            float* out, hipStream_t stream);
 
 // Shape of the workgroups' tiles and parts along K for a product.
-enum class TileKind { k256, k128, k64x128, k64, k32 };
+enum class TileKind { k256, k128, k64, k32 };  // rows; columns: 256, else 128 (split: not the first)
 struct Plan {
   TileKind kind;
   int parts;
 };
 // few_rows: tiles of fewer than 128 rows too (operand A in rows).
-Plan plan_product(int64_t M, int64_t N, int64_t K, int pairs, bool few_rows,
+Plan plan_product(int64_t M, int64_t N, int64_t K, bool split, bool few_rows,
                   size_t partial_bytes);
 
 using Shape256 = Shape<4, 2, 2, 4>;
 using Shape128 = Shape<2, 2, 2, 2>;
-using Shape64x128 = Shape<1, 2, 2, 2>;
-using Shape64 = Shape<2, 2, 1, 4>;
-using Shape32 = Shape<1, 2, 1, 4>;
+using Shape64 = Shape<1, 2, 2, 2>;
+using Shape32 = Shape<1, 2, 1, 2>;
 constexpr int tile_m(TileKind k) {
   return k == TileKind::k256   ? Shape256::BM
          : k == TileKind::k128 ? Shape128::BM
-         : k == TileKind::k32  ? Shape32::BM
-                               : Shape64::BM;
+         : k == TileKind::k64  ? Shape64::BM
+                               : Shape32::BM;
 }
-constexpr int tile_n(TileKind k) {
-  return k == TileKind::k128 || k == TileKind::k64x128 ? Shape128::BN : Shape256::BN;
-}
+constexpr int tile_n(TileKind k) { return k == TileKind::k256 ? Shape256::BN : Shape128::BN; }
 
 // Calls f(shape) for the kind.
 template <typename F>
@@ -114,7 +111,6 @@ hipError_t with_tile(TileKind kind, F&& f) {
   switch (kind) {
     case TileKind::k256: return f(Shape256{});
     case TileKind::k128: return f(Shape128{});
-    case TileKind::k64x128: return f(Shape64x128{});
     case TileKind::k64: return f(Shape64{});
     default: return f(Shape32{});
   }

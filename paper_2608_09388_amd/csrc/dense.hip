@@ -7,7 +7,6 @@
 // plus what parts cost (their fp32 sums written and read back, a second launch).
 #include <algorithm>
 #include <mutex>
-#include <cstdlib>
 
 #include "dense.h"
 #include "dense_epilogue.h"
@@ -24,33 +23,31 @@ struct Args {
   int count_is_k;
   Store store;
   float* partials;
-  int parts, tm, tn;
+  int parts, tn;  // parts of K, columns of tiles
 };
 
-template <class S, bool AROWS, bool BROWS, int PAIRS>
+template <class S, bool AROWS, bool BROWS, bool SPLIT>
 __global__ __launch_bounds__(S::THREADS) void product_kernel(Args a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  int tm, tn;
-  tile_of(blockIdx.x, a.tm, a.tn, &tm, &tn);
-  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
   int64_t M = a.M, K = a.K;
   if (a.count != nullptr) {
     const int64_t left = rows_left(a.count, a.row0, a.count_is_k ? a.K : a.M);
-    if (a.count_is_k) {
+    if (a.count_is_k)
       K = a.A.k = a.B.k = left;
-    } else {
+    else
       M = a.A.extent = left;
-      if (m0 >= M) return;
-    }
     if (*a.count != a.full) {
       if (a.A.alt != nullptr) a.A.p = a.A.alt, a.A.ld = a.A.alt_ld;
       if (a.B.alt != nullptr) a.B.p = a.B.alt, a.B.ld = a.B.alt_ld;
     }
   }
+  int tm, tn;
+  if (!tile_of(blockIdx.x, (int)((M + S::BM - 1) / S::BM), a.tn, &tm, &tn)) return;
+  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
   const int KT = (int)((K + BK - 1) / BK), per = (KT + a.parts - 1) / a.parts;
   const int t0 = min(KT, (int)blockIdx.y * per), t1 = min(KT, t0 + per);
-  constexpr bool BF16 = PAIRS == 1;
-  Tile<S, AROWS, BROWS, PAIRS> tile;
+  constexpr bool BF16 = !SPLIT;
+  Tile<S, AROWS, BROWS, SPLIT> tile;
   const auto fetch = [&](int64_t row, int64_t col) {
     Fetched<BF16> g{};
     if (a.parts == 1 && row < M && col < a.N)
@@ -155,26 +152,27 @@ __global__ __launch_bounds__(1024) void sum_rows_kernel(const float* parts, int6
 
 constexpr int64_t kMostPartial = (int64_t)64 << 20;
 
-template <class S, bool AROWS, bool BROWS, int PAIRS>
-hipError_t run(const Args& a, hipStream_t stream) {
-  auto kern = product_kernel<S, AROWS, BROWS, PAIRS>;
+template <class S, bool AROWS, bool BROWS, bool SPLIT>
+hipError_t run(const Args& a, int tiles, hipStream_t stream) {
+  auto kern = product_kernel<S, AROWS, BROWS, SPLIT>;
+  constexpr int lds = S::template lds<SPLIT>();
   static std::once_flag once;
   static hipError_t attr = hipSuccess;
   std::call_once(once, [&] {
     attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   });
   if (attr != hipSuccess) return attr;
-  kern<<<dim3(a.tm * a.tn, a.parts), S::THREADS, S::LDS, stream>>>(a);
+  kern<<<dim3(tiles, a.parts), S::THREADS, lds, stream>>>(a);
   return hipGetLastError();
 }
 
-template <class S, int PAIRS>
-hipError_t run_orders(const Args& a, bool ar, bool br, hipStream_t stream) {
-  if constexpr (S::BM >= 128)
-    if (!ar && !br) return run<S, false, false, PAIRS>(a, stream);
-  if (ar && br) return run<S, true, true, PAIRS>(a, stream);
-  if (ar && !br) return run<S, true, false, PAIRS>(a, stream);
+template <class S, bool SPLIT>
+hipError_t run_orders(const Args& a, int tiles, bool ar, bool br, hipStream_t stream) {
+  if constexpr (S::BM >= 128)  // a cols operand has 128 rows at least
+    if (!ar && !br) return run<S, false, false, SPLIT>(a, tiles, stream);
+  if (ar && br) return run<S, true, true, SPLIT>(a, tiles, stream);
+  if (ar && !br) return run<S, true, false, SPLIT>(a, tiles, stream);
   return hipErrorInvalidValue;
 }
 
@@ -188,33 +186,47 @@ size_t partial_bytes(int64_t M, int64_t N, int64_t K) {
   return (size_t)(mn > kMostPartial / parts ? kMostPartial : mn * parts);
 }
 
-// Times in us.  A step is 64 of K in one workgroup's tile; workgroups of 256 x 256
-// have a CU to themselves, the others share it with one more.
-Plan plan_product(int64_t M, int64_t N, int64_t K, int pairs, bool few_rows,
+// Times in us, from the figures at the top.  A CU holds `slots` workgroups of a kind; a
+// step of 64 of K takes `latency` or, of as many as are there, `work` each; a tile has
+// `fixed` beside its steps.
+Plan plan_product(int64_t M, int64_t N, int64_t K, bool split, bool few_rows,
                   size_t partial_bytes) {
   struct Kind {
     TileKind kind;
     int slots;
-    double step;
+    double latency, work, fixed;
   };
-  static constexpr Kind kinds[] = {{TileKind::k256, 256, 1.9},
-                                   {TileKind::k128, 512, 1.2},
-                                   {TileKind::k64x128, 768, 1.2},
-                                   {TileKind::k64, 512, 1.4},
-                                   {TileKind::k32, 512, 1.2}};
+  static constexpr Kind plain[] = {{TileKind::k256, 1, 1.8, 1.8, 14.0},
+                                   {TileKind::k128, 2, 0.7, 0.51, 5.2},
+                                   {TileKind::k64, 3, 0.6, 0.34, 2.8},
+                                   {TileKind::k32, 4, 0.5, 0.25, 2.5}};
+  static constexpr Kind terms[] = {{TileKind::k128, 1, 2.8, 2.8, 8.0},
+                                   {TileKind::k64, 1, 2.0, 2.0, 5.0},
+                                   {TileKind::k32, 1, 1.6, 1.6, 4.0}};
+  constexpr int kCUs = 256;
   const int64_t KT = (K + BK - 1) / BK;
-  if (const char* e = getenv("SHC_TILE")) { int v = atoi(e); return Plan{(TileKind)(v % 10), v / 10 > 0 ? v / 10 : 1}; }
   Plan best{TileKind::k128, 1};
   double least = 1e300;
-  for (const Kind& k : kinds) {
+  const Kind* kinds = split ? terms : plain;
+  for (int i = 0; i < (split ? 3 : 4); ++i) {
+    const Kind& k = kinds[i];
     if (!few_rows && tile_m(k.kind) < 128) continue;
     const int64_t tiles = ((M + tile_m(k.kind) - 1) / tile_m(k.kind)) *
                           ((N + tile_n(k.kind) - 1) / tile_n(k.kind));
+    // few rows of tiles share what they read of B with few others: its 128 bytes of a
+    // step for every column come from memory, at 6.2 TB/s
+    const double read = tile_n(k.kind) * 128.0 * kCUs / 6.2e6 /
+                        (double)((M + tile_m(k.kind) - 1) / tile_m(k.kind)) * (split ? 3 : 1);
     for (int parts = 1; parts <= 64; parts = parts < 4 ? parts + 1 : parts + parts / 2) {
       if (parts > 1 && (KT < 2 * parts || (double)parts * M * N * 4 > (double)partial_bytes)) break;
-      const double rounds = (double)((tiles * parts + k.slots - 1) / k.slots);
-      const double steps = (double)((KT + parts - 1) / parts) * pairs;
-      double t = rounds * (steps * k.step + 2.0);
+      const int64_t rounds = tiles * parts / (kCUs * k.slots);
+      const int64_t rest = tiles * parts % (kCUs * k.slots);
+      const double steps = (double)((KT + parts - 1) / parts);
+      const auto round = [&](double here) {
+        return steps * std::max(k.latency, here * std::max(k.work, read)) + k.fixed;
+      };
+      double t = rounds * round(k.slots);
+      if (rest > 0) t += round((double)((rest + kCUs - 1) / kCUs));
       if (parts > 1) t += 4.0 + (double)parts * M * N * 8 / 4e6;
       if (t < least) least = t, best = {k.kind, parts};
     }
@@ -224,7 +236,7 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, int pairs, bool few_rows,
 
 hipError_t launch_product(const Product& p, hipStream_t stream) {
   if (p.M <= 0 || p.N <= 0) return hipSuccess;
-  Plan plan = plan_product(p.M, p.N, p.K, p.split ? kPairs : 1, p.a_rows,
+  Plan plan = plan_product(p.M, p.N, p.K, p.split, p.a_rows,
                            p.partials != nullptr ? p.partial_bytes : 0);
   Args a;
   a.A = p.A, a.B = p.B;
@@ -236,11 +248,14 @@ hipError_t launch_product(const Product& p, hipStream_t stream) {
   const int64_t tm = (p.M + tile_m(plan.kind) - 1) / tile_m(plan.kind);
   const int64_t tn = (p.N + tile_n(plan.kind) - 1) / tile_n(plan.kind);
   if (tm * tn >= (int64_t)1 << 22) return hipErrorInvalidConfiguration;
-  a.tm = (int)tm, a.tn = (int)tn;
+  a.tn = (int)tn;
+  const int tiles = (int)(tm * tn);
   hipError_t e = with_tile(plan.kind, [&](auto shape) {
     using S = decltype(shape);
-    return p.split ? run_orders<S, kPairs>(a, p.a_rows, p.b_rows, stream)
-                   : run_orders<S, 1>(a, p.a_rows, p.b_rows, stream);
+    if constexpr (S::BM <= 128)
+      if (p.split) return run_orders<S, true>(a, tiles, p.a_rows, p.b_rows, stream);
+    return p.split ? hipErrorInvalidValue
+                   : run_orders<S, false>(a, tiles, p.a_rows, p.b_rows, stream);
   });
   if (e != hipSuccess || plan.parts == 1) return e;
   const int64_t threads = p.M * ((p.N + 7) / 8);

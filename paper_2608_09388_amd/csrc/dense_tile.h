@@ -1,9 +1,9 @@
 // The matrix product of the dense layers (linear.hip, xent.hip): one workgroup's
 // tile of D = A B^T in fp32, from bf16 operands in either order,
 //
-//   D[m][n] = sum over p, k of A_p[m][k] B_p[n][k],
+//   D[m][n] = sum over k of A[m][k] B[n][k],
 //
-// p over the term pairs of split fp32 operands (one pair for bf16).  An operand's
+// or from fp32 operands as three bf16 terms each (`split`).  An operand's
 // element (r, k) is at r * ld + k ("rows": the sum runs along memory) or at
 // k * ld + r ("cols": it runs across rows), so that x W, dz W^T and x^T dz read
 // their tensors as they are.
@@ -28,6 +28,11 @@
 // contiguous kilobyte.  Fragments of a cols operand come from the transposing LDS
 // read: 16 lanes give the addresses of 4 x 16 elements and each gets a column.
 //
+// Split fp32: x = h + m + l, and of the nine products of terms the six largest, h h in
+// one sum and the others, at most 2^-7 of it, in a second.  The three planes of both
+// operands pass through LDS together, 32 of k at a time in three buffers, so that a
+// fragment is read once for its two or three products.
+//
 // The products run transposed (D^T = B A^T): a lane holds columns 8 b + 4 (lane / 32)
 // + e of row lane % 32 of a 32 x 32 block.  At the end they pass through LDS, 32 rows of
 // the wavefront's 64 columns at a time, so that 8 lanes have 64 adjacent columns of a
@@ -48,7 +53,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-constexpr int BK = 64;
+constexpr int BK = 64, BKS = 32;  // of k to a step; split
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct Operand {
@@ -66,32 +71,35 @@ struct Operand {
   const int32_t* idx;
 };
 
-// Term pairs of split fp32 products, the small ones first: terms of A and B in
-// two bits each.  (2, 2), (1, 2) and (2, 1) are below fp32's last place.
-constexpr int kPairs = 6;
-__device__ __forceinline__ int pair_a(int p) { return (0x012010 >> (4 * (5 - p))) & 0xF; }
-__device__ __forceinline__ int pair_b(int p) { return (0x210100 >> (4 * (5 - p))) & 0xF; }
-
 template <int MB_, int NB_, int WM_, int WN_>
 struct Shape {
   static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_;
   static constexpr int BM = 32 * MB * WM, BN = 32 * NB * WN, NW = WM * WN, THREADS = 64 * NW;
   static constexpr int LDS_A = BM * BK * 2, LDS_B = BN * BK * 2, STAGE = LDS_A + LDS_B;
-  static constexpr int LDS = 2 * STAGE;
+  // split: three planes of half a step in three buffers
+  static constexpr int SPLIT_A = BM * BKS * 2, SPLIT_B = BN * BKS * 2,
+                       SPLIT_STAGE = 3 * (SPLIT_A + SPLIT_B), SPLIT_BUFFERS = 3;
+  template <bool SPLIT>
+  static constexpr int lds() {
+    return SPLIT ? SPLIT_BUFFERS * SPLIT_STAGE : 2 * STAGE;
+  }
 };
 
-// What the place of a chunk in its row of LDS is XORed with: rows operand, 8 chunks
-// to row r (a read takes 16 rows at a time, two of them 256 bytes of banks); cols
-// operand, 16 or more chunks to row k (32 lanes have 64 bytes of 4 rows).
-__device__ __forceinline__ int rows_key(int r) { return (r >> 1) & 7; }
+// What the place of a chunk in its row of LDS is XORed with: rows operand, 8 chunks (or 4,
+// split) to row r (a read takes 16 rows at a time, two or four of them 256 bytes of
+// banks); cols operand, 16 or more chunks to row k (32 lanes have 64 bytes of 4 rows).
+template <int K>
+__device__ __forceinline__ int rows_key(int r) {
+  return K == 64 ? (r >> 1) & 7 : (r >> 2) & 3;
+}
 __device__ __forceinline__ int cols_key(int k) { return (k & 3) << 2; }
 
 // One operand's side of the tile.
-template <int R, bool ROWS, int NW>
+template <int R, bool ROWS, int NW, int K_>
 struct Side {
-  static constexpr int INSTR = R * BK * 2 / 1024;          // loads of a kilobyte
+  static constexpr int INSTR = R * K_ * 2 / 1024;  // loads of a kilobyte
   static constexpr int PER_WAVE = (INSTR + NW - 1) / NW;
-  const char* base;   // first element of the tile at k = 0 of the current pair
+  const char* base;   // first element of the tile at k = 0
   int64_t bytes;      // from there to the end of what the tile may read
   int64_t step;       // bytes from one k step to the next
   uint32_t off;       // the lane's byte offset of its first load
@@ -104,17 +112,19 @@ struct Side {
       base = reinterpret_cast<const char*>(o.p + r0 * o.ld);
       const int64_t left = o.extent - r0 < R ? o.extent - r0 : R;
       bytes = ((left - 1) * o.ld + o.k) * 2;
-      step = BK * 2;
-      const int r = w * 8 + (lane >> 3);
-      kl = ((lane & 7) ^ rows_key(r)) * 8;
+      constexpr int C = K_ / 8, RL = 64 / C;  // chunks of a row; rows of a load
+      static_assert(RL * NW % 16 == 0, "the key repeats");
+      step = K_ * 2;
+      const int r = w * RL + lane / C;
+      kl = ((lane % C) ^ rows_key<K_>(r)) * 8;
       off = (uint32_t)((r * o.ld + kl) * 2);
-      inc = (int32_t)(8 * NW * o.ld * 2);
+      inc = (int32_t)(RL * NW * o.ld * 2);
     } else {
       constexpr int S = R / 8, KR = 64 / S;  // chunks of a row; rows of a load
       base = reinterpret_cast<const char*>(o.p + r0);
       const int64_t left = o.extent - r0;    // a multiple of 8
       bytes = ((o.k - 1) * o.ld + left) * 2;
-      step = o.ld * BK * 2;
+      step = o.ld * K_ * 2;
       kl = w * KR + lane / S;
       static_assert(R >= 128, "16 chunks to a row");
       const int c = (lane % S) ^ cols_key(kl);
@@ -122,7 +132,7 @@ struct Side {
       inc = (int32_t)(KR * NW * o.ld * 2);
     }
   }
-  // loads k step kt (K elements in all) of the pair at `plane` bytes into lds
+  // loads step kt (K elements in all) of the plane `plane` bytes on into lds
   __device__ __forceinline__ void load(char* lds, int64_t plane, int kt, int64_t K, int w) const {
     const int64_t at = plane + kt * step;
     int64_t left = bytes - kt * step;
@@ -134,7 +144,7 @@ struct Side {
       if (INSTR % NW != 0 && i * NW + w >= INSTR) break;
       uint32_t o = off == 0xFFFFFFF0u ? off : off + i * inc;
       if constexpr (ROWS) {
-        if ((int64_t)kt * BK + kl >= K) o = 0xFFFFFFF0u;
+        if ((int64_t)kt * K_ + kl >= K) o = 0xFFFFFFF0u;
       } else {
         static_assert((64 / (R / 8) * NW) % 4 == 0 || INSTR <= NW, "the key repeats");
       }
@@ -152,7 +162,7 @@ __device__ __forceinline__ s16x4 read_transposed(const char* __restrict__ p) {
 }
 
 // Fragments of 32 rows by 16 k: lane l has row l % 32, k 8 (l / 32) to 8 (l / 32) + 7.
-template <int R, bool ROWS>
+template <int R, bool ROWS, int K_>
 struct Frags {
   int at;  // LDS byte offset of the lane in the first fragment; others by XOR
 
@@ -161,7 +171,7 @@ struct Frags {
     const int h = lane >> 5;
     if constexpr (ROWS) {
       const int r = r0 + (lane & 31);
-      at = r * 128 + ((h ^ rows_key(r)) * 16);
+      at = r * (K_ * 2) + ((h ^ rows_key<K_>(r)) * 16);
     } else {
       const int i = lane & 15, k = 8 * h + (i >> 2);
       const int c = r0 / 8 + ((lane >> 4) & 1) * 2 + ((i & 3) >> 1);
@@ -171,7 +181,7 @@ struct Frags {
   // rows 32 f on, k 16 s on
   __device__ __forceinline__ bf16x8 get(const char* lds, int f, int s) const {
     if constexpr (ROWS) {
-      return *reinterpret_cast<const bf16x8*>(lds + (at ^ (s * 32)) + f * 32 * 128);
+      return *reinterpret_cast<const bf16x8*>(lds + (at ^ (s * 32)) + f * 32 * (K_ * 2));
     } else {
       // 64 bytes a fragment; f & 3 meets the key's bits (r0 is a multiple of 32 MB or NB)
       const char* p = lds + (at ^ ((f & 3) * 64)) + (f >> 2) * 256 + s * 16 * R * 2;
@@ -187,6 +197,17 @@ struct Frags {
   }
 };
 
+// Waits until all but the last VM of the wavefront's loads and all of its LDS accesses
+// are done, then for the workgroup.  No access to memory moves across; the compiler
+// sees the wait and adds none of its own for what it covers.
+template <int VM>
+__device__ __forceinline__ void wait_and_sync() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((VM & 15) | (7 << 4) | ((VM >> 4) << 14));
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // Element (r, k) of a split operand as it was given; 0 outside of it.
 template <bool ROWS>
 __device__ __forceinline__ float original(const Operand& o, int64_t r, int64_t k, int64_t R,
@@ -201,44 +222,55 @@ __device__ __forceinline__ float original(const Operand& o, int64_t r, int64_t k
 // are scaled back.
 constexpr float kSplitScale = 0x1p24f, kSplitBack = 0x1p-48f;
 
-template <class S, bool AROWS, bool BROWS, int PAIRS>
+template <class S, bool AROWS, bool BROWS, bool SPLIT>
 struct Tile {
   static constexpr int MB = S::MB, NB = S::NB;
+  static constexpr int LDS = S::template lds<SPLIT>();
   f32x16 acc[MB][NB];
 
   // The tile at (m0, n0) of the M x N of which both operands hold enough rows,
-  // over steps [t0, t1) of 64 along K.  smem: S::LDS bytes at a multiple of 1024.
+  // over steps [t0, t1) of 64 along K.  smem: LDS bytes at a multiple of 1024.
   __device__ __forceinline__ void run(const Operand& A, const Operand& B, int64_t M, int64_t N,
                                       int64_t K, int64_t m0, int64_t n0, int t0, int t1,
                                       char* smem) {
-    const int lane = threadIdx.x & 63;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = w / S::WN, wn = w % S::WN;
-    Side<S::BM, AROWS, S::NW> sa;
-    Side<S::BN, BROWS, S::NW> sb;
-    sa.init(A, m0, w, lane);
-    sb.init(B, n0, w, lane);
-    Frags<S::BM, AROWS> fa;
-    Frags<S::BN, BROWS> fb;
-    fa.init(wm * 32 * MB, lane);
-    fb.init(wn * 32 * NB, lane);
+    clear(acc);
+    if (t0 >= t1) return;
+    if constexpr (SPLIT) {
+      run_split(A, B, m0, n0, t0 * (BK / BKS),
+                (int)min((int64_t)t1 * (BK / BKS), (K + BKS - 1) / BKS), smem);
+      again(A, B, M, N, K, row_of(m0, 0, 0) - ((threadIdx.x & 63) >> 3),
+            col_of(n0) - (threadIdx.x & 7) * 8, t0, t1);
+    } else {
+      run_plain(A, B, m0, n0, t0, t1, smem);
+    }
+  }
+
+  static __device__ __forceinline__ void clear(f32x16 (&a)[MB][NB]) {
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int j = 0; j < NB; ++j)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    if (t0 >= t1) return;
+        for (int e = 0; e < 16; ++e) a[i][j][e] = 0.f;
+  }
 
-    int lp = 0, lk = t0;  // the next step to load: its pair, and its place along K
+  __device__ __forceinline__ void run_plain(const Operand& A, const Operand& B, int64_t m0,
+                                            int64_t n0, int t0, int t1, char* smem) {
+    const int lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Side<S::BM, AROWS, S::NW, BK> sa;
+    Side<S::BN, BROWS, S::NW, BK> sb;
+    sa.init(A, m0, w, lane);
+    sb.init(B, n0, w, lane);
+    Frags<S::BM, AROWS, BK> fa;
+    Frags<S::BN, BROWS, BK> fb;
+    fa.init(w / S::WN * 32 * MB, lane);
+    fb.init(w % S::WN * 32 * NB, lane);
     const int64_t ka = A.k, kb = B.k;
-    const auto load = [&](int buf) {
+    const auto load = [&](int t, int buf) {
       char* to = smem + buf * S::STAGE;
-      const int64_t pa = PAIRS == 1 ? 0 : pair_a(lp) * A.plane * 2;
-      const int64_t pb = PAIRS == 1 ? 0 : pair_b(lp) * B.plane * 2;
-      sa.load(to, pa, lk, ka, w);
-      sb.load(to + S::LDS_A, pb, lk, kb, w);
-      if (++lk == t1 && PAIRS > 1) lk = t0, ++lp;
+      sa.load(to, 0, t, ka, w);
+      sb.load(to + S::LDS_A, 0, t, kb, w);
     };
     bf16x8 a0[MB][2], b0[NB][2], a1[MB][2], b1[NB][2];
     const auto read = [&](bf16x8(&a)[MB][2], bf16x8(&b)[NB][2], int buf, int h) {
@@ -261,25 +293,132 @@ struct Tile {
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j][s], a[i][s], acc[i][j], 0, 0,
                                                                 0);
     };
-    // Waits and barriers in one asm block each: no access to LDS moves across.
-    const int steps = PAIRS * (t1 - t0);
-    load(0);
-    if (steps > 1) load(1);
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    load(t0, 0);
+    if (t0 + 1 < t1) load(t0 + 1, 1);
+    wait_and_sync<0>();
     read(a0, b0, 0, 0);
     int buf = 0;
-    for (int t = 0; t < steps; ++t) {
+    for (int t = t0; t < t1; ++t) {
       read(a1, b1, buf, 1);
       multiply(a0, b0);
       __builtin_amdgcn_sched_barrier(0);  // the products are not moved behind the wait
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      if (t + 2 < steps) load(buf);
+      wait_and_sync<0>();
+      if (t + 2 < t1) load(t + 2, buf);
       buf ^= 1;
-      if (t + 1 < steps) read(a0, b0, buf, 0);
+      if (t + 1 < t1) read(a0, b0, buf, 0);
       multiply(a1, b1);
     }
-    if constexpr (PAIRS > 1)
-      again(A, B, M, N, K, m0 + wm * 32 * MB, n0 + wn * 32 * NB, t0, t1);
+  }
+
+  // Steps of 32 of k, their fragments read while the step before is multiplied; a load
+  // has two steps to arrive.
+  __device__ __forceinline__ void run_split(const Operand& A, const Operand& B, int64_t m0,
+                                            int64_t n0, int t0, int t1, char* smem) {
+    const int lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Side<S::BM, AROWS, S::NW, BKS> sa;
+    Side<S::BN, BROWS, S::NW, BKS> sb;
+    sa.init(A, m0, w, lane);
+    sb.init(B, n0, w, lane);
+    Frags<S::BM, AROWS, BKS> fa;
+    Frags<S::BN, BROWS, BKS> fb;
+    fa.init(w / S::WN * 32 * MB, lane);
+    fb.init(w % S::WN * 32 * NB, lane);
+    const int64_t ka = A.k, kb = B.k;
+    constexpr int BUFFERS = S::SPLIT_BUFFERS;
+    constexpr int LOADS = 3 * (decltype(sa)::PER_WAVE + decltype(sb)::PER_WAVE);
+    static_assert(decltype(sa)::INSTR % S::NW == 0 && decltype(sb)::INSTR % S::NW == 0,
+                  "every wavefront has as many loads");
+    const auto load = [&](int t) {
+      char* to = smem + (t - t0) % BUFFERS * S::SPLIT_STAGE;
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        sa.load(to + p * S::SPLIT_A, p * A.plane * 2, t, ka, w);
+        sb.load(to + 3 * S::SPLIT_A + p * S::SPLIT_B, p * B.plane * 2, t, kb, w);
+      }
+    };
+    f32x16 low[MB][NB];
+    clear(low);
+    bf16x8 a0[3][MB][2], b0[3][NB][2], a1[3][MB][2], b1[3][NB][2];
+    const auto read = [&](bf16x8(&a)[3][MB][2], bf16x8(&b)[3][NB][2], int t) {
+      const char* from = smem + (t - t0) % BUFFERS * S::SPLIT_STAGE;
+#pragma unroll
+      for (int p = 0; p < 3; ++p)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+            b[p][j][s] = fb.get(from + 3 * S::SPLIT_A + p * S::SPLIT_B, j, s);
+#pragma unroll
+          for (int i = 0; i < MB; ++i) a[p][i][s] = fa.get(from + p * S::SPLIT_A, i, s);
+        }
+    };
+    const auto multiply = [&](const bf16x8(&a)[3][MB][2], const bf16x8(&b)[3][NB][2]) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+          for (int q = 0; q < 3 - p; ++q)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+              for (int j = 0; j < NB; ++j) {
+                f32x16& to = p + q == 0 ? acc[i][j] : low[i][j];
+                to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[q][j][s], a[p][i][s], to, 0, 0, 0);
+              }
+    };
+    // Step t is in registers; t + 1 has arrived when all but the last step's loads have.
+    // The steady loop has no condition in it: past a branch the compiler waits for the
+    // reads that are under way.
+    const auto steady = [&](int t, bf16x8(&a)[3][MB][2], bf16x8(&b)[3][NB][2],
+                            bf16x8(&an)[3][MB][2], bf16x8(&bn)[3][NB][2]) {
+      wait_and_sync<LOADS*(BUFFERS - 2)>();
+      load(t + BUFFERS);
+      read(an, bn, t + 1);
+      multiply(a, b);
+      // one wavefront to a SIMD: loads and reads are issued between the products
+      constexpr int READS = 3 * 2 * (MB * (AROWS ? 1 : 2) + NB * (BROWS ? 1 : 2));
+      constexpr int PRODUCTS = 6 * 2 * MB * NB;
+#pragma unroll
+      for (int i = 0; i < READS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an LDS read
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);    // a product
+      }
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x10, 1, 0);  // a load
+        if (READS + i < PRODUCTS) __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto last = [&](int t, bf16x8(&a)[3][MB][2], bf16x8(&b)[3][NB][2],
+                          bf16x8(&an)[3][MB][2], bf16x8(&bn)[3][NB][2]) {
+      wait_and_sync<0>();
+      if (t + BUFFERS < t1) load(t + BUFFERS);
+      if (t + 1 < t1) read(an, bn, t + 1);
+      multiply(a, b);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int t = t0; t < t0 + BUFFERS && t < t1; ++t) load(t);
+    if (t0 + BUFFERS <= t1)
+      wait_and_sync<LOADS*(BUFFERS - 1)>();
+    else
+      wait_and_sync<0>();
+    read(a0, b0, t0);
+    int t = t0;
+    for (; t + 1 + BUFFERS < t1; t += 2) {
+      steady(t, a0, b0, a1, b1);
+      steady(t + 1, a1, b1, a0, b0);
+    }
+    for (; t < t1; t += 2) {
+      last(t, a0, b0, a1, b1);
+      if (t + 1 < t1) last(t + 1, a1, b1, a0, b0);
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[i][j] += low[i][j];
   }
 
   // Scales the sums of split products back.  Sums that are not finite (an infinity, a
@@ -338,7 +477,7 @@ struct Tile {
   template <typename G, typename Fetch, typename F>
   __device__ __forceinline__ void each(int64_t m0, int64_t n0, char* smem, G (&got)[4],
                                        Fetch&& fetch, F&& f) const {
-    static_assert(NB == 2 && S::NW * 8192 <= S::LDS, "64 columns to a wavefront");
+    static_assert(NB == 2 && S::NW * 8192 <= LDS, "64 columns to a wavefront");
     const int lane = threadIdx.x & 63;
     char* mine = smem + (threadIdx.x >> 6) * 8192;
     const int r = lane & 31, h = lane >> 5, r8 = lane >> 3, q = lane & 7;
@@ -384,16 +523,19 @@ struct Tile {
   }
 };
 
-// The tile of workgroup b of tm x tn: a contiguous range of tiles to an XCD, in
+// The tile of workgroup b of tm x tn, false past them (tm counts the live rows' tiles,
+// so that these spread evenly): a contiguous range of tiles to an XCD, in
 // bands of kBand rows of tiles taken column by column, so that the tiles an XCD
 // works on at a time share rows of both operands in its L2.
 constexpr int kBand = 4;
-__device__ __forceinline__ void tile_of(int b, int tm, int tn, int* m, int* n) {
+__device__ __forceinline__ bool tile_of(int b, int tm, int tn, int* m, int* n) {
+  if (b >= tm * tn) return false;
   const int t = xcd_tile(b, tm * tn);
   const int band = t / (kBand * tn), rows = min(tm - band * kBand, kBand);
   const int r = t - band * kBand * tn;
   *m = band * kBand + r % rows;
   *n = r / rows;
+  return true;
 }
 
 // Rows that a device count leaves of `all` from row0 on (count NULL: all).

@@ -141,15 +141,14 @@ struct Logits {
 };
 
 // The logits of a tile: M rows are live.  False where none is.
-template <class S, int PAIRS>
-__device__ __forceinline__ bool logits_tile(Logits& a, Tile<S, true, true, PAIRS>& tile,
+template <class S, bool SPLIT>
+__device__ __forceinline__ bool logits_tile(Logits& a, Tile<S, true, true, SPLIT>& tile,
                                             int64_t* m0, int64_t* n0, int64_t* M, int* tn,
                                             char* smem) {
-  int tm;
-  tile_of(blockIdx.x, a.tm, a.tn, &tm, tn);
-  *m0 = (int64_t)tm * S::BM, *n0 = (int64_t)*tn * S::BN;
   *M = a.A.extent = rows_left(a.count, a.row0, a.rows);
-  if (*m0 >= *M) return false;
+  int tm;
+  if (!tile_of(blockIdx.x, (int)((*M + S::BM - 1) / S::BM), a.tn, &tm, tn)) return false;
+  *m0 = (int64_t)tm * S::BM, *n0 = (int64_t)*tn * S::BN;
   if (a.A.alt != nullptr && *a.count != a.full) a.A.p = a.A.alt, a.A.ld = a.A.alt_ld;
   tile.run(a.A, a.B, *M, a.V, a.C, *m0, *n0, 0, (int)((a.C + BK - 1) / BK), smem);
   return true;
@@ -212,16 +211,17 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 enum Keep { kNothing, kExps, kLogits };
 constexpr float kExpScale = 32768.f;
 
-template <class S, int PAIRS, Keep KEEP>
+template <class S, bool SPLIT, Keep KEEP>
 __global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  Tile<S, true, true, PAIRS> tile;
+  Tile<S, true, true, SPLIT> tile;
   int64_t m0, n0, M;
   int tn;
-  if (!logits_tile<S, PAIRS>(a, tile, &m0, &n0, &M, &tn, smem)) return;
+  if (!logits_tile<S, SPLIT>(a, tile, &m0, &n0, &M, &tn, smem)) return;
   // per row and 64 columns, behind what the tile passes its sums through
   constexpr int BLOCKS = S::BN / 64;
-  static_assert(S::NW * 8192 + (2 * BLOCKS + 1) * S::BM * 4 <= S::LDS, "fits the tile's LDS");
+  static_assert(S::NW * 8192 + (2 * BLOCKS + 1) * S::BM * 4 <= S::template lds<SPLIT>(),
+                "fits the tile's LDS");
   float* most = reinterpret_cast<float*>(smem + S::NW * 8192);  // [BLOCKS][BM]
   float* sums = most + BLOCKS * S::BM;
   int32_t* label = reinterpret_cast<int32_t*>(sums + BLOCKS * S::BM);  // [BM]
@@ -390,15 +390,16 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const float2* parts, in
   if (loss != nullptr) loss[to] = z == -__builtin_inff() && l == l ? -z : l - z;
 }
 
-template <class S, int PAIRS>
+template <class S, bool SPLIT>
 __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  Tile<S, true, true, PAIRS> tile;
+  Tile<S, true, true, SPLIT> tile;
   int64_t m0, n0, M;
   int tn;
-  if (!logits_tile<S, PAIRS>(a, tile, &m0, &n0, &M, &tn, smem)) return;
+  if (!logits_tile<S, SPLIT>(a, tile, &m0, &n0, &M, &tn, smem)) return;
   // the rows' label, lse and weight, behind what the tile passes its sums through
-  static_assert(S::NW * 8192 + 3 * S::BM * 4 <= S::LDS, "fits the tile's LDS");
+  static_assert(S::NW * 8192 + 3 * S::BM * 4 <= S::template lds<SPLIT>(),
+                "fits the tile's LDS");
   int32_t* label = reinterpret_cast<int32_t*>(smem + S::NW * 8192);
   float* lse = reinterpret_cast<float*>(label + S::BM);
   float* weight = lse + S::BM;
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
     grad_of(z, label[r] - (int)col, lse[r], weight[r]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += z[e];
-    if (col < a.width) put8<PAIRS == 1>(a.dz, row, a.ld_dz, (int)(col / 8), a.width, z);
+    if (col < a.width) put8<!SPLIT>(a.dz, row, a.ld_dz, (int)(col / 8), a.width, z);
   });
   if (a.sums == nullptr) return;
   // over the wavefront's rows: the lane's, then the lanes' of the same columns
@@ -508,7 +509,7 @@ Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass
     w.dz = take(packed_bytes(w.rows, V, !bf16));
     w.dz32 = take(bf16 ? 0 : (size_t)w.rows * V * 4);
     w.kept = take(bf16 && kept ? (size_t)w.rows * w.width * 4 : 0);
-    w.sums = take((size_t)(w.rows / 64 + 4) * V * 4);
+    w.sums = take((size_t)(w.rows / 32 + 4) * V * 4);  // 32 rows to a part at least
     w.acc = take(w.pieces > 1 ? (size_t)V * C * 4 : 0);
     w.partial_bytes = std::max(partial_bytes(w.rows, C, V), partial_bytes(V, C, w.rows));
     w.partials = take(w.partial_bytes);
@@ -526,32 +527,32 @@ char* byte(void* ws, size_t at) { return static_cast<char*>(ws) + at; }
   } while (0)
 
 enum class Logit { kStats, kStatsExps, kStatsLogits, kGrad };
-template <class S, int PAIRS, Logit WHAT>
+template <class S, bool SPLIT, Logit WHAT>
 hipError_t run_logits(const Logits& a, hipStream_t stream) {
   constexpr Keep keep = WHAT == Logit::kStatsExps     ? kExps
                         : WHAT == Logit::kStatsLogits ? kLogits
                                                       : kNothing;
   void (*kern)(Logits);
   if constexpr (WHAT == Logit::kGrad)
-    kern = logit_grad_kernel<S, PAIRS>;
+    kern = logit_grad_kernel<S, SPLIT>;
   else
-    kern = logit_stats_kernel<S, PAIRS, keep>;
+    kern = logit_stats_kernel<S, SPLIT, keep>;
+  constexpr int lds = S::template lds<SPLIT>();
   static std::once_flag once;
   static hipError_t attr = hipSuccess;
   std::call_once(once, [&] {
     attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   });
   if (attr != hipSuccess) return attr;
-  kern<<<a.tm * a.tn, S::THREADS, S::LDS, stream>>>(a);
+  kern<<<a.tm * a.tn, S::THREADS, lds, stream>>>(a);
   return hipGetLastError();
 }
 
 // `kind` receives the tile that was taken.
 template <Logit WHAT>
 hipError_t launch_logits(Logits a, bool bf16, TileKind* kind, hipStream_t stream) {
-  TileKind k = plan_product(a.rows, a.V, a.C, bf16 ? 1 : kPairs, true, 0).kind;
-  if (k == TileKind::k32 && a.rows > 64) k = TileKind::k64;  // sums: 64 rows to a part
+  const TileKind k = plan_product(a.rows, a.V, a.C, !bf16, true, 0).kind;
   *kind = k;
   const int64_t tm = (a.rows + tile_m(k) - 1) / tile_m(k);
   const int64_t tn = (a.V + tile_n(k) - 1) / tile_n(k);
@@ -559,10 +560,9 @@ hipError_t launch_logits(Logits a, bool bf16, TileKind* kind, hipStream_t stream
   a.tm = (int)tm, a.tn = (int)tn;
   return with_tile(k, [&](auto shape) {
     using S = decltype(shape);
-    if constexpr (WHAT == Logit::kStatsExps)
-      return run_logits<S, 1, WHAT>(a, stream);
-    else
-      return bf16 ? run_logits<S, 1, WHAT>(a, stream) : run_logits<S, kPairs, WHAT>(a, stream);
+    if constexpr (WHAT != Logit::kStatsExps && S::BM <= 128)
+      if (!bf16) return run_logits<S, true, WHAT>(a, stream);
+    return bf16 ? run_logits<S, false, WHAT>(a, stream) : hipErrorInvalidValue;
   });
 }
 
@@ -707,7 +707,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
                           : launch_from_kept<false, kLogits>(f, stream));
     } else {
       SHC_LAUNCH(launch_logits<Logit::kGrad>(g, a.bf16, &kind, stream));
-      per = kind == TileKind::k256 ? 128 : kind == TileKind::k32 ? 32 : 64;
+      per = kind == TileKind::k256 ? 128 : kind == TileKind::k128 ? 64 : 32;  // a wavefront's
     }
     if (a.db != nullptr) {
       join_sums_kernel<<<(a.V + 63) / 64, 1024, 0, stream>>>(g.sums, per, rows, count, row0, a.V,
