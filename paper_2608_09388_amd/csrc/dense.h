@@ -89,9 +89,10 @@ struct Plan {
   TileKind kind;
   int parts;
 };
-// few_rows: tiles of fewer than 128 rows too (operand A in rows).
+// few_rows: tiles of fewer than 128 rows too (operand A in rows); logits: the epilogues
+// of xent.hip.
 Plan plan_product(int64_t M, int64_t N, int64_t K, bool split, bool few_rows,
-                  size_t partial_bytes);
+                  size_t partial_bytes, bool logits = false);
 
 using Shape256 = Shape<4, 2, 2, 4>;
 using Shape128 = Shape<2, 2, 2, 2>;

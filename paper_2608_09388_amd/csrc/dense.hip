@@ -150,7 +150,7 @@ __global__ __launch_bounds__(1024) void sum_rows_kernel(const float* parts, int6
   out[c] = accumulate ? out[c] + s : s;
 }
 
-constexpr int64_t kMostPartial = (int64_t)64 << 20;
+constexpr int64_t kMostPartial = (int64_t)128 << 20;
 
 template <class S, bool AROWS, bool BROWS, bool SPLIT>
 hipError_t run(const Args& a, int tiles, hipStream_t stream) {
@@ -190,19 +190,19 @@ size_t partial_bytes(int64_t M, int64_t N, int64_t K) {
 // step of 64 of K takes `latency` or, of as many as are there, `work` each; a tile has
 // `fixed` beside its steps.
 Plan plan_product(int64_t M, int64_t N, int64_t K, bool split, bool few_rows,
-                  size_t partial_bytes) {
+                  size_t partial_bytes, bool logits) {
   struct Kind {
     TileKind kind;
     int slots;
-    double latency, work, fixed;
+    double latency, work, fixed, fixed_logits;
   };
-  static constexpr Kind plain[] = {{TileKind::k256, 1, 1.8, 1.8, 14.0},
-                                   {TileKind::k128, 2, 0.7, 0.51, 5.2},
-                                   {TileKind::k64, 3, 0.6, 0.34, 2.8},
-                                   {TileKind::k32, 4, 0.5, 0.25, 2.5}};
-  static constexpr Kind terms[] = {{TileKind::k128, 1, 2.8, 2.8, 8.0},
-                                   {TileKind::k64, 1, 2.0, 2.0, 5.0},
-                                   {TileKind::k32, 1, 1.6, 1.6, 4.0}};
+  static constexpr Kind plain[] = {{TileKind::k256, 1, 1.8, 1.8, 14.0, 10.8},
+                                   {TileKind::k128, 2, 0.7, 0.51, 5.2, 5.8},
+                                   {TileKind::k64, 3, 0.6, 0.34, 2.8, 4.9},
+                                   {TileKind::k32, 4, 0.5, 0.25, 2.5, 4.5}};
+  static constexpr Kind terms[] = {{TileKind::k128, 1, 2.8, 2.8, 8.0, 8.0},
+                                   {TileKind::k64, 1, 2.0, 2.0, 5.0, 6.0},
+                                   {TileKind::k32, 1, 1.6, 1.6, 4.0, 5.0}};
   constexpr int kCUs = 256;
   const int64_t KT = (K + BK - 1) / BK;
   Plan best{TileKind::k128, 1};
@@ -223,7 +223,8 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, bool split, bool few_rows,
       const int64_t rest = tiles * parts % (kCUs * k.slots);
       const double steps = (double)((KT + parts - 1) / parts);
       const auto round = [&](double here) {
-        return steps * std::max(k.latency, here * std::max(k.work, read)) + k.fixed;
+        return steps * std::max(k.latency, here * std::max(k.work, read)) +
+               (logits ? k.fixed_logits : k.fixed);
       };
       double t = rounds * round(k.slots);
       if (rest > 0) t += round((double)((rest + kCUs - 1) / kCUs));

@@ -39,7 +39,8 @@ using namespace dense;
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kLabelsPerBlock = 4096;  // 256 threads, 16 each
+constexpr int kLabels = 4;  // a thread's
+constexpr int kLabelsPerBlock = 256 * kLabels;
 
 __device__ __forceinline__ int64_t label_at(const void* labels, int id64, int64_t stride,
                                             int64_t i) {
@@ -57,6 +58,15 @@ struct Labels {
     const int64_t y = get(i);
     return y >= 0 && y < V;
   }
+  // the thread's labels of a block, all loads under way at once; -1 past the last
+  __device__ __forceinline__ void get_block(int64_t i0, int64_t n, int (&y)[kLabels]) const {
+    int64_t x[kLabels];
+#pragma unroll
+    for (int q = 0; q < kLabels; ++q) x[q] = get(i0 + q * 256 < n ? i0 + q * 256 : n - 1);
+#pragma unroll
+    for (int q = 0; q < kLabels; ++q)
+      y[q] = i0 + q * 256 < n && x[q] >= 0 && x[q] < V ? (int)x[q] : -1;
+  }
 };
 
 // Live rows of every block of labels.
@@ -64,12 +74,10 @@ __global__ __launch_bounds__(256) void count_labels_kernel(Labels l, int64_t n, 
   __shared__ int total;
   if (threadIdx.x == 0) total = 0;
   __syncthreads();
-  int c = 0;
+  int y[kLabels], c = 0;
+  l.get_block((int64_t)blockIdx.x * kLabelsPerBlock + threadIdx.x, n, y);
 #pragma unroll
-  for (int q = 0; q < 16; ++q) {
-    const int64_t i = (int64_t)blockIdx.x * kLabelsPerBlock + q * 256 + threadIdx.x;
-    c += __popcll(__ballot(i < n && l.live(i)));
-  }
+  for (int q = 0; q < kLabels; ++q) c += __popcll(__ballot(y[q] >= 0));
   if ((threadIdx.x & 63) == 0) atomicAdd(&total, c);  // whole numbers: any order
   __syncthreads();
   if (threadIdx.x == 0) counts[blockIdx.x] = total;
@@ -84,12 +92,21 @@ struct LiveRows {
 };
 
 // The live rows in ascending order, their number, and the results of the others.
-__global__ __launch_bounds__(256) void list_rows_kernel(Labels l, int64_t n, const int32_t* counts,
-                                                        LiveRows rows, int32_t* count,
-                                                        const float* weight, const float* lse_in,
-                                                        float* loss, float* lse) {
-  __shared__ int wave[4], before[4];
+__global__ __launch_bounds__(256) void list_rows_kernel(
+    Labels l, int64_t n, const int32_t* __restrict__ counts, LiveRows rows, int32_t* count,
+    const float* __restrict__ weight, const float* __restrict__ lse_in, float* __restrict__ loss,
+    float* __restrict__ lse) {
+  __shared__ int wave[kLabels][4], before[4];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t i0 = (int64_t)blockIdx.x * kLabelsPerBlock + threadIdx.x;
+  uint64_t mask[kLabels];
+  int y[kLabels];
+  l.get_block(i0, n, y);
+#pragma unroll
+  for (int q = 0; q < kLabels; ++q) {
+    mask[q] = __ballot(y[q] >= 0);
+    if (lane == 0) wave[q][w] = __popcll(mask[q]);
+  }
   int c = 0;
   for (int b = threadIdx.x; b < (int)blockIdx.x; b += 256) c += counts[b];
 #pragma unroll
@@ -97,25 +114,21 @@ __global__ __launch_bounds__(256) void list_rows_kernel(Labels l, int64_t n, con
   if (lane == 0) before[w] = c;
   __syncthreads();
   int base = before[0] + before[1] + before[2] + before[3];
-  for (int q = 0; q < 16; ++q) {
-    const int64_t i = (int64_t)blockIdx.x * kLabelsPerBlock + q * 256 + threadIdx.x;
-    const bool live = i < n && l.live(i);
-    const uint64_t mask = __ballot(live);
-    __syncthreads();
-    if (lane == 0) wave[w] = __popcll(mask);
-    __syncthreads();
-    int at = base + __popcll(mask & ((1ull << lane) - 1));
-    for (int p = 0; p < w; ++p) at += wave[p];
-    if (live) {
+#pragma unroll
+  for (int q = 0; q < kLabels; ++q) {
+    const int64_t i = i0 + q * 256;
+    int at = base + __popcll(mask[q] & ((1ull << lane) - 1));
+    for (int p = 0; p < w; ++p) at += wave[q][p];
+    if (y[q] >= 0) {
       rows.idx[at] = (int32_t)i;
-      rows.label[at] = (int32_t)l.get(i);
+      rows.label[at] = y[q];
       rows.weight[at] = weight != nullptr ? weight[i] : 1.f;
       if (lse_in != nullptr) rows.lse[at] = lse_in[i];
     } else if (i < n) {
       if (loss != nullptr) loss[i] = 0.f;
       if (lse != nullptr) lse[i] = 0.f;
     }
-    base += wave[0] + wave[1] + wave[2] + wave[3];
+    base += wave[q][0] + wave[q][1] + wave[q][2] + wave[q][3];
   }
   if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *count = base;
 }
@@ -552,7 +565,7 @@ hipError_t run_logits(const Logits& a, hipStream_t stream) {
 // `kind` receives the tile that was taken.
 template <Logit WHAT>
 hipError_t launch_logits(Logits a, bool bf16, TileKind* kind, hipStream_t stream) {
-  const TileKind k = plan_product(a.rows, a.V, a.C, !bf16, true, 0).kind;
+  const TileKind k = plan_product(a.rows, a.V, a.C, !bf16, true, 0, true).kind;
   *kind = k;
   const int64_t tm = (a.rows + tile_m(k) - 1) / tile_m(k);
   const int64_t tn = (a.V + tile_n(k) - 1) / tile_n(k);

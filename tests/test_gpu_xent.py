@@ -19,6 +19,8 @@ SHAPES = [
     (130, 16, 4000, 0.2, 0, 0), (129, 64, 512, 0.05, 64, 0), (300, 200, 520, 0.0, 8, 0),
     (513, 130, 300, 0.9, 6, 0), (1000, 40, 10, 0.1, 0, 0), (5, 1000, 70, 0.0, 0, 0),
     (700, 72, 1025, 0.33, 0, 0), (40, 8, 20000, 0.0, 0, 0), (257, 513, 63, 0.5, 1, 3),
+    (300, 520, 1100, 0.3, 0, 0), (1300, 640, 136, 0.5, 8, 0), (2, 1024, 3001, 0.0, 0, 0),
+    (2100, 24, 700, 0.1, 0, 0),
 ]
 
 
@@ -271,14 +273,14 @@ def test_many_labels():
     assert float((loss[live] - ref[live]).abs().max()) < 1e-5
 
 
-@pytest.mark.parametrize("dtype,V", [("f32", (1 << 20) + 8)])
-def test_pieces_of_rows(dtype, V):
+@pytest.mark.parametrize("C", [16, 128])   # logits taken again, logits kept
+def test_pieces_of_rows(C):
     """More pairs of row and class than a piece holds: the gradient of W over two pieces."""
-    n, C = 300, 16
+    n, V = 300, (1 << 20) + 8
     g = torch.Generator(device="cuda")
     g.manual_seed(1)
     x = torch.randn((n, C), generator=g, device="cuda")
-    W = torch.randn((V, C), generator=g, device="cuda") * 0.5
+    W = torch.randn((V, C), generator=g, device="cuda") * (2.0 * C ** -0.5)
     labels = torch.randint(0, V, (n,), generator=g, device="cuda")
     dx, dW, db = torch.empty_like(x), torch.empty_like(W), torch.empty(V, device="cuda")
     old = torch.randn((V, C), generator=g, device="cuda") * 1e-3
