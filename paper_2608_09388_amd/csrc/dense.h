@@ -33,6 +33,7 @@ struct Product {
   Operand A, B;
   bool a_rows, b_rows;  // the order of each operand (see dense_tile.h)
   bool split;           // fp32 as three bf16 terms
+  bool direct;          // fp32 of at most kFewRows rows as it is (with split; A in rows)
   int64_t M, N, K;
   // the device count of live rows, from row0 on, bounds M (rows of D) or K; NULL: all
   const int32_t* count;
@@ -91,8 +92,12 @@ struct Plan {
 };
 // few_rows: tiles of fewer than 128 rows too (operand A in rows); logits: the epilogues
 // of xent.hip.
-Plan plan_product(int64_t M, int64_t N, int64_t K, bool split, bool few_rows,
-                  size_t partial_bytes, bool logits = false);
+Plan plan_product(int64_t M, int64_t N, int64_t K, Mode mode, bool few_rows,
+                  size_t partial_bytes, bool logits = false, double* time = nullptr);
+
+// Rows of fp32 up to which a product reads its operands as they are: the packing of the
+// second one would move more than the product.
+constexpr int64_t kFewRows = 32;
 
 using Shape256 = Shape<4, 2, 2, 4>;
 using Shape128 = Shape<2, 2, 2, 2>;

@@ -26,7 +26,7 @@ struct Args {
   int parts, tn;  // parts of K, columns of tiles
 };
 
-template <class S, bool AROWS, bool BROWS, bool SPLIT>
+template <class S, bool AROWS, bool BROWS, Mode MODE>
 __global__ __launch_bounds__(S::THREADS) void product_kernel(Args a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   int64_t M = a.M, K = a.K;
@@ -46,8 +46,8 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(Args a) {
   const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
   const int KT = (int)((K + BK - 1) / BK), per = (KT + a.parts - 1) / a.parts;
   const int t0 = min(KT, (int)blockIdx.y * per), t1 = min(KT, t0 + per);
-  constexpr bool BF16 = !SPLIT;
-  Tile<S, AROWS, BROWS, SPLIT> tile;
+  constexpr bool BF16 = MODE == kPlain;
+  Tile<S, AROWS, BROWS, MODE> tile;
   const auto fetch = [&](int64_t row, int64_t col) {
     Fetched<BF16> g{};
     if (a.parts == 1 && row < M && col < a.N)
@@ -152,10 +152,10 @@ __global__ __launch_bounds__(1024) void sum_rows_kernel(const float* parts, int6
 
 constexpr int64_t kMostPartial = (int64_t)128 << 20;
 
-template <class S, bool AROWS, bool BROWS, bool SPLIT>
+template <class S, bool AROWS, bool BROWS, Mode MODE>
 hipError_t run(const Args& a, int tiles, hipStream_t stream) {
-  auto kern = product_kernel<S, AROWS, BROWS, SPLIT>;
-  constexpr int lds = S::template lds<SPLIT>();
+  auto kern = product_kernel<S, AROWS, BROWS, MODE>;
+  constexpr int lds = S::template lds<MODE>();
   static std::once_flag once;
   static hipError_t attr = hipSuccess;
   std::call_once(once, [&] {
@@ -167,12 +167,12 @@ hipError_t run(const Args& a, int tiles, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <class S, bool SPLIT>
+template <class S, Mode MODE>
 hipError_t run_orders(const Args& a, int tiles, bool ar, bool br, hipStream_t stream) {
   if constexpr (S::BM >= 128)  // a cols operand has 128 rows at least
-    if (!ar && !br) return run<S, false, false, SPLIT>(a, tiles, stream);
-  if (ar && br) return run<S, true, true, SPLIT>(a, tiles, stream);
-  if (ar && !br) return run<S, true, false, SPLIT>(a, tiles, stream);
+    if (!ar && !br) return run<S, false, false, MODE>(a, tiles, stream);
+  if (ar && br) return run<S, true, true, MODE>(a, tiles, stream);
+  if (ar && !br) return run<S, true, false, MODE>(a, tiles, stream);
   return hipErrorInvalidValue;
 }
 
@@ -189,8 +189,8 @@ size_t partial_bytes(int64_t M, int64_t N, int64_t K) {
 // Times in us, from the figures at the top.  A CU holds `slots` workgroups of a kind; a
 // step of 64 of K takes `latency` or, of as many as are there, `work` each; a tile has
 // `fixed` beside its steps.
-Plan plan_product(int64_t M, int64_t N, int64_t K, bool split, bool few_rows,
-                  size_t partial_bytes, bool logits) {
+Plan plan_product(int64_t M, int64_t N, int64_t K, Mode mode, bool few_rows,
+                  size_t partial_bytes, bool logits, double* time) {
   struct Kind {
     TileKind kind;
     int slots;
@@ -203,12 +203,13 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, bool split, bool few_rows,
   static constexpr Kind terms[] = {{TileKind::k128, 1, 2.8, 2.8, 8.0, 8.0},
                                    {TileKind::k64, 1, 2.0, 2.0, 5.0, 6.0},
                                    {TileKind::k32, 1, 1.6, 1.6, 4.0, 5.0}};
+  static constexpr Kind direct[] = {{TileKind::k32, 8, 1.2, 0.3, 3.0, 4.0}};
   constexpr int kCUs = 256;
   const int64_t KT = (K + BK - 1) / BK;
   Plan best{TileKind::k128, 1};
   double least = 1e300;
-  const Kind* kinds = split ? terms : plain;
-  for (int i = 0; i < (split ? 3 : 4); ++i) {
+  const Kind* kinds = mode == kDirect ? direct : mode == kSplit ? terms : plain;
+  for (int i = 0; i < (mode == kDirect ? 1 : mode == kSplit ? 3 : 4); ++i) {
     const Kind& k = kinds[i];
     if (!few_rows && tile_m(k.kind) < 128) continue;
     const int64_t tiles = ((M + tile_m(k.kind) - 1) / tile_m(k.kind)) *
@@ -216,7 +217,7 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, bool split, bool few_rows,
     // few rows of tiles share what they read of B with few others: its 128 bytes of a
     // step for every column come from memory, at 6.2 TB/s
     const double read = tile_n(k.kind) * 128.0 * kCUs / 6.2e6 /
-                        (double)((M + tile_m(k.kind) - 1) / tile_m(k.kind)) * (split ? 3 : 1);
+                        (double)((M + tile_m(k.kind) - 1) / tile_m(k.kind)) * (mode == kPlain ? 1 : mode == kSplit ? 3 : 2);
     for (int parts = 1; parts <= 64; parts = parts < 4 ? parts + 1 : parts + parts / 2) {
       if (parts > 1 && (KT < 2 * parts || (double)parts * M * N * 4 > (double)partial_bytes)) break;
       const int64_t rounds = tiles * parts / (kCUs * k.slots);
@@ -232,13 +233,14 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, bool split, bool few_rows,
       if (t < least) least = t, best = {k.kind, parts};
     }
   }
+  if (time != nullptr) *time = least;
   return best;
 }
 
 hipError_t launch_product(const Product& p, hipStream_t stream) {
   if (p.M <= 0 || p.N <= 0) return hipSuccess;
-  Plan plan = plan_product(p.M, p.N, p.K, p.split, p.a_rows,
-                           p.partials != nullptr ? p.partial_bytes : 0);
+  const Plan plan = plan_product(p.M, p.N, p.K, p.direct ? kDirect : p.split ? kSplit : kPlain,
+                                 p.a_rows, p.partials != nullptr ? p.partial_bytes : 0);
   Args a;
   a.A = p.A, a.B = p.B;
   a.M = p.M, a.N = p.N, a.K = p.K;
@@ -253,10 +255,12 @@ hipError_t launch_product(const Product& p, hipStream_t stream) {
   const int tiles = (int)(tm * tn);
   hipError_t e = with_tile(plan.kind, [&](auto shape) {
     using S = decltype(shape);
+    if constexpr (S::BM == 32)
+      if (p.direct) return run_orders<S, kDirect>(a, tiles, p.a_rows, p.b_rows, stream);
     if constexpr (S::BM <= 128)
-      if (p.split) return run_orders<S, true>(a, tiles, p.a_rows, p.b_rows, stream);
+      if (p.split) return run_orders<S, kSplit>(a, tiles, p.a_rows, p.b_rows, stream);
     return p.split ? hipErrorInvalidValue
-                   : run_orders<S, false>(a, tiles, p.a_rows, p.b_rows, stream);
+                   : run_orders<S, kPlain>(a, tiles, p.a_rows, p.b_rows, stream);
   });
   if (e != hipSuccess || plan.parts == 1) return e;
   const int64_t threads = p.M * ((p.N + 7) / 8);

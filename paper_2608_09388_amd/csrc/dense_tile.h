@@ -28,6 +28,9 @@
 // contiguous kilobyte.  Fragments of a cols operand come from the transposing LDS
 // read: 16 lanes give the addresses of 4 x 16 elements and each gets a column.
 //
+// Few rows of fp32 (32 at most) are not split: the second operand is read once, from
+// memory into registers, for the fp32 matrix cores.
+//
 // Split fp32: x = h + m + l, and of the nine products of terms the six largest, h h in
 // one sum and the others, at most 2^-7 of it, in a second.  The three planes of both
 // operands pass through LDS together, 32 of k at a time in three buffers, so that a
@@ -71,6 +74,9 @@ struct Operand {
   const int32_t* idx;
 };
 
+// How a tile multiplies: bf16, fp32 in three terms, fp32 from memory.
+enum Mode { kPlain, kSplit, kDirect };
+
 template <int MB_, int NB_, int WM_, int WN_>
 struct Shape {
   static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_;
@@ -79,9 +85,10 @@ struct Shape {
   // split: three planes of half a step in three buffers
   static constexpr int SPLIT_A = BM * BKS * 2, SPLIT_B = BN * BKS * 2,
                        SPLIT_STAGE = 3 * (SPLIT_A + SPLIT_B), SPLIT_BUFFERS = 3;
-  template <bool SPLIT>
-  static constexpr int lds() {
-    return SPLIT ? SPLIT_BUFFERS * SPLIT_STAGE : 2 * STAGE;
+  template <Mode MODE>
+  static constexpr int lds() {  // direct: for the epilogues alone
+    return MODE == kDirect ? NW * 8192 + 2048 : MODE == kSplit ? SPLIT_BUFFERS * SPLIT_STAGE
+                                                               : 2 * STAGE;
   }
 };
 
@@ -222,10 +229,10 @@ __device__ __forceinline__ float original(const Operand& o, int64_t r, int64_t k
 // are scaled back.
 constexpr float kSplitScale = 0x1p24f, kSplitBack = 0x1p-48f;
 
-template <class S, bool AROWS, bool BROWS, bool SPLIT>
+template <class S, bool AROWS, bool BROWS, Mode MODE>
 struct Tile {
   static constexpr int MB = S::MB, NB = S::NB;
-  static constexpr int LDS = S::template lds<SPLIT>();
+  static constexpr int LDS = S::template lds<MODE>();
   f32x16 acc[MB][NB];
 
   // The tile at (m0, n0) of the M x N of which both operands hold enough rows,
@@ -235,7 +242,9 @@ struct Tile {
                                       char* smem) {
     clear(acc);
     if (t0 >= t1) return;
-    if constexpr (SPLIT) {
+    if constexpr (MODE == kDirect) {
+      run_direct(A, B, M, N, K, m0, n0, t0, t1);
+    } else if constexpr (MODE == kSplit) {
       run_split(A, B, m0, n0, t0 * (BK / BKS),
                 (int)min((int64_t)t1 * (BK / BKS), (K + BKS - 1) / BKS), smem);
       again(A, B, M, N, K, row_of(m0, 0, 0) - ((threadIdx.x & 63) >> 3),
@@ -419,6 +428,63 @@ struct Tile {
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int j = 0; j < NB; ++j) acc[i][j] += low[i][j];
+  }
+
+  // 8 of k at a time, 4 adjacent ones to a lane: lane l has row l % 32 of both operands.
+  // A cols operand is read 32 columns of a row of memory at a time.
+  __device__ __forceinline__ void run_direct(const Operand& A, const Operand& B, int64_t M,
+                                             int64_t N, int64_t K, int64_t m0, int64_t n0, int t0,
+                                             int t1) {
+    static_assert(MODE != kDirect || (AROWS && MB == 1 && S::WM == 1), "few rows");
+    const int r = threadIdx.x & 31, h = (threadIdx.x >> 5) & 1;
+    const int64_t k0 = (int64_t)t0 * BK, end = (int64_t)t1 * BK < K ? (int64_t)t1 * BK : K;
+    const int64_t n = col_of(n0) - (threadIdx.x & 7) * 8 + r;
+    // rows past the last repeat row 0, whose values are not kept
+    const int64_t ra = m0 + r < M ? m0 + r : 0;
+    const float* a = A.f32 + (A.idx != nullptr ? (int64_t)A.idx[ra] : ra) * A.f32_ld;
+    const float* b[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int64_t nj = n + 32 * j < N ? n + 32 * j : 0;
+      b[j] = BROWS ? B.f32 + nj * B.f32_ld : B.f32 + nj;
+    }
+    const auto step = [&](int64_t k, int left) {  // left: of k that is there, from k on
+      rowops::f32x4_a4 x, y[NB];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) y[j][e] = 0.f;
+      }
+      if (left >= 4) x = *reinterpret_cast<const rowops::f32x4_a4*>(a + k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (left < 4 && e < left) x[e] = a[k + e];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        if constexpr (BROWS) {
+          if (left >= 4) y[j] = *reinterpret_cast<const rowops::f32x4_a4*>(b[j] + k);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (left < 4 && e < left) y[j][e] = b[j][k + e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (e < left) y[j][e] = b[j][(k + e) * B.f32_ld];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+          acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(y[j][e], x[e], acc[0][j], 0, 0, 0);
+    };
+    int64_t k = k0;
+    for (; k + 32 <= end; k += 32) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) step(k + 8 * u + 4 * h, 4);
+    }
+    for (; k < end; k += 8) step(k + 4 * h, (int)min((int64_t)4, end - k - 4 * h));
   }
 
   // Scales the sums of split products back.  Sums that are not finite (an infinity, a

@@ -151,6 +151,13 @@ Operand plain(const void* p, int64_t ld, int64_t n, int64_t C, bool rows_order) 
   o.k = rows_order ? C : n;
   return o;
 }
+// fp32 rows for a product that reads them as they are.
+Operand direct_rows(const void* p, int64_t ld) {
+  Operand o{};
+  o.f32 = static_cast<const float*>(p);
+  o.f32_ld = ld;
+  return o;
+}
 // Packs the rows at `to` unless they can be read as they are.
 hipError_t operand(const void* p, int64_t ld, int64_t n, int32_t C, bool bf16, bool rows_order,
                    void* to, bool packed, Operand* o, hipStream_t stream) {
@@ -197,9 +204,15 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
   const bool aligned = linear_aligned(a, false);
   const Forward w = forward_layout(a.n, a.Cin, a.Cout, a.bf16, aligned);
   Product p{};
-  SHC_LAUNCH(operand(a.x, a.ldx, a.n, a.Cin, a.bf16, true, byte(a.ws, w.x), false, &p.A, stream));
-  SHC_LAUNCH(operand(a.W, a.ldw, a.Cin, a.Cout, a.bf16, false, byte(a.ws, w.W), false, &p.B,
-                     stream));
+  p.direct = !a.bf16 && a.n <= kFewRows;
+  if (p.direct) {
+    p.A = direct_rows(a.x, a.ldx), p.B = direct_rows(a.W, a.ldw);
+  } else {
+    SHC_LAUNCH(operand(a.x, a.ldx, a.n, a.Cin, a.bf16, true, byte(a.ws, w.x), false, &p.A,
+                       stream));
+    SHC_LAUNCH(operand(a.W, a.ldw, a.Cin, a.Cout, a.bf16, false, byte(a.ws, w.W), false, &p.B,
+                       stream));
+  }
   p.a_rows = true, p.b_rows = false, p.split = !a.bf16;
   p.M = a.n, p.N = a.Cout, p.K = a.Cin;
   p.store.bias = a.bias, p.store.act = a.act;
@@ -248,9 +261,11 @@ hipError_t launch_linear_backward(const LinearArgs& a, hipStream_t stream) {
   // the packed rows of dz in bf16 are read as they are: their width is dz's
   const int32_t dzC = a.bf16 && write ? (int32_t)ld : a.Cout;
   Operand rows{}, cols{};
+  const bool few = !a.bf16 && a.n <= kFewRows;
   if (a.n > 0) {
     void* to = byte(a.ws, w.dz);
-    SHC_LAUNCH(operand(dz, ld, a.n, dzC, a.bf16, true, to, false, &rows, stream));
+    const bool pack = !few || a.dW != nullptr;
+    SHC_LAUNCH(operand(dz, ld, a.n, dzC, a.bf16, true, to, !pack, &rows, stream));
     SHC_LAUNCH(operand(dz, ld, a.n, dzC, a.bf16, false, to, true, &cols, stream));
   }
   Product p{};
@@ -258,9 +273,14 @@ hipError_t launch_linear_backward(const LinearArgs& a, hipStream_t stream) {
   p.partials = reinterpret_cast<float*>(byte(a.ws, w.partials));
   p.partial_bytes = w.partial_bytes;
   if (a.dx != nullptr && a.n > 0) {
-    p.A = rows;
-    SHC_LAUNCH(operand(a.W, a.ldw, a.Cin, a.Cout, a.bf16, true, byte(a.ws, w.W), false, &p.B,
-                       stream));
+    p.direct = few;
+    if (few) {
+      p.A = direct_rows(dz, ld), p.B = direct_rows(a.W, a.ldw);
+    } else {
+      p.A = rows;
+      SHC_LAUNCH(operand(a.W, a.ldw, a.Cin, a.Cout, a.bf16, true, byte(a.ws, w.W), false, &p.B,
+                         stream));
+    }
     p.a_rows = p.b_rows = true;
     p.M = a.n, p.N = a.Cin, p.K = a.Cout;
     p.store.out = a.dx, p.store.ld_out = a.lddx;
@@ -271,6 +291,7 @@ hipError_t launch_linear_backward(const LinearArgs& a, hipStream_t stream) {
       SHC_LAUNCH(operand(a.x, a.ldx, a.n, a.Cin, a.bf16, false, byte(a.ws, w.x), false, &p.A,
                          stream));
     p.B = cols;
+    p.direct = false;
     p.a_rows = p.b_rows = false;
     p.M = a.Cin, p.N = a.Cout, p.K = a.n;
     p.store.out = a.dW, p.store.ld_out = a.lddW;

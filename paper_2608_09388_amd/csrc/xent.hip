@@ -26,6 +26,10 @@
 //   the rounding of dz to bf16, nothing); fp32, or with db, the logits in fp32.  One pass
 //   over them gives dz.  For short rows the product is cheaper than that pass
 //   (`keeps`).
+//
+// Few logits of long rows (some tiles of them, which would leave most CUs idle) are one
+// product cut along C and joined in the workspace, at most 2^21 of them in fp32; all
+// passes start from there (`cut_logits`).
 #include <algorithm>
 #include <mutex>
 
@@ -154,8 +158,8 @@ struct Logits {
 };
 
 // The logits of a tile: M rows are live.  False where none is.
-template <class S, bool SPLIT>
-__device__ __forceinline__ bool logits_tile(Logits& a, Tile<S, true, true, SPLIT>& tile,
+template <class S, Mode MODE>
+__device__ __forceinline__ bool logits_tile(Logits& a, Tile<S, true, true, MODE>& tile,
                                             int64_t* m0, int64_t* n0, int64_t* M, int* tn,
                                             char* smem) {
   *M = a.A.extent = rows_left(a.count, a.row0, a.rows);
@@ -224,16 +228,16 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 enum Keep { kNothing, kExps, kLogits };
 constexpr float kExpScale = 32768.f;
 
-template <class S, bool SPLIT, Keep KEEP>
+template <class S, Mode MODE, Keep KEEP>
 __global__ __launch_bounds__(S::THREADS) void logit_stats_kernel(Logits a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  Tile<S, true, true, SPLIT> tile;
+  Tile<S, true, true, MODE> tile;
   int64_t m0, n0, M;
   int tn;
-  if (!logits_tile<S, SPLIT>(a, tile, &m0, &n0, &M, &tn, smem)) return;
+  if (!logits_tile<S, MODE>(a, tile, &m0, &n0, &M, &tn, smem)) return;
   // per row and 64 columns, behind what the tile passes its sums through
   constexpr int BLOCKS = S::BN / 64;
-  static_assert(S::NW * 8192 + (2 * BLOCKS + 1) * S::BM * 4 <= S::template lds<SPLIT>(),
+  static_assert(S::NW * 8192 + (2 * BLOCKS + 1) * S::BM * 4 <= S::template lds<MODE>(),
                 "fits the tile's LDS");
   float* most = reinterpret_cast<float*>(smem + S::NW * 8192);  // [BLOCKS][BM]
   float* sums = most + BLOCKS * S::BM;
@@ -309,6 +313,7 @@ struct FromKept {
   const float2* parts;
   int tile;  // columns of a tile of parts
   int V;
+  const float* bias;  // what the logits lack, or NULL
   LiveRows live;
   void* dz;
   int width, dz_width;
@@ -351,6 +356,11 @@ __global__ __launch_bounds__(256) void from_kept_kernel(FromKept a) {
         for (int e = 0; e < 8; ++e) z[e] *= wt;
       } else {
         rowops::load_channels<8>(static_cast<const float*>(a.kept) + row * a.width, v, a.width, z);
+        if (a.bias != nullptr) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (col + e < V) z[e] += a.bias[col + e];
+        }
         grad_of(z, y, lse, wt);
       }
       if (col + 8 > V) {
@@ -403,15 +413,42 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const float2* parts, in
   if (loss != nullptr) loss[to] = z == -__builtin_inff() && l == l ? -z : l - z;
 }
 
-template <class S, bool SPLIT>
+// Statistics of the live rows from their logits less the bias, a workgroup to a row.
+__global__ __launch_bounds__(256) void row_stats_kernel(const float* logits, int V,
+                                                        const int32_t* count, const float* bias,
+                                                        LiveRows live, float* loss, float* lse) {
+  __shared__ float2 part[4];
+  const int64_t row = blockIdx.x;
+  if (row >= *count) return;
+  const float* z = logits + row * V;
+  float2 t = {-__builtin_inff(), 0.f};
+#pragma unroll 4
+  for (int v = threadIdx.x; v < V; v += 256)
+    t = join(t, float2{z[v] + (bias != nullptr ? bias[v] : 0.f), 1.f});
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1)
+    t = join(t, float2{__shfl_xor(t.x, d, 64), __shfl_xor(t.y, d, 64)});
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = t;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < 4; ++w) t = join(t, part[w]);
+  const int y = live.label[row];
+  const float at = z[y] + (bias != nullptr ? bias[y] : 0.f), l = t.x + __logf(t.y);
+  const int64_t to = live.idx[row];
+  live.lse[row] = l;
+  if (lse != nullptr) lse[to] = l;
+  if (loss != nullptr) loss[to] = at == -__builtin_inff() && l == l ? -at : l - at;
+}
+
+template <class S, Mode MODE>
 __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  Tile<S, true, true, SPLIT> tile;
+  Tile<S, true, true, MODE> tile;
   int64_t m0, n0, M;
   int tn;
-  if (!logits_tile<S, SPLIT>(a, tile, &m0, &n0, &M, &tn, smem)) return;
+  if (!logits_tile<S, MODE>(a, tile, &m0, &n0, &M, &tn, smem)) return;
   // the rows' label, lse and weight, behind what the tile passes its sums through
-  static_assert(S::NW * 8192 + 3 * S::BM * 4 <= S::template lds<SPLIT>(),
+  static_assert(S::NW * 8192 + 3 * S::BM * 4 <= S::template lds<MODE>(),
                 "fits the tile's LDS");
   int32_t* label = reinterpret_cast<int32_t*>(smem + S::NW * 8192);
   float* lse = reinterpret_cast<float*>(label + S::BM);
@@ -435,7 +472,7 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
     grad_of(z, label[r] - (int)col, lse[r], weight[r]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += z[e];
-    if (col < a.width) put8<!SPLIT>(a.dz, row, a.ld_dz, (int)(col / 8), a.width, z);
+    if (col < a.width) put8<MODE == kPlain>(a.dz, row, a.ld_dz, (int)(col / 8), a.width, z);
   });
   if (a.sums == nullptr) return;
   // over the wavefront's rows: the lane's, then the lanes' of the same columns
@@ -485,9 +522,20 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(Labels l, int64_t n, con
 
 struct Layout {
   int64_t width, rows, pieces;  // columns of dz, rows and number of the pieces
-  size_t idx, label, weight, lse, count, counts, x, W, parts, at_label, kept, dz, dz32, sums, acc, partials,
+  size_t idx, label, weight, lse, count, counts, x, W, logits, parts, at_label, kept, dz, dz32, sums, acc, partials,
       partial_bytes, total;
 };
+
+// Logits that are one product, cut along C, where that is faster by more than the launch
+// that it costs: 5 us.
+constexpr int64_t kMostCut = (int64_t)1 << 21;
+bool cut_logits(int64_t n, int32_t C, int32_t V, Mode mode) {
+  if (n > kMostCut / V) return false;
+  double whole, cut;
+  plan_product(n, V, C, mode, true, 0, true, &whole);
+  const Plan plan = plan_product(n, V, C, mode, true, partial_bytes(n, V, C), false, &cut);
+  return plan.parts > 1 && cut + 5.0 < whole;
+}
 
 // Whether the step keeps the logits or their exponentials.
 bool keeps(int32_t C, bool bf16) { return C >= (bf16 ? 512 : 128); }
@@ -512,6 +560,9 @@ Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass
   w.counts = take((size_t)((n + kLabelsPerBlock - 1) / kLabelsPerBlock) * 4);
   w.x = take(packed_bytes(n, C, !bf16));
   w.W = take(bf16 && aligned && C % 8 == 0 ? 0 : packed_bytes(V, C, !bf16));
+  const int64_t cut_rows = std::min<int64_t>(n, kMostCut / V);
+  w.logits = take((size_t)cut_rows * V * 4);
+  w.partial_bytes = partial_bytes(cut_rows, V, C);
   if (pass != XentPass::kBackward) {
     w.parts = take((size_t)((V + 127) / 128) * n * 8);
     w.at_label = take((size_t)n * 4);
@@ -524,9 +575,10 @@ Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass
     w.kept = take(bf16 && kept ? (size_t)w.rows * w.width * 4 : 0);
     w.sums = take((size_t)(w.rows / 32 + 4) * V * 4);  // 32 rows to a part at least
     w.acc = take(w.pieces > 1 ? (size_t)V * C * 4 : 0);
-    w.partial_bytes = std::max(partial_bytes(w.rows, C, V), partial_bytes(V, C, w.rows));
-    w.partials = take(w.partial_bytes);
+    w.partial_bytes = std::max(w.partial_bytes,
+                               std::max(partial_bytes(w.rows, C, V), partial_bytes(V, C, w.rows)));
   }
+  w.partials = take(w.partial_bytes);
   w.total = at;
   return w;
 }
@@ -540,17 +592,17 @@ char* byte(void* ws, size_t at) { return static_cast<char*>(ws) + at; }
   } while (0)
 
 enum class Logit { kStats, kStatsExps, kStatsLogits, kGrad };
-template <class S, bool SPLIT, Logit WHAT>
+template <class S, Mode MODE, Logit WHAT>
 hipError_t run_logits(const Logits& a, hipStream_t stream) {
   constexpr Keep keep = WHAT == Logit::kStatsExps     ? kExps
                         : WHAT == Logit::kStatsLogits ? kLogits
                                                       : kNothing;
   void (*kern)(Logits);
   if constexpr (WHAT == Logit::kGrad)
-    kern = logit_grad_kernel<S, SPLIT>;
+    kern = logit_grad_kernel<S, MODE>;
   else
-    kern = logit_stats_kernel<S, SPLIT, keep>;
-  constexpr int lds = S::template lds<SPLIT>();
+    kern = logit_stats_kernel<S, MODE, keep>;
+  constexpr int lds = S::template lds<MODE>();
   static std::once_flag once;
   static hipError_t attr = hipSuccess;
   std::call_once(once, [&] {
@@ -565,7 +617,10 @@ hipError_t run_logits(const Logits& a, hipStream_t stream) {
 // `kind` receives the tile that was taken.
 template <Logit WHAT>
 hipError_t launch_logits(Logits a, bool bf16, TileKind* kind, hipStream_t stream) {
-  const TileKind k = plan_product(a.rows, a.V, a.C, !bf16, true, 0, true).kind;
+  const bool direct = !bf16 && a.full <= kFewRows;
+  const TileKind k =
+      plan_product(a.rows, a.V, a.C, direct ? kDirect : bf16 ? kPlain : kSplit, true, 0, true)
+          .kind;
   *kind = k;
   const int64_t tm = (a.rows + tile_m(k) - 1) / tile_m(k);
   const int64_t tn = (a.V + tile_n(k) - 1) / tile_n(k);
@@ -573,9 +628,11 @@ hipError_t launch_logits(Logits a, bool bf16, TileKind* kind, hipStream_t stream
   a.tm = (int)tm, a.tn = (int)tn;
   return with_tile(k, [&](auto shape) {
     using S = decltype(shape);
+    if constexpr (WHAT != Logit::kStatsExps && S::BM == 32)
+      if (direct) return run_logits<S, kDirect, WHAT>(a, stream);
     if constexpr (WHAT != Logit::kStatsExps && S::BM <= 128)
-      if (!bf16) return run_logits<S, true, WHAT>(a, stream);
-    return bf16 ? run_logits<S, false, WHAT>(a, stream) : hipErrorInvalidValue;
+      if (!bf16) return run_logits<S, kSplit, WHAT>(a, stream);
+    return bf16 ? run_logits<S, kPlain, WHAT>(a, stream) : hipErrorInvalidValue;
   });
 }
 
@@ -654,7 +711,8 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
   const int64_t Wwidth = W_as_is ? a.C : packed_width(a.C);
   const uint16_t* Wp = static_cast<const uint16_t*>(a.W);
   int64_t Wld = a.ldw;
-  if (!W_as_is) {
+  const bool few = !a.bf16 && a.n <= kFewRows;
+  if (!W_as_is && !few) {
     uint16_t* to = reinterpret_cast<uint16_t*>(byte(a.ws, w.W));
     SHC_LAUNCH(launch_pack(Pack{a.W, a.ldw, a.V, a.V, a.C, !a.bf16, nullptr, nullptr, 0, -1, to},
                            stream));
@@ -685,9 +743,28 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
     return hipGetLastError();
   };
   const bool products = a.dx != nullptr || a.dW != nullptr;
+  const bool cut = cut_logits(a.n, a.C, a.V, few ? kDirect : a.bf16 ? kPlain : kSplit);
+  if (cut) {
+    Product p{};
+    p.A = x_of(0, a.n, true), p.B = W_of(true);
+    p.a_rows = p.b_rows = true;
+    p.split = !a.bf16, p.direct = few;
+    p.M = a.n, p.N = a.V, p.K = a.C;
+    p.count = count, p.full = a.n;
+    p.store.out32 = reinterpret_cast<float*>(byte(a.ws, w.logits));
+    p.partials = reinterpret_cast<float*>(byte(a.ws, w.partials));
+    p.partial_bytes = partial_bytes(a.n, a.V, a.C);
+    SHC_LAUNCH(launch_product(p, stream));
+    if (pass != XentPass::kBackward) {
+      row_stats_kernel<<<(int)a.n, 256, 0, stream>>>(
+          p.store.out32, a.V, count, a.bias, live_from(0), a.loss,
+          pass == XentPass::kForward ? a.lse : nullptr);
+      SHC_LAUNCH(hipGetLastError());
+    }
+  }
   const bool keep =
-      pass == XentPass::kStep && keeps(a.C, a.bf16) && (products || a.db != nullptr);
-  if (pass != XentPass::kBackward && !keep) {  // 3. statistics, loss and lse
+      !cut && pass == XentPass::kStep && keeps(a.C, a.bf16) && (products || a.db != nullptr);
+  if (pass != XentPass::kBackward && !keep && !cut) {  // 3. statistics, loss and lse
     g.A = x_of(0, a.n, true);
     g.rows = a.n, g.row0 = 0, g.live = live_from(0);
     SHC_LAUNCH(launch_logits<Logit::kStats>(g, a.bf16, &kind, stream));
@@ -707,14 +784,16 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
     g.width = (int)dz_ld;
     g.sums = a.db != nullptr ? reinterpret_cast<float*>(byte(a.ws, w.sums)) : nullptr;
     int per = 64;  // rows to a part of the sums
-    if (keep) {
-      const bool exps = a.bf16 && a.db == nullptr;
-      g.kept = a.bf16 && !exps ? byte(a.ws, w.kept) : g.dz;
-      SHC_LAUNCH(exps ? launch_logits<Logit::kStatsExps>(g, a.bf16, &kind, stream)
-                      : launch_logits<Logit::kStatsLogits>(g, a.bf16, &kind, stream));
-      SHC_LAUNCH(join(row0, rows));
-      const FromKept f{g.kept, rows, count, row0, g.parts, tile_n(kind), a.V, g.live, g.dz,
-                       (int)dz_ld, (int)dz_ld, g.sums};
+    if (keep || cut) {
+      const bool exps = !cut && a.bf16 && a.db == nullptr;
+      g.kept = cut ? byte(a.ws, w.logits) : a.bf16 && !exps ? byte(a.ws, w.kept) : g.dz;
+      if (keep) {
+        SHC_LAUNCH(exps ? launch_logits<Logit::kStatsExps>(g, a.bf16, &kind, stream)
+                        : launch_logits<Logit::kStatsLogits>(g, a.bf16, &kind, stream));
+        SHC_LAUNCH(join(row0, rows));
+      }
+      const FromKept f{g.kept, rows, count, row0, g.parts, cut ? 0 : tile_n(kind), a.V, cut ? a.bias : nullptr,
+                       g.live, g.dz, cut ? a.V : (int)dz_ld, (int)dz_ld, g.sums};
       SHC_LAUNCH(exps     ? launch_from_kept<true, kExps>(f, stream)
                  : a.bf16 ? launch_from_kept<true, kLogits>(f, stream)
                           : launch_from_kept<false, kLogits>(f, stream));
@@ -742,6 +821,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
     if (a.dx != nullptr) {
       p.A = d, p.A.extent = rows, p.A.k = w.width;
       p.B = W_of(false);
+      p.direct = few;
       p.a_rows = true, p.b_rows = false;
       p.M = rows, p.N = a.C, p.K = a.V;
       p.store.out = a.dx, p.store.ld_out = a.lddx, p.store.to = idx + row0;
@@ -749,6 +829,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
     }
     if (a.dW != nullptr) {
       p.A = d, p.A.extent = w.width, p.A.k = rows;
+      p.direct = false;
       p.B = x_of(row0, rows, false);
       p.a_rows = p.b_rows = false;
       p.M = a.V, p.N = a.C, p.K = rows;
