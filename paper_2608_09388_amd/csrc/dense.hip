@@ -200,10 +200,10 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, Mode mode, bool few_rows,
                                    {TileKind::k128, 2, 0.7, 0.51, 5.2, 5.8},
                                    {TileKind::k64, 3, 0.6, 0.34, 2.8, 4.9},
                                    {TileKind::k32, 4, 0.5, 0.25, 2.5, 4.5}};
-  static constexpr Kind terms[] = {{TileKind::k128, 1, 2.8, 2.8, 8.0, 8.0},
-                                   {TileKind::k64, 1, 2.0, 2.0, 5.0, 6.0},
-                                   {TileKind::k32, 1, 1.6, 1.6, 4.0, 5.0}};
-  static constexpr Kind direct[] = {{TileKind::k32, 8, 1.2, 0.3, 3.0, 4.0}};
+  static constexpr Kind terms[] = {{TileKind::k128, 1, 2.6, 2.8, 8.0, 8.0},
+                                   {TileKind::k64, 1, 1.5, 2.0, 5.0, 6.0},
+                                   {TileKind::k32, 1, 1.2, 1.6, 4.0, 5.0}};
+  static constexpr Kind direct[] = {{TileKind::k32, 8, 1.9, 0.85, 3.0, 4.0}};
   constexpr int kCUs = 256;
   const int64_t KT = (K + BK - 1) / BK;
   Plan best{TileKind::k128, 1};
@@ -228,7 +228,8 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, Mode mode, bool few_rows,
                (logits ? k.fixed_logits : k.fixed);
       };
       double t = rounds * round(k.slots);
-      if (rest > 0) t += round((double)((rest + kCUs - 1) / kCUs));
+      if (rest > 0)
+        t += round(rest < kCUs ? (double)rest / kCUs : (double)((rest + kCUs - 1) / kCUs));
       if (parts > 1) t += 4.0 + (double)parts * M * N * 8 / 4e6;
       if (t < least) least = t, best = {k.kind, parts};
     }

@@ -47,6 +47,8 @@
 // multiple of 8 elements and less than 2^21 apart (see `direct`).
 #pragma once
 
+#include <type_traits>
+
 #include "row_ops.h"
 
 namespace shc {
@@ -448,43 +450,44 @@ struct Tile {
       const int64_t nj = n + 32 * j < N ? n + 32 * j : 0;
       b[j] = BROWS ? B.f32 + nj * B.f32_ld : B.f32 + nj;
     }
-    const auto step = [&](int64_t k, int left) {  // left: of k that is there, from k on
-      rowops::f32x4_a4 x, y[NB];
+    // U times 8 of k, all loads ahead of the products; the lane's first k, and how many
+    // of its 4 are there
+    const auto steps = [&](int64_t k, int left, auto uc) {
+      constexpr int U = decltype(uc)::value;
+      rowops::f32x4_a4 x[U], y[U][NB];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] = 0.f;
-#pragma unroll
-        for (int j = 0; j < NB; ++j) y[j][e] = 0.f;
-      }
-      if (left >= 4) x = *reinterpret_cast<const rowops::f32x4_a4*>(a + k);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (left < 4 && e < left) x[e] = a[k + e];
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        if constexpr (BROWS) {
-          if (left >= 4) y[j] = *reinterpret_cast<const rowops::f32x4_a4*>(b[j] + k);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (left < 4 && e < left) y[j][e] = b[j][k + e];
+      for (int u = 0; u < U; ++u) {
+        const int64_t at = k + 8 * u;
+        if (left >= 4) {
+          x[u] = *reinterpret_cast<const rowops::f32x4_a4*>(a + at);
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (e < left) y[j][e] = b[j][(k + e) * B.f32_ld];
+          for (int e = 0; e < 4; ++e) x[u][e] = e < left ? a[at + e] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          if (BROWS && left >= 4) {
+            y[u][j] = *reinterpret_cast<const rowops::f32x4_a4*>(b[j] + at);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              y[u][j][e] = e < left ? b[j][(at + e) * (BROWS ? 1 : B.f32_ld)] : 0.f;
+          }
         }
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
-          acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(y[j][e], x[e], acc[0][j], 0, 0, 0);
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+            acc[0][j] =
+                __builtin_amdgcn_mfma_f32_32x32x2f32(y[u][j][e], x[u][e], acc[0][j], 0, 0, 0);
     };
     int64_t k = k0;
-    for (; k + 32 <= end; k += 32) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) step(k + 8 * u + 4 * h, 4);
-    }
-    for (; k < end; k += 8) step(k + 4 * h, (int)min((int64_t)4, end - k - 4 * h));
+    for (; k + 64 <= end; k += 64) steps(k + 4 * h, 4, std::integral_constant<int, 8>{});
+    for (; k < end; k += 8)
+      steps(k + 4 * h, (int)min((int64_t)4, end - k - 4 * h), std::integral_constant<int, 1>{});
   }
 
   // Scales the sums of split products back.  Sums that are not finite (an infinity, a
