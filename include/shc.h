@@ -891,7 +891,7 @@ int shc_distill_top_step(const void* logits, int64_t logits_stride, int64_t n_ro
  * - bf16 products are exact and summed in fp32; fp32 products are formed from
  *   three bf16 terms of each operand (six products, 2^-23 of a product left out
  *   at most), sums that are not finite or beyond 2^80 again on the fp32 matrix
- *   cores.  Every output is rounded once, but for dz (below), which is rounded to
+ *   cores, as are all of up to 32 rows but those of dW.  Every output is rounded once, but for dz (below), which is rounded to
  *   `dtype` before the products of a backward take it.
  * - Sums have a fixed order that follows the sizes and alignments: results repeat
  *   bit for bit.
@@ -966,7 +966,8 @@ int shc_linear_backward(const void* dout, int64_t dout_stride, const void* x, in
  * shc_linear_cross_entropy_backward -- gradients from lse as written.
  * shc_linear_cross_entropy_step     -- loss and gradients.
  * The backward and the step hold dz for up to 2^30 (bf16) or 2^28 (fp32) pairs of
- * row and class at a time in the workspace.  `pass` of the workspace query: 0
+ * row and class at a time in the workspace, the step for bf16 from C = 512 on also
+ * as many fp32 logits (db needs them).  `pass` of the workspace query: 0
  * forward, 1 backward, 2 step; `aligned` speaks of W alone.
  */
 #define SHC_XENT_FORWARD 0
@@ -1003,8 +1004,8 @@ int shc_linear_cross_entropy_step(const void* x, int64_t x_stride, int64_t n_row
  *   grads: host array of `count` tensors (0 to 65,536), read during the call: numel
  *   elements (below 2^40) of dtype at `data`, contiguous, aligned to their elements;
  *   data may be NULL where numel is 0.  shc_clip_grads writes every tensor's `out`,
- *   which may be its own data, and may overlap no other region of the call
- *   (SHC_ERR_INVALID_ARG); shc_grad_norm ignores it.
+ *   which may be its own data, and may overlap no other region of the call, norm
+ *   among them (SHC_ERR_INVALID_ARG); shc_grad_norm ignores it.
  *   norm: one fp32 on the device; squares are summed in fp64, in a fixed order.
  *   max_norm not negative, not NaN; an infinity never clips.
  * An infinite norm makes the factor 0 and an infinite element NaN, a NaN norm makes

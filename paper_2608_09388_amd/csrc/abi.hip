@@ -1590,8 +1590,8 @@ shc::ClipTensor* clip_list(const shc_grad* grads, int64_t count, bool outs, int*
   return t;
 }
 
-// No output overlaps another region, but for its own data as a whole.
-int check_outs(const shc::ClipTensor* t, int64_t count) {
+// No output overlaps another region, but for its own data as a whole, nor the norm.
+int check_outs(const shc::ClipTensor* t, int64_t count, const float* norm) {
   struct Region {
     uintptr_t first, end;
     int64_t tensor;
@@ -1599,7 +1599,9 @@ int check_outs(const shc::ClipTensor* t, int64_t count) {
   };
   auto* r = static_cast<Region*>(malloc((size_t)(2 * count + 1) * sizeof(Region)));
   if (r == nullptr) return fail(SHC_ERR_CAPACITY, "out of host memory");
-  int64_t n = 0;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(norm);
+  r[0] = {at, at + sizeof(float), count, false};
+  int64_t n = 1;
   for (int64_t i = 0; i < count; ++i) {
     if (t[i].numel == 0) continue;
     const uintptr_t bytes = (uintptr_t)t[i].numel * (t[i].bf16 ? 2 : 4);
@@ -1618,8 +1620,9 @@ int check_outs(const shc::ClipTensor* t, int64_t count) {
     any_end = std::max(any_end, r[i].end);
   }
   free(r);
+  if (bad == count) return fail(SHC_ERR_INVALID_ARG, "an output overlaps norm");
   if (bad >= 0)
-    return fail(SHC_ERR_INVALID_ARG, "grads[%lld]: an output overlaps another tensor",
+    return fail(SHC_ERR_INVALID_ARG, "grads[%lld]: an output overlaps another tensor or norm",
                 (long long)bad);
   return SHC_OK;
 }
@@ -1798,7 +1801,7 @@ int shc_clip_grads(const shc_grad* grads, int64_t count, const float* norm, floa
   int rc;
   shc::ClipTensor* t = clip_list(grads, count, true, &rc);
   if (t == nullptr) return rc;
-  rc = check_outs(t, count);
+  rc = check_outs(t, count, norm);
   if (rc == SHC_OK)
     rc = hip_status(shc::launch_clip_grads(t, count, norm, max_norm, stream),
                     "clip_grads launch");

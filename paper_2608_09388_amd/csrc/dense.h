@@ -111,6 +111,10 @@ constexpr int tile_m(TileKind k) {
 }
 constexpr int tile_n(TileKind k) { return k == TileKind::k256 ? Shape256::BN : Shape128::BN; }
 
+// Tiles of a launch, for fewer than 2^32 threads.  Products of fewer than 2^22 tiles of
+// 128 x 128 have fewer with every kind: four of 32 rows and 128 threads in the place of one.
+constexpr int64_t kMostTiles = (int64_t)1 << 24;
+
 // Calls f(shape) for the kind.
 template <typename F>
 hipError_t with_tile(TileKind kind, F&& f) {

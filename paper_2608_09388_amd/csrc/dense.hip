@@ -251,7 +251,7 @@ hipError_t launch_product(const Product& p, hipStream_t stream) {
   a.parts = plan.parts;
   const int64_t tm = (p.M + tile_m(plan.kind) - 1) / tile_m(plan.kind);
   const int64_t tn = (p.N + tile_n(plan.kind) - 1) / tile_n(plan.kind);
-  if (tm * tn >= (int64_t)1 << 22) return hipErrorInvalidConfiguration;
+  if (tm * tn >= kMostTiles) return hipErrorInvalidConfiguration;
   a.tn = (int)tn;
   const int tiles = (int)(tm * tn);
   hipError_t e = with_tile(plan.kind, [&](auto shape) {

@@ -624,7 +624,7 @@ hipError_t launch_logits(Logits a, bool bf16, TileKind* kind, hipStream_t stream
   *kind = k;
   const int64_t tm = (a.rows + tile_m(k) - 1) / tile_m(k);
   const int64_t tn = (a.V + tile_n(k) - 1) / tile_n(k);
-  if (tm * tn >= (int64_t)1 << 22) return hipErrorInvalidConfiguration;
+  if (tm * tn >= kMostTiles) return hipErrorInvalidConfiguration;
   a.tm = (int)tm, a.tn = (int)tn;
   return with_tile(k, [&](auto shape) {
     using S = decltype(shape);
@@ -654,7 +654,10 @@ size_t xent_workspace_bytes(int64_t n, int32_t C, int32_t V, bool bf16, bool ali
 
 hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
   const Layout w = layout(a.n, a.C, a.V, a.bf16, xent_aligned(a), pass);
-  const bool grads = pass != XentPass::kForward;
+  // a step without gradients is a forward pass
+  const bool grads = pass != XentPass::kForward &&
+                     (a.dx != nullptr || a.dW != nullptr || a.db != nullptr);
+  if (pass == XentPass::kBackward && !grads) return hipSuccess;
   const Labels labels{a.labels, a.id64, a.label_stride, a.V};
   int32_t* idx = reinterpret_cast<int32_t*>(byte(a.ws, w.idx));
   const auto live_from = [&](int64_t row0) {
@@ -762,8 +765,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
       SHC_LAUNCH(hipGetLastError());
     }
   }
-  const bool keep =
-      !cut && pass == XentPass::kStep && keeps(a.C, a.bf16) && (products || a.db != nullptr);
+  const bool keep = !cut && pass == XentPass::kStep && keeps(a.C, a.bf16) && grads;
   if (pass != XentPass::kBackward && !keep && !cut) {  // 3. statistics, loss and lse
     g.A = x_of(0, a.n, true);
     g.rows = a.n, g.row0 = 0, g.live = live_from(0);
@@ -807,7 +809,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
       SHC_LAUNCH(hipGetLastError());
     }
     if (!products) continue;
-    if (!a.bf16)
+    if (!a.bf16 && (!few || a.dW != nullptr))
       SHC_LAUNCH(launch_pack(Pack{g.dz, dz_ld, rows, rows, a.V, 1, nullptr, count, row0, -1, dz},
                              stream));
     Operand d{};

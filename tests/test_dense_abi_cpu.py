@@ -176,3 +176,11 @@ def test_clip(lib):
 
 def test_struct_layout():
     assert ctypes.sizeof(shc.Grad) == 32
+
+
+@pytest.mark.parametrize("out,off", [(2 * A, 0), (2 * A, 396), (A, 396), (A, 0)])
+def test_clip_refuses_an_output_over_the_norm(lib, out, off):
+    t, n = grads((A, out, 100, 0))
+    norm = out + off
+    assert lib.shc_clip_grads(t, n, norm, 1.0, None) == -1
+    assert "norm" in err(lib)
