@@ -966,7 +966,7 @@ int shc_linear_backward(const void* dout, int64_t dout_stride, const void* x, in
  * shc_linear_cross_entropy_backward -- gradients from lse as written.
  * shc_linear_cross_entropy_step     -- loss and gradients.
  * The backward and the step hold dz for up to 2^30 (bf16) or 2^28 (fp32) pairs of
- * row and class at a time in the workspace, the step for bf16 from C = 512 on also
+ * row and class at a time in the workspace, the step for bf16 from C = 768 on also
  * as many fp32 logits (db needs them).  `pass` of the workspace query: 0
  * forward, 1 backward, 2 step; `aligned` speaks of W alone.
  */

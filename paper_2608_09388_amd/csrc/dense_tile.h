@@ -596,7 +596,7 @@ struct Tile {
 // so that these spread evenly): a contiguous range of tiles to an XCD, in
 // bands of kBand rows of tiles taken column by column, so that the tiles an XCD
 // works on at a time share rows of both operands in its L2.
-constexpr int kBand = 4;
+constexpr int kBand = 8;
 __device__ __forceinline__ bool tile_of(int b, int tm, int tn, int* m, int* n) {
   if (b >= tm * tn) return false;
   const int t = xcd_tile(b, tm * tn);

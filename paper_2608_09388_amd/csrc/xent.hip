@@ -24,7 +24,7 @@
 //   exponentials relative to the maximum of their tile's columns, in fp16 times 2^15
 //   (off by 2^-12 of their value, 2^-40 of the tile's largest at the small end: next to
 //   the rounding of dz to bf16, nothing); fp32, or with db, the logits in fp32.  One pass
-//   over them gives dz.  For short rows the product is cheaper than that pass
+//   over them gives dz.  For short rows in bf16 the product is cheaper than that pass
 //   (`keeps`).
 //
 // Few logits of long rows (some tiles of them, which would leave most CUs idle) are one
@@ -537,8 +537,13 @@ bool cut_logits(int64_t n, int32_t C, int32_t V, Mode mode) {
   return plan.parts > 1 && cut + 5.0 < whole;
 }
 
-// Whether the step keeps the logits or their exponentials.
-bool keeps(int32_t C, bool bf16) { return C >= (bf16 ? 512 : 128); }
+// Whether the step keeps the logits or their exponentials, or forms them twice.  8,192
+// rows by 16,384 classes, us kept / twice at C = 128, 256, 512, 1,024: bf16 without db
+// 419 / 403, 474 / 483, 643 / 692, 935 / 1,108; bf16 with db, which keeps four bytes of a
+// logit, 629 / 497 at 256, 767 / 706, 1,055 / 1,124; fp32 1,336 / 1,467, 1,797 / 2,090,
+// 2,827 / 3,428, 5,112 / 6,442.  Below these widths a step's bits are those of a forward
+// and a backward pass, also where 4% would be had (fp32 1,200 / 1,258 at 64).
+bool keeps(int32_t C, bool bf16, bool db) { return C >= (!bf16 ? 128 : db ? 768 : 256); }
 
 Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass pass) {
   Layout w{};
@@ -568,8 +573,8 @@ Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass
     w.at_label = take((size_t)n * 4);
   }
   if (pass != XentPass::kForward) {
-    // fp32 logits become dz where they are; bf16 exponentials too (a step without db)
-    const bool kept = pass == XentPass::kStep && keeps(C, bf16);
+    // kept fp32 logits become dz where they are; bf16 exponentials too (a step without db)
+    const bool kept = pass == XentPass::kStep && keeps(C, bf16, true);
     w.dz = take(packed_bytes(w.rows, V, !bf16));
     w.dz32 = take(bf16 ? 0 : (size_t)w.rows * V * 4);
     w.kept = take(bf16 && kept ? (size_t)w.rows * w.width * 4 : 0);
@@ -765,7 +770,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
       SHC_LAUNCH(hipGetLastError());
     }
   }
-  const bool keep = !cut && pass == XentPass::kStep && keeps(a.C, a.bf16) && grads;
+  const bool keep = !cut && pass == XentPass::kStep && keeps(a.C, a.bf16, a.db != nullptr) && grads;
   if (pass != XentPass::kBackward && !keep && !cut) {  // 3. statistics, loss and lse
     g.A = x_of(0, a.n, true);
     g.rows = a.n, g.row0 = 0, g.live = live_from(0);
