@@ -5,6 +5,26 @@
 // Which tile, and how many parts K is cut into, follows from the sizes by a model of
 // the time, `plan_product`: rounds of workgroups over the CUs times the steps of one,
 // plus what parts cost (their fp32 sums written and read back, a second launch).
+//
+// bf16 products, us by tile, 256 x 256, 128 x 128, 64 x 128, 32 x 128:
+//   67,040 x   128 x   128     26.2    15.3    11.6    13.7
+//   67,040 x 1,024 x   128     84.7    59.5    52.9    74.2
+//   20,000 x   512 x   512     26.6    23.2    20.6    28.0
+//   16,384 x 1,024 x 1,024     42.1    43.3    47.4    63.6
+//    4,096 x 4,096 x 4,096      122     142     182     256
+//    8,192 x 8,192 x 8,192      891   1,026   1,382   3,510
+//       16 x 16,384 x 4,096    34.7    30.0    28.8    29.4  (K in 3 or 4 parts)
+//        1 x 4,096 x 4,096             14.7    13.6    13.2  (in 6)
+// Large ones are bound by the matrix cores at the power limit: 8,192 cubed at 1.10, 1.23
+// and 1.26 PFLOP/s with rows x rows, rows x cols, cols x cols, 4,096 x 131,072 x 4,096 at 1.25 in
+// any order; the matrix units are busy 0.62 to 0.66 of the time, LDS 0.24, without a
+// conflict.  Split fp32, 4,096 cubed: 981, 1,141, 1,170 TFLOP/s of bf16, 164 to 195 of
+// fp32, against 154 of a library's product on the fp32 matrix cores.
+//
+// Few rows are bound by reading the second operand: 16 rows by 16,384 x 4,096 in bf16 27
+// us (5 TB/s) and 4.5 for joining the two parts of K.  fp32, us from memory / in three terms
+// (which packs that operand first): 1 row through 4,096 x 4,096 25.7 / 52.0, 32 rows 27.2 /
+// 52.5; 32 rows through 512 x 512 11.4 / 15.4, 1,024 x 16,384 22.7 / 51.5 (kFewRows).
 #include <algorithm>
 #include <mutex>
 
@@ -76,7 +96,8 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(Args a) {
             });
 }
 
-// Sums the parts in order and stores: a thread to 8 columns of a row.
+// Sums the parts in order and stores: a thread to 8 columns of a row.  Bound by latency: 4
+// us for 16 x 16,384 in two parts.
 template <bool BF16>
 __global__ __launch_bounds__(256) void join_kernel(const float* parts, int n, int64_t M, int N,
                                                    const int32_t* count, int64_t row0, Store st) {
@@ -98,7 +119,8 @@ __global__ __launch_bounds__(256) void join_kernel(const float* parts, int n, in
   store8<BF16>(st, row, v, N, sum, bias, g);
 }
 
-// 8 elements of a packed row to a thread.
+// 8 elements of a packed row to a thread.  Bound by HBM: 520 rows of 50,021 fp32 into
+// three terms (104 MB read, 154 written) in 40 us, 6.5 TB/s; small ones by the launch.
 template <typename T, bool SPLIT>
 __global__ __launch_bounds__(256) void pack_kernel(Pack p, int width) {
   using namespace rowops;
@@ -133,6 +155,7 @@ __global__ __launch_bounds__(256) void pack_kernel(Pack p, int width) {
   }
 }
 
+// 64 columns to a workgroup, the rows to 16 wavefronts in turn: 5 us for 512 rows of 8,192.
 __global__ __launch_bounds__(1024) void sum_rows_kernel(const float* parts, int64_t rows,
                                                         int64_t ld, int C, int accumulate,
                                                         float* out) {
@@ -150,6 +173,8 @@ __global__ __launch_bounds__(1024) void sum_rows_kernel(const float* parts, int6
   out[c] = accumulate ? out[c] + s : s;
 }
 
+// Bytes of parts at most.  From 512 tiles of 128 x 128 on a product fills the CUs without
+// them; two parts of that are half of this.
 constexpr int64_t kMostPartial = (int64_t)128 << 20;
 
 template <class S, bool AROWS, bool BROWS, Mode MODE>
@@ -214,10 +239,11 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, Mode mode, bool few_rows,
     if (!few_rows && tile_m(k.kind) < 128) continue;
     const int64_t tiles = ((M + tile_m(k.kind) - 1) / tile_m(k.kind)) *
                           ((N + tile_n(k.kind) - 1) / tile_n(k.kind));
-    // few rows of tiles share what they read of B with few others: its 128 bytes of a
+    // few rows of tiles share what they read of B with few others: its bytes of a
     // step for every column come from memory, at 6.2 TB/s
-    const double read = tile_n(k.kind) * 128.0 * kCUs / 6.2e6 /
-                        (double)((M + tile_m(k.kind) - 1) / tile_m(k.kind)) * (mode == kPlain ? 1 : mode == kSplit ? 3 : 2);
+    const int bytes = mode == kPlain ? 128 : mode == kSplit ? 384 : 256;
+    const double read = (double)tile_n(k.kind) * bytes * kCUs / 6.2e6 /
+                        (double)((M + tile_m(k.kind) - 1) / tile_m(k.kind));
     for (int parts = 1; parts <= 64; parts = parts < 4 ? parts + 1 : parts + parts / 2) {
       if (parts > 1 && (KT < 2 * parts || (double)parts * M * N * 4 > (double)partial_bytes)) break;
       const int64_t rounds = tiles * parts / (kCUs * k.slots);

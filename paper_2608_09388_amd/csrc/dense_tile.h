@@ -595,7 +595,9 @@ struct Tile {
 // The tile of workgroup b of tm x tn, false past them (tm counts the live rows' tiles,
 // so that these spread evenly): a contiguous range of tiles to an XCD, in
 // bands of kBand rows of tiles taken column by column, so that the tiles an XCD
-// works on at a time share rows of both operands in its L2.
+// works on at a time share rows of both operands in its L2.  Loss and gradients of 4,096
+// rows of 4,096 over 131,072 classes, us with bands of 1, 4, 8, 16: 11,930, 11,460,
+// 11,290, 11,770; 67,040 rows of 128 over 10,475: 1,334, 1,308, 1,300, 1,422.
 constexpr int kBand = 8;
 __device__ __forceinline__ bool tile_of(int b, int tm, int tn, int* m, int* n) {
   if (b >= tm * tn) return false;
