@@ -28,7 +28,7 @@ __device__ __forceinline__ float normal_cdf(float z, float* bell) {
 }
 
 __device__ __forceinline__ float act_of(int act, float z) {
-  if (act == kActRelu) return z > 0.f ? z : 0.f;
+  if (act == kActRelu) return z < 0.f ? 0.f : z;  // a NaN stays one
   if (act == kActGelu) {
     float bell;
     return z * normal_cdf(z, &bell);
@@ -38,7 +38,7 @@ __device__ __forceinline__ float act_of(int act, float z) {
 }
 
 __device__ __forceinline__ float slope_of(int act, float z) {
-  if (act == kActRelu) return z > 0.f ? 1.f : 0.f;
+  if (act == kActRelu) return z <= 0.f ? 0.f : 1.f;  // of a NaN 1, so that dout's is kept
   if (act == kActGelu) {
     float bell;
     const float cdf = normal_cdf(z, &bell);

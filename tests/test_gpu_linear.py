@@ -1,4 +1,6 @@
 """The dense linear layer and its gradients against the 64-bit oracle."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -240,3 +242,28 @@ def test_padding_behind_rows_is_not_read_into_sums():
                       for s in ((70, Cin), (Cin, Cout)))
             shc.linear_backward(d.t, x.t, W.t, dx=dx, dW=dW)
             assert bool(torch.isfinite(dx).all()) and bool(torch.isfinite(dW).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_activations_of_nan_and_infinities(dtype):
+    """A NaN stays one, here too with ReLU; the gradient through it is not lost."""
+    nan, inf = float("nan"), float("inf")
+    z = torch.full((1, 8), 0.5, device="cuda", dtype=TDT[dtype])
+    bias = torch.zeros(8, device="cuda")
+    bias[1], bias[2], bias[3] = nan, inf, -inf
+    eye = torch.eye(8, device="cuda", dtype=TDT[dtype])
+    for act in ACTS:
+        out = shc.linear(z, eye, bias, act=act)[0].tolist()
+        assert math.isnan(out[1]) and out[2] == inf
+        if act == shc.SHC_ACT_NONE:
+            assert out[3] == -inf
+        elif act == shc.SHC_ACT_RELU:
+            assert out[3] == 0
+        else:
+            assert math.isnan(out[3])
+        assert all(math.isfinite(out[k]) for k in (0, 4, 5, 6, 7))
+    pre = z.clone()
+    pre[0, 1], pre[0, 2] = nan, -inf
+    dx = torch.empty_like(z)
+    shc.linear_backward(torch.ones_like(z), z, eye, pre, dx=dx, act=shc.SHC_ACT_RELU)
+    assert dx[0].tolist() == [1, 1, 0, 1, 1, 1, 1, 1]
