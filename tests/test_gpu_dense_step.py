@@ -211,3 +211,44 @@ def test_refusals_of_the_binding():
     with pytest.raises(shc.ShcError, match="act"):
         shc.sparse_linear(S, 4, torch.zeros((16, 16), **f), None, torch.zeros((4, 16), **f),
                           shc.SHC_ACT_GELU)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_beyond_four_gigabytes(dtype):
+    """Every row tensor with its rows so far apart that offsets pass 32 bits gives what adjacent
+    rows give, bit for bit."""
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    n, C, N, far = 2300, 72, 88, (1 << 20) - 8
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+
+    def near(rows, width):
+        return torch.randn((rows, width), generator=g, device="cuda").to(t)
+
+    buf = torch.empty(n * far, dtype=t, device="cuda")
+    used = [0]
+
+    def apart(values):
+        """The values in columns of the buffer that no other tensor has."""
+        rows, width = values.shape
+        view = torch.as_strided(buf, (rows, width), (far, 1), used[0])
+        used[0] += 256
+        view.copy_(values)
+        return view
+
+    x, W, dout, pre = near(n, C), near(C, N), near(n, N), near(n, N)
+    table, labels = near(n, C), torch.randint(-3, n, (n,), generator=g, device="cuda")
+
+    def run(place):
+        X, T = place(x), place(table)
+        out, kept = place(torch.zeros_like(dout)), place(torch.zeros_like(dout))
+        dx, dW = place(torch.zeros_like(x)), place(torch.zeros_like(W))
+        res = place(dout)
+        shc.linear(X, place(W), out=out, act=shc.SHC_ACT_GELU, residual=res, pre=kept)
+        shc.linear_backward(res, X, place(W), place(pre), dx, dW, act=shc.SHC_ACT_SILU)
+        ex, eT = place(torch.zeros_like(x)), place(torch.zeros_like(table))
+        loss = shc.linear_cross_entropy_step(X, T, labels, dx=ex, dW=eT)
+        return [r.clone() for r in (out, kept, dx, dW, loss, ex, eT)]
+
+    for a, b in zip(run(lambda v: v.clone()), run(apart)):
+        assert torch.equal(a, b)
