@@ -891,7 +891,8 @@ int shc_distill_top_step(const void* logits, int64_t logits_stride, int64_t n_ro
  * - bf16 products are exact and summed in fp32; fp32 products are formed from
  *   three bf16 terms of each operand (six products, 2^-23 of a product left out
  *   at most), sums that are not finite or beyond 2^80 again on the fp32 matrix
- *   cores, as are all of up to 32 rows but those of dW.  Every output is rounded once, but for dz (below), which is rounded to
+ *   cores, as are all of up to 32 rows and of small linear layers, but for those of
+ *   dW.  Every output is rounded once, but for dz (below), which is rounded to
  *   `dtype` before the products of a backward take it.
  * - Sums have a fixed order that follows the sizes and alignments: results repeat
  *   bit for bit.

@@ -184,6 +184,17 @@ hipError_t operand(const void* p, int64_t ld, int64_t n, int32_t C, bool bf16, b
                      stream);
 }
 
+// Whether a product of fp32 rows, M x N over K, goes to the fp32 matrix cores as its operands
+// are: few rows, for which packing the second operand moves more than the product, and small
+// products, where the packing's launches cost more than the slower instructions.  M x K x N,
+// us so / in three terms: 58,059 x 35 x 64 22.5 / 34.3, 67,040 x 128 x 128 46.7 / 63.1, 64 x 4,096
+// x 4,096 44.7 / 54.7, 256 x 512 x 512 12.2 / 16.5, 5,000 x 300 x 300 19.1 / 24.8; 20,000 x 512 x 64
+// 50.7 / 49.1, 1,023 x 1,001 x 2,503 113.5 / 59.9, 84,210 x 1,216 x 166 730 / 514.
+bool direct_pays(int64_t M, int64_t K, int64_t N) {
+  constexpr int64_t kMost = 1200000000;  // of whole tiles
+  return M <= kFewRows || (M + 31) / 32 * 32 * ((N + 127) / 128 * 128) <= kMost / K;
+}
+
 #define SHC_LAUNCH(...)                    \
   do {                                     \
     const hipError_t _e = (__VA_ARGS__);   \
@@ -210,7 +221,7 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
   const bool aligned = linear_aligned(a, false);
   const Forward w = forward_layout(a.n, a.Cin, a.Cout, a.bf16, aligned);
   Product p{};
-  p.direct = !a.bf16 && a.n <= kFewRows;
+  p.direct = !a.bf16 && direct_pays(a.n, a.Cin, a.Cout);
   if (p.direct) {
     p.A = direct_rows(a.x, a.ldx), p.B = direct_rows(a.W, a.ldw);
   } else {
@@ -267,10 +278,10 @@ hipError_t launch_linear_backward(const LinearArgs& a, hipStream_t stream) {
   // the packed rows of dz in bf16 are read as they are: their width is dz's
   const int32_t dzC = a.bf16 && write ? (int32_t)ld : a.Cout;
   Operand rows{}, cols{};
-  const bool few = !a.bf16 && a.n <= kFewRows;
+  const bool dx_direct = !a.bf16 && direct_pays(a.n, a.Cout, a.Cin);
   if (a.n > 0) {
     void* to = byte(a.ws, w.dz);
-    const bool pack = !few || a.dW != nullptr;
+    const bool pack = a.dW != nullptr || !dx_direct;
     SHC_LAUNCH(operand(dz, ld, a.n, dzC, a.bf16, true, to, !pack, &rows, stream));
     SHC_LAUNCH(operand(dz, ld, a.n, dzC, a.bf16, false, to, true, &cols, stream));
   }
@@ -279,8 +290,8 @@ hipError_t launch_linear_backward(const LinearArgs& a, hipStream_t stream) {
   p.partials = reinterpret_cast<float*>(byte(a.ws, w.partials));
   p.partial_bytes = w.partial_bytes;
   if (a.dx != nullptr && a.n > 0) {
-    p.direct = few;
-    if (few) {
+    p.direct = dx_direct;
+    if (dx_direct) {
       p.A = direct_rows(dz, ld), p.B = direct_rows(a.W, a.ldw);
     } else {
       p.A = rows;

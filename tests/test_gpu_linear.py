@@ -267,3 +267,33 @@ def test_activations_of_nan_and_infinities(dtype):
     dx = torch.empty_like(z)
     shc.linear_backward(torch.ones_like(z), z, eye, pre, dx=dx, act=shc.SHC_ACT_RELU)
     assert dx[0].tolist() == [1, 1, 0, 1, 1, 1, 1, 1]
+
+
+@pytest.mark.parametrize("shape", [(3001, 3003, 210, 3, 0), (40, 6000, 12000, 0, 0),
+                                   (9000, 1500, 130, 0, 2)])
+def test_large_fp32(shape):
+    """Products that are formed in three terms, forward and backward, and values that these do
+    not hold: those rows and columns give what fp32 gives, no bit of the others changes."""
+    n, Cin, Cout, extra, off = shape
+    c = Case(n, Cin, Cout, extra, off, "f32")
+    dout = c.rows(n, Cout)
+    x, W, d = (t.get() for t in (c.x, c.W, dout))
+    out = shc.linear(c.x.t, c.W.t, f32(c.b))
+    dx, dW = torch.empty((n, Cin), device="cuda"), torch.empty((Cin, Cout), device="cuda")
+    db = torch.empty(Cout, device="cuda")
+    shc.linear_backward(dout.t, c.x.t, c.W.t, dx=dx, dW=dW, db=db)
+    for got, ref, size, K in (
+            (out, x @ W + c.b, np.abs(x) @ np.abs(W) + np.abs(c.b), Cin),
+            (dx, d @ W.T, np.abs(d) @ np.abs(W).T, Cout),
+            (dW, x.T @ d, np.abs(x).T @ np.abs(d), n), (db, d.sum(0), np.abs(d).sum(0), n)):
+        off_by = np.abs(got.double().cpu().numpy() - ref)
+        # a rounding of every sum, six products of terms, the one that is left out
+        assert np.all(off_by <= (K + 16) * 2.0 ** -24 * size)
+    c.x.t[7, 3], c.x.t[11, Cin - 1] = float("nan"), 2.0 ** 110
+    again = shc.linear(c.x.t, c.W.t, f32(c.b))
+    assert bool(torch.isnan(again[7]).all())
+    ref = 2.0 ** 110 * W[Cin - 1]
+    assert np.all(np.abs(again[11].double().cpu().numpy() - ref) <= 2.0 ** -22 * np.abs(ref) + 1e6)
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[7] = rest[11] = False
+    assert torch.equal(again[rest], out[rest])
