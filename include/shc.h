@@ -893,7 +893,8 @@ int shc_distill_top_step(const void* logits, int64_t logits_stride, int64_t n_ro
  *   at most), sums that are not finite or beyond 2^80 again on the fp32 matrix
  *   cores, as are all of up to 32 rows and of small linear layers, but for those of
  *   dW.  Every output is rounded once, but for dz (below), which is rounded to
- *   `dtype` before the products of a backward take it.
+ *   `dtype` before the products of a backward take it (not so of up to 64 rows of
+ *   the cross entropy, where it is two bf16 terms).
  * - Sums have a fixed order that follows the sizes and alignments: results repeat
  *   bit for bit.
  * - A workspace query takes `aligned`: 1 where every row tensor that the call

@@ -33,7 +33,8 @@ struct Product {
   Operand A, B;
   bool a_rows, b_rows;  // the order of each operand (see dense_tile.h)
   bool split;           // fp32 as three bf16 terms
-  bool direct;          // fp32 of at most kFewRows rows as it is (with split; A in rows)
+  bool direct;          // fp32 as it is (with split; A in rows)
+  bool a_low;           // A (bf16) is the sum of two terms, `plane` apart
   int64_t M, N, K;
   // the device count of live rows, from row0 on, bounds M (rows of D) or K; NULL: all
   const int32_t* count;

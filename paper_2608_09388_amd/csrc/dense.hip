@@ -40,10 +40,11 @@ struct Args {
   int64_t M, N, K;
   const int32_t* count;
   int64_t row0, full;
-  int count_is_k;
+  int count_is_k, a_low;
   Store store;
   float* partials;
   int parts, tn;  // parts of K, columns of tiles
+  int join;       // the sums go to partials
 };
 
 template <class S, bool AROWS, bool BROWS, Mode MODE>
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(Args a) {
   Tile<S, AROWS, BROWS, MODE> tile;
   const auto fetch = [&](int64_t row, int64_t col) {
     Fetched<BF16> g{};
-    if (a.parts == 1 && row < M && col < a.N)
+    if (!a.join && row < M && col < a.N)
       g = fetch8<BF16>(a.store, row, (int)(col / 8), (int)a.N);
     return g;
   };
@@ -78,7 +79,12 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(Args a) {
   Fetched<BF16> got[4];
   if constexpr (S::MB == 1) tile.fetch_block(m0, n0, 0, got, fetch);
   tile.run(a.A, a.B, M, a.N, K, m0, n0, t0, t1, smem);
-  if (a.parts > 1) {
+  if constexpr (BF16 && !AROWS)
+    if (a.a_low) {
+      a.A.p += a.A.plane;
+      tile.add(a.A, a.B, M, a.N, K, m0, n0, t0, t1, smem);
+    }
+  if (a.join) {
     float* to = a.partials + (int64_t)blockIdx.y * a.M * a.N;
     tile.each(m0, n0, smem, [&](int64_t row, int64_t col, const float (&v)[8]) {
       if (row < M && col < a.N)
@@ -266,16 +272,24 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, Mode mode, bool few_rows,
 
 hipError_t launch_product(const Product& p, hipStream_t stream) {
   if (p.M <= 0 || p.N <= 0) return hipSuccess;
-  const Plan plan = plan_product(p.M, p.N, p.K, p.direct ? kDirect : p.split ? kSplit : kPlain,
+  // two terms of A in rows: as many rows again, joined with the first as parts of K are
+  const bool twice = p.a_low && p.a_rows;
+  const int64_t M = twice ? 2 * p.M : p.M;
+  if (twice && (p.partial_bytes < (size_t)M * p.N * 4 || p.A.plane != p.M * p.A.ld))
+    return hipErrorInvalidValue;
+  const Plan plan = plan_product(M, p.N, p.K, p.direct ? kDirect : p.split ? kSplit : kPlain,
                                  p.a_rows, p.partials != nullptr ? p.partial_bytes : 0);
   Args a;
   a.A = p.A, a.B = p.B;
-  a.M = p.M, a.N = p.N, a.K = p.K;
-  a.count = p.count, a.row0 = p.row0, a.full = p.full, a.count_is_k = p.count_is_k;
+  a.M = M, a.N = p.N, a.K = p.K;
+  if (twice) a.A.extent = M;
+  a.count = twice ? nullptr : p.count;
+  a.row0 = p.row0, a.full = p.full, a.count_is_k = p.count_is_k, a.a_low = p.a_low;
   a.store = p.store;
   a.partials = p.partials;
   a.parts = plan.parts;
-  const int64_t tm = (p.M + tile_m(plan.kind) - 1) / tile_m(plan.kind);
+  a.join = plan.parts > 1 || twice;
+  const int64_t tm = (M + tile_m(plan.kind) - 1) / tile_m(plan.kind);
   const int64_t tn = (p.N + tile_n(plan.kind) - 1) / tile_n(plan.kind);
   if (tm * tn >= kMostTiles) return hipErrorInvalidConfiguration;
   a.tn = (int)tn;
@@ -289,15 +303,16 @@ hipError_t launch_product(const Product& p, hipStream_t stream) {
     return p.split ? hipErrorInvalidValue
                    : run_orders<S, kPlain>(a, tiles, p.a_rows, p.b_rows, stream);
   });
-  if (e != hipSuccess || plan.parts == 1) return e;
+  if (e != hipSuccess || !a.join) return e;
+  const int parts = twice ? 2 * plan.parts : plan.parts;
   const int64_t threads = p.M * ((p.N + 7) / 8);
   const int blocks = (int)((threads + 255) / 256);
   const int32_t* rows = p.count_is_k ? nullptr : p.count;
   if (p.split)
-    join_kernel<false><<<blocks, 256, 0, stream>>>(p.partials, plan.parts, p.M, (int)p.N, rows,
+    join_kernel<false><<<blocks, 256, 0, stream>>>(p.partials, parts, p.M, (int)p.N, rows,
                                                    p.row0, p.store);
   else
-    join_kernel<true><<<blocks, 256, 0, stream>>>(p.partials, plan.parts, p.M, (int)p.N, rows,
+    join_kernel<true><<<blocks, 256, 0, stream>>>(p.partials, parts, p.M, (int)p.N, rows,
                                                   p.row0, p.store);
   return hipGetLastError();
 }

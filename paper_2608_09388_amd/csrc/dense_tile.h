@@ -28,8 +28,8 @@
 // contiguous kilobyte.  Fragments of a cols operand come from the transposing LDS
 // read: 16 lanes give the addresses of 4 x 16 elements and each gets a column.
 //
-// Few rows of fp32 (32 at most) are not split: the second operand is read once, from
-// memory into registers, for the fp32 matrix cores.
+// Few rows of fp32 and small products are not split: both operands are read from memory
+// into registers, for the fp32 matrix cores.
 //
 // Split fp32: x = h + m + l, and of the nine products of terms the six largest, h h in
 // one sum and the others, at most 2^-7 of it, in a second.  The three planes of both
@@ -66,7 +66,7 @@ struct Operand {
   int64_t ld;      // elements from row to row of memory (r of rows, k of cols)
   int64_t extent;  // r that may be read (cols: a multiple of 8)
   int64_t k;       // k that may be read (rows: a multiple of 8)
-  int64_t plane;   // elements from term to term of a split fp32 operand
+  int64_t plane;   // elements from term to term of an operand of several
   // where a device count of rows is below their number: the chosen rows, packed
   const uint16_t* alt;
   int64_t alt_ld;
@@ -243,6 +243,12 @@ struct Tile {
                                       int64_t K, int64_t m0, int64_t n0, int t0, int t1,
                                       char* smem) {
     clear(acc);
+    add(A, B, M, N, K, m0, n0, t0, t1, smem);
+  }
+  // adds to what the tile holds (bf16)
+  __device__ __forceinline__ void add(const Operand& A, const Operand& B, int64_t M, int64_t N,
+                                      int64_t K, int64_t m0, int64_t n0, int t0, int t1,
+                                      char* smem) {
     if (t0 >= t1) return;
     if constexpr (MODE == kDirect) {
       run_direct(A, B, M, N, K, m0, n0, t0, t1);

@@ -22,10 +22,15 @@
 // - in the backward, from the logits again, in the epilogue of their product;
 // - in the step, from what its forward kept of the piece: bf16 without db, the
 //   exponentials relative to the maximum of their tile's columns, in fp16 times 2^15
-//   (off by 2^-12 of their value, 2^-40 of the tile's largest at the small end: next to
+//   (off by 2^-11 of their value, 2^-40 of the tile's largest at the small end: next to
 //   the rounding of dz to bf16, nothing); fp32, or with db, the logits in fp32.  One pass
 //   over them gives dz.  For short rows in bf16 the product is cheaper than that pass
 //   (`keeps`).
+// The rounding of dz is mostly that of the rows' labels: at random over many rows, all of the
+// gradient over few (7 rows: 0.0028 of it, 0.0017 with two terms).  Up to kFine rows of
+// bf16 dz is two terms, the rounded one and the rest, and multiplied twice: as twice the
+// rows for dx, which reads W once, one step of K more for dW.  Steps, us with two terms / one:
+// 7 x 448 x 3,456 45 / 41, 64 x 4,096 x 32,000 302 / 265, 16 x 4,096 x 131,072 980 / 898.
 //
 // Few logits of long rows (some tiles of them, which would leave most CUs idle) are one
 // product cut along C and joined in the workspace, at most 2^21 of them in fp32; all
@@ -48,6 +53,7 @@ using namespace dense;
 
 namespace {
 
+constexpr int64_t kFine = 64;  // rows of bf16 whose dz is two terms
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kLabels = 4;  // a thread's
 constexpr int kLabelsPerBlock = 256 * kLabels;
@@ -159,9 +165,26 @@ struct Logits {
   // gradient
   void* dz;
   int64_t ld_dz;
+  int64_t low;  // bf16: elements from dz to its second term, 0 without one
   int width;
   float* sums;  // [tm * WM][V] or NULL
 };
+
+// 8 values of dz, in bf16 with what the rounding leaves.  Not of what is not finite, where
+// that would be a NaN.
+template <bool BF16>
+__device__ __forceinline__ void put_dz(void* dz, int64_t low, int64_t row, int64_t ld, int v,
+                                       int width, const float (&z)[8]) {
+  put8<BF16>(dz, row, ld, v, width, z);
+  if constexpr (BF16)
+    if (low != 0) {
+      float t[8];
+      rowops::Row<uint16_t>::widen(rowops::Row<uint16_t>::narrow(z), t);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = __builtin_isfinite(t[e]) ? z[e] - t[e] : 0.f;
+      put8<true>(static_cast<uint16_t*>(dz) + low, row, ld, v, width, t);
+    }
+}
 
 // The logits of a tile: M rows are live.  False where none is.
 template <class S, Mode MODE>
@@ -323,6 +346,7 @@ struct FromKept {
   const float* bias;  // what the logits lack, or NULL
   LiveRows live;
   void* dz;
+  int64_t low;  // as Logits'
   int width, dz_width;
   float* sums;  // [ceil(rows / 64)][V] or NULL
 };
@@ -377,7 +401,7 @@ __global__ __launch_bounds__(256) void from_kept_kernel(FromKept a) {
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] += z[e];
-      put8<BF16>(a.dz, row, a.dz_width, v, a.dz_width, z);
+      put_dz<BF16>(a.dz, a.low, row, a.dz_width, v, a.dz_width, z);
     }
   }
   if (a.sums == nullptr) return;
@@ -479,7 +503,8 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
     grad_of(z, label[r] - (int)col, lse[r], weight[r]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += z[e];
-    if (col < a.width) put8<MODE == kPlain>(a.dz, row, a.ld_dz, (int)(col / 8), a.width, z);
+    if (col < a.width)
+      put_dz<MODE == kPlain>(a.dz, a.low, row, a.ld_dz, (int)(col / 8), a.width, z);
   });
   if (a.sums == nullptr) return;
   // over the wavefront's rows: the lane's, then the lanes' of the same columns
@@ -586,13 +611,17 @@ Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass
   if (pass != XentPass::kForward) {
     // kept fp32 logits become dz where they are; bf16 exponentials too (a step without db)
     const bool kept = pass == XentPass::kStep && keeps(C, bf16, true);
-    w.dz = take(packed_bytes(w.rows, V, !bf16));
+    // two terms of up to kFine rows, and no less for more rows
+    const int64_t dz_rows = bf16 ? std::max(w.rows, std::min(2 * n, 2 * kFine)) : w.rows;
+    w.dz = take(packed_bytes(dz_rows, V, !bf16));
     w.dz32 = take(bf16 ? 0 : (size_t)w.rows * V * 4);
     w.kept = take(bf16 && kept ? (size_t)w.rows * w.width * 4 : 0);
     w.sums = take((size_t)(w.rows / 32 + 4) * V * 4);  // 32 rows to a part at least
     w.acc = take(w.pieces > 1 ? (size_t)V * C * 4 : 0);
     w.partial_bytes = std::max(w.partial_bytes,
                                std::max(partial_bytes(w.rows, C, V), partial_bytes(V, C, w.rows)));
+    if (bf16)  // dx of dz's two terms
+      w.partial_bytes = std::max(w.partial_bytes, (size_t)(std::min(n, kFine) * C) * 8);
   }
   w.partials = take(w.partial_bytes);
   w.total = at;
@@ -791,6 +820,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
   if (!grads) return hipSuccess;
   // 4. gradients, a piece of the live rows at a time
   const int64_t dz_ld = a.bf16 ? w.width : a.V;
+  const bool fine = a.bf16 && a.n <= kFine;
   uint16_t* dz = reinterpret_cast<uint16_t*>(byte(a.ws, w.dz));
   float* acc = reinterpret_cast<float*>(byte(a.ws, w.acc));
   for (int64_t piece = 0; piece < w.pieces; ++piece) {
@@ -799,6 +829,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
     g.rows = rows, g.row0 = row0, g.live = live_from(row0);
     g.dz = a.bf16 ? static_cast<void*>(dz) : byte(a.ws, w.dz32);
     g.ld_dz = dz_ld;
+    g.low = fine ? rows * dz_ld : 0;
     g.width = (int)dz_ld;
     g.sums = a.db != nullptr ? reinterpret_cast<float*>(byte(a.ws, w.sums)) : nullptr;
     int per = 64;  // rows to a part of the sums
@@ -811,7 +842,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
         SHC_LAUNCH(join(row0, rows));
       }
       const FromKept f{g.kept,  rows,  count, row0, g.parts, cut ? 0 : tile_n(kind),
-                       a.V,     cut ? a.bias : nullptr,     g.live,  g.dz,
+                       a.V,     cut ? a.bias : nullptr,     g.live,  g.dz,  g.low,
                        cut ? a.V : (int)dz_ld, (int)dz_ld, g.sums};
       SHC_LAUNCH(exps     ? launch_from_kept<true, kExps>(f, stream)
                  : a.bf16 ? launch_from_kept<true, kLogits>(f, stream)
@@ -833,7 +864,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
     d.p = dz, d.ld = w.width, d.plane = rows * w.width;
     if (!a.bf16) d.f32 = static_cast<const float*>(g.dz), d.f32_ld = dz_ld;
     Product p{};
-    p.split = !a.bf16;
+    p.split = !a.bf16, p.a_low = fine;
     p.count = count, p.row0 = row0, p.full = a.n;
     p.partials = reinterpret_cast<float*>(byte(a.ws, w.partials));
     p.partial_bytes = w.partial_bytes;

@@ -296,3 +296,44 @@ def test_pieces_of_rows(C):
     for got, ref in ((dx, q @ W.double()), (dW, q.t() @ x.double()), (db, q.sum(0)),
                      (dW2, q.t() @ x.double() + old.double())):
         assert float((got - ref).norm() / ref.norm()) < 2e-6
+
+
+@pytest.mark.parametrize("shape", [(1, 448, 3456), (7, 448, 3456), (7, 72, 1000), (64, 128, 300),
+                                   (3, 2048, 100), (33, 64, 5000)])
+@pytest.mark.parametrize("with_db", [False, True])
+def test_few_rows_in_bf16(shape, with_db):
+    """Up to 64 rows dz is not rounded to bf16: gradients are off by their own rounding, half a
+    step of 8 significand bits or 2^-8, by 2^-11 of the terms for exponentials kept in fp16 (half
+    a step of 11 bits, 2^-11) and dz's second term (the rounding of what is at most 2^-8 of it,
+    2^-16), and by fp32's sums.  (dz rounded once would be off by 2^-8 of the terms.)"""
+    n, C, V = shape
+    c = Case(n, C, V, 0.2 if n > 5 else 0.0, 0, 0, "bf16")
+    ids, w = c.ids(), f32(c.w)
+    x, W = c.x.get(), c.W.get()
+    weight = np.ones(n) if c.w is None else wide(c.w)
+    z = x @ W.T
+    z -= z.max(1, keepdims=True)
+    p = np.exp(z) / np.exp(z).sum(1, keepdims=True)
+    y = ids.cpu().numpy()
+    live = (y >= 0) & (y < V)
+    dz = p.copy()
+    dz[np.flatnonzero(live), y[live]] -= 1
+    dz *= np.where(live, weight, 0)[:, None]
+    # an fp32 logit is off by (C + 16) 2^-24 of its terms, lse by a few of its last bits, and
+    # dz of its probability by as much; a kept exponential by 2^-40 of the row's largest
+    off = ((C + 16) * 2.0 ** -24 * (np.abs(x) @ np.abs(W).T)).max() + 2.0 ** -18
+    slack = weight.max() * (p * 2 * off + 2.0 ** -39) * live[:, None]
+    for step in (False, True):
+        dx, dW, db = c.grads()
+        kw = dict(dx=dx.t, dW=dW.t, db=db.t[0] if with_db else None)
+        if step:
+            shc.linear_cross_entropy_step(c.x.t, c.W.t, ids, w, **kw)
+        else:
+            lse = torch.empty(n, device="cuda")
+            shc.linear_cross_entropy(c.x.t, c.W.t, ids, lse=lse)
+            shc.linear_cross_entropy_backward(c.x.t, c.W.t, ids, lse, w, **kw)
+        for got, ref, size, more in ((dx, dz @ W, np.abs(dz) @ np.abs(W), slack @ np.abs(W)),
+                                     (dW, dz.T @ x, np.abs(dz).T @ np.abs(x), slack.T @ np.abs(x))):
+            rest = 2.0 ** -11 + 2.0 ** -16 + (V + n) * 2.0 ** -24
+            bound = 2.0 ** -8 * np.abs(ref) + rest * size + more
+            assert np.all(np.abs(got.t.double().cpu().numpy() - ref) <= 1.01 * bound + 1e-30)
