@@ -75,7 +75,7 @@ def test_gradients_in_bf16():
 
 
 def test_gradients_against_differences():
-    """Along a random direction of every parameter, the fp64 network's loss as the judge."""
+    """Along a random direction of every parameter, the fp64 network's loss as the measure."""
     head, x, n, labels = setup(blocks=1, p=0.2)
     head.forward(x, n)
     head.backward(labels, n)
