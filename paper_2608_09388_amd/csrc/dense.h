@@ -18,6 +18,7 @@ constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3;
 struct Store {
   const float* add32;
   float* out32;  // both [M][N], N apart
+  const float* scale;  // of the sums, on the device, or NULL
   const float* bias;
   int act;
   const void* res;

@@ -113,6 +113,10 @@ __device__ __forceinline__ void store8(const Store& s, int64_t row, int v, int N
     rowops::store_channels<8>(s.out32 + row * N, v, N, f);
     return;
   }
+  if (s.scale != nullptr) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] *= *s.scale;
+  }
   if (s.bias != nullptr) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] += bias[e];

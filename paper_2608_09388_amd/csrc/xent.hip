@@ -26,6 +26,10 @@
 //   the rounding of dz to bf16, nothing); fp32, or with db, the logits in fp32.  One pass
 //   over them gives dz.  For short rows in bf16 the product is cheaper than that pass
 //   (`keeps`).
+// dz in bf16 is off by less the nearer it is below a power of two: with row weights it is
+// formed times a factor in [1, 2] that makes the largest one a power of two, which the sums
+// over it undo (624 rows of weights 0.8e-3 to 2.4e-3: gradients off by
+// 0.0022 in place of 0.0025, of which 0.0016 is their own rounding).
 // The rounding of dz is mostly that of the rows' labels: at random over many rows, all of the
 // gradient over few (7 rows: 0.0028 of it, 0.0017 with two terms).  Up to kFine rows of
 // bf16 dz is two terms, the rounded one and the rest, and multiplied twice: as twice the
@@ -85,9 +89,24 @@ struct Labels {
   }
 };
 
-// Live rows of every block of labels.
-__global__ __launch_bounds__(256) void count_labels_kernel(Labels l, int64_t n, int32_t* counts) {
+// The largest finite weight, without its sign, of the thread's live rows (0 without any).
+__device__ __forceinline__ float most_weight(const float* weight, int64_t i0,
+                                             const int (&y)[kLabels]) {
+  float m = 0.f;
+#pragma unroll
+  for (int q = 0; q < kLabels; ++q)
+    if (y[q] >= 0) {
+      const float w = fabsf(weight[i0 + q * 256]);
+      m = w < __builtin_inff() ? fmaxf(m, w) : m;
+    }
+  return rowops::lanes_reduce<64>(m, rowops::MaxOp{});
+}
+
+// Live rows of every block of labels, and their largest weight (`weight` not NULL).
+__global__ __launch_bounds__(256) void count_labels_kernel(Labels l, int64_t n, int32_t* counts,
+                                                           const float* weight, float* most) {
   __shared__ int total;
+  __shared__ float top[4];
   if (threadIdx.x == 0) total = 0;
   __syncthreads();
   int y[kLabels], c = 0;
@@ -95,8 +114,14 @@ __global__ __launch_bounds__(256) void count_labels_kernel(Labels l, int64_t n, 
 #pragma unroll
   for (int q = 0; q < kLabels; ++q) c += __popcll(__ballot(y[q] >= 0));
   if ((threadIdx.x & 63) == 0) atomicAdd(&total, c);  // whole numbers: any order
+  if (weight != nullptr) {
+    const float m = most_weight(weight, (int64_t)blockIdx.x * kLabelsPerBlock + threadIdx.x, y);
+    if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = m;
+  }
   __syncthreads();
   if (threadIdx.x == 0) counts[blockIdx.x] = total;
+  if (threadIdx.x == 0 && weight != nullptr)
+    most[blockIdx.x] = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
 }
 
 // What the epilogues need of the live rows, in their order.
@@ -107,12 +132,15 @@ struct LiveRows {
   float* lse;
 };
 
-// The live rows in ascending order, their number, and the results of the others.
+// The live rows in ascending order, their number, and the results of the others.  scale (NULL:
+// not asked for): what dz in bf16 is multiplied by, so that the largest weight becomes a power
+// of two, and what undoes it (1 where there is no such weight).
 __global__ __launch_bounds__(256) void list_rows_kernel(
     Labels l, int64_t n, const int32_t* __restrict__ counts, LiveRows rows, int32_t* count,
     const float* __restrict__ weight, const float* __restrict__ lse_in, float* __restrict__ loss,
-    float* __restrict__ lse) {
+    float* __restrict__ lse, const float* __restrict__ most, float* scale) {
   __shared__ int wave[kLabels][4], before[4];
+  __shared__ float top[4];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int64_t i0 = (int64_t)blockIdx.x * kLabelsPerBlock + threadIdx.x;
   uint64_t mask[kLabels];
@@ -128,7 +156,23 @@ __global__ __launch_bounds__(256) void list_rows_kernel(
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) c += __shfl_xor(c, d, 64);
   if (lane == 0) before[w] = c;
+  const bool last = blockIdx.x == gridDim.x - 1;
+  if (last && scale != nullptr) {
+    float m = most_weight(weight, i0, y);
+    for (int b = threadIdx.x; b < (int)blockIdx.x; b += 256) m = fmaxf(m, most[b]);
+    m = rowops::lanes_reduce<64>(m, rowops::MaxOp{});
+    if (lane == 0) top[w] = m;
+  }
   __syncthreads();
+  if (last && scale != nullptr && threadIdx.x == 0) {
+    const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    const uint32_t bits = __float_as_uint(m);
+    // m is f 2^e, f in [1, 2): times 2 / f
+    const float f = __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u);
+    const bool normal = m >= 0x1p-126f && m < 0x1p126f;
+    scale[0] = normal ? 2.f / f : 1.f;
+    scale[1] = normal ? f * 0.5f : 1.f;
+  }
   int base = before[0] + before[1] + before[2] + before[3];
 #pragma unroll
   for (int q = 0; q < kLabels; ++q) {
@@ -146,7 +190,7 @@ __global__ __launch_bounds__(256) void list_rows_kernel(
     }
     base += wave[q][0] + wave[q][1] + wave[q][2] + wave[q][3];
   }
-  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *count = base;
+  if (last && threadIdx.x == 0) *count = base;
 }
 
 struct Logits {
@@ -166,6 +210,7 @@ struct Logits {
   void* dz;
   int64_t ld_dz;
   int64_t low;  // bf16: elements from dz to its second term, 0 without one
+  const float* scale;  // of dz, or NULL
   int width;
   float* sums;  // [tm * WM][V] or NULL
 };
@@ -347,6 +392,7 @@ struct FromKept {
   LiveRows live;
   void* dz;
   int64_t low;  // as Logits'
+  const float* scale;
   int width, dz_width;
   float* sums;  // [ceil(rows / 64)][V] or NULL
 };
@@ -360,13 +406,14 @@ __global__ __launch_bounds__(256) void from_kept_kernel(FromKept a) {
   const int64_t r1 = r0 + 64 < live ? r0 + 64 : live;
   const int v = blockIdx.y * 64 + lane, col = 8 * v;
   const int V = a.V;
+  const float scale = a.scale != nullptr ? *a.scale : 1.f;
   float sum[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) sum[e] = 0.f;
   if (col < a.dz_width) {
 #pragma unroll 2
     for (int64_t row = r0 + w; row < r1; row += 4) {
-      const float lse = a.live.lse[row], wt = a.live.weight[row];
+      const float lse = a.live.lse[row], wt = a.live.weight[row] * scale;
       const int y = a.live.label[row] - col;
       float z[8];
       if constexpr (KEEP == kExps) {
@@ -484,11 +531,12 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
   int32_t* label = reinterpret_cast<int32_t*>(smem + S::NW * 8192);
   float* lse = reinterpret_cast<float*>(label + S::BM);
   float* weight = lse + S::BM;
+  const float scale = a.scale != nullptr ? *a.scale : 1.f;
   for (int r = threadIdx.x; r < S::BM; r += S::THREADS)
     if (m0 + r < M) {
       label[r] = a.live.label[m0 + r];
       lse[r] = a.live.lse[m0 + r];
-      weight[r] = a.live.weight[m0 + r];
+      weight[r] = a.live.weight[m0 + r] * scale;
     }
   __syncthreads();
   float sum[8], bias[8];
@@ -521,7 +569,8 @@ __global__ __launch_bounds__(S::THREADS) void logit_grad_kernel(Logits a) {
 // before gave (`first` 0) or to what db holds (`accumulate`).
 __global__ __launch_bounds__(1024) void join_sums_kernel(const float* sums, int rows_per_part,
                                                          int64_t rows, const int32_t* count,
-                                                         int64_t row0, int V, int add, float* db) {
+                                                         int64_t row0, int V, int add, const float* scale,
+                                                         float* db) {
   __shared__ float part[16][64];
   const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
   const int64_t c = (int64_t)blockIdx.x * 64 + x;
@@ -535,6 +584,7 @@ __global__ __launch_bounds__(1024) void join_sums_kernel(const float* sums, int 
   __syncthreads();
   if (y != 0 || c >= V) return;
   for (int q = 1; q < 16; ++q) s += part[q][x];
+  if (scale != nullptr) s *= *scale;
   db[c] = add ? db[c] + s : s;
 }
 
@@ -554,7 +604,7 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(Labels l, int64_t n, con
 
 struct Layout {
   int64_t width, rows, pieces;  // columns of dz, rows and number of the pieces
-  size_t idx, label, weight, lse, count, counts, x, W, logits, parts, at_label, kept, dz, dz32,
+  size_t idx, label, weight, lse, count, counts, most, scale, x, W, logits, parts, at_label, kept, dz, dz32,
       sums, acc, partials, partial_bytes, total;
 };
 
@@ -599,6 +649,8 @@ Layout layout(int64_t n, int32_t C, int32_t V, bool bf16, bool aligned, XentPass
   w.lse = take((size_t)n * 4);
   w.count = take(4);
   w.counts = take((size_t)((n + kLabelsPerBlock - 1) / kLabelsPerBlock) * 4);
+  w.most = take((size_t)((n + kLabelsPerBlock - 1) / kLabelsPerBlock) * 4);
+  w.scale = take(8);
   w.x = take(packed_bytes(n, C, !bf16));
   w.W = take(bf16 && aligned && C % 8 == 0 ? 0 : packed_bytes(V, C, !bf16));
   const int64_t cut_rows = std::min<int64_t>(n, kMostCut / V);
@@ -727,14 +779,19 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
   // 1. the live rows
   const int blocks = (int)((a.n + kLabelsPerBlock - 1) / kLabelsPerBlock);
   int32_t* counts = reinterpret_cast<int32_t*>(byte(a.ws, w.counts));
+  float* most = reinterpret_cast<float*>(byte(a.ws, w.most));
+  float* scale = a.bf16 && grads && a.weight != nullptr
+                     ? reinterpret_cast<float*>(byte(a.ws, w.scale))
+                     : nullptr;
   if (blocks > 1) {
-    count_labels_kernel<<<blocks, 256, 0, stream>>>(labels, a.n, counts);
+    count_labels_kernel<<<blocks, 256, 0, stream>>>(labels, a.n, counts,
+                                                    scale != nullptr ? a.weight : nullptr, most);
     SHC_LAUNCH(hipGetLastError());
   }
   const bool back = pass == XentPass::kBackward;
   list_rows_kernel<<<blocks, 256, 0, stream>>>(
       labels, a.n, counts, live_from(0), count, a.weight, back ? a.lse : nullptr,
-      back ? nullptr : a.loss, pass == XentPass::kForward ? a.lse : nullptr);
+      back ? nullptr : a.loss, pass == XentPass::kForward ? a.lse : nullptr, most, scale);
   SHC_LAUNCH(hipGetLastError());
   const bool as_is = a.bf16 && direct(a.x, a.ldx, a.C);
   const int64_t xwidth = packed_width(a.C);
@@ -821,6 +878,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
   // 4. gradients, a piece of the live rows at a time
   const int64_t dz_ld = a.bf16 ? w.width : a.V;
   const bool fine = a.bf16 && a.n <= kFine;
+  const float* undo = scale != nullptr ? scale + 1 : nullptr;
   uint16_t* dz = reinterpret_cast<uint16_t*>(byte(a.ws, w.dz));
   float* acc = reinterpret_cast<float*>(byte(a.ws, w.acc));
   for (int64_t piece = 0; piece < w.pieces; ++piece) {
@@ -830,6 +888,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
     g.dz = a.bf16 ? static_cast<void*>(dz) : byte(a.ws, w.dz32);
     g.ld_dz = dz_ld;
     g.low = fine ? rows * dz_ld : 0;
+    g.scale = scale;
     g.width = (int)dz_ld;
     g.sums = a.db != nullptr ? reinterpret_cast<float*>(byte(a.ws, w.sums)) : nullptr;
     int per = 64;  // rows to a part of the sums
@@ -842,7 +901,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
         SHC_LAUNCH(join(row0, rows));
       }
       const FromKept f{g.kept,  rows,  count, row0, g.parts, cut ? 0 : tile_n(kind),
-                       a.V,     cut ? a.bias : nullptr,     g.live,  g.dz,  g.low,
+                       a.V,     cut ? a.bias : nullptr,     g.live,  g.dz,  g.low, scale,
                        cut ? a.V : (int)dz_ld, (int)dz_ld, g.sums};
       SHC_LAUNCH(exps     ? launch_from_kept<true, kExps>(f, stream)
                  : a.bf16 ? launch_from_kept<true, kLogits>(f, stream)
@@ -853,7 +912,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
     }
     if (a.db != nullptr) {
       join_sums_kernel<<<(a.V + 63) / 64, 1024, 0, stream>>>(g.sums, per, rows, count, row0, a.V,
-                                                             piece > 0 || a.accumulate, a.db);
+                                                             piece > 0 || a.accumulate, undo, a.db);
       SHC_LAUNCH(hipGetLastError());
     }
     if (!products) continue;
@@ -865,6 +924,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
     if (!a.bf16) d.f32 = static_cast<const float*>(g.dz), d.f32_ld = dz_ld;
     Product p{};
     p.split = !a.bf16, p.a_low = fine;
+    p.store.scale = undo;
     p.count = count, p.row0 = row0, p.full = a.n;
     p.partials = reinterpret_cast<float*>(byte(a.ws, w.partials));
     p.partial_bytes = w.partial_bytes;
@@ -885,6 +945,7 @@ hipError_t launch_xent(const XentArgs& a, XentPass pass, hipStream_t stream) {
       p.M = a.V, p.N = a.C, p.K = rows;
       p.count_is_k = true;
       p.store = Store{};
+      p.store.scale = undo;
       p.store.add32 = piece > 0 ? acc : nullptr;
       if (piece + 1 < w.pieces) {
         p.store.out32 = acc;
