@@ -93,12 +93,13 @@ __global__ __launch_bounds__(S::THREADS) void product_kernel(Args a) {
     return;
   }
   if constexpr (S::MB > 1) tile.fetch_block(m0, n0, 0, got, fetch);
+  const float scale = scale_of(a.store);
   float bias[8];
   if (tile.col_of(n0) < a.N) bias8(a.store, (int)(tile.col_of(n0) / 8), (int)a.N, bias);
   tile.each(m0, n0, smem, got, fetch,
             [&](int64_t row, int64_t col, const float (&v)[8], const Fetched<BF16>& g) {
               if (row < M && col < a.N)
-                store8<BF16>(a.store, row, (int)(col / 8), (int)a.N, v, bias, g);
+                store8<BF16>(a.store, row, (int)(col / 8), (int)a.N, v, scale, bias, g);
             });
 }
 
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(256) void join_kernel(const float* parts, int n, in
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += f[e];
   }
-  store8<BF16>(st, row, v, N, sum, bias, g);
+  store8<BF16>(st, row, v, N, sum, scale_of(st), bias, g);
 }
 
 // 8 elements of a packed row to a thread.  Bound by HBM: 520 rows of 50,021 fp32 into

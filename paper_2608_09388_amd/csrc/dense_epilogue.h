@@ -93,14 +93,17 @@ __device__ __forceinline__ Fetched<BF16> fetch8(const Store& s, int64_t row, int
   }
   return g;
 }
+__device__ __forceinline__ float scale_of(const Store& s) {
+  return s.scale != nullptr ? *s.scale : 1.f;
+}
 __device__ __forceinline__ void bias8(const Store& s, int v, int N, float (&b)[8]) {
   if (s.bias != nullptr) rowops::load_channels<8>(s.bias, v, N, b);
 }
 
 template <bool BF16>
 __device__ __forceinline__ void store8(const Store& s, int64_t row, int v, int N,
-                                       const float (&values)[8], const float (&bias)[8],
-                                       const Fetched<BF16>& g) {
+                                       const float (&values)[8], float scale,
+                                       const float (&bias)[8], const Fetched<BF16>& g) {
   float f[8], x[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) f[e] = values[e];
@@ -113,10 +116,8 @@ __device__ __forceinline__ void store8(const Store& s, int64_t row, int v, int N
     rowops::store_channels<8>(s.out32 + row * N, v, N, f);
     return;
   }
-  if (s.scale != nullptr) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] *= *s.scale;
-  }
+  for (int e = 0; e < 8; ++e) f[e] *= scale;
   if (s.bias != nullptr) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] += bias[e];
