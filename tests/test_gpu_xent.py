@@ -337,3 +337,51 @@ def test_few_rows_in_bf16(shape, with_db):
             rest = 2.0 ** -11 + 2.0 ** -16 + (V + n) * 2.0 ** -24
             bound = 2.0 ** -8 * np.abs(ref) + rest * size + more
             assert np.all(np.abs(got.t.double().cpu().numpy() - ref) <= 1.01 * bound + 1e-30)
+
+
+@pytest.mark.parametrize("n", [40, 70, 3000])
+def test_weights_of_any_size(n):
+    """The factor that dz in bf16 is formed with follows the largest weight of a row that counts:
+    weights times a power of two give gradients times it, bit for bit; none, tiny, huge and
+    infinite ones give what they say."""
+    c = Case(n, 64, 96, 0.2, 0, 0, "bf16")
+    ids = c.ids()
+    w = torch.rand(n, generator=torch.Generator().manual_seed(3)).cuda() + 0.5
+    w[c.labels >= 96] = float("inf")  # of padding
+    w[c.labels < 0] = float("nan")
+
+    def grads(weight):
+        dx, dW, db = c.grads()
+        shc.linear_cross_entropy_step(c.x.t, c.W.t, ids, weight, dx=dx.t, dW=dW.t, db=db.t[0])
+        return dx.t.clone(), dW.t.clone(), db.t.clone()
+
+    first = grads(w)
+    assert all(bool(torch.isfinite(g).all()) for g in first)
+    for k in (-30, -1, 40):
+        for a, b in zip(grads(w * 2.0 ** k), first):
+            assert torch.equal(a, b * 2.0 ** k)
+    assert all(bool((g == 0).all()) for g in grads(torch.zeros_like(w)))
+    x, W = c.x.get(), c.W.get()
+    dz = np.exp(x @ W.T)
+    dz /= dz.sum(1, keepdims=True)
+    live = (c.labels >= 0) & (c.labels < 96)
+    dz[np.flatnonzero(live), c.labels[live]] -= 1
+    dz = np.abs(dz * live[:, None])
+    # what the terms of a gradient add up to: past 2^127 a sum of fp32 may pass its range on the
+    # way, whatever it ends at
+    terms = [torch.as_tensor(t, device="cuda") for t in
+             (dz @ np.abs(W), dz.T @ np.abs(x), dz.sum(0)[None])]
+    for size in (1e-42, 1e-38, 2e38):
+        got = grads(torch.full_like(w, size))
+        ref = grads(torch.ones_like(w))
+        for a, b, t in zip(got, ref, terms):
+            a, b = a.double(), b.double() * float(np.float32(size))
+            fits = t * size < 2.0 ** 127
+            assert bool(fits.any()) or size > 1
+            slack = 2.0 ** -6 * b.abs().max() + 1e-40
+            assert bool(((a - b).abs()[fits] <= slack).all())
+    one = torch.ones_like(w)
+    row = int(np.flatnonzero((c.labels >= 0) & (c.labels < 96))[0])
+    one[row] = float("inf")
+    rest = torch.arange(n, device="cuda") != row
+    assert torch.equal(grads(one)[0][rest], grads(torch.ones_like(w))[0][rest])
