@@ -420,8 +420,9 @@ __global__ __launch_bounds__(256) void from_kept_kernel(FromKept a) {
         typedef _Float16 half8 __attribute__((ext_vector_type(8)));
         const half8 x = *reinterpret_cast<const half8*>(static_cast<const _Float16*>(a.kept) +
                                                         row * a.width + col);
-        const float m = finite_or_0(a.parts[(int64_t)(col / a.tile) * a.rows + row].x);
-        const float f = lse == -__builtin_inff()
+        // a tile of nothing but -inf has probability 0, unless the row is a NaN
+        const float m = a.parts[(int64_t)(col / a.tile) * a.rows + row].x;
+        const float f = m == -__builtin_inff() && lse == lse
                             ? 0.f
                             : __builtin_amdgcn_exp2f((m - lse) * kLog2e) * (1.f / kExpScale);
 #pragma unroll
