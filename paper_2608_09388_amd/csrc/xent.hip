@@ -256,19 +256,13 @@ __device__ __forceinline__ void load_bias(float (&b)[8], const float* bias, int6
   }
 }
 
-// e^(z - by) of N logits in place, as one multiplication and addition before the
-// power of two: the rounding of by log2(e) is below that of by itself.  Past 2^100 (masks
-// of the type's lowest value) the difference is taken first.
+// e^(z - by) of N logits in place.  The difference comes first: z log2(e) - by log2(e) in
+// one multiplication and addition is off by half a step of by log2(e), a factor of 2^2 at
+// 1e8 (masks of a large finite number) and past fp32 at 1e10, also where z is `by` itself.
 template <int N>
 __device__ __forceinline__ void exps_less(float (&z)[N], float by) {
-  if (fabsf(by) < 0x1p100f) {
-    const float scaled = -by * kLog2e;
 #pragma unroll
-    for (int e = 0; e < N; ++e) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], kLog2e, scaled));
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) z[e] = __builtin_amdgcn_exp2f((z[e] - by) * kLog2e);
-  }
+  for (int e = 0; e < N; ++e) z[e] = __builtin_amdgcn_exp2f((z[e] - by) * kLog2e);
 }
 
 // dz of N logits, y the label less the first one's column.  lse = -inf: a row of nothing

@@ -89,3 +89,38 @@ def test_a_logit_that_is_not_a_number_beside_masked_tiles(C, dtype):
     for what, loss, lse, dx, dW, db in run_all(c):
         for t in (loss, lse, dx.t, dW.t) + (() if db is None else (db.t,)):
             assert bool(torch.isnan(t).all()), what
+
+
+FINITE = [-1e4, -1e8, -1e9, -1e10, -1e12, -1e18, -1e20, -1e30, float(np.finfo(np.float32).min)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", WIDTHS)
+@pytest.mark.parametrize("value", FINITE)
+def test_tiles_of_finite_masks(C, dtype, value):
+    """A finite number as a mask: probability 0 as with -inf, the loss of a label there finite."""
+    for mask in (np.arange(V) < 512, np.arange(V) >= 100, np.arange(V) % 3 == 1):
+        check_masked(masked(C, dtype, mask, value, 0.0), mask)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", WIDTHS)
+@pytest.mark.parametrize("value", FINITE)
+def test_every_class_masked(C, dtype, value):
+    """All classes at the mask's value.  u = 2^-24: lse and the logits are off by a rounding of
+    their size each, loss by three, lse - z being rounded too, beside 1e-3 for all else; a
+    probability stays within [0, 1] whatever these are, so that no dz passes the row's weight."""
+    c = Case(N, C, V, 0.0, 0, 0, dtype)
+    c.b = np.full(V, value, np.float32)
+    ref = c.oracle()
+    off = 4 * 2.0 ** -24 * abs(value) + 1e-3
+    w = np.ones(N) if c.w is None else wide(c.w)
+    W, x = np.abs(c.W.get()), np.abs(c.x.get())
+    most_dx = w[:, None] * (W.sum(0)[None] + W[c.labels])
+    most_dW = (w @ x)[None] + np.zeros((V, 1))
+    for what, loss, lse, dx, dW, db in run_all(c):
+        assert np.all(np.abs(loss.double().cpu().numpy() - ref["loss"]) <= off), what
+        assert np.all(np.abs(lse.double().cpu().numpy() - ref["lse"]) <= off), what
+        assert np.all(np.abs(dx.get()) <= 1.01 * most_dx), what
+        assert np.all(np.abs(dW.get()) <= 1.01 * most_dW), what
+        assert db is None or np.all(np.abs(db.get()) <= 1.01 * w.sum()), what
