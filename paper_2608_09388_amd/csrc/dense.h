@@ -52,6 +52,13 @@ struct Product {
 size_t partial_bytes(int64_t M, int64_t N, int64_t K);
 hipError_t launch_product(const Product& p, hipStream_t stream);
 
+// Whether the loads of a tile of R rows (or columns) of an operand stay within kReach of its
+// first element: of a rows operand all R rows, of a cols operand the BK rows of a step.
+inline bool in_reach(const Operand& o, bool rows_order, int64_t R) {
+  const int64_t ld = o.alt_ld > o.ld ? o.alt_ld : o.ld;
+  return (rows_order ? (R - 1) * ld + BK : (BK - 1) * ld + R) * 2 <= kReach;
+}
+
 // Whether rows of C elements, ld apart, can be read as they are (bf16).
 inline bool direct(const void* p, int64_t ld, int64_t C) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && C % 8 == 0 &&
@@ -93,9 +100,11 @@ struct Plan {
   int parts;
 };
 // few_rows: tiles of fewer than 128 rows too (operand A in rows); logits: the epilogues
-// of xent.hip.
+// of xent.hip; reach: an operand A in rows that a tile has to reach, or NULL.
 Plan plan_product(int64_t M, int64_t N, int64_t K, Mode mode, bool few_rows,
-                  size_t partial_bytes, bool logits = false, double* time = nullptr);
+                  size_t partial_bytes, bool logits = false, double* time = nullptr,
+                  const Operand* reach = nullptr);
+Plan plan_of(const Product& p);
 
 // Rows of fp32 up to which a product reads its operands as they are: the packing of the
 // second one would move more than the product.

@@ -222,7 +222,7 @@ size_t partial_bytes(int64_t M, int64_t N, int64_t K) {
 // step of 64 of K takes `latency` or, of as many as are there, `work` each; a tile has
 // `fixed` beside its steps.
 Plan plan_product(int64_t M, int64_t N, int64_t K, Mode mode, bool few_rows,
-                  size_t partial_bytes, bool logits, double* time) {
+                  size_t partial_bytes, bool logits, double* time, const Operand* reach) {
   struct Kind {
     TileKind kind;
     int slots;
@@ -244,6 +244,7 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, Mode mode, bool few_rows,
   for (int i = 0; i < (mode == kDirect ? 1 : mode == kSplit ? 3 : 4); ++i) {
     const Kind& k = kinds[i];
     if (!few_rows && tile_m(k.kind) < 128) continue;
+    if (reach != nullptr && !in_reach(*reach, true, tile_m(k.kind))) continue;
     const int64_t tiles = ((M + tile_m(k.kind) - 1) / tile_m(k.kind)) *
                           ((N + tile_n(k.kind) - 1) / tile_n(k.kind));
     // few rows of tiles share what they read of B with few others: its bytes of a
@@ -271,6 +272,15 @@ Plan plan_product(int64_t M, int64_t N, int64_t K, Mode mode, bool few_rows,
   return best;
 }
 
+// Rows of dz are as far apart as there are classes, up to 2^24: a tile of 64 of them is
+// within reach, one of 128 up to 8,454,000 classes, one of 256 up to 4,210,000.
+Plan plan_of(const Product& p) {
+  const Mode mode = p.direct ? kDirect : p.split ? kSplit : kPlain;
+  return plan_product(p.a_low && p.a_rows ? 2 * p.M : p.M, p.N, p.K, mode, p.a_rows,
+                      p.partials != nullptr ? p.partial_bytes : 0, false, nullptr,
+                      p.a_rows && !p.direct ? &p.A : nullptr);
+}
+
 hipError_t launch_product(const Product& p, hipStream_t stream) {
   if (p.M <= 0 || p.N <= 0) return hipSuccess;
   // two terms of A in rows: as many rows again, joined with the first as parts of K are
@@ -278,8 +288,11 @@ hipError_t launch_product(const Product& p, hipStream_t stream) {
   const int64_t M = twice ? 2 * p.M : p.M;
   if (twice && (p.partial_bytes < (size_t)M * p.N * 4 || p.A.plane != p.M * p.A.ld))
     return hipErrorInvalidValue;
-  const Plan plan = plan_product(M, p.N, p.K, p.direct ? kDirect : p.split ? kSplit : kPlain,
-                                 p.a_rows, p.partials != nullptr ? p.partial_bytes : 0);
+  const Plan plan = plan_of(p);
+  // direct products have offsets of 64 bits
+  if (!p.direct && p.K > 0 &&
+      (!in_reach(p.A, p.a_rows, tile_m(plan.kind)) || !in_reach(p.B, p.b_rows, tile_n(plan.kind))))
+    return hipErrorInvalidValue;
   Args a;
   a.A = p.A, a.B = p.B;
   a.M = M, a.N = p.N, a.K = p.K;

@@ -44,7 +44,9 @@
 // Loads past the ends give zeros: a buffer descriptor covers exactly the rows that
 // are there, and chunks past a row's end get an offset outside of it.  Operands
 // start at multiples of 16 bytes, with rows of a multiple of 8 elements, a
-// multiple of 8 elements and less than 2^21 apart (see `direct`).
+// multiple of 8 elements apart.  A load's place is a 32-bit offset from the tile's first
+// element, and a descriptor covers kReach bytes: how far apart rows may be follows from how
+// many a tile has (see `in_reach`).
 #pragma once
 
 #include <type_traits>
@@ -59,6 +61,7 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr int BK = 64, BKS = 32;  // of k to a step; split
+constexpr int64_t kReach = 0x7FFFFFF0;  // bytes from a tile's first element that a load reaches
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct Operand {
@@ -145,7 +148,7 @@ struct Side {
   __device__ __forceinline__ void load(char* lds, int64_t plane, int kt, int64_t K, int w) const {
     const int64_t at = plane + kt * step;
     int64_t left = bytes - kt * step;
-    if (left > 0x7FFFFFF0) left = 0x7FFFFFF0;
+    if (left > kReach) left = kReach;
     const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base + at), 0, (int)left,
                                                       0x00020000);
 #pragma unroll
