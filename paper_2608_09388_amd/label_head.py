@@ -121,7 +121,7 @@ class LabelHead:
         clipped to max_norm together."""
         p, w, g = self.params, self.weights, self.grads
         if n == 0:
-            for t in g.values():
+            for t in (*g.values(), self.norm):
                 t.zero_()
             return self.loss[:0]
         there = ((labels >= 0) & (labels < self.classes)).sum().clamp_(min=1)
