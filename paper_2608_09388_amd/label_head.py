@@ -120,12 +120,12 @@ class LabelHead:
         """Loss [n] against labels [n], and self.grads of the mean over the labelled rows,
         clipped to max_norm together."""
         p, w, g = self.params, self.weights, self.grads
+        self.there = ((labels >= 0) & (labels < self.classes)).sum().clamp_(min=1)
         if n == 0:
             for t in (*g.values(), self.norm):
                 t.zero_()
             return self.loss[:0]
-        there = ((labels >= 0) & (labels < self.classes)).sum().clamp_(min=1)
-        self.weight[:n] = 1.0 / there
+        self.weight[:n] = 1.0 / self.there
         shc.linear_cross_entropy_step(self.y[-1][:n], w["T"], labels, self.weight, None, self.loss,
                                       self.dy, g["T"], ws=self.ws)
         for k in reversed(range(self.blocks)):
@@ -140,6 +140,11 @@ class LabelHead:
         shc.grad_norm(g.values(), self.norm, ws=self.ws)
         shc.clip_grads(g.values(), self.norm, self.max_norm)
         return self.loss[:n]
+
+    def mean_loss(self, loss: torch.Tensor) -> torch.Tensor:
+        """The mean that the last backward's gradients are of, from its losses: over the rows
+        with a label (0 without one)."""
+        return loss.sum() / self.there
 
     def update(self, lr: float):
         for k, v in self.params.items():
@@ -184,7 +189,7 @@ def main():
         mask = (torch.rand(B * V, generator=g, device="cuda") < 0.1).to(torch.uint8)
         loss = head.step(x, mask, labels, a.lr)
         if s % 10 == 0 or s == a.steps - 1:
-            print(f"step {s}: {loss.numel()} rows, mean loss {float(loss.mean()):.4f}, "
+            print(f"step {s}: {loss.numel()} rows, mean loss {float(head.mean_loss(loss)):.4f}, "
                   f"gradient norm {float(head.norm):.4f}", flush=True)
 
 
