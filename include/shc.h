@@ -894,7 +894,8 @@ int shc_distill_top_step(const void* logits, int64_t logits_stride, int64_t n_ro
  *   cores, as are all of up to 32 rows and of small linear layers, but for those of
  *   dW.  Every output is rounded once, but for dz (below), which is rounded to
  *   `dtype` before the products of a backward take it (not so of up to 64 rows of
- *   the cross entropy, where it is two bf16 terms).
+ *   the cross entropy, where it is two bf16 terms).  Gradients in bf16 are off by
+ *   0.0022 to 0.0024 of their norm for that, 0.0017 of it their own rounding.
  * - Sums have a fixed order that follows the sizes and alignments: results repeat
  *   bit for bit.
  * - A workspace query takes `aligned`: 1 where every row tensor that the call
@@ -917,7 +918,8 @@ int shc_distill_top_step(const void* logits, int64_t logits_stride, int64_t n_ro
  *   of Cout; bias [Cout] or NULL; residual NULL for none, and may be out itself.
  *   pre: z (rounded), for the backward, or NULL.   act: any SHC_ACT_*.
  * A NaN in z gives NaN with every act, also SHC_ACT_RELU (where the sparse layers
- * give 0); -inf gives NaN with SHC_ACT_GELU and SHC_ACT_SILU.
+ * give 0); -inf gives NaN with SHC_ACT_GELU and SHC_ACT_SILU.  GELU's Phi is off by
+ * 7.5e-8 and some roundings at most, of 1: far below 0 that is more than Phi.
  */
 size_t shc_linear_workspace(int64_t n_rows, int32_t Cin, int32_t Cout, int32_t dtype,
                             int32_t aligned);
@@ -932,7 +934,8 @@ int shc_linear(const void* x, int64_t x_stride, int64_t n_rows, int32_t Cin, con
  *
  *   dz = dout act'(z),   dx = dz W^T,   dW = x^T dz,   db = sum over rows of dz
  *
- * (act' of SHC_ACT_RELU is 0 at 0; the residual's gradient is dout itself).
+ * (act' of SHC_ACT_RELU is 0 at 0, of SHC_ACT_GELU and SHC_ACT_SILU a NaN at an infinite
+ * z; the residual's gradient is dout itself).
  *   dout, pre [n_rows] rows of Cout (pre may be NULL with SHC_ACT_NONE); dx
  *   [n_rows] rows of Cin, dW [Cin] rows of Cout, db [Cout] fp32; each output may
  *   be NULL.  db sums dz before it is rounded.
@@ -947,8 +950,10 @@ int shc_linear_backward(const void* dout, int64_t dout_stride, const void* x, in
                         hipStream_t stream);
 
 /*
- * Cross entropy of a linear layer's logits over V classes, none of which is
- * written to memory, with W the table of V rows of C that shc_embed_rows reads too:
+ * Cross entropy of a linear layer's logits over V classes, with W the table of V rows
+ * of C that shc_embed_rows reads too.  No caller provides or keeps the logits: the
+ * forward writes them only where they are 2^21 or fewer, the gradients hold a piece of
+ * rows at a time (below):
  *
  *   z_v = x . W_v + bias_v,   lse = log of sum exp z,   loss = lse - z_label
  *   dz_v = w (exp(z_v - lse) - [v = label])
@@ -961,6 +966,13 @@ int shc_linear_backward(const void* dout, int64_t dout_stride, const void* x, in
  *   left out.
  *   loss, lse [n_rows] fp32, row_weight [n_rows] fp32 = w, the upstream gradient of
  *   every row's loss, or NULL (1).  dx, dW and db may each be NULL.
+ *   row_weight: dz in bf16 is formed times the factor in [1, 2] that makes the largest
+ *   |w| of the call's rows a power of two, which its sums undo: a row's gradient is
+ *   rounded as that weight has it, and sums pass fp32's range up to a factor of 2 early.
+ *   Probabilities are exp(z - lse) with lse in fp32, whose rounding scales a row's by up
+ *   to e^(2^-24 |lse|): they add up to 1 no more in a row of nothing but logits of 10^6
+ *   and more in size, but none passes 1.  Classes may be masked by a bias of -inf or of any
+ *   finite number.
  *   A logit of -inf (by its bias) has probability 0; a label there makes the loss
  *   +inf, the gradient stays finite; in a row of nothing but -inf every probability
  *   is 0.  NaN, +inf or a sum without end in a row makes its results NaN, and those
@@ -970,9 +982,11 @@ int shc_linear_backward(const void* dout, int64_t dout_stride, const void* x, in
  * shc_linear_cross_entropy_backward -- gradients from lse as written.
  * shc_linear_cross_entropy_step     -- loss and gradients.
  * The backward and the step hold dz for up to 2^30 (bf16) or 2^28 (fp32) pairs of
- * row and class at a time in the workspace, the step for bf16 from C = 768 on also
- * as many fp32 logits (db needs them).  `pass` of the workspace query: 0
- * forward, 1 backward, 2 step; `aligned` speaks of W alone.
+ * row and class (256 rows at least) at a time in the workspace, fp32 in ten bytes a
+ * pair, the step for bf16 from C = 768 on also as many fp32 logits, for db.  The query
+ * does not know whether db is asked for, nor which rows are padding.  4,096 rows of 4,096
+ * over 131,072 classes in bf16: 1.2 GiB for a backward, 3.3 GiB for a step.  `pass` of the
+ * query: 0 forward, 1 backward, 2 step; `aligned` speaks of W alone.
  */
 #define SHC_XENT_FORWARD 0
 #define SHC_XENT_BACKWARD 1

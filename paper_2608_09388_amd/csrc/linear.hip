@@ -11,8 +11,8 @@
 // multiples of 16 bytes or are not a multiple of 8 long, fp32 rows, which become three
 // bf16 terms) are packed into the workspace first.
 //
-// Forward, 8,192 rows, 16,384 -> 4,096, bf16, 931 us (1.18 PFLOP/s); backward of 4,096 ->
-// 8,192 1,013 us, 95 of them dz and db (4.2 TB/s), the products at 1.18 PFLOP/s.
+// Forward, 8,192 rows, 16,384 -> 4,096, bf16, 909 us (1.21 PFLOP/s); backward of 4,096 ->
+// 8,192 989 us, 95 of them dz and db (4.2 TB/s), the products at 1.23 PFLOP/s.
 // 67,040 rows of 128 -> 128 with GELU, residual and z kept: 22 us (3.1 TB/s).
 #include <algorithm>
 

@@ -1,4 +1,4 @@
-// Cross entropy of a linear layer's logits, without keeping them, and its gradients.
+// Cross entropy of a linear layer's logits, and its gradients, without all of them in memory.
 // For a row x_i with label y_i in [0, V) and the table W [V][C]:
 //
 //   z_v = x_i . W_v + b_v,  lse_i = log sum exp z_v,  loss_i = lse_i - z_{y_i}
@@ -12,7 +12,7 @@
 //
 // Forward: one product over all of V whose epilogue takes every row's maximum and sum
 // of exponentials over the tile's columns and the label's logit; a second launch joins
-// the tiles.  Nothing of size rows x V is written.
+// the tiles.  Nothing of size rows x V is written, but for few logits (`cut_logits`).
 //
 // Gradients: for a piece of rows at a time dz [rows][V] (bf16, rounded once from fp32, or
 // fp32), and the products dz W and dz^T x over it; db from the unrounded dz, summed
@@ -41,9 +41,9 @@
 // passes start from there (`cut_logits`).
 //
 // 16 rows of 4,096 over 131,072 classes in bf16: 192 us, the table read at 6.2 TB/s in 174.
-// Loss and gradients of 4,096 such rows: 11.5 ms, three products at 1.11 to 1.2
-// PFLOP/s, the power limit, and 0.4 ms for dz.  67,040 rows of 128 over 10,475 classes,
-// gradients: 1,343 us; logits to dz 650 (exponentials and stores beside short products),
+// Loss and gradients of 4,096 such rows: 11.3 ms, three products at 1.12 to 1.22
+// PFLOP/s, the power limit, and 0.4 ms for dz.  67,040 rows of 128 over 10,475 classes, loss:
+// 634 us; gradients: 1,342 us; logits to dz 650 (exponentials and stores beside short products),
 // dx 410 and dW 275 from reading dz.
 #include <algorithm>
 #include <mutex>
