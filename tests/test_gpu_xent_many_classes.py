@@ -57,6 +57,8 @@ def reference(x, W, labels):
     (256, 1024, 4500008, "bf16"),   # past what a tile of 256 rows reaches
     (64, 1024, 8500000, "bf16"),    # two terms: 128 rows
     (200, 256, 8500003, "f32"),
+    (64, 72, 1 << 24, "bf16"),      # the most classes
+    (300, 40, (1 << 24) - 1, "bf16"),
 ])
 def test_gradients(n, C, V, dtype):
     """In the 2-norm of a row.  h is half a step of the type (bf16 2^-8; fp32's is in `sums`): a
