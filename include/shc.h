@@ -918,8 +918,8 @@ int shc_distill_top_step(const void* logits, int64_t logits_stride, int64_t n_ro
  *   of Cout; bias [Cout] or NULL; residual NULL for none, and may be out itself.
  *   pre: z (rounded), for the backward, or NULL.   act: any SHC_ACT_*.
  * A NaN in z gives NaN with every act, also SHC_ACT_RELU (where the sparse layers
- * give 0); -inf gives NaN with SHC_ACT_GELU and SHC_ACT_SILU.  GELU's Phi is off by
- * 7.5e-8 and some roundings at most, of 1: far below 0 that is more than Phi.
+ * give 0); -inf gives NaN with SHC_ACT_GELU and SHC_ACT_SILU.  GELU's Phi is
+ * within 7.5e-8 and some roundings; of its own size 5e-5 at z = -3, 2e-3 at -5.
  */
 size_t shc_linear_workspace(int64_t n_rows, int32_t Cin, int32_t Cout, int32_t dtype,
                             int32_t aligned);
